@@ -462,6 +462,85 @@ ETV_API int32_t etv_commit_path_indices(const etv_cache_desc *h_desc, const void
                                 const int32_t *new_len, int32_t fast, int32_t *kept_len, int32_t *status,
                                 void *stream);
 
+/* ---------------------------------------------------------------------------
+ * The prefix cache in 4 bits -- the committed prefix of Section 3.1 in 4.25 bits
+ * an element.  What it holds of a row of d channels of one KV head are groups of
+ * 32 consecutive channels, each with 32 codes and one scale byte:
+ *   codes   uint8 [rows, d/2]   e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and the sign (bit 3);
+ *                               channel 2i in the low, 2i+1 in the high half of byte i
+ *   scales  uint8 [rows, d/32]  s stands for 2^(s-127); 255 for NaN throughout the group
+ * element = value of its code * 2^(s-127), exact in bf16 and fp32 for 2 <= s <= 252.
+ * A group is written from its 32 values x:
+ *   a = max |x|; e = exponent of a rounded to two significant bits (1.75 * 2^k counts as 2^(k+1));
+ *   s = e + 127 - 2, held within 2 .. 252; code = nearest e2m1 value of x / 2^(s-127), ties to the even code, beyond 6
+ *   to 6.  So nothing is off by more than a quarter of a.  A group with an infinity or a NaN in it gets s = 255.
+ * Row order, codes and scales alike, K and V in tensors of their own; layer l starts layer_rows rows after layer l-1:
+ *   contiguous (block_size == 0)  [B, Hkv, P_cap]: position p of head h of sequence b is row (b * Hkv + h) * P_cap + p
+ *   paged (multiple of 16)        [num_blocks, Hkv, block_size], blocks by block_table as in attention
+ * codes are 16-byte aligned, scales 4-byte aligned.  d is 64 or 128; the unquantised side is fp32 or bf16.
+ * ------------------------------------------------------------------------- */
+typedef struct etv_q4_desc {
+    int32_t B;
+    int32_t rows;       /* rows a sequence has on the unquantised side (T_max of the tree rows for the commit) */
+    int32_t Hkv, d;
+    int32_t dtype;      /* ETV_F32 | ETV_BF16 */
+    int32_t n_layers;
+    int32_t W;          /* etv_commit_accepted_kv_q4: row length of acc_nodes and slot_map */
+    int32_t block_size; /* 0: contiguous; a multiple of 16: paged */
+    int32_t max_blocks;
+    int32_t num_blocks;
+    int32_t P_cap;
+    int32_t reserved;
+    int64_t layer_rows; /* cache rows between consecutive layers */
+} etv_q4_desc;
+
+/* quantize_kv_q4 -- rows 0 .. n_rows[b]-1 of k and v go to positions prefix_len[b] .. of the cache, for every layer and in
+ * one launch: a prompt's rows, or with rows == 1 a decoded token's.  prefix_len_out[b] = prefix_len[b] + n_rows[b].
+ *   Status bits: ETV_COMMIT_BAD_LEN (n_rows outside [0, rows]), ETV_COMMIT_CAPACITY (beyond capacity[b], P_cap or the block
+ *   table, or a negative prefix_len), ETV_COMMIT_BAD_BLOCK.  A sequence that fails a check is left untouched
+ *   (prefix_len_out = prefix_len).
+ *  k, v  in  [n_layers, B, rows, Hkv, d], 16-byte aligned;  prefix_len, n_rows, capacity int32 [B]
+ *  prefix_len_out int32 [B] (must not alias prefix_len: several workgroups read it);  status int32 [B]
+ * Two sequences of one call must not share a block that is written. */
+ETV_API int32_t etv_quantize_kv_q4(const etv_q4_desc *h_desc, const void *k, const void *v, uint8_t *k_codes, uint8_t *k_scales,
+                           uint8_t *v_codes, uint8_t *v_scales, const int32_t *block_table, const int32_t *prefix_len,
+                           const int32_t *n_rows, const int32_t *capacity, int32_t *prefix_len_out, int32_t *status,
+                           void *stream);
+
+/* commit_accepted_kv_q4 -- etv_commit_accepted_kv into a 4-bit cache: the accepted rows of the step's tree K/V buffer are
+ * quantised as they are appended.  Arguments, checks, slot_map and status bits as there; the tree rows are in a buffer of
+ * their own (no in-place form: the verification pass needs them unrounded), and prefix_len_out must not alias prefix_len.
+ *  kt, vt  in  [n_layers, B, rows, Hkv, d] */
+ETV_API int32_t etv_commit_accepted_kv_q4(const etv_q4_desc *h_desc, const void *kt, const void *vt, uint8_t *k_codes,
+                                  uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales, const int32_t *block_table,
+                                  const int32_t *prefix_len, const int32_t *capacity, const int32_t *n_nodes,
+                                  const int32_t *acc_nodes, const int32_t *accept_len, int32_t *prefix_len_out,
+                                  int32_t *slot_map, int32_t *status, void *stream);
+
+/* dequantize_kv_q4 -- positions first[b] .. first[b] + n_rows[b] - 1 of the cache into rows 0 .. of k and v, for every layer
+ * and in one launch; the rows behind n_rows[b] are zeros, and so are all rows of a sequence that fails a check.
+ *   Status bits: ETV_COMMIT_BAD_LEN (first negative, n_rows outside [0, rows]), ETV_COMMIT_CAPACITY (beyond P_cap or the
+ *   block table), ETV_COMMIT_BAD_BLOCK.
+ *  first, n_rows in int32 [B];  k, v out [n_layers, B, rows, Hkv, d], 16-byte aligned;  status out int32 [B] */
+ETV_API int32_t etv_dequantize_kv_q4(const etv_q4_desc *h_desc, const uint8_t *k_codes, const uint8_t *k_scales,
+                             const uint8_t *v_codes, const uint8_t *v_scales, const int32_t *block_table,
+                             const int32_t *first, const int32_t *n_rows, void *k, void *v, int32_t *status, void *stream);
+
+/* tree_verify_attention_q4 -- etv_tree_verify_attention against a prefix in a 4-bit cache (one layer of it); T_max == 1 is
+ * plain decoding.  q, out, kt, vt, bitmask, n_nodes, lse and the result are as there, h_desc->dtype being the type of
+ * q, kt, vt and out; the tree rows are never quantised and always in a buffer of their own.  A row that sees no key gives
+ * zeros and lse = -inf.  A key in a block outside [0, num_blocks) counts as NaN.
+ * h_desc: block_size 0 or a multiple of 16, num_blocks used when paged; flags: ETV_ATTN_FLAG_GENERIC or 0; any sign of scale.
+ * workspace: etv_tree_verify_attention_q4_workspace_bytes(h_desc) bytes, 256-byte aligned.
+ * Supported: dtype F32 or BF16, d in {64, 128}, Hq % Hkv == 0, 1 <= T_max <= ETV_ATTN_MAX_TREE. */
+ETV_API size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h_desc);
+
+ETV_API int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h_desc, const void *q, const uint8_t *k_codes,
+                                     const uint8_t *k_scales, const uint8_t *v_codes, const uint8_t *v_scales,
+                                     const int32_t *block_table, const int32_t *prefix_len, const void *kt, const void *vt,
+                                     const uint64_t *bitmask, const int32_t *n_nodes, void *out, float *lse, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

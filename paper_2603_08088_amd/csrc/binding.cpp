@@ -3,10 +3,11 @@
 // 9 us per attention call: longer than the kernel.  Here one template turns the arguments into those of the C prototype in
 // eagletv.h: a pointer parameter takes a device-resident contiguous tensor or None, a descriptor any object with the buffer
 // of that struct, an integer an int or what has __index__ (numpy's integers, tensors of one); the trailing stream is the
-// current one.  The GIL is released around the call.
+// current one.  The GIL is released around the call.  HERE: the tensors must be on the device whose stream that is.
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -22,9 +23,9 @@ struct Refused {};  // a Python exception is set
 
 template <class T>
 constexpr bool is_desc = std::is_same_v<T, const etv_attn_desc *> || std::is_same_v<T, const etv_commit_desc *> ||
-                         std::is_same_v<T, const etv_cache_desc *>;
+                         std::is_same_v<T, const etv_cache_desc *> || std::is_same_v<T, const etv_q4_desc *>;
 
-template <class T>
+template <class T, bool HERE>
 T arg(PyObject *o) {
     if constexpr (std::is_integral_v<T>) {
         if (!PyIndex_Check(o)) {
@@ -58,14 +59,18 @@ T arg(PyObject *o) {
             PyErr_SetString(PyExc_AssertionError, "device-resident contiguous tensors only");
             throw Refused{};
         }
+        if (HERE && t.get_device() != c10::hip::current_device()) {
+            PyErr_Format(PyExc_ValueError, "tensor on device %d, the current device is %d", (int)t.get_device(), (int)c10::hip::current_device());
+            throw Refused{};
+        }
         return static_cast<T>(t.data_ptr());
     }
 }
 
-template <class... A, std::size_t... I>
+template <bool HERE, class... A, std::size_t... I>
 int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I...>) {
     std::tuple<A...> v;
-    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>>(args[I])), ...);  // left to right; the stream is last
+    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>, HERE>(args[I])), ...);  // left to right; the stream is last
     std::get<sizeof...(A) - 1>(v) = c10::hip::getCurrentHIPStream().stream();
     int32_t rc;
     Py_BEGIN_ALLOW_THREADS;
@@ -77,13 +82,13 @@ int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I..
 template <class... A>
 constexpr Py_ssize_t arity(int32_t (*)(A...)) { return sizeof...(A) - 1; }
 
-template <auto F>
+template <auto F, bool HERE = false>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     constexpr Py_ssize_t want = arity(F);
     if (n != want) return PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
     try {
-        return PyLong_FromLong(apply(F, args, std::make_index_sequence<want>{}));
+        return PyLong_FromLong(apply<HERE>(F, args, std::make_index_sequence<want>{}));
     } catch (const Refused &) {
         return nullptr;
     }
@@ -137,10 +142,13 @@ PyObject *commit_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define ETV_METHOD(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name>, METH_FASTCALL, nullptr}
+#define ETV_METHOD_HERE(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name, true>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree), ETV_METHOD(tree_verify_attention),
                          ETV_METHOD(tree_verify_attention_static), ETV_METHOD(safe_gather_paths), ETV_METHOD(evaluate_posterior),
                          ETV_METHOD(commit_accepted_kv), ETV_METHOD(verify_epilogue), ETV_METHOD(lm_head_argmax),
                          ETV_METHOD(pack_lm_head), ETV_METHOD(replicate_branches), ETV_METHOD(commit_path_indices),
+                         ETV_METHOD_HERE(quantize_kv_q4), ETV_METHOD_HERE(commit_accepted_kv_q4), ETV_METHOD_HERE(dequantize_kv_q4),
+                         ETV_METHOD_HERE(tree_verify_attention_q4),
                          {"commit_desc", (PyCFunction)(void (*)(void))commit_desc, METH_FASTCALL, nullptr},
                          {"empty_i32", (PyCFunction)(void (*)(void))empty_i32, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
