@@ -1,4 +1,8 @@
 // tree_verify_attention_q4: tree attention against a prefix whose K and V are held in 4 bits (format: eagletv.h).
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "etv_common.h"
 
 namespace etv {
@@ -14,8 +18,15 @@ struct Q4Attn {
     void *out;
     float *lse;
     int B, T_max, Hq, Hkv, G, block_size, max_blocks, num_blocks, P_cap, P_max, words;
-    float scale_log2;  // of the scores, times log2(e)
+    float scale_log2;  // of the scores, times log2(e); the matrix kernel: its magnitude
+    uint32_t flip;     // matrix kernel: 0x80008000 where the scale is negative (it goes into q), else 0
     uint32_t inv_bs;
+    // matrix kernel: a sequence's prefix in splits of `chunk` keys, one slot each, and with more than one split a slot more for
+    // the tree.  Partials, if slots > 1: part_o [B * Hkv][slots][row_groups * 32 * RW][D], part_ml (reference, sum) alike.
+    int chunk, nsplit, slots, row_groups, units;
+    uint32_t inv_g, inv_hkv, inv_slots, inv_groups;
+    float *part_o;
+    float2 *part_ml;
 };
 
 constexpr float kQ4Ln2 = 0.6931471805599453f;
@@ -124,6 +135,585 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
     if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.T_max + k] = l == 0.f ? -INFINITY : (m + log2f(l)) * kQ4Ln2;
 }
 
+// ------------------------------------------------------------------------------------------------
+// The matrix kernel.  With the G * T_max query rows of a KV head packed into rows r = t * G + g, a wavefront has 32 of them and
+// takes 64 keys at a time:
+//   S^T[key, r]  = K Q^T     v_mfma_scale_f32_32x32x64_f8f6f4: K as the cache holds it (fp4, its scale bytes the instruction's),
+//                            16 bytes a lane straight from memory, q in NQ parts of 6 bits (e2m3)
+//   P^T          = exp2(S^T * scale - reference)   a lane has 32 keys of one row; the reference follows the maximum lazily
+//   O^T[d, r]   += V^T P^T   bf16: V is converted (exactly) into an LDS tile and comes back through the transpose read; P stays
+//                            in registers as the product's B operand
+// The parts of q: with e the exponent of its group's maximum, part x is q less the parts before it, rounded to e2m3 at scale
+// 2^(e - 2 - 4x).  Three parts leave at most 2^-14 of the group's maximum, which is half a unit of the bf16 there; fp32 takes
+// six (2^-26).  Six-bit and four-bit operands run at four times the bf16 rate, so three parts cost less than one bf16 product,
+// and K needs neither a conversion nor LDS.
+// fp32: P in three bf16 parts, exactly, and the tree's K, V and q likewise (products with parts below 2^-24 left out).
+// RW wavefronts of a workgroup share the keys and have rows of their own, the 4 / RW groups of them share the rows: few rows
+// (a token, a small tree) leave reading the cache as the work, and every wavefront reads keys of its own.
+typedef int q4_i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t q4_u32x6 __attribute__((ext_vector_type(6)));
+typedef float q4_f32x16 __attribute__((ext_vector_type(16)));
+typedef float q4_f32x32 __attribute__((ext_vector_type(32)));
+typedef __bf16 q4_bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 q4_bf16x8 __attribute__((ext_vector_type(8)));
+typedef short q4_s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
+
+constexpr int kQ4Tile = 64;      // keys
+constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the reference before the outputs are rescaled
+
+// Dynamic LDS: V tiles [key groups][2 if rows are shared out, else 1][64][D] bf16, afterwards the outputs [4][32][D + 4] fp32.
+template <int D, int RW>
+struct Q4Geo {
+    static constexpr int ROW = 2 * D, TILE = kQ4Tile * ROW, KW = 4 / RW, BUFS = RW > 1 ? 2 : 1;
+    static constexpr int OUT_ROW = D + 4;  // floats; four on from a multiple of the banks
+    static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
+    static constexpr int LDS = TILES > OUT ? TILES : OUT;
+};
+
+template <int OPA, int OPB>
+__device__ __forceinline__ q4_f32x16 q4_scores(uint4 k, q4_u32x6 q, q4_f32x16 c, uint32_t k_scale, uint32_t q_scale) {
+    const q4_i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0}, b = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 2, OPA, (int)k_scale, OPB, (int)q_scale);
+}
+__device__ __forceinline__ uint32_t q4_pair(float a, float b) {
+    const q4_f32x2 v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, q4_bf16x2));
+}
+// a, b = hi + mid + lo exactly (24 bits in three bf16); what is not finite stays in hi
+__device__ __forceinline__ void q4_split(float a, float b, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
+    const auto upper = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+    const auto halves = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+    hi = halves(a, b);
+    a -= upper(a); b -= upper(b);
+    mid = halves(a, b);
+    lo = halves(a - upper(a), b - upper(b));
+}
+__device__ __forceinline__ float q4_half_max(float v) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float q4_half_sum(float v) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float q4_max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+// Positions of 16-byte pieces within a row of the V tile: the lanes of a store, which have rows of their own, and those of a
+// transpose read both reach all banks.
+template <int D>
+__device__ __forceinline__ int q4_swizzle(int row) { return D == 128 ? (((row & 3) << 1) | ((row >> 2) & 1)) : ((row & 2) << 1); }
+
+template <int D, bool F32, int RW>
+struct Q4Wave {
+    static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 3, QW = F32 ? 2 : 1;
+    using G = Q4Geo<D, RW>;
+    const Q4Attn &p;
+    uint8_t *smem;
+    int lane, r, hh, kg, wr, stage;
+    q4_f32x16 o[DB];
+    float m, l;
+
+    __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (G::BUFS > 1 ? stage & 1 : 0)) * G::TILE; }
+    // Between the stores of a V tile and its reads.  Rows shared out: every wavefront has stored its part; the next tile goes to the
+    // other buffer, which all have read before this barrier.  Else the tile is the wavefront's own, and LDS keeps its order.
+    __device__ __forceinline__ void staged() const {
+        if constexpr (RW > 1) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            __builtin_amdgcn_s_barrier();
+        }
+        asm volatile("" ::: "memory");
+    }
+
+    // P^T of 64 keys from their scores; key 32 kb + x is seen where bit x of vis[kb] is set (MASKED).
+    template <bool MASKED>
+    __device__ __forceinline__ void softmax(q4_f32x16 (&s)[2], uint64_t vis, q4_bf16x8 (&pf)[NP][2][2]) {
+        if (MASKED) {
+            const uint32_t v[2] = {(uint32_t)vis >> (4 * hh), (uint32_t)(vis >> 32) >> (4 * hh)};
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
+        }
+        float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+#pragma unroll
+        for (int i = 1; i < 16; i++) top = q4_max3(top, s[0][i], s[1][i]);
+        top = q4_half_max(top) * p.scale_log2;
+        const bool lift = top > m + kQ4Lazy;
+        if (__any(lift)) {
+            const float next = lift ? top : m, alpha = lift ? __builtin_amdgcn_exp2f(m - next) : 1.f;
+            m = next;
+            l *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) o[db][i] *= alpha;
+        }
+        const float off = m == -INFINITY ? 0.f : -m;
+        float sum[2] = {0.f, 0.f};
+        uint32_t pk[NP][2][8];
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, off)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][i + 1], p.scale_log2, off));
+                if constexpr (F32) {
+                    q4_split(a, b, pk[0][kb][i >> 1], pk[1][kb][i >> 1], pk[NP - 1][kb][i >> 1]);
+                    sum[kb] += a + b;
+                } else {
+                    // the weights rounded to bf16 are the weights: the sum takes them as the product does
+                    pk[0][kb][i >> 1] = q4_pair(a, b);
+                    sum[kb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i >> 1]),
+                                                              __builtin_bit_cast(q4_bf16x2, 0x3f803f80u), sum[kb], false);
+                }
+            }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int x = 0; x < NP; x++)
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+                for (int st = 0; st < 2; st++)
+                    pf[x][kb][st] = __builtin_bit_cast(q4_bf16x8, (uint4{pk[x][kb][4 * st], pk[x][kb][4 * st + 1], pk[x][kb][4 * st + 2], pk[x][kb][4 * st + 3]}));
+    }
+
+    // O^T += V^T P^T over the tile, with the first `parts` of P
+    template <int PARTS>
+    __device__ __forceinline__ void accumulate(const uint8_t *v, const q4_bf16x8 (&pf)[NP][2][2]) {
+        const int i16 = lane & 15, vrow = 4 * hh + (i16 >> 2), piece = 2 * (lane >> 4 & 1) + ((i16 & 3) >> 1), sub = 8 * (i16 & 1);
+        const int sw = q4_swizzle<D>(vrow);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int st = 0; st < 2; st++) {
+                const uint8_t *const row = v + (32 * kb + 16 * st + vrow) * G::ROW + sub;
+#pragma unroll
+                for (int db = 0; db < DB; db++) {
+                    const int at = ((4 * db + piece) ^ sw) << 4;
+                    const q4_s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)(row + at));
+                    const q4_s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)(row + 8 * G::ROW + at));
+                    const q4_bf16x8 a = __builtin_shufflevector(__builtin_bit_cast(q4_bf16x4, v0), __builtin_bit_cast(q4_bf16x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                    for (int x = 0; x < PARTS; x++) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[x][kb][st], o[db], 0, 0, 0);
+                }
+            }
+    }
+};
+
+// Eight consecutive channels of an unquantised row as NP bf16 parts.
+__device__ __forceinline__ void q4_eight(const uint16_t *p, uint32_t flip, uint4 (&part)[1]) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    part[0] = uint4{w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
+}
+__device__ __forceinline__ void q4_eight(const float *p, uint32_t flip, uint4 (&part)[3]) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    const uint32_t f = flip & 0x80000000u;
+    const auto fl = [f](float x) { return __uint_as_float(__float_as_uint(x) ^ f); };
+    q4_split(fl(a.x), fl(a.y), part[0].x, part[1].x, part[2].x);
+    q4_split(fl(a.z), fl(a.w), part[0].y, part[1].y, part[2].y);
+    q4_split(fl(b.x), fl(b.y), part[0].z, part[1].z, part[2].z);
+    q4_split(fl(b.z), fl(b.w), part[0].w, part[1].w, part[2].w);
+}
+// the values that are not finite out of eight bf16 (first parts); true if there were any
+__device__ __forceinline__ bool q4_take_out(uint4 &w) {
+    const auto ill = [](uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+    const auto keep = [&](uint32_t x) { return x & ~((ill(x) >> 15) * 0xffffu); };
+    const bool any = (ill(w.x) | ill(w.y) | ill(w.z) | ill(w.w)) != 0;
+    w = uint4{keep(w.x), keep(w.y), keep(w.z), keep(w.w)};
+    return any;
+}
+
+// One row's eight channels from its sums, and its lse by the first of the threads.
+template <typename T>
+__device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int head, int piece, int D, bool node, float ref, float sum, const float (&acc)[8]) {
+    const float inv = node && sum != 0.f ? 1.f / sum : 0.f;  // a NaN sum stays one
+    T *const dst = static_cast<T *>(p.out) + (((size_t)b * p.T_max + t) * p.Hq + head) * D + 8 * piece;
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = inv == 0.f ? float4{0, 0, 0, 0} : float4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        const float4 c = inv == 0.f ? float4{0, 0, 0, 0} : float4{acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv};
+        reinterpret_cast<float4 *>(dst)[0] = a;
+        reinterpret_cast<float4 *>(dst)[1] = c;
+    } else {
+        uint4 v = {q4_pair(acc[0] * inv, acc[1] * inv), q4_pair(acc[2] * inv, acc[3] * inv), q4_pair(acc[4] * inv, acc[5] * inv), q4_pair(acc[6] * inv, acc[7] * inv)};
+        *reinterpret_cast<uint4 *>(dst) = inv == 0.f ? uint4{0, 0, 0, 0} : v;
+    }
+    if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
+}
+
+template <int D, bool F32, int RW>
+__global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
+    using T = std::conditional_t<F32, float, uint16_t>;
+    using Wave = Q4Wave<D, F32, RW>;
+    using G = Q4Geo<D, RW>;
+    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t q4_smem[];
+    const int tid = threadIdx.x;
+    Wave w{p, q4_smem};
+    w.lane = tid & 63;
+    w.r = w.lane & 31;
+    w.hh = w.lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    w.kg = wave / RW;
+    w.wr = wave % RW;
+    w.stage = 0;
+    w.m = -INFINITY;
+    w.l = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; db++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) w.o[db][i] = 0.f;
+    const int r = w.r, hh = w.hh;
+
+    // The row groups of a unit read the same keys: their workgroups are eight apart, on one of the eight XCDs.
+    uint32_t group, slot, kvh;
+    const uint32_t unit = fast_div(blockIdx.x >> 3, (uint32_t)p.row_groups, p.inv_groups, group) * 8 + (blockIdx.x & 7);
+    if (unit >= (uint32_t)p.units) return;
+    const uint32_t bh = fast_div(unit, (uint32_t)p.slots, p.inv_slots, slot);
+    const int b = (int)fast_div(bh, (uint32_t)p.Hkv, p.inv_hkv, kvh);
+    const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max);
+    const bool whole = p.slots == 1, tree_here = whole || (int)slot == p.nsplit;
+    const int k0 = whole ? 0 : tree_here ? P : min(P, (int)slot * p.chunk), k1 = whole || tree_here ? P : min(P, k0 + p.chunk);
+    if (!tree_here && k0 >= k1) return;
+    uint32_t g;
+    const int t = (int)fast_div(group * 32 * RW + 32 * w.wr + r, (uint32_t)p.G, p.inv_g, g);
+    const size_t q_row = (((size_t)b * p.T_max + min(t, p.T_max - 1)) * p.Hq + kvh * p.G + g) * D;
+    uint32_t rem;
+    const bool live = (int)fast_div(group * 32 * RW, (uint32_t)p.G, p.inv_g, rem) < n;  // has the workgroup a row?
+    if (!live && !whole) return;
+    bool ill = false;  // the tree's V holds values that are not finite
+
+    if (live && tree_here) {
+        // The tree: bf16 parts throughout.  n >= 1 here.
+        const T *const kt = static_cast<const T *>(p.kt), *const vt = static_cast<const T *>(p.vt);
+        uint4 qf[D / 16][NP];
+#pragma unroll
+        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, p.flip, qf[kk]);
+        for (int first = 0; first < n; first += kQ4Tile * KW) {  // the same number of rounds for every wavefront
+            const int base = first + kQ4Tile * w.kg;
+            q4_f32x16 s[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
+                const int key = min(base + 32 * kb + r, n - 1);
+                const T *const row = kt + (((size_t)b * p.T_max + key) * p.Hkv + kvh) * D + 8 * hh;
+                bool bad = false;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; kk++) {
+                    uint4 kf[NP];
+                    q4_eight(row + 16 * kk, 0, kf);
+                    if constexpr (F32) bad |= q4_take_out(kf[0]);  // the products of its parts would be NaN
+#pragma unroll
+                    for (int x = 0; x < NP; x++)
+#pragma unroll
+                        for (int y = 0; x + y < NP; y++)
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q4_bf16x8, kf[x]), __builtin_bit_cast(q4_bf16x8, qf[kk][y]),
+                                                                            s[kb], 0, 0, 0);
+                }
+                if constexpr (F32)
+                    if (__any(bad)) {  // rare: these scores from the rows themselves
+                        for (int i = 0; i < 16; i++) {
+                            const int j = min(base + 32 * kb + 8 * (i >> 2) + 4 * hh + (i & 3), n - 1);
+                            const T *const kr = kt + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D, *const qr = static_cast<const T *>(p.q) + q_row;
+                            float sum = 0.f;
+                            for (int c = 0; c < D; c++) sum = fmaf(q4_elem(kr, c), q4_elem(qr, c), sum);
+                            s[kb][i] = p.flip ? -sum : sum;
+                        }
+                    }
+            }
+            uint64_t vis = 0;
+            if (base < n && t < n) {
+                vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)];
+                if (n - base < 64) vis &= (1ull << (n - base)) - 1;
+            }
+            q4_bf16x8 pf[NP][2][2];
+            w.template softmax<true>(s, vis, pf);
+            // V, one bf16 part of it at a time
+            const auto stage_part = [&](int part) {
+                uint8_t *const tile = w.tile();
+                for (int c = w.lane + 64 * w.wr; c < kQ4Tile * D / 8; c += 64 * RW) {
+                    const int key = c / (D / 8), piece = c % (D / 8);
+                    uint4 vf[NP];
+                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, 0, vf);
+                    if constexpr (F32) {
+                        uint4 first_part = vf[0];
+                        const bool bad = q4_take_out(first_part);
+                        ill |= bad && base + key < n;
+                        if (bad) {  // the other parts of such a value are NaN
+                            uint4 &x = vf[1], &y = vf[2];
+                            const auto only = [](uint32_t hi, uint32_t v) { return v & ~(((((hi & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu); };
+                            x = uint4{only(vf[0].x, x.x), only(vf[0].y, x.y), only(vf[0].z, x.z), only(vf[0].w, x.w)};
+                            y = uint4{only(vf[0].x, y.x), only(vf[0].y, y.y), only(vf[0].z, y.z), only(vf[0].w, y.w)};
+                        }
+                        vf[0] = first_part;
+                    } else {
+                        ill |= q4_take_out(vf[0]) && base + key < n;
+                    }
+                    uint4 v = vf[0];
+                    if constexpr (F32) v = part == 0 ? vf[0] : part == 1 ? vf[1] : vf[2];
+                    if (base + key >= n) v = uint4{0, 0, 0, 0};
+                    *reinterpret_cast<uint4 *>(tile + key * G::ROW + ((piece ^ q4_swizzle<D>(key)) << 4)) = v;
+                }
+                w.staged();
+            };
+            stage_part(0);
+            w.template accumulate<NP>(w.tile(), pf);
+            w.stage++;
+            if constexpr (F32) {
+                stage_part(1);
+                w.template accumulate<2>(w.tile(), pf);
+                w.stage++;
+                stage_part(2);
+                w.template accumulate<1>(w.tile(), pf);
+                w.stage++;
+            }
+        }
+    }
+
+    if (live && k0 < k1) {
+        // q as six-bit parts; a group with something that is not finite is NaN
+        q4_u32x6 qp[NQ][KM];
+        uint32_t qs[QW][KM];
+#pragma unroll
+        for (int i = 0; i < KM; i++) {
+            const T *const src = static_cast<const T *>(p.q) + q_row + 32 * (2 * i + hh);
+            float x[32];
+#pragma unroll
+            for (int c = 0; c < 32; c += 8) {
+                if constexpr (F32) {
+                    const float4 a = *reinterpret_cast<const float4 *>(src + c), d = *reinterpret_cast<const float4 *>(src + c + 4);
+                    x[c] = a.x; x[c + 1] = a.y; x[c + 2] = a.z; x[c + 3] = a.w; x[c + 4] = d.x; x[c + 5] = d.y; x[c + 6] = d.z; x[c + 7] = d.w;
+                } else {
+                    const uint4 a = *reinterpret_cast<const uint4 *>(src + c);
+                    const uint32_t ws[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int j = 0; j < 4; j++) { x[c + 2 * j] = __uint_as_float(ws[j] << 16); x[c + 2 * j + 1] = __uint_as_float(ws[j] & 0xffff0000u); }
+                }
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < 32; c++) {
+                x[c] = __uint_as_float(__float_as_uint(x[c]) ^ (p.flip & 0x80000000u));
+                top = max(top, __float_as_uint(x[c]) & 0x7fffffffu);
+            }
+            const uint32_t e = max(top >> 23, 4 * NQ + 2u) - 2;  // every part's scale byte is at least 1
+            qs[0][i] = e | (e - 4) << 8 | (e - 8) << 16 | (NQ > 3 ? (e - 12) << 24 : 0u);
+            if constexpr (NQ > 3) qs[QW - 1][i] = (e - 16) | (e - 20) << 8;
+            if (top >= 0x7f800000u)
+                for (int j = 0; j < QW; j++) qs[j][i] = 0xffffffffu;
+#pragma unroll
+            for (int y = 0; y < NQ; y++) {
+                const float scale = __uint_as_float((e - 4 * y) << 23);
+                q4_f32x16 even, odd;  // the instruction takes two of 16 and interleaves them
+#pragma unroll
+                for (int c = 0; c < 16; c++) { even[c] = x[2 * c]; odd[c] = x[2 * c + 1]; }
+                qp[y][i] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+                if (y + 1 < NQ) {
+                    const q4_f32x32 done = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(qp[y][i], scale);
+#pragma unroll
+                    for (int c = 0; c < 32; c++) x[c] -= done[c];
+                }
+            }
+        }
+
+        // What a lane reads of a tile: of key row r of both key blocks the groups 2i + hh (K: all; V: pieces shared out over RW).
+        constexpr int NC = 2 * KM, VC = (NC + RW - 1) / RW;  // pieces (key block, i) of a lane's two rows; of V per wavefront
+        uint4 kc[2][KM], vc[VC];
+        uint32_t ks[2], vs[2];
+        int ids[2] = {0, 0}, at[2] = {0, 0};
+        const bool paged = p.block_size != 0;
+        const auto fetch_ids = [&](int base) {  // where a tile's rows are; positions are held within the split
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++) {
+                const int pos = min(base + 32 * kb + r, k1 - 1);
+                at[kb] = pos;
+                if (paged) {
+                    uint32_t off;
+                    ids[kb] = p.block_table[(size_t)b * p.max_blocks + fast_div((uint32_t)pos, (uint32_t)p.block_size, p.inv_bs, off)];
+                    at[kb] = (int)off;
+                }
+            }
+        };
+        const auto load_tile = [&](int base) {
+            uint64_t row[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++) {
+                bool known = true;
+                if (paged) {
+                    known = ids[kb] >= 0 && ids[kb] < p.num_blocks;
+                    row[kb] = (uint64_t)(uint32_t)(known ? ids[kb] : 0) * (uint32_t)(p.Hkv * p.block_size) + (uint32_t)((int)kvh * p.block_size + at[kb]);
+                } else {
+                    row[kb] = ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap + (uint32_t)at[kb];
+                }
+#pragma unroll
+                for (int i = 0; i < KM; i++) kc[kb][i] = *reinterpret_cast<const uint4 *>(p.codes[0] + row[kb] * (D / 2) + 16 * (2 * i + hh));
+                if constexpr (D == 128) {
+                    ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + row[kb] * 4) >> (8 * hh);
+                    vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + row[kb] * 4) >> (8 * hh);
+                } else {
+                    ks[kb] = p.scales[0][row[kb] * 2 + hh];
+                    vs[kb] = p.scales[1][row[kb] * 2 + hh];
+                }
+                if (!known) ks[kb] = 0xffffffffu;
+                if (!known || base + 32 * kb + r >= k1) vs[kb] = 0x7f7f7f7fu;  // weighs nothing, and is a number
+            }
+#pragma unroll
+            for (int j = 0; j < VC; j++) {
+                const int c = min(j * RW + w.wr, NC - 1), kb = c / KM, i = c % KM;
+                vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
+            }
+        };
+        const int span = kQ4Tile * KW, mine = k0 + kQ4Tile * w.kg;
+        fetch_ids(mine);
+        load_tile(mine);
+        fetch_ids(mine + span);
+        for (int first = k0; first < k1; first += span) {
+            const int base = first + kQ4Tile * w.kg;
+            uint8_t *const tile = w.tile();
+#pragma unroll
+            for (int j = 0; j < VC; j++) {
+                const int c = j * RW + w.wr, kb = c / KM, i = c % KM;
+                if (NC % RW != 0 && c >= NC) break;  // uniform
+                const float f = q4_scale((kb ? vs[1] : vs[0]) >> (16 * i) & 255u);
+                const uint32_t in[4] = {vc[j].x, vc[j].y, vc[j].z, vc[j].w};
+                uint8_t *const row = tile + (32 * kb + r) * G::ROW;
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    uint4 v;
+                    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 0));
+                    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 1));
+                    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 2));
+                    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 3));
+                    *reinterpret_cast<uint4 *>(row + (((4 * (2 * i + hh) + x) ^ q4_swizzle<D>(r)) << 4)) = v;
+                }
+            }
+            q4_f32x16 s[2];
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[0][i] = s[1][i] = 0.f;
+#define Q4_PART(y)                                                                                  \
+    s[0] = q4_scores<0, (y) & 3>(kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                   \
+    s[1] = q4_scores<0, (y) & 3>(kc[1][0], qp[y][0], s[1], ks[1], qs[(y) >> 2][0]);                   \
+    if constexpr (KM == 2) {                                                                        \
+        s[0] = q4_scores<2, (y) & 3>(kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]); \
+        s[1] = q4_scores<2, (y) & 3>(kc[1][KM - 1], qp[y][KM - 1], s[1], ks[1], qs[(y) >> 2][KM - 1]); \
+    }
+            Q4_PART(0)
+            Q4_PART(1)
+            Q4_PART(2)
+            if constexpr (NQ > 3) {
+                Q4_PART(3)
+                Q4_PART(4)
+                Q4_PART(5)
+            }
+#undef Q4_PART
+            if (first + span < k1) {
+                load_tile(base + span);
+                fetch_ids(base + 2 * span);
+            }
+            q4_bf16x8 pf[NP][2][2];
+            if (base + kQ4Tile <= k1) w.template softmax<false>(s, 0, pf);
+            else w.template softmax<true>(s, base < k1 ? (1ull << (k1 - base)) - 1 : 0, pf);
+            w.staged();
+            w.template accumulate<NP>(tile, pf);
+            w.stage++;
+        }
+    }
+
+    w.l = q4_half_sum(w.l);
+    // Values of the tree's V that are not finite were left out: added here to the rows that see them, whose outputs are then
+    // not finite whatever the weight.  (The barriers also end the last reads of the V tiles.)
+    __shared__ int s_ill;
+    if (tid == 0) s_ill = 0;
+    __syncthreads();
+    if (ill) s_ill = 1;
+    __syncthreads();
+    if (s_ill) {
+        for (int j = 0; j < n; j++) {
+            if ((j / kQ4Tile) % KW != w.kg) continue;  // uniform: each key once
+            const bool see = t < n && (p.bitmask[((size_t)b * p.T_max + min(t, p.T_max - 1)) * p.words + (j >> 6)] >> (j & 63) & 1);
+            const T *const row = static_cast<const T *>(p.vt) + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D + 4 * hh;
+#pragma unroll
+            for (int db = 0; db < DB; db++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    const float v = q4_elem(row, 32 * db + 8 * (i >> 2) + (i & 3));
+                    if (see && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) w.o[db][i] += v;
+                }
+        }
+    }
+
+    // Outputs through LDS: the key groups of a row are joined, and rows are stored in one piece.
+    float *const mine = reinterpret_cast<float *>(q4_smem) + wave * 32 * G::OUT_ROW + r * G::OUT_ROW + 4 * hh;
+    float2 *const ml = reinterpret_cast<float2 *>(q4_smem + 4 * 32 * G::OUT_ROW * 4);
+#pragma unroll
+    for (int db = 0; db < DB; db++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4 *>(mine + 32 * db + 2 * i) = float4{w.o[db][i], w.o[db][i + 1], w.o[db][i + 2], w.o[db][i + 3]};
+    if (hh == 0) ml[wave * 32 + r] = float2{w.m, w.l};
+    __syncthreads();
+    for (int c = tid; c < 32 * RW * (D / 8); c += 256) {
+        const int row = c / (D / 8), piece = c % (D / 8), chunk = row / 32;  // chunk: the wavefront among the RW
+        const uint32_t packed = group * 32 * RW + row;
+        uint32_t gg;
+        const int tt = (int)fast_div(packed, (uint32_t)p.G, p.inv_g, gg);
+        float ref = -INFINITY, sum = 0.f, acc[8] = {};
+#pragma unroll
+        for (int x = 0; x < KW; x++) ref = fmaxf(ref, ml[(x * RW + chunk) * 32 + (row & 31)].x);
+        const float zero = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+        for (int x = 0; x < KW; x++) {
+            const float2 part = ml[(x * RW + chunk) * 32 + (row & 31)];
+            const float f = KW == 1 ? 1.f : __builtin_amdgcn_exp2f(part.x - zero);
+            const float *const src = reinterpret_cast<const float *>(q4_smem) + ((x * RW + chunk) * 32 + (row & 31)) * G::OUT_ROW + 8 * piece;
+            sum += f * part.y;
+#pragma unroll
+            for (int j = 0; j < 8; j++) acc[j] += f * src[j];
+        }
+        if (!whole) {
+            if (tt >= n) continue;
+            const size_t at = ((size_t)bh * p.slots + slot) * (size_t)(p.row_groups * 32 * RW) + packed;
+            float4 *const dst = reinterpret_cast<float4 *>(p.part_o + at * D + 8 * piece);
+            dst[0] = float4{acc[0], acc[1], acc[2], acc[3]};
+            dst[1] = float4{acc[4], acc[5], acc[6], acc[7]};
+            if (piece == 0) p.part_ml[at] = float2{ref, sum};
+            continue;
+        }
+        if (tt >= p.T_max) continue;
+        const int head = (int)kvh * p.G + (int)gg;
+        q4_finish<T>(p, b, tt, head, piece, D, tt < n, ref, sum, acc);
+    }
+}
+
+// The partials of a row joined, split by split and the tree's last.  A thread has eight channels; grid (ceil(T_max * Hq / (2048 / D)), B).
+template <int D, bool F32>
+__global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p, int rows_padded) {
+    using T = std::conditional_t<F32, float, uint16_t>;
+    const int b = blockIdx.y, piece = threadIdx.x % (D / 8), x = blockIdx.x * (2048 / D) + threadIdx.x / (D / 8);
+    if (x >= p.T_max * p.Hq) return;
+    const int t = x / p.Hq, head = x % p.Hq, kvh = head / p.G;
+    const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max), used = (P + p.chunk - 1) / p.chunk;
+    float ref = -INFINITY, sum = 0.f, acc[8] = {};
+    if (t < n) {
+        const size_t row0 = ((size_t)(b * p.Hkv + kvh) * p.slots) * rows_padded + (size_t)t * p.G + head % p.G;
+        const auto slot_of = [&](int s) { return s == used ? p.nsplit : s; };
+        for (int s = 0; s <= used; s++) ref = fmaxf(ref, p.part_ml[row0 + (size_t)slot_of(s) * rows_padded].x);
+        const float zero = ref == -INFINITY ? 0.f : ref;
+        for (int s = 0; s <= used; s++) {
+            const size_t at = row0 + (size_t)slot_of(s) * rows_padded;
+            const float2 ml = p.part_ml[at];
+            const float f = __builtin_amdgcn_exp2f(ml.x - zero);
+            const float4 a = reinterpret_cast<const float4 *>(p.part_o + at * D + 8 * piece)[0], c = reinterpret_cast<const float4 *>(p.part_o + at * D + 8 * piece)[1];
+            sum += f * ml.y;
+            acc[0] += f * a.x; acc[1] += f * a.y; acc[2] += f * a.z; acc[3] += f * a.w;
+            acc[4] += f * c.x; acc[5] += f * c.y; acc[6] += f * c.z; acc[7] += f * c.w;
+        }
+    }
+    q4_finish<T>(p, b, t, head, piece, D, t < n, ref, sum, acc);
+}
+
 // What is wrong with a descriptor by itself.
 static int32_t q4_check_desc(const etv_attn_desc *h) {
     if (!h) return ETV_ERR_INVALID_ARG;
@@ -134,14 +724,77 @@ static int32_t q4_check_desc(const etv_attn_desc *h) {
     if (h->P_max < 0 || h->kv_split < 0 || h->block_size < 0) return ETV_ERR_INVALID_ARG;
     if (h->block_size % 16 != 0) return ETV_ERR_UNSUPPORTED;
     if (h->block_size > 0 && (h->max_blocks < 1 || h->num_blocks < 1)) return ETV_ERR_INVALID_ARG;
+    if ((int64_t)h->Hkv * h->block_size > INT32_MAX || h->P_max > INT32_MAX - 4096) return ETV_ERR_UNSUPPORTED;
     if (h->P_max > (h->block_size > 0 ? (int64_t)h->max_blocks * h->block_size : (int64_t)h->P_cap)) return ETV_ERR_INVALID_ARG;
-    if (h->scale != h->scale || (h->flags & ~ETV_ATTN_FLAG_GENERIC) != 0) return ETV_ERR_INVALID_ARG;
+    if (h->scale != 0.f && !(fabsf(h->scale) >= 1e-30f && fabsf(h->scale) <= 1e30f)) return ETV_ERR_INVALID_ARG;  // also NaN
+    if ((h->flags & ~ETV_ATTN_FLAG_GENERIC) != 0) return ETV_ERR_INVALID_ARG;
     return ETV_OK;
+}
+
+struct Q4Plan {
+    int rw, row_groups, chunk, nsplit, slots;
+    int64_t units;
+    size_t rows() const { return (size_t)units * row_groups * 32 * rw; }
+    size_t workspace(int d) const { return slots == 1 ? 256 : rows() * ((size_t)d * 4 + 8) + 256; }
+};
+
+static Q4Plan q4_plan(const etv_attn_desc *h) {
+    Q4Plan pl{};
+    const int rows = h->T_max * (h->Hq / h->Hkv);
+    pl.rw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    pl.row_groups = (rows + 32 * pl.rw - 1) / (32 * pl.rw);
+    const int span = kQ4Tile * (4 / pl.rw);
+    const int64_t seqs = (int64_t)std::max(1, h->B) * h->Hkv;
+    const int tiles = std::max(1, (h->P_max + span - 1) / span);  // rounds of a workgroup over the longest prefix
+    int best = 1;
+    if (h->kv_split > 0) {
+        pl.chunk = (h->kv_split + 63) / 64 * 64;
+        best = std::max(1, (int)((h->P_max + (int64_t)pl.chunk - 1) / pl.chunk));
+    } else {
+        // two workgroups a compute unit; a round costs 1, starting and joining a workgroup 3, the second launch 5 and a little more for
+        // every split whose rows it reads
+        double least = 1e30;
+        for (int ns = 1; ns <= std::min(tiles, 256); ns++) {
+            const int per = (tiles + ns - 1) / ns;
+            if (ns > 1 && (tiles + per - 1) / per != ns) continue;
+            const double full = (double)seqs * pl.row_groups * ns / 512, turns = full < 4 ? std::ceil(full) : full + 0.5;
+            const double cost = turns * (3 + per) + (ns > 1 ? 5 + 0.1 * ns + 3e-5 * (double)seqs * rows * ns : (h->T_max + span - 1) / span);
+            if (cost < least) least = cost, best = ns, pl.chunk = per * span;
+        }
+    }
+    pl.nsplit = best;
+    pl.slots = best == 1 ? 1 : best + 1;
+    pl.units = seqs * pl.slots;
+    return pl;
+}
+
+template <int D, bool F32, int RW>
+static int32_t launch_q4(const Q4Attn &p, unsigned grid, hipStream_t st) {
+    constexpr int lds = Q4Geo<D, RW>::LDS;
+    static_assert(lds <= 80 * 1024, "two workgroups a compute unit");
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) {
+        g_last_hip_error = (int32_t)e;
+        return ETV_ERR_HIP;
+    }
+    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW>), dim3(grid), dim3(256), lds, st, p);
+    return check_launch();
+}
+
+template <int D, bool F32>
+static int32_t run_q4(const Q4Plan &pl, const Q4Attn &p, hipStream_t st) {
+    const unsigned grid = (unsigned)((pl.units + 7) / 8 * 8 * pl.row_groups);
+    const int32_t rc = pl.rw == 1 ? launch_q4<D, F32, 1>(p, grid, st) : pl.rw == 2 ? launch_q4<D, F32, 2>(p, grid, st) : launch_q4<D, F32, 4>(p, grid, st);
+    if (rc != ETV_OK || pl.slots == 1) return rc;
+    hipLaunchKernelGGL((join_q4_kernel<D, F32>), dim3((p.T_max * p.Hq + 2048 / D - 1) / (2048 / D), p.B), dim3(256), 0, st, p, pl.row_groups * 32 * pl.rw);
+    return check_launch();
 }
 
 }  // namespace etv
 
-extern "C" size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h) { return etv::q4_check_desc(h) == ETV_OK ? 256 : 0; }
+extern "C" size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h) {
+    return etv::q4_check_desc(h) == ETV_OK ? etv::q4_plan(h).workspace(h->d) : 0;
+}
 
 extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const void *q, const uint8_t *k_codes, const uint8_t *k_scales,
                                                 const uint8_t *v_codes, const uint8_t *v_scales, const int32_t *block_table,
@@ -157,7 +810,10 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
                             (uintptr_t)workspace;
     if (align & 15 || ((uintptr_t)k_scales | (uintptr_t)v_scales) & 3) return ETV_ERR_INVALID_ARG;
     if (h->B == 0) return ETV_OK;
-    (void)workspace_bytes;
+    const etv::Q4Plan pl = etv::q4_plan(h);
+    const bool generic = (h->flags & ETV_ATTN_FLAG_GENERIC) != 0;
+    if (!generic && pl.units * pl.row_groups > INT32_MAX - 65536) return ETV_ERR_UNSUPPORTED;
+    if (!generic && pl.slots > 1 && (!workspace || workspace_bytes < pl.workspace(h->d))) return ETV_ERR_WORKSPACE_TOO_SMALL;
     etv::Q4Attn p{};
     p.q = q; p.kt = kt; p.vt = vt;
     p.codes[0] = k_codes; p.codes[1] = v_codes; p.scales[0] = k_scales; p.scales[1] = v_scales;
@@ -168,11 +824,24 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
     p.words = (h->T_max + 63) / 64;
     p.inv_bs = h->block_size ? etv::fast_div_inv(h->block_size) : 0;
     p.scale_log2 = (h->scale == 0.f ? 1.0f / sqrtf((float)h->d) : h->scale) * 1.4426950408889634f;
-    const dim3 grid(h->T_max, h->Hq, h->B);
     hipStream_t st = etv::as_stream(stream);
-    if (h->dtype == ETV_F32 && h->d == 64) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<float, 64>), grid, dim3(64), 0, st, p);
-    else if (h->dtype == ETV_F32) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<float, 128>), grid, dim3(64), 0, st, p);
-    else if (h->d == 64) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 64>), grid, dim3(64), 0, st, p);
-    else hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 128>), grid, dim3(64), 0, st, p);
-    return etv::check_launch();
+    if (generic) {
+        const dim3 grid(h->T_max, h->Hq, h->B);
+        if (h->dtype == ETV_F32 && h->d == 64) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<float, 64>), grid, dim3(64), 0, st, p);
+        else if (h->dtype == ETV_F32) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<float, 128>), grid, dim3(64), 0, st, p);
+        else if (h->d == 64) hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 64>), grid, dim3(64), 0, st, p);
+        else hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 128>), grid, dim3(64), 0, st, p);
+        return etv::check_launch();
+    }
+    p.flip = p.scale_log2 < 0 ? 0x80008000u : 0;
+    p.scale_log2 = fabsf(p.scale_log2);
+    p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.units = (int)pl.units;
+    p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_slots = etv::fast_div_inv(p.slots);
+    p.inv_groups = etv::fast_div_inv(p.row_groups);
+    if (pl.slots > 1) {
+        p.part_o = static_cast<float *>(workspace);
+        p.part_ml = reinterpret_cast<float2 *>(p.part_o + pl.rows() * h->d);
+    }
+    if (h->dtype == ETV_F32) return h->d == 64 ? etv::run_q4<64, true>(pl, p, st) : etv::run_q4<128, true>(pl, p, st);
+    return h->d == 64 ? etv::run_q4<64, false>(pl, p, st) : etv::run_q4<128, false>(pl, p, st);
 }

@@ -64,7 +64,7 @@ def attn_desc(**kw):
 @pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(T_max=0), -1), (dict(T_max=257), -2), (dict(Hq=9), -1), (dict(Hkv=0), -1), (dict(d=96), -2),
                                    (dict(dtype=7), -2), (dict(block_size=8), -2), (dict(block_size=-16), -1), (dict(num_blocks=0), -1),
                                    (dict(max_blocks=0), -1), (dict(P_max=145), -1), (dict(P_max=-1), -1), (dict(block_size=0, P_cap=99), -1),
-                                   (dict(kv_split=-1), -1), (dict(flags=api.ATTN_FLAG_WIDE), -1), (dict(scale=float("nan")), -1),
+                                   (dict(kv_split=-1), -1), (dict(flags=api.ATTN_FLAG_WIDE), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(scale=1e-38), -1),
                                    (dict(B=70000), -2), (dict(B=0), 0)])
 def test_attention_descriptors(kw, rc):
     assert attend(attn_desc(**kw)) == rc
