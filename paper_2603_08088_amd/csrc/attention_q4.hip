@@ -24,7 +24,7 @@ struct Q4Attn {
     // matrix kernel: a sequence's prefix in splits of `chunk` keys, one slot each, and with more than one split a slot more for
     // the tree.  Partials, if slots > 1: part_o [B * Hkv][slots][row_groups * 32 * RW][D], part_ml (reference, sum) alike.
     int chunk, nsplit, slots, row_groups, units;
-    uint32_t inv_g, inv_hkv, inv_slots, inv_groups;
+    uint32_t inv_g, inv_hkv, inv_seqs, inv_groups;
     float *part_o;
     float2 *part_ml;
 };
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
 
 // ------------------------------------------------------------------------------------------------
 // The matrix kernel.  With the G * T_max query rows of a KV head packed into rows r = t * G + g, a wavefront has 32 of them and
-// takes 64 keys at a time:
+// takes 32 or 64 keys at a time:
 //   S^T[key, r]  = K Q^T     v_mfma_scale_f32_32x32x64_f8f6f4: K as the cache holds it (fp4, its scale bytes the instruction's),
 //                            16 bytes a lane straight from memory, q in NQ parts of 6 bits (e2m3)
 //   P^T          = exp2(S^T * scale - reference)   a lane has 32 keys of one row; the reference follows the maximum lazily
@@ -159,18 +159,32 @@ typedef __bf16 q4_bf16x8 __attribute__((ext_vector_type(8)));
 typedef short q4_s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
 
-constexpr int kQ4Tile = 64;      // keys
 constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the reference before the outputs are rescaled
 
-// Dynamic LDS: V tiles [key groups][2 if rows are shared out, else 1][64][D] bf16, afterwards the outputs [4][32][D + 4] fp32.
+// Dynamic LDS: V tiles [key groups][2 if rows are shared out, else 1][keys][D] bf16, afterwards 64 channels at a time of the
+// outputs [4][32][64 + 4] fp32.
 template <int D, int RW>
 struct Q4Geo {
-    static constexpr int ROW = 2 * D, TILE = kQ4Tile * ROW, KW = 4 / RW, BUFS = RW > 1 ? 2 : 1;
-    static constexpr int OUT_ROW = D + 4;  // floats; four on from a multiple of the banks
+    static constexpr int KB = RW == 1 ? 1 : 2, KEYS = 32 * KB;  // key blocks and keys of a tile
+    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = RW > 1 ? 2 : 1;
+    static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
     static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
 };
 
+// 32 values to six bits (e2m3) and back.  These conversions work in several passes and read their scale in each, so
+// the result must not lie on an operand.  The builtins let it lie on the scale (q then lost its lower parts, in a build with
+// fewer registers): hence the early-clobbered results, and the wait states a following matrix instruction may need.
+__device__ __forceinline__ q4_u32x6 q4_to_six_bits(q4_f32x16 even, q4_f32x16 odd, float scale) {
+    q4_u32x6 r;
+    asm volatile("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 7" : "=&v"(r) : "v"(even), "v"(odd), "v"(scale));
+    return r;
+}
+__device__ __forceinline__ q4_f32x32 q4_from_six_bits(q4_u32x6 x, float scale) {
+    q4_f32x32 r;
+    asm volatile("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 7" : "=&v"(r) : "v"(x), "v"(scale));
+    return r;
+}
 template <int OPA, int OPB>
 __device__ __forceinline__ q4_f32x16 q4_scores(uint4 k, q4_u32x6 q, q4_f32x16 c, uint32_t k_scale, uint32_t q_scale) {
     const q4_i32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0}, b = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0};
@@ -209,6 +223,7 @@ template <int D, bool F32, int RW>
 struct Q4Wave {
     static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 3, QW = F32 ? 2 : 1;
     using G = Q4Geo<D, RW>;
+    static constexpr int KB = G::KB;
     const Q4Attn &p;
     uint8_t *smem;
     int lane, r, hh, kg, wr, stage;
@@ -227,19 +242,19 @@ struct Q4Wave {
         asm volatile("" ::: "memory");
     }
 
-    // P^T of 64 keys from their scores; key 32 kb + x is seen where bit x of vis[kb] is set (MASKED).
+    // P^T of a tile from its scores; key x is seen where bit x of vis is set (MASKED).
     template <bool MASKED>
-    __device__ __forceinline__ void softmax(q4_f32x16 (&s)[2], uint64_t vis, q4_bf16x8 (&pf)[NP][2][2]) {
+    __device__ __forceinline__ void softmax(q4_f32x16 (&s)[KB], uint64_t vis, q4_bf16x8 (&pf)[NP][KB][2]) {
         if (MASKED) {
             const uint32_t v[2] = {(uint32_t)vis >> (4 * hh), (uint32_t)(vis >> 32) >> (4 * hh)};
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++)
+            for (int kb = 0; kb < KB; kb++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
         }
-        float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+        float top = __builtin_elementwise_maximum(s[0][0], s[KB - 1][15]);
 #pragma unroll
-        for (int i = 1; i < 16; i++) top = q4_max3(top, s[0][i], s[1][i]);
+        for (int i = 1; i < 16; i++) top = KB == 2 ? q4_max3(top, s[0][i], s[KB - 1][i - 1]) : i & 1 ? q4_max3(top, s[0][i], s[0][i & 14]) : top;
         top = q4_half_max(top) * p.scale_log2;
         const bool lift = top > m + kQ4Lazy;
         if (__any(lift)) {
@@ -252,28 +267,29 @@ struct Q4Wave {
                 for (int i = 0; i < 16; i++) o[db][i] *= alpha;
         }
         const float off = m == -INFINITY ? 0.f : -m;
-        float sum[2] = {0.f, 0.f};
-        uint32_t pk[NP][2][8];
+        float sum[2] = {0.f, 0.f};  // two chains
+        uint32_t pk[NP][KB][8];
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
+        for (int kb = 0; kb < KB; kb++)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, off)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][i + 1], p.scale_log2, off));
                 if constexpr (F32) {
                     q4_split(a, b, pk[0][kb][i >> 1], pk[1][kb][i >> 1], pk[NP - 1][kb][i >> 1]);
-                    sum[kb] += a + b;
+                    sum[KB == 2 ? kb : i >> 1 & 1] += a + b;
                 } else {
                     // the weights rounded to bf16 are the weights: the sum takes them as the product does
                     pk[0][kb][i >> 1] = q4_pair(a, b);
-                    sum[kb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i >> 1]),
-                                                              __builtin_bit_cast(q4_bf16x2, 0x3f803f80u), sum[kb], false);
+                    float &part = sum[KB == 2 ? kb : i >> 1 & 1];
+                    part = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i >> 1]),
+                                                           __builtin_bit_cast(q4_bf16x2, 0x3f803f80u), part, false);
                 }
             }
         l += sum[0] + sum[1];
 #pragma unroll
         for (int x = 0; x < NP; x++)
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++)
+            for (int kb = 0; kb < KB; kb++)
 #pragma unroll
                 for (int st = 0; st < 2; st++)
                     pf[x][kb][st] = __builtin_bit_cast(q4_bf16x8, (uint4{pk[x][kb][4 * st], pk[x][kb][4 * st + 1], pk[x][kb][4 * st + 2], pk[x][kb][4 * st + 3]}));
@@ -281,11 +297,11 @@ struct Q4Wave {
 
     // O^T += V^T P^T over the tile, with the first `parts` of P
     template <int PARTS>
-    __device__ __forceinline__ void accumulate(const uint8_t *v, const q4_bf16x8 (&pf)[NP][2][2]) {
+    __device__ __forceinline__ void accumulate(const uint8_t *v, const q4_bf16x8 (&pf)[NP][KB][2]) {
         const int i16 = lane & 15, vrow = 4 * hh + (i16 >> 2), piece = 2 * (lane >> 4 & 1) + ((i16 & 3) >> 1), sub = 8 * (i16 & 1);
         const int sw = q4_swizzle<D>(vrow);
 #pragma unroll
-        for (int kb = 0; kb < 2; kb++)
+        for (int kb = 0; kb < KB; kb++)
 #pragma unroll
             for (int st = 0; st < 2; st++) {
                 const uint8_t *const row = v + (32 * kb + 16 * st + vrow) * G::ROW + sub;
@@ -347,7 +363,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
     using G = Q4Geo<D, RW>;
-    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW;
+    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS;
     extern __shared__ __attribute__((aligned(1024))) uint8_t q4_smem[];
     const int tid = threadIdx.x;
     Wave w{p, q4_smem};
@@ -370,7 +386,8 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     uint32_t group, slot, kvh;
     const uint32_t unit = fast_div(blockIdx.x >> 3, (uint32_t)p.row_groups, p.inv_groups, group) * 8 + (blockIdx.x & 7);
     if (unit >= (uint32_t)p.units) return;
-    const uint32_t bh = fast_div(unit, (uint32_t)p.slots, p.inv_slots, slot);
+    uint32_t bh;
+    slot = fast_div(unit, (uint32_t)(p.B * p.Hkv), p.inv_seqs, bh);  // the trees' workgroups, which are short, come last
     const int b = (int)fast_div(bh, (uint32_t)p.Hkv, p.inv_hkv, kvh);
     const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max);
     const bool whole = p.slots == 1, tree_here = whole || (int)slot == p.nsplit;
@@ -383,94 +400,6 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     const bool live = (int)fast_div(group * 32 * RW, (uint32_t)p.G, p.inv_g, rem) < n;  // has the workgroup a row?
     if (!live && !whole) return;
     bool ill = false;  // the tree's V holds values that are not finite
-
-    if (live && tree_here) {
-        // The tree: bf16 parts throughout.  n >= 1 here.
-        const T *const kt = static_cast<const T *>(p.kt), *const vt = static_cast<const T *>(p.vt);
-        uint4 qf[D / 16][NP];
-#pragma unroll
-        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, p.flip, qf[kk]);
-        for (int first = 0; first < n; first += kQ4Tile * KW) {  // the same number of rounds for every wavefront
-            const int base = first + kQ4Tile * w.kg;
-            q4_f32x16 s[2];
-#pragma unroll
-            for (int kb = 0; kb < 2; kb++) {
-#pragma unroll
-                for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
-                const int key = min(base + 32 * kb + r, n - 1);
-                const T *const row = kt + (((size_t)b * p.T_max + key) * p.Hkv + kvh) * D + 8 * hh;
-                bool bad = false;
-#pragma unroll
-                for (int kk = 0; kk < D / 16; kk++) {
-                    uint4 kf[NP];
-                    q4_eight(row + 16 * kk, 0, kf);
-                    if constexpr (F32) bad |= q4_take_out(kf[0]);  // the products of its parts would be NaN
-#pragma unroll
-                    for (int x = 0; x < NP; x++)
-#pragma unroll
-                        for (int y = 0; x + y < NP; y++)
-                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q4_bf16x8, kf[x]), __builtin_bit_cast(q4_bf16x8, qf[kk][y]),
-                                                                            s[kb], 0, 0, 0);
-                }
-                if constexpr (F32)
-                    if (__any(bad)) {  // rare: these scores from the rows themselves
-                        for (int i = 0; i < 16; i++) {
-                            const int j = min(base + 32 * kb + 8 * (i >> 2) + 4 * hh + (i & 3), n - 1);
-                            const T *const kr = kt + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D, *const qr = static_cast<const T *>(p.q) + q_row;
-                            float sum = 0.f;
-                            for (int c = 0; c < D; c++) sum = fmaf(q4_elem(kr, c), q4_elem(qr, c), sum);
-                            s[kb][i] = p.flip ? -sum : sum;
-                        }
-                    }
-            }
-            uint64_t vis = 0;
-            if (base < n && t < n) {
-                vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)];
-                if (n - base < 64) vis &= (1ull << (n - base)) - 1;
-            }
-            q4_bf16x8 pf[NP][2][2];
-            w.template softmax<true>(s, vis, pf);
-            // V, one bf16 part of it at a time
-            const auto stage_part = [&](int part) {
-                uint8_t *const tile = w.tile();
-                for (int c = w.lane + 64 * w.wr; c < kQ4Tile * D / 8; c += 64 * RW) {
-                    const int key = c / (D / 8), piece = c % (D / 8);
-                    uint4 vf[NP];
-                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, 0, vf);
-                    if constexpr (F32) {
-                        uint4 first_part = vf[0];
-                        const bool bad = q4_take_out(first_part);
-                        ill |= bad && base + key < n;
-                        if (bad) {  // the other parts of such a value are NaN
-                            uint4 &x = vf[1], &y = vf[2];
-                            const auto only = [](uint32_t hi, uint32_t v) { return v & ~(((((hi & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu); };
-                            x = uint4{only(vf[0].x, x.x), only(vf[0].y, x.y), only(vf[0].z, x.z), only(vf[0].w, x.w)};
-                            y = uint4{only(vf[0].x, y.x), only(vf[0].y, y.y), only(vf[0].z, y.z), only(vf[0].w, y.w)};
-                        }
-                        vf[0] = first_part;
-                    } else {
-                        ill |= q4_take_out(vf[0]) && base + key < n;
-                    }
-                    uint4 v = vf[0];
-                    if constexpr (F32) v = part == 0 ? vf[0] : part == 1 ? vf[1] : vf[2];
-                    if (base + key >= n) v = uint4{0, 0, 0, 0};
-                    *reinterpret_cast<uint4 *>(tile + key * G::ROW + ((piece ^ q4_swizzle<D>(key)) << 4)) = v;
-                }
-                w.staged();
-            };
-            stage_part(0);
-            w.template accumulate<NP>(w.tile(), pf);
-            w.stage++;
-            if constexpr (F32) {
-                stage_part(1);
-                w.template accumulate<2>(w.tile(), pf);
-                w.stage++;
-                stage_part(2);
-                w.template accumulate<1>(w.tile(), pf);
-                w.stage++;
-            }
-        }
-    }
 
     if (live && k0 < k1) {
         // q as six-bit parts; a group with something that is not finite is NaN
@@ -509,24 +438,24 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 q4_f32x16 even, odd;  // the instruction takes two of 16 and interleaves them
 #pragma unroll
                 for (int c = 0; c < 16; c++) { even[c] = x[2 * c]; odd[c] = x[2 * c + 1]; }
-                qp[y][i] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+                qp[y][i] = q4_to_six_bits(even, odd, scale);
                 if (y + 1 < NQ) {
-                    const q4_f32x32 done = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(qp[y][i], scale);
+                    const q4_f32x32 done = q4_from_six_bits(qp[y][i], scale);
 #pragma unroll
                     for (int c = 0; c < 32; c++) x[c] -= done[c];
                 }
             }
         }
 
-        // What a lane reads of a tile: of key row r of both key blocks the groups 2i + hh (K: all; V: pieces shared out over RW).
-        constexpr int NC = 2 * KM, VC = (NC + RW - 1) / RW;  // pieces (key block, i) of a lane's two rows; of V per wavefront
-        uint4 kc[2][KM], vc[VC];
-        uint32_t ks[2], vs[2];
-        int ids[2] = {0, 0}, at[2] = {0, 0};
+        // What a lane reads of a tile: of key row r of each key block the groups 2i + hh (K: all; V: pieces shared out over RW).
+        constexpr int NC = KB * KM, VC = (NC + RW - 1) / RW;  // pieces (key block, i) of a lane's rows; of V per wavefront
+        uint4 kc[KB][KM], vc[VC];
+        uint32_t ks[KB], vs[KB];
+        int ids[KB] = {}, at[KB] = {};
         const bool paged = p.block_size != 0;
         const auto fetch_ids = [&](int base) {  // where a tile's rows are; positions are held within the split
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++) {
+            for (int kb = 0; kb < KB; kb++) {
                 const int pos = min(base + 32 * kb + r, k1 - 1);
                 at[kb] = pos;
                 if (paged) {
@@ -537,9 +466,9 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             }
         };
         const auto load_tile = [&](int base) {
-            uint64_t row[2];
+            uint64_t row[KB];
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++) {
+            for (int kb = 0; kb < KB; kb++) {
                 bool known = true;
                 if (paged) {
                     known = ids[kb] >= 0 && ids[kb] < p.num_blocks;
@@ -562,21 +491,21 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
 #pragma unroll
             for (int j = 0; j < VC; j++) {
                 const int c = min(j * RW + w.wr, NC - 1), kb = c / KM, i = c % KM;
-                vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
+                vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
             }
         };
-        const int span = kQ4Tile * KW, mine = k0 + kQ4Tile * w.kg;
+        const int span = KEYS * KW, mine = k0 + KEYS * w.kg;
         fetch_ids(mine);
         load_tile(mine);
         fetch_ids(mine + span);
         for (int first = k0; first < k1; first += span) {
-            const int base = first + kQ4Tile * w.kg;
+            const int base = first + KEYS * w.kg;
             uint8_t *const tile = w.tile();
 #pragma unroll
             for (int j = 0; j < VC; j++) {
                 const int c = j * RW + w.wr, kb = c / KM, i = c % KM;
                 if (NC % RW != 0 && c >= NC) break;  // uniform
-                const float f = q4_scale((kb ? vs[1] : vs[0]) >> (16 * i) & 255u);
+                const float f = q4_scale((kb ? vs[KB - 1] : vs[0]) >> (16 * i) & 255u);
                 const uint32_t in[4] = {vc[j].x, vc[j].y, vc[j].z, vc[j].w};
                 uint8_t *const row = tile + (32 * kb + r) * G::ROW;
 #pragma unroll
@@ -589,15 +518,16 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                     *reinterpret_cast<uint4 *>(row + (((4 * (2 * i + hh) + x) ^ q4_swizzle<D>(r)) << 4)) = v;
                 }
             }
-            q4_f32x16 s[2];
+            q4_f32x16 s[KB];
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[0][i] = s[1][i] = 0.f;
-#define Q4_PART(y)                                                                                  \
-    s[0] = q4_scores<0, (y) & 3>(kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                   \
-    s[1] = q4_scores<0, (y) & 3>(kc[1][0], qp[y][0], s[1], ks[1], qs[(y) >> 2][0]);                   \
-    if constexpr (KM == 2) {                                                                        \
-        s[0] = q4_scores<2, (y) & 3>(kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]); \
-        s[1] = q4_scores<2, (y) & 3>(kc[1][KM - 1], qp[y][KM - 1], s[1], ks[1], qs[(y) >> 2][KM - 1]); \
+            for (int i = 0; i < 16; i++) s[0][i] = s[KB - 1][i] = 0.f;
+#define Q4_PART(y)                                                                                                     \
+    s[0] = q4_scores<0, (y) & 3>(kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                                      \
+    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(kc[KB - 1][0], qp[y][0], s[KB - 1], ks[KB - 1], qs[(y) >> 2][0]); \
+    if constexpr (KM == 2) {                                                                                           \
+        s[0] = q4_scores<2, (y) & 3>(kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]);                   \
+        if constexpr (KB == 2)                                                                                         \
+            s[KB - 1] = q4_scores<2, (y) & 3>(kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], ks[KB - 1], qs[(y) >> 2][KM - 1]); \
     }
             Q4_PART(0)
             Q4_PART(1)
@@ -612,12 +542,100 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 load_tile(base + span);
                 fetch_ids(base + 2 * span);
             }
-            q4_bf16x8 pf[NP][2][2];
-            if (base + kQ4Tile <= k1) w.template softmax<false>(s, 0, pf);
+            q4_bf16x8 pf[NP][KB][2];
+            if (base + KEYS <= k1) w.template softmax<false>(s, 0, pf);
             else w.template softmax<true>(s, base < k1 ? (1ull << (k1 - base)) - 1 : 0, pf);
             w.staged();
             w.template accumulate<NP>(tile, pf);
             w.stage++;
+        }
+    }
+
+    if (live && tree_here) {
+        // The tree: bf16 parts throughout.  n >= 1 here.
+        const T *const kt = static_cast<const T *>(p.kt), *const vt = static_cast<const T *>(p.vt);
+        uint4 qf[D / 16][NP];
+#pragma unroll
+        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, p.flip, qf[kk]);
+        for (int first = 0; first < n; first += KEYS * KW) {  // the same number of rounds for every wavefront
+            const int base = first + KEYS * w.kg;
+            q4_f32x16 s[KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
+                const int key = min(base + 32 * kb + r, n - 1);
+                const T *const row = kt + (((size_t)b * p.T_max + key) * p.Hkv + kvh) * D + 8 * hh;
+                bool bad = false;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; kk++) {
+                    uint4 kf[NP];
+                    q4_eight(row + 16 * kk, 0, kf);
+                    if constexpr (F32) bad |= q4_take_out(kf[0]);  // the products of its parts would be NaN
+#pragma unroll
+                    for (int x = 0; x < NP; x++)
+#pragma unroll
+                        for (int y = 0; x + y < NP; y++)
+                            s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q4_bf16x8, kf[x]), __builtin_bit_cast(q4_bf16x8, qf[kk][y]),
+                                                                            s[kb], 0, 0, 0);
+                }
+                if constexpr (F32)
+                    if (__any(bad)) {  // rare: these scores from the rows themselves
+                        for (int i = 0; i < 16; i++) {
+                            const int j = min(base + 32 * kb + 8 * (i >> 2) + 4 * hh + (i & 3), n - 1);
+                            const T *const kr = kt + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D, *const qr = static_cast<const T *>(p.q) + q_row;
+                            float sum = 0.f;
+                            for (int c = 0; c < D; c++) sum = fmaf(q4_elem(kr, c), q4_elem(qr, c), sum);
+                            s[kb][i] = p.flip ? -sum : sum;
+                        }
+                    }
+            }
+            uint64_t vis = 0;
+            if (base < n && t < n) {
+                vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)] >> (base & 63);
+                if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
+            }
+            q4_bf16x8 pf[NP][KB][2];
+            w.template softmax<true>(s, vis, pf);
+            // V, one bf16 part of it at a time
+            const auto stage_part = [&](int part) {
+                uint8_t *const tile = w.tile();
+                for (int c = w.lane + 64 * w.wr; c < KEYS * D / 8; c += 64 * RW) {
+                    const int key = c / (D / 8), piece = c % (D / 8);
+                    uint4 vf[NP];
+                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, 0, vf);
+                    if constexpr (F32) {
+                        uint4 first_part = vf[0];
+                        const bool bad = q4_take_out(first_part);
+                        ill |= bad && base + key < n;
+                        if (bad) {  // the other parts of such a value are NaN
+                            uint4 &x = vf[1], &y = vf[2];
+                            const auto only = [](uint32_t hi, uint32_t v) { return v & ~(((((hi & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu); };
+                            x = uint4{only(vf[0].x, x.x), only(vf[0].y, x.y), only(vf[0].z, x.z), only(vf[0].w, x.w)};
+                            y = uint4{only(vf[0].x, y.x), only(vf[0].y, y.y), only(vf[0].z, y.z), only(vf[0].w, y.w)};
+                        }
+                        vf[0] = first_part;
+                    } else {
+                        ill |= q4_take_out(vf[0]) && base + key < n;
+                    }
+                    uint4 v = vf[0];
+                    if constexpr (F32) v = part == 0 ? vf[0] : part == 1 ? vf[1] : vf[2];
+                    if (base + key >= n) v = uint4{0, 0, 0, 0};
+                    *reinterpret_cast<uint4 *>(tile + key * G::ROW + ((piece ^ q4_swizzle<D>(key)) << 4)) = v;
+                }
+                w.staged();
+            };
+            stage_part(0);
+            w.template accumulate<NP>(w.tile(), pf);
+            w.stage++;
+            if constexpr (F32) {
+                stage_part(1);
+                w.template accumulate<2>(w.tile(), pf);
+                w.stage++;
+                stage_part(2);
+                w.template accumulate<1>(w.tile(), pf);
+                w.stage++;
+            }
         }
     }
 
@@ -631,7 +649,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     __syncthreads();
     if (s_ill) {
         for (int j = 0; j < n; j++) {
-            if ((j / kQ4Tile) % KW != w.kg) continue;  // uniform: each key once
+            if ((j / KEYS) % KW != w.kg) continue;  // uniform: each key once
             const bool see = t < n && (p.bitmask[((size_t)b * p.T_max + min(t, p.T_max - 1)) * p.words + (j >> 6)] >> (j & 63) & 1);
             const T *const row = static_cast<const T *>(p.vt) + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D + 4 * hh;
 #pragma unroll
@@ -644,46 +662,51 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         }
     }
 
-    // Outputs through LDS: the key groups of a row are joined, and rows are stored in one piece.
-    float *const mine = reinterpret_cast<float *>(q4_smem) + wave * 32 * G::OUT_ROW + r * G::OUT_ROW + 4 * hh;
+    // Outputs through LDS, 64 channels at a time: the key groups of a row are joined, and rows are stored in one piece.
+    float *const mine = reinterpret_cast<float *>(q4_smem) + (wave * 32 + r) * G::OUT_ROW + 4 * hh;
     float2 *const ml = reinterpret_cast<float2 *>(q4_smem + 4 * 32 * G::OUT_ROW * 4);
-#pragma unroll
-    for (int db = 0; db < DB; db++)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4 *>(mine + 32 * db + 2 * i) = float4{w.o[db][i], w.o[db][i + 1], w.o[db][i + 2], w.o[db][i + 3]};
     if (hh == 0) ml[wave * 32 + r] = float2{w.m, w.l};
-    __syncthreads();
-    for (int c = tid; c < 32 * RW * (D / 8); c += 256) {
-        const int row = c / (D / 8), piece = c % (D / 8), chunk = row / 32;  // chunk: the wavefront among the RW
-        const uint32_t packed = group * 32 * RW + row;
-        uint32_t gg;
-        const int tt = (int)fast_div(packed, (uint32_t)p.G, p.inv_g, gg);
-        float ref = -INFINITY, sum = 0.f, acc[8] = {};
 #pragma unroll
-        for (int x = 0; x < KW; x++) ref = fmaxf(ref, ml[(x * RW + chunk) * 32 + (row & 31)].x);
-        const float zero = ref == -INFINITY ? 0.f : ref;
+    for (int half = 0; half < D / 64; half++) {
+        if (half) __syncthreads();
 #pragma unroll
-        for (int x = 0; x < KW; x++) {
-            const float2 part = ml[(x * RW + chunk) * 32 + (row & 31)];
-            const float f = KW == 1 ? 1.f : __builtin_amdgcn_exp2f(part.x - zero);
-            const float *const src = reinterpret_cast<const float *>(q4_smem) + ((x * RW + chunk) * 32 + (row & 31)) * G::OUT_ROW + 8 * piece;
-            sum += f * part.y;
+        for (int db = 0; db < 2; db++)
 #pragma unroll
-            for (int j = 0; j < 8; j++) acc[j] += f * src[j];
+            for (int i = 0; i < 16; i += 4) {
+                const q4_f32x16 &o = w.o[2 * half + db];
+                *reinterpret_cast<float4 *>(mine + 32 * db + 2 * i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            }
+        __syncthreads();
+        for (int c = tid; c < 32 * RW * 8; c += 256) {
+            const int row = c >> 3, piece = c & 7, chunk = row / 32;  // chunk: the wavefront among the RW
+            const uint32_t packed = group * 32 * RW + row;
+            uint32_t gg;
+            const int tt = (int)fast_div(packed, (uint32_t)p.G, p.inv_g, gg);
+            float ref = -INFINITY, sum = 0.f, acc[8] = {};
+#pragma unroll
+            for (int x = 0; x < KW; x++) ref = fmaxf(ref, ml[(x * RW + chunk) * 32 + (row & 31)].x);
+            const float zero = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+            for (int x = 0; x < KW; x++) {
+                const float2 part = ml[(x * RW + chunk) * 32 + (row & 31)];
+                const float f = KW == 1 ? 1.f : __builtin_amdgcn_exp2f(part.x - zero);
+                const float *const src = reinterpret_cast<const float *>(q4_smem) + ((x * RW + chunk) * 32 + (row & 31)) * G::OUT_ROW + 8 * piece;
+                sum += f * part.y;
+#pragma unroll
+                for (int j = 0; j < 8; j++) acc[j] += f * src[j];
+            }
+            if (!whole) {
+                if (tt >= n) continue;
+                const size_t at = ((size_t)bh * p.slots + slot) * (size_t)(p.row_groups * 32 * RW) + packed;
+                float4 *const dst = reinterpret_cast<float4 *>(p.part_o + at * D + 64 * half + 8 * piece);
+                dst[0] = float4{acc[0], acc[1], acc[2], acc[3]};
+                dst[1] = float4{acc[4], acc[5], acc[6], acc[7]};
+                if (piece == 0 && half == 0) p.part_ml[at] = float2{ref, sum};
+                continue;
+            }
+            if (tt >= p.T_max) continue;
+            q4_finish<T>(p, b, tt, (int)kvh * p.G + (int)gg, 8 * half + piece, D, tt < n, ref, sum, acc);
         }
-        if (!whole) {
-            if (tt >= n) continue;
-            const size_t at = ((size_t)bh * p.slots + slot) * (size_t)(p.row_groups * 32 * RW) + packed;
-            float4 *const dst = reinterpret_cast<float4 *>(p.part_o + at * D + 8 * piece);
-            dst[0] = float4{acc[0], acc[1], acc[2], acc[3]};
-            dst[1] = float4{acc[4], acc[5], acc[6], acc[7]};
-            if (piece == 0) p.part_ml[at] = float2{ref, sum};
-            continue;
-        }
-        if (tt >= p.T_max) continue;
-        const int head = (int)kvh * p.G + (int)gg;
-        q4_finish<T>(p, b, tt, head, piece, D, tt < n, ref, sum, acc);
     }
 }
 
@@ -743,7 +766,7 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     const int rows = h->T_max * (h->Hq / h->Hkv);
     pl.rw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     pl.row_groups = (rows + 32 * pl.rw - 1) / (32 * pl.rw);
-    const int span = kQ4Tile * (4 / pl.rw);
+    const int span = (pl.rw == 1 ? 32 : 64) * (4 / pl.rw);
     const int64_t seqs = (int64_t)std::max(1, h->B) * h->Hkv;
     const int tiles = std::max(1, (h->P_max + span - 1) / span);  // rounds of a workgroup over the longest prefix
     int best = 1;
@@ -836,7 +859,7 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
     p.flip = p.scale_log2 < 0 ? 0x80008000u : 0;
     p.scale_log2 = fabsf(p.scale_log2);
     p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.units = (int)pl.units;
-    p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_slots = etv::fast_div_inv(p.slots);
+    p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_seqs = etv::fast_div_inv(p.B * p.Hkv);
     p.inv_groups = etv::fast_div_inv(p.row_groups);
     if (pl.slots > 1) {
         p.part_o = static_cast<float *>(workspace);
