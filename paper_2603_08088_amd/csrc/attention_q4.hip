@@ -159,6 +159,8 @@ typedef __bf16 q4_bf16x8 __attribute__((ext_vector_type(8)));
 typedef short q4_s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
 
+// memory that no kernel writes while it is read: uniform addresses go through scalar loads
+typedef __attribute__((address_space(4))) const int32_t *const_ids;
 constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the reference before the outputs are rescaled
 
 // Dynamic LDS: V tiles [key groups][2 if rows are shared out, else 1][keys][D] bf16, afterwards 64 channels at a time of the
@@ -166,6 +168,7 @@ constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the refere
 template <int D, int RW>
 struct Q4Geo {
     static constexpr int KB = RW == 1 ? 1 : 2, KEYS = 32 * KB;  // key blocks and keys of a tile
+    static constexpr int AHEAD = RW == 1 ? 2 : 1;                // tiles whose codes are on their way
     static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = RW > 1 ? 2 : 1;
     static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
     static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
@@ -242,16 +245,17 @@ struct Q4Wave {
         asm volatile("" ::: "memory");
     }
 
-    // P^T of a tile from its scores; key x is seen where bit x of vis is set (MASKED).
-    template <bool MASKED>
-    __device__ __forceinline__ void softmax(q4_f32x16 (&s)[KB], uint64_t vis, q4_bf16x8 (&pf)[NP][KB][2]) {
-        if (MASKED) {
-            const uint32_t v[2] = {(uint32_t)vis >> (4 * hh), (uint32_t)(vis >> 32) >> (4 * hh)};
+    // Keys whose bit of vis is clear are not seen.
+    __device__ __forceinline__ void mask(q4_f32x16 (&s)[KB], uint64_t vis) const {
+        const uint32_t v[2] = {(uint32_t)vis >> (4 * hh), (uint32_t)(vis >> 32) >> (4 * hh)};
 #pragma unroll
-            for (int kb = 0; kb < KB; kb++)
+        for (int kb = 0; kb < KB; kb++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
-        }
+            for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
+    }
+
+    // P^T of a tile from its scores.
+    __device__ __forceinline__ void softmax(const q4_f32x16 (&s)[KB], q4_bf16x8 (&pf)[NP][KB][2]) {
         float top = __builtin_elementwise_maximum(s[0][0], s[KB - 1][15]);
 #pragma unroll
         for (int i = 1; i < 16; i++) top = KB == 2 ? q4_max3(top, s[0][i], s[KB - 1][i - 1]) : i & 1 ? q4_max3(top, s[0][i], s[0][i & 14]) : top;
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
     using G = Q4Geo<D, RW>;
-    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS;
+    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS, AHEAD = G::AHEAD;
     extern __shared__ __attribute__((aligned(1024))) uint8_t q4_smem[];
     const int tid = threadIdx.x;
     Wave w{p, q4_smem};
@@ -449,64 +453,88 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
 
         // What a lane reads of a tile: of key row r of each key block the groups 2i + hh (K: all; V: pieces shared out over RW).
         constexpr int NC = KB * KM, VC = (NC + RW - 1) / RW;  // pieces (key block, i) of a lane's rows; of V per wavefront
-        uint4 kc[KB][KM], vc[VC];
-        uint32_t ks[KB], vs[KB];
-        int ids[KB] = {}, at[KB] = {};
+        struct Codes {
+            uint4 kc[KB][KM], vc[VC];
+            uint32_t ks[KB], vs[KB];  // as they lie in memory: nothing may wait for them where they are asked for
+            uint32_t bad[KB];         // all ones: a block outside the pool
+        } ahead[AHEAD];
+        // Blocks are multiples of 16 positions and tiles begin at multiples of 32: the lanes r < 16 of a key block share a block of the
+        // pool, and so do the others.  Ids come by scalar loads, a tile earlier than the codes.
         const bool paged = p.block_size != 0;
-        const auto fetch_ids = [&](int base) {  // where a tile's rows are; positions are held within the split
+        const const_ids table = (const_ids)(uintptr_t)(p.block_table + (paged ? (size_t)b * p.max_blocks : 0));
+        struct Ids {
+            int id[KB][2], begin[KB][2];  // begin: the block's first position
+        } ids;
+        const auto fetch_ids = [&](int base) {  // positions are held within the split
+            if (!paged) return;
 #pragma unroll
-            for (int kb = 0; kb < KB; kb++) {
-                const int pos = min(base + 32 * kb + r, k1 - 1);
-                at[kb] = pos;
-                if (paged) {
+            for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    const int pos = min(base + 32 * kb + 16 * x, k1 - 1);
                     uint32_t off;
-                    ids[kb] = p.block_table[(size_t)b * p.max_blocks + fast_div((uint32_t)pos, (uint32_t)p.block_size, p.inv_bs, off)];
-                    at[kb] = (int)off;
+                    ids.id[kb][x] = table[fast_div((uint32_t)pos, (uint32_t)p.block_size, p.inv_bs, off)];
+                    ids.begin[kb][x] = pos - (int)off;
                 }
-            }
         };
-        const auto load_tile = [&](int base) {
+        const auto load_tile = [&](Codes &to, int base) {
             uint64_t row[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
+                const int pos = min(base + 32 * kb + r, k1 - 1);
                 bool known = true;
                 if (paged) {
-                    known = ids[kb] >= 0 && ids[kb] < p.num_blocks;
-                    row[kb] = (uint64_t)(uint32_t)(known ? ids[kb] : 0) * (uint32_t)(p.Hkv * p.block_size) + (uint32_t)((int)kvh * p.block_size + at[kb]);
+                    uint64_t first[2];
+#pragma unroll
+                    for (int x = 0; x < 2; x++) {
+                        const int id = ids.id[kb][x];
+                        first[x] = ((uint64_t)(uint32_t)(id >= 0 && id < p.num_blocks ? id : 0) * p.Hkv + kvh) * (uint32_t)p.block_size - ids.begin[kb][x];
+                    }
+                    row[kb] = (r < 16 ? first[0] : first[1]) + pos;
+                    known = (uint32_t)(r < 16 ? ids.id[kb][0] : ids.id[kb][1]) < (uint32_t)p.num_blocks;
                 } else {
-                    row[kb] = ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap + (uint32_t)at[kb];
+                    row[kb] = ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap + (uint32_t)pos;
                 }
 #pragma unroll
-                for (int i = 0; i < KM; i++) kc[kb][i] = *reinterpret_cast<const uint4 *>(p.codes[0] + row[kb] * (D / 2) + 16 * (2 * i + hh));
+                for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(p.codes[0] + row[kb] * (D / 2) + 16 * (2 * i + hh));
                 if constexpr (D == 128) {
-                    ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + row[kb] * 4) >> (8 * hh);
-                    vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + row[kb] * 4) >> (8 * hh);
+                    to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + row[kb] * 4);
+                    to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + row[kb] * 4);
                 } else {
-                    ks[kb] = p.scales[0][row[kb] * 2 + hh];
-                    vs[kb] = p.scales[1][row[kb] * 2 + hh];
+                    to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + row[kb] * 2);
+                    to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + row[kb] * 2);
                 }
-                if (!known) ks[kb] = 0xffffffffu;
-                if (!known || base + 32 * kb + r >= k1) vs[kb] = 0x7f7f7f7fu;  // weighs nothing, and is a number
+                to.bad[kb] = known ? 0u : 0xffffffffu;
             }
 #pragma unroll
             for (int j = 0; j < VC; j++) {
                 const int c = min(j * RW + w.wr, NC - 1), kb = c / KM, i = c % KM;
-                vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
+                to.vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
             }
         };
         const int span = KEYS * KW, mine = k0 + KEYS * w.kg;
         fetch_ids(mine);
-        load_tile(mine);
-        fetch_ids(mine + span);
-        for (int first = k0; first < k1; first += span) {
+#pragma unroll
+        for (int x = 0; x < AHEAD; x++) {
+            load_tile(ahead[x], mine + x * span);
+            fetch_ids(mine + (x + 1) * span);
+        }
+        const auto step = [&](Codes &from, int first) {
             const int base = first + KEYS * w.kg;
             uint8_t *const tile = w.tile();
+            uint32_t k_scale[KB], v_scale[KB];  // the lane's groups in bytes 0 and 2
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) {
+                k_scale[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
+                // what weighs nothing is a number
+                v_scale[kb] = from.bad[kb] || base + 32 * kb + r >= k1 ? 0x7f7f7f7fu : from.vs[kb] >> (8 * hh);
+            }
 #pragma unroll
             for (int j = 0; j < VC; j++) {
                 const int c = j * RW + w.wr, kb = c / KM, i = c % KM;
                 if (NC % RW != 0 && c >= NC) break;  // uniform
-                const float f = q4_scale((kb ? vs[KB - 1] : vs[0]) >> (16 * i) & 255u);
-                const uint32_t in[4] = {vc[j].x, vc[j].y, vc[j].z, vc[j].w};
+                const float f = q4_scale((kb ? v_scale[KB - 1] : v_scale[0]) >> (16 * i) & 255u);
+                const uint32_t in[4] = {from.vc[j].x, from.vc[j].y, from.vc[j].z, from.vc[j].w};
                 uint8_t *const row = tile + (32 * kb + r) * G::ROW;
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
@@ -522,12 +550,12 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
 #pragma unroll
             for (int i = 0; i < 16; i++) s[0][i] = s[KB - 1][i] = 0.f;
 #define Q4_PART(y)                                                                                                     \
-    s[0] = q4_scores<0, (y) & 3>(kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                                      \
-    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(kc[KB - 1][0], qp[y][0], s[KB - 1], ks[KB - 1], qs[(y) >> 2][0]); \
+    s[0] = q4_scores<0, (y) & 3>(from.kc[0][0], qp[y][0], s[0], k_scale[0], qs[(y) >> 2][0]);                                      \
+    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(from.kc[KB - 1][0], qp[y][0], s[KB - 1], k_scale[KB - 1], qs[(y) >> 2][0]); \
     if constexpr (KM == 2) {                                                                                           \
-        s[0] = q4_scores<2, (y) & 3>(kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]);                   \
+        s[0] = q4_scores<2, (y) & 3>(from.kc[0][KM - 1], qp[y][KM - 1], s[0], k_scale[0], qs[(y) >> 2][KM - 1]);                   \
         if constexpr (KB == 2)                                                                                         \
-            s[KB - 1] = q4_scores<2, (y) & 3>(kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], ks[KB - 1], qs[(y) >> 2][KM - 1]); \
+            s[KB - 1] = q4_scores<2, (y) & 3>(from.kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], k_scale[KB - 1], qs[(y) >> 2][KM - 1]); \
     }
             Q4_PART(0)
             Q4_PART(1)
@@ -538,17 +566,21 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 Q4_PART(5)
             }
 #undef Q4_PART
-            if (first + span < k1) {
-                load_tile(base + span);
-                fetch_ids(base + 2 * span);
+            if (first + AHEAD * span < k1) {
+                load_tile(from, base + AHEAD * span);
+                fetch_ids(base + (AHEAD + 1) * span);
             }
             q4_bf16x8 pf[NP][KB][2];
-            if (base + KEYS <= k1) w.template softmax<false>(s, 0, pf);
-            else w.template softmax<true>(s, base < k1 ? (1ull << (k1 - base)) - 1 : 0, pf);
+            if (base + KEYS > k1) w.mask(s, base < k1 ? (1ull << (k1 - base)) - 1 : 0);
+            w.softmax(s, pf);
             w.staged();
             w.template accumulate<NP>(tile, pf);
             w.stage++;
-        }
+        };
+        for (int first = k0; first < k1; first += AHEAD * span)
+#pragma unroll
+            for (int x = 0; x < AHEAD; x++)
+                if (first + x * span < k1) step(ahead[x], first + x * span);  // uniform
     }
 
     if (live && tree_here) {
@@ -596,7 +628,8 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
             }
             q4_bf16x8 pf[NP][KB][2];
-            w.template softmax<true>(s, vis, pf);
+            w.mask(s, vis);
+            w.softmax(s, pf);
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
                 uint8_t *const tile = w.tile();
