@@ -163,13 +163,13 @@ typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
 typedef __attribute__((address_space(4))) const int32_t *const_ids;
 constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the reference before the outputs are rescaled
 
-// Dynamic LDS: V tiles [key groups][2 if rows are shared out, else 1][keys][D] bf16, afterwards 64 channels at a time of the
+// Dynamic LDS: V tiles [key groups][2][keys][D] bf16, afterwards 64 channels at a time of the
 // outputs [4][32][64 + 4] fp32.
 template <int D, int RW>
 struct Q4Geo {
     static constexpr int KB = RW == 1 ? 1 : 2, KEYS = 32 * KB;  // key blocks and keys of a tile
-    static constexpr int AHEAD = RW == 1 ? 2 : 1;                // tiles whose codes are on their way
-    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = RW > 1 ? 2 : 1;
+    static constexpr int AHEAD = RW == 1 ? 2 : 1;                // tiles whose codes are on their way besides the next one's
+    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = 2;
     static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
     static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
@@ -233,7 +233,7 @@ struct Q4Wave {
     q4_f32x16 o[DB];
     float m, l;
 
-    __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (G::BUFS > 1 ? stage & 1 : 0)) * G::TILE; }
+    __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (stage & 1)) * G::TILE; }
     // Between the stores of a V tile and its reads.  Rows shared out: every wavefront has stored its part; the next tile goes to the
     // other buffer, which all have read before this barrier.  Else the tile is the wavefront's own, and LDS keeps its order.
     __device__ __forceinline__ void staged() const {
@@ -254,8 +254,8 @@ struct Q4Wave {
             for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
     }
 
-    // P^T of a tile from its scores.
-    __device__ __forceinline__ void softmax(const q4_f32x16 (&s)[KB], q4_bf16x8 (&pf)[NP][KB][2]) {
+    // The reference of a row follows its maximum.
+    __device__ __forceinline__ void reference(const q4_f32x16 (&s)[KB]) {
         float top = __builtin_elementwise_maximum(s[0][0], s[KB - 1][15]);
 #pragma unroll
         for (int i = 1; i < 16; i++) top = KB == 2 ? q4_max3(top, s[0][i], s[KB - 1][i - 1]) : i & 1 ? q4_max3(top, s[0][i], s[0][i & 14]) : top;
@@ -270,6 +270,10 @@ struct Q4Wave {
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[db][i] *= alpha;
         }
+    }
+
+    // P^T of a tile from its scores.
+    __device__ __forceinline__ void weights(const q4_f32x16 (&s)[KB], q4_bf16x8 (&pf)[NP][KB][2]) {
         const float off = m == -INFINITY ? 0.f : -m;
         float sum[2] = {0.f, 0.f};  // two chains
         uint32_t pk[NP][KB][8];
@@ -362,7 +366,7 @@ __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int hea
     if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
 }
 
-template <int D, bool F32, int RW>
+template <int D, bool F32, int RW, bool PAGED>
 __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
@@ -452,48 +456,58 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         }
 
         // What a lane reads of a tile: of key row r of each key block the groups 2i + hh (K: all; V: pieces shared out over RW).
-        constexpr int NC = KB * KM, VC = (NC + RW - 1) / RW;  // pieces (key block, i) of a lane's rows; of V per wavefront
+        constexpr int NC = KB * KM, VC = NC < RW ? 1 : NC / RW, VW = NC < RW ? 2 : 4;  // pieces (key block, i); a wavefront's of V, their words
         struct Codes {
-            uint4 kc[KB][KM], vc[VC];
+            uint4 kc[KB][KM];
+            uint32_t vc[VC][VW];
             uint32_t ks[KB], vs[KB];  // as they lie in memory: nothing may wait for them where they are asked for
             uint32_t bad[KB];         // all ones: a block outside the pool
-        } ahead[AHEAD];
+        };
+        const auto piece_of = [&](int j) { return NC < RW ? w.wr / 2 : j * RW + w.wr; };  // NC < RW: half a piece each
+        const int half = NC < RW ? w.wr & 1 : 0;
         // Blocks are multiples of 16 positions and tiles begin at multiples of 32: the lanes r < 16 of a key block share a block of the
         // pool, and so do the others.  Ids come by scalar loads, a tile earlier than the codes.
-        const bool paged = p.block_size != 0;
-        const const_ids table = (const_ids)(uintptr_t)(p.block_table + (paged ? (size_t)b * p.max_blocks : 0));
+        const const_ids table = (const_ids)(uintptr_t)(PAGED ? p.block_table + (size_t)b * p.max_blocks : nullptr);
+        const uint64_t seq_row = PAGED ? 0 : ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap;
+        const uint32_t block_rows = PAGED ? (uint32_t)(p.Hkv * p.block_size) : 0;
         struct Ids {
-            int id[KB][2], begin[KB][2];  // begin: the block's first position
+            int id[KB][2];
+            uint32_t off[KB][2];  // of the first of the 16 positions within its block, plus the head's rows
         } ids;
         const auto fetch_ids = [&](int base) {  // positions are held within the split
-            if (!paged) return;
+            if constexpr (PAGED)
 #pragma unroll
-            for (int kb = 0; kb < KB; kb++)
+                for (int kb = 0; kb < KB; kb++)
 #pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    const int pos = min(base + 32 * kb + 16 * x, k1 - 1);
-                    uint32_t off;
-                    ids.id[kb][x] = table[fast_div((uint32_t)pos, (uint32_t)p.block_size, p.inv_bs, off)];
-                    ids.begin[kb][x] = pos - (int)off;
-                }
+                    for (int x = 0; x < 2; x++) {
+                        const int pos = min(base + 32 * kb + 16 * x, (k1 - 1) & ~15);
+                        // fast_div without conditions, which would leave the scalar unit
+                        int q = (int)__umulhi((uint32_t)pos, p.inv_bs), off = pos - q * p.block_size;
+                        const int over = (p.block_size - 1 - off) >> 31;
+                        q -= over;
+                        off -= p.block_size & over;
+                        ids.id[kb][x] = table[q];
+                        ids.off[kb][x] = (uint32_t)off + kvh * (uint32_t)p.block_size;
+                    }
         };
         const auto load_tile = [&](Codes &to, int base) {
             uint64_t row[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
-                const int pos = min(base + 32 * kb + r, k1 - 1);
-                bool known = true;
-                if (paged) {
+                if constexpr (PAGED) {
                     uint64_t first[2];
+                    uint32_t bad[2];
 #pragma unroll
                     for (int x = 0; x < 2; x++) {
                         const int id = ids.id[kb][x];
-                        first[x] = ((uint64_t)(uint32_t)(id >= 0 && id < p.num_blocks ? id : 0) * p.Hkv + kvh) * (uint32_t)p.block_size - ids.begin[kb][x];
+                        bad[x] = (uint32_t)((id | (p.num_blocks - 1 - id)) >> 31);  // all ones: negative or too large
+                        first[x] = (uint64_t)((uint32_t)id & ~bad[x]) * block_rows + ids.off[kb][x];
                     }
-                    row[kb] = (r < 16 ? first[0] : first[1]) + pos;
-                    known = (uint32_t)(r < 16 ? ids.id[kb][0] : ids.id[kb][1]) < (uint32_t)p.num_blocks;
+                    row[kb] = (r < 16 ? first[0] : first[1]) + (uint32_t)(r & 15);  // the 16 positions are the block's throughout
+                    to.bad[kb] = r < 16 ? bad[0] : bad[1];
                 } else {
-                    row[kb] = ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap + (uint32_t)pos;
+                    row[kb] = seq_row + (uint32_t)min(base + 32 * kb + r, k1 - 1);
+                    to.bad[kb] = 0;
                 }
 #pragma unroll
                 for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(p.codes[0] + row[kb] * (D / 2) + 16 * (2 * i + hh));
@@ -504,58 +518,58 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                     to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + row[kb] * 2);
                     to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + row[kb] * 2);
                 }
-                to.bad[kb] = known ? 0u : 0xffffffffu;
             }
 #pragma unroll
             for (int j = 0; j < VC; j++) {
-                const int c = min(j * RW + w.wr, NC - 1), kb = c / KM, i = c % KM;
-                to.vc[j] = *reinterpret_cast<const uint4 *>(p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh));
-            }
-        };
-        const int span = KEYS * KW, mine = k0 + KEYS * w.kg;
-        fetch_ids(mine);
-#pragma unroll
-        for (int x = 0; x < AHEAD; x++) {
-            load_tile(ahead[x], mine + x * span);
-            fetch_ids(mine + (x + 1) * span);
-        }
-        const auto step = [&](Codes &from, int first) {
-            const int base = first + KEYS * w.kg;
-            uint8_t *const tile = w.tile();
-            uint32_t k_scale[KB], v_scale[KB];  // the lane's groups in bytes 0 and 2
-#pragma unroll
-            for (int kb = 0; kb < KB; kb++) {
-                k_scale[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
-                // what weighs nothing is a number
-                v_scale[kb] = from.bad[kb] || base + 32 * kb + r >= k1 ? 0x7f7f7f7fu : from.vs[kb] >> (8 * hh);
-            }
-#pragma unroll
-            for (int j = 0; j < VC; j++) {
-                const int c = j * RW + w.wr, kb = c / KM, i = c % KM;
-                if (NC % RW != 0 && c >= NC) break;  // uniform
-                const float f = q4_scale((kb ? v_scale[KB - 1] : v_scale[0]) >> (16 * i) & 255u);
-                const uint32_t in[4] = {from.vc[j].x, from.vc[j].y, from.vc[j].z, from.vc[j].w};
-                uint8_t *const row = tile + (32 * kb + r) * G::ROW;
-#pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    uint4 v;
-                    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 0));
-                    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 1));
-                    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 2));
-                    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in[x], f, 3));
-                    *reinterpret_cast<uint4 *>(row + (((4 * (2 * i + hh) + x) ^ q4_swizzle<D>(r)) << 4)) = v;
+                const int c = piece_of(j), kb = c / KM, i = c % KM;
+                const uint8_t *const at = p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh);
+                if constexpr (VW == 4) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(at);
+                    to.vc[j][0] = v.x; to.vc[j][1] = v.y; to.vc[j][VW - 2] = v.z; to.vc[j][VW - 1] = v.w;
+                } else {
+                    const uint2 v = *reinterpret_cast<const uint2 *>(at + 8 * half);
+                    to.vc[j][0] = v.x; to.vc[j][1] = v.y;
                 }
             }
-            q4_f32x16 s[KB];
+        };
+        // V of a tile as bf16 into LDS.
+        const auto put_v = [&](const Codes &from, int base, uint8_t *tile) {
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[0][i] = s[KB - 1][i] = 0.f;
-#define Q4_PART(y)                                                                                                     \
-    s[0] = q4_scores<0, (y) & 3>(from.kc[0][0], qp[y][0], s[0], k_scale[0], qs[(y) >> 2][0]);                                      \
-    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(from.kc[KB - 1][0], qp[y][0], s[KB - 1], k_scale[KB - 1], qs[(y) >> 2][0]); \
-    if constexpr (KM == 2) {                                                                                           \
-        s[0] = q4_scores<2, (y) & 3>(from.kc[0][KM - 1], qp[y][KM - 1], s[0], k_scale[0], qs[(y) >> 2][KM - 1]);                   \
-        if constexpr (KB == 2)                                                                                         \
-            s[KB - 1] = q4_scores<2, (y) & 3>(from.kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], k_scale[KB - 1], qs[(y) >> 2][KM - 1]); \
+            for (int j = 0; j < VC; j++) {
+                const int c = piece_of(j), kb = c / KM, i = c % KM;
+                const uint32_t vs = kb ? from.vs[KB - 1] : from.vs[0], bad = kb ? from.bad[KB - 1] : from.bad[0];
+                // keys that weigh nothing have to be numbers
+                const uint32_t none = bad | (uint32_t)((k1 - 1 - (base + 32 * kb + r)) >> 31);
+                const uint32_t byte = (vs >> (8 * hh + 16 * i) & 255u & ~none) | (127u & none);
+                const float f = q4_scale(byte);
+                uint8_t *const row = tile + (32 * kb + r) * G::ROW;
+#pragma unroll
+                for (int x = 0; x < VW; x++) {
+                    const uint32_t in = from.vc[j][x];
+                    uint4 v;
+                    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 0));
+                    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 1));
+                    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 2));
+                    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 3));
+                    *reinterpret_cast<uint4 *>(row + (((4 * (2 * i + hh) + 2 * half + x) ^ q4_swizzle<D>(r)) << 4)) = v;
+                }
+            }
+        };
+        const auto scores = [&](const Codes &from, q4_f32x16 (&s)[KB]) {
+            uint32_t ks[KB];  // the lane's groups in bytes 0 and 2
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) {
+                ks[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
+            }
+#define Q4_PART(y)                                                                                                              \
+    s[0] = q4_scores<0, (y) & 3>(from.kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                                          \
+    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(from.kc[KB - 1][0], qp[y][0], s[KB - 1], ks[KB - 1], qs[(y) >> 2][0]); \
+    if constexpr (KM == 2) {                                                                                                    \
+        s[0] = q4_scores<2, (y) & 3>(from.kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]);                       \
+        if constexpr (KB == 2)                                                                                                  \
+            s[KB - 1] = q4_scores<2, (y) & 3>(from.kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], ks[KB - 1], qs[(y) >> 2][KM - 1]); \
     }
             Q4_PART(0)
             Q4_PART(1)
@@ -566,21 +580,56 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 Q4_PART(5)
             }
 #undef Q4_PART
-            if (first + AHEAD * span < k1) {
-                load_tile(from, base + AHEAD * span);
-                fetch_ids(base + (AHEAD + 1) * span);
-            }
-            q4_bf16x8 pf[NP][KB][2];
-            if (base + KEYS > k1) w.mask(s, base < k1 ? (1ull << (k1 - base)) - 1 : 0);
-            w.softmax(s, pf);
-            w.staged();
-            w.template accumulate<NP>(tile, pf);
-            w.stage++;
         };
-        for (int first = k0; first < k1; first += AHEAD * span)
+
+        // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials, and
+        // stores the next tile's V (into the other buffer) between its value products: the matrix and the vector unit are both busy
+        // within one wavefront.  Codes of the tiles behind are on their way; beyond the split they are a held row's, unused.
+        const int span = KEYS * KW, mine = k0 + KEYS * w.kg, rounds = (k1 - k0 + span - 1) / span;
+        Codes start, ahead[AHEAD];
+        q4_f32x16 sa[KB], sb[KB];
+        fetch_ids(mine);
+        load_tile(start, mine);
 #pragma unroll
-            for (int x = 0; x < AHEAD; x++)
-                if (first + x * span < k1) step(ahead[x], first + x * span);  // uniform
+        for (int x = 0; x < AHEAD; x++) {
+            fetch_ids(mine + (x + 1) * span);
+            load_tile(ahead[x], mine + (x + 1) * span);
+        }
+        fetch_ids(mine + (AHEAD + 1) * span);
+        put_v(start, mine, w.tile());
+        scores(start, sa);
+        w.staged();
+        const auto step = [&](int t, Codes &next, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
+            const int base = mine + t * span;
+            const uint8_t *const tile = w.tile();
+            w.stage++;
+            q4_bf16x8 pf[NP][KB][2];
+            w.reference(s);
+            scores(next, s_next);
+            w.weights(s, pf);
+            w.template accumulate<NP>(tile, pf);
+            put_v(next, base + span, w.tile());
+            load_tile(next, base + (AHEAD + 1) * span);
+            fetch_ids(base + (AHEAD + 2) * span);
+            w.staged();
+        };
+        int t = 0;
+        for (; t + 2 < rounds; t += 2) {
+            step(t, ahead[0], sa, sb);
+            step(t + 1, ahead[AHEAD - 1], sb, sa);
+        }
+        if (t + 1 < rounds) {
+            step(t, ahead[0], sa, sb);
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) sa[kb] = sb[kb];
+        }
+        const int base = mine + (rounds - 1) * span;
+        if (base + KEYS > k1) w.mask(sa, base < k1 ? (1ull << (k1 - base)) - 1 : 0);
+        q4_bf16x8 pf[NP][KB][2];
+        w.reference(sa);
+        w.weights(sa, pf);
+        w.template accumulate<NP>(w.tile(), pf);
+        w.stage++;
     }
 
     if (live && tree_here) {
@@ -629,7 +678,8 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             }
             q4_bf16x8 pf[NP][KB][2];
             w.mask(s, vis);
-            w.softmax(s, pf);
+            w.reference(s);
+            w.weights(s, pf);
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
                 uint8_t *const tile = w.tile();
@@ -824,23 +874,28 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     return pl;
 }
 
-template <int D, bool F32, int RW>
+template <int D, bool F32, int RW, bool PAGED>
 static int32_t launch_q4(const Q4Attn &p, unsigned grid, hipStream_t st) {
     constexpr int lds = Q4Geo<D, RW>::LDS;
     static_assert(lds <= 80 * 1024, "two workgroups a compute unit");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) {
         g_last_hip_error = (int32_t)e;
         return ETV_ERR_HIP;
     }
-    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW>), dim3(grid), dim3(256), lds, st, p);
+    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED>), dim3(grid), dim3(256), lds, st, p);
     return check_launch();
+}
+
+template <int D, bool F32, int RW>
+static int32_t launch_q4_form(const Q4Attn &p, unsigned grid, hipStream_t st) {
+    return p.block_size ? launch_q4<D, F32, RW, true>(p, grid, st) : launch_q4<D, F32, RW, false>(p, grid, st);
 }
 
 template <int D, bool F32>
 static int32_t run_q4(const Q4Plan &pl, const Q4Attn &p, hipStream_t st) {
     const unsigned grid = (unsigned)((pl.units + 7) / 8 * 8 * pl.row_groups);
-    const int32_t rc = pl.rw == 1 ? launch_q4<D, F32, 1>(p, grid, st) : pl.rw == 2 ? launch_q4<D, F32, 2>(p, grid, st) : launch_q4<D, F32, 4>(p, grid, st);
+    const int32_t rc = pl.rw == 1 ? launch_q4_form<D, F32, 1>(p, grid, st) : pl.rw == 2 ? launch_q4_form<D, F32, 2>(p, grid, st) : launch_q4_form<D, F32, 4>(p, grid, st);
     if (rc != ETV_OK || pl.slots == 1) return rc;
     hipLaunchKernelGGL((join_q4_kernel<D, F32>), dim3((p.T_max * p.Hq + 2048 / D - 1) / (2048 / D), p.B), dim3(256), 0, st, p, pl.row_groups * 32 * pl.rw);
     return check_launch();
