@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
+#include <utility>
 
 #include "etv_common.h"
 
@@ -222,6 +223,11 @@ __device__ __forceinline__ float q4_max3(float a, float b, float c) {
 template <int D>
 __device__ __forceinline__ int q4_swizzle(int row) { return D == 128 ? (((row & 3) << 1) | ((row >> 2) & 1)) : ((row & 2) << 1); }
 
+template <class F, int... I>
+__device__ __forceinline__ void q4_each(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void q4_for(F f) { q4_each(f, std::make_integer_sequence<int, N>{}); }
+
 template <int D, bool F32, int RW>
 struct Q4Wave {
     static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 3, QW = F32 ? 2 : 1;
@@ -231,7 +237,7 @@ struct Q4Wave {
     uint8_t *smem;
     int lane, r, hh, kg, wr, stage;
     q4_f32x16 o[DB];
-    float m, l;
+    float m, off, sum[2];  // reference (log2), what is added to a score; the row's sum in two chains
 
     __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (stage & 1)) * G::TILE; }
     // Between the stores of a V tile and its reads.  Rows shared out: every wavefront has stored its part; the next tile goes to the
@@ -254,75 +260,77 @@ struct Q4Wave {
             for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
     }
 
+    // The largest score of the lane's half of a row, piece x of 8 KB.
+    template <int X>
+    __device__ __forceinline__ static void raise(float (&top)[2], const q4_f32x16 (&s)[KB]) {
+        constexpr int kb = X % KB, i = X / KB * 2;
+        float &to = top[KB == 2 ? kb : X & 1];
+        to = X < 2 ? __builtin_elementwise_maximum(s[kb][i], s[kb][i + 1]) : q4_max3(to, s[kb][i], s[kb][i + 1]);
+    }
     // The reference of a row follows its maximum.
-    __device__ __forceinline__ void reference(const q4_f32x16 (&s)[KB]) {
-        float top = __builtin_elementwise_maximum(s[0][0], s[KB - 1][15]);
-#pragma unroll
-        for (int i = 1; i < 16; i++) top = KB == 2 ? q4_max3(top, s[0][i], s[KB - 1][i - 1]) : i & 1 ? q4_max3(top, s[0][i], s[0][i & 14]) : top;
-        top = q4_half_max(top) * p.scale_log2;
+    __device__ __forceinline__ void reference(const float (&tops)[2]) {
+        const float top = q4_half_max(__builtin_elementwise_maximum(tops[0], tops[1])) * p.scale_log2;
         const bool lift = top > m + kQ4Lazy;
         if (__any(lift)) {
             const float next = lift ? top : m, alpha = lift ? __builtin_amdgcn_exp2f(m - next) : 1.f;
             m = next;
-            l *= alpha;
+            sum[0] *= alpha;
+            sum[1] *= alpha;
 #pragma unroll
             for (int db = 0; db < DB; db++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) o[db][i] *= alpha;
         }
+        off = m == -INFINITY ? 0.f : -m;
     }
 
-    // P^T of a tile from its scores.
-    __device__ __forceinline__ void weights(const q4_f32x16 (&s)[KB], q4_bf16x8 (&pf)[NP][KB][2]) {
-        const float off = m == -INFINITY ? 0.f : -m;
-        float sum[2] = {0.f, 0.f};  // two chains
-        uint32_t pk[NP][KB][8];
-#pragma unroll
-        for (int kb = 0; kb < KB; kb++)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][i], p.scale_log2, off)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][i + 1], p.scale_log2, off));
-                if constexpr (F32) {
-                    q4_split(a, b, pk[0][kb][i >> 1], pk[1][kb][i >> 1], pk[NP - 1][kb][i >> 1]);
-                    sum[KB == 2 ? kb : i >> 1 & 1] += a + b;
-                } else {
-                    // the weights rounded to bf16 are the weights: the sum takes them as the product does
-                    pk[0][kb][i >> 1] = q4_pair(a, b);
-                    float &part = sum[KB == 2 ? kb : i >> 1 & 1];
-                    part = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i >> 1]),
-                                                           __builtin_bit_cast(q4_bf16x2, 0x3f803f80u), part, false);
-                }
-            }
-        l += sum[0] + sum[1];
-#pragma unroll
-        for (int x = 0; x < NP; x++)
-#pragma unroll
-            for (int kb = 0; kb < KB; kb++)
-#pragma unroll
-                for (int st = 0; st < 2; st++)
-                    pf[x][kb][st] = __builtin_bit_cast(q4_bf16x8, (uint4{pk[x][kb][4 * st], pk[x][kb][4 * st + 1], pk[x][kb][4 * st + 2], pk[x][kb][4 * st + 3]}));
+    // P^T: pair x of a tile's 8 KB pairs of scores to weights.
+    template <int X>
+    __device__ __forceinline__ void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8]) {
+        constexpr int kb = X / 8, i = X % 8;
+        const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][2 * i], p.scale_log2, off)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][2 * i + 1], p.scale_log2, off));
+        if constexpr (F32) {
+            q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
+            sum[X & 1] += a + b;
+        } else {
+            // the weights rounded to bf16 are the weights: the sum takes them as the product does
+            pk[0][kb][i] = q4_pair(a, b);
+            sum[X & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i]), __builtin_bit_cast(q4_bf16x2, 0x3f803f80u),
+                                                         sum[X & 1], false);
+        }
     }
 
-    // O^T += V^T P^T over the tile, with the first `parts` of P
-    template <int PARTS>
-    __device__ __forceinline__ void accumulate(const uint8_t *v, const q4_bf16x8 (&pf)[NP][KB][2]) {
+    // V^T of 16 keys (16 x of the tile) and 32 channels (32 db ..)
+    __device__ __forceinline__ q4_bf16x8 v_fragment(const uint8_t *v, int x, int db) const {
         const int i16 = lane & 15, vrow = 4 * hh + (i16 >> 2), piece = 2 * (lane >> 4 & 1) + ((i16 & 3) >> 1), sub = 8 * (i16 & 1);
-        const int sw = q4_swizzle<D>(vrow);
+        const uint8_t *const at = v + (16 * x + vrow) * G::ROW + sub + (((4 * db + piece) ^ q4_swizzle<D>(vrow)) << 4);
+        const q4_s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)at);
+        const q4_s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)(at + 8 * G::ROW));
+        return __builtin_shufflevector(__builtin_bit_cast(q4_bf16x4, v0), __builtin_bit_cast(q4_bf16x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // O^T of 32 channels += V^T P^T over 16 keys, with the first PARTS of P
+    template <int PARTS>
+    __device__ __forceinline__ void multiply(q4_bf16x8 v, int x, int db, const uint32_t (&pk)[NP][KB][8]) {
 #pragma unroll
-        for (int kb = 0; kb < KB; kb++)
+        for (int y = 0; y < PARTS; y++) {
+            const uint32_t(&w)[8] = pk[y][x / 2];
+            const uint4 f = {w[4 * (x & 1)], w[4 * (x & 1) + 1], w[4 * (x & 1) + 2], w[4 * (x & 1) + 3]};
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(q4_bf16x8, f), o[db], 0, 0, 0);
+        }
+    }
+    // The same one after the other, where there is nothing to do meanwhile.
+    __device__ __forceinline__ void softmax(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8]) {
+        float tops[2];
+        q4_for<8 * KB>([&](auto x) { raise<decltype(x)::value>(tops, s); });
+        reference(tops);
+        q4_for<8 * KB>([&](auto x) { weigh<decltype(x)::value>(s, pk); });
+    }
+    template <int PARTS>
+    __device__ __forceinline__ void accumulate(const uint8_t *v, const uint32_t (&pk)[NP][KB][8]) {
 #pragma unroll
-            for (int st = 0; st < 2; st++) {
-                const uint8_t *const row = v + (32 * kb + 16 * st + vrow) * G::ROW + sub;
+        for (int x = 0; x < 2 * KB; x++)
 #pragma unroll
-                for (int db = 0; db < DB; db++) {
-                    const int at = ((4 * db + piece) ^ sw) << 4;
-                    const q4_s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)(row + at));
-                    const q4_s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((q4_lds_s16x4 *)(row + 8 * G::ROW + at));
-                    const q4_bf16x8 a = __builtin_shufflevector(__builtin_bit_cast(q4_bf16x4, v0), __builtin_bit_cast(q4_bf16x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                    for (int x = 0; x < PARTS; x++) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[x][kb][st], o[db], 0, 0, 0);
-                }
-            }
+            for (int db = 0; db < DB; db++) multiply<PARTS>(v_fragment(v, x, db), x, db, pk);
     }
 };
 
@@ -383,7 +391,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     w.wr = wave % RW;
     w.stage = 0;
     w.m = -INFINITY;
-    w.l = 0.f;
+    w.off = w.sum[0] = w.sum[1] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; db++)
 #pragma unroll
@@ -462,14 +470,14 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             uint32_t vc[VC][VW];
             uint32_t ks[KB], vs[KB];  // as they lie in memory: nothing may wait for them where they are asked for
             uint32_t bad[KB];         // all ones: a block outside the pool
+            uint32_t row[KB];
         };
         const auto piece_of = [&](int j) { return NC < RW ? w.wr / 2 : j * RW + w.wr; };  // NC < RW: half a piece each
         const int half = NC < RW ? w.wr & 1 : 0;
         // Blocks are multiples of 16 positions and tiles begin at multiples of 32: the lanes r < 16 of a key block share a block of the
         // pool, and so do the others.  Ids come by scalar loads, a tile earlier than the codes.
         const const_ids table = (const_ids)(uintptr_t)(PAGED ? p.block_table + (size_t)b * p.max_blocks : nullptr);
-        const uint64_t seq_row = PAGED ? 0 : ((uint64_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap;
-        const uint32_t block_rows = PAGED ? (uint32_t)(p.Hkv * p.block_size) : 0;
+        const uint32_t seq_row = PAGED ? 0 : ((uint32_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap, block_rows = PAGED ? (uint32_t)(p.Hkv * p.block_size) : 0;
         struct Ids {
             int id[KB][2];
             uint32_t off[KB][2];  // of the first of the 16 positions within its block, plus the head's rows
@@ -490,96 +498,87 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                         ids.off[kb][x] = (uint32_t)off + kvh * (uint32_t)p.block_size;
                     }
         };
-        const auto load_tile = [&](Codes &to, int base) {
-            uint64_t row[KB];
+        // A lane's rows (of a layer, fewer than 2^32) in the cache.
+        const auto place = [&](Codes &to, int base) {
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
                 if constexpr (PAGED) {
-                    uint64_t first[2];
-                    uint32_t bad[2];
+                    uint32_t first[2], bad[2];
 #pragma unroll
                     for (int x = 0; x < 2; x++) {
                         const int id = ids.id[kb][x];
                         bad[x] = (uint32_t)((id | (p.num_blocks - 1 - id)) >> 31);  // all ones: negative or too large
-                        first[x] = (uint64_t)((uint32_t)id & ~bad[x]) * block_rows + ids.off[kb][x];
+                        first[x] = ((uint32_t)id & ~bad[x]) * block_rows + ids.off[kb][x];
                     }
-                    row[kb] = (r < 16 ? first[0] : first[1]) + (uint32_t)(r & 15);  // the 16 positions are the block's throughout
+                    to.row[kb] = (r < 16 ? first[0] : first[1]) + (uint32_t)(r & 15);  // the 16 positions are the block's throughout
                     to.bad[kb] = r < 16 ? bad[0] : bad[1];
                 } else {
-                    row[kb] = seq_row + (uint32_t)min(base + 32 * kb + r, k1 - 1);
+                    to.row[kb] = seq_row + (uint32_t)min(base + 32 * kb + r, k1 - 1);
                     to.bad[kb] = 0;
                 }
-#pragma unroll
-                for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(p.codes[0] + row[kb] * (D / 2) + 16 * (2 * i + hh));
-                if constexpr (D == 128) {
-                    to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + row[kb] * 4);
-                    to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + row[kb] * 4);
-                } else {
-                    to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + row[kb] * 2);
-                    to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + row[kb] * 2);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < VC; j++) {
-                const int c = piece_of(j), kb = c / KM, i = c % KM;
-                const uint8_t *const at = p.codes[1] + (kb ? row[KB - 1] : row[0]) * (D / 2) + 16 * (2 * i + hh);
-                if constexpr (VW == 4) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(at);
-                    to.vc[j][0] = v.x; to.vc[j][1] = v.y; to.vc[j][VW - 2] = v.z; to.vc[j][VW - 1] = v.w;
-                } else {
-                    const uint2 v = *reinterpret_cast<const uint2 *>(at + 8 * half);
-                    to.vc[j][0] = v.x; to.vc[j][1] = v.y;
-                }
             }
         };
-        // V of a tile as bf16 into LDS.
-        const auto put_v = [&](const Codes &from, int base, uint8_t *tile) {
+        const auto load_k = [&](Codes &to, int kb) {
+            const uint8_t *const codes = p.codes[0] + 16 * hh + (uint64_t)to.row[kb] * (D / 2);
 #pragma unroll
-            for (int j = 0; j < VC; j++) {
-                const int c = piece_of(j), kb = c / KM, i = c % KM;
-                const uint32_t vs = kb ? from.vs[KB - 1] : from.vs[0], bad = kb ? from.bad[KB - 1] : from.bad[0];
-                // keys that weigh nothing have to be numbers
-                const uint32_t none = bad | (uint32_t)((k1 - 1 - (base + 32 * kb + r)) >> 31);
-                const uint32_t byte = (vs >> (8 * hh + 16 * i) & 255u & ~none) | (127u & none);
-                const float f = q4_scale(byte);
-                uint8_t *const row = tile + (32 * kb + r) * G::ROW;
-#pragma unroll
-                for (int x = 0; x < VW; x++) {
-                    const uint32_t in = from.vc[j][x];
-                    uint4 v;
-                    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 0));
-                    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 1));
-                    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 2));
-                    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 3));
-                    *reinterpret_cast<uint4 *>(row + (((4 * (2 * i + hh) + 2 * half + x) ^ q4_swizzle<D>(r)) << 4)) = v;
-                }
+            for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(codes + 32 * i);
+            if constexpr (D == 128) {
+                to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + (uint64_t)to.row[kb] * 4);
+                to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + (uint64_t)to.row[kb] * 4);
+            } else {
+                to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + (uint64_t)to.row[kb] * 2);
+                to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + (uint64_t)to.row[kb] * 2);
             }
         };
-        const auto scores = [&](const Codes &from, q4_f32x16 (&s)[KB]) {
-            uint32_t ks[KB];  // the lane's groups in bytes 0 and 2
+        const auto load_v = [&](Codes &to, int j) {
+            const int c = piece_of(j), kb = c / KM, i = c % KM;
+            const uint8_t *const at = p.codes[1] + 16 * hh + (uint64_t)(kb ? to.row[KB - 1] : to.row[0]) * (D / 2) + 32 * i;
+            if constexpr (VW == 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(at);
+                to.vc[j][0] = v.x; to.vc[j][1] = v.y; to.vc[j][VW - 2] = v.z; to.vc[j][VW - 1] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2 *>(at + 8 * half);
+                to.vc[j][0] = v.x; to.vc[j][1] = v.y;
+            }
+        };
+        const auto load_tile = [&](Codes &to, int base) {
+            place(to, base);
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++) load_k(to, kb);
+#pragma unroll
+            for (int j = 0; j < VC; j++) load_v(to, j);
+        };
+        // V of a tile as bf16 into LDS, eight channels of unit u.
+        const auto put_v = [&](const Codes &from, const uint32_t (&vsc)[KB], uint8_t *tile, int u) {
+            {
+                const int j = u / VW, x = u % VW, c = piece_of(j), kb = c / KM, i = c % KM;
+                const uint32_t vs = kb ? vsc[KB - 1] : vsc[0];
+                const float f = q4_scale(vs >> (16 * i) & 255u);
+                const uint32_t in = from.vc[j][x];
+                uint4 v;
+                v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 0));
+                v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 1));
+                v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 2));
+                v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 3));
+                *reinterpret_cast<uint4 *>(tile + (32 * kb + r) * G::ROW + (((4 * (2 * i + hh) + 2 * half + x) ^ q4_swizzle<D>(r)) << 4)) = v;
+            }
+        };
+        // Scores: product X of a tile's QK, y the part of q.
+        constexpr int QK = NQ * KM * KB, PV = 2 * KB * DB, UNITS = VC * VW;
+        const auto score = [&](auto x, const Codes &from, const uint32_t (&ks)[KB], q4_f32x16 (&s)[KB]) {
+            constexpr int X = decltype(x)::value, kb = X % KB, i = X / KB % KM, y = X / (KB * KM);
+            s[kb] = q4_scores<2 * i, y & 3>(from.kc[kb][i], qp[y][i], s[kb], ks[kb], qs[y >> 2][i]);
+        };
+        // a lane's groups in bytes 0 and 2 of the scales; V's keys that weigh nothing have to be numbers
+        const auto clear = [&](const Codes &from, int base, uint32_t (&ks)[KB], uint32_t (&vs)[KB], q4_f32x16 (&s)[KB]) {
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
                 ks[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
+                const uint32_t none = from.bad[kb] | (uint32_t)((k1 - 1 - (base + 32 * kb + r)) >> 31);
+                vs[kb] = (from.vs[kb] >> (8 * hh) & ~none) | (0x7f7f7f7fu & none);
 #pragma unroll
                 for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
             }
-#define Q4_PART(y)                                                                                                              \
-    s[0] = q4_scores<0, (y) & 3>(from.kc[0][0], qp[y][0], s[0], ks[0], qs[(y) >> 2][0]);                                          \
-    if constexpr (KB == 2) s[KB - 1] = q4_scores<0, (y) & 3>(from.kc[KB - 1][0], qp[y][0], s[KB - 1], ks[KB - 1], qs[(y) >> 2][0]); \
-    if constexpr (KM == 2) {                                                                                                    \
-        s[0] = q4_scores<2, (y) & 3>(from.kc[0][KM - 1], qp[y][KM - 1], s[0], ks[0], qs[(y) >> 2][KM - 1]);                       \
-        if constexpr (KB == 2)                                                                                                  \
-            s[KB - 1] = q4_scores<2, (y) & 3>(from.kc[KB - 1][KM - 1], qp[y][KM - 1], s[KB - 1], ks[KB - 1], qs[(y) >> 2][KM - 1]); \
-    }
-            Q4_PART(0)
-            Q4_PART(1)
-            Q4_PART(2)
-            if constexpr (NQ > 3) {
-                Q4_PART(3)
-                Q4_PART(4)
-                Q4_PART(5)
-            }
-#undef Q4_PART
         };
 
         // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials, and
@@ -595,22 +594,43 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             fetch_ids(mine + (x + 1) * span);
             load_tile(ahead[x], mine + (x + 1) * span);
         }
-        fetch_ids(mine + (AHEAD + 1) * span);
-        put_v(start, mine, w.tile());
-        scores(start, sa);
+        uint32_t ks[KB], vs[KB], pk[NP][KB][8];
+        float tops[2];
+        clear(start, mine, ks, vs, sa);
+#pragma unroll
+        for (int u = 0; u < UNITS; u++) put_v(start, vs, w.tile(), u);
+        q4_for<QK>([&](auto x) { score(x, start, ks, sa); });
+        q4_for<8 * KB>([&](auto x) { Wave::template raise<decltype(x)::value>(tops, sa); });
         w.staged();
         const auto step = [&](int t, Codes &next, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
             const int base = mine + t * span;
             const uint8_t *const tile = w.tile();
             w.stage++;
-            q4_bf16x8 pf[NP][KB][2];
-            w.reference(s);
-            scores(next, s_next);
-            w.weights(s, pf);
-            w.template accumulate<NP>(tile, pf);
-            put_v(next, base + span, w.tile());
-            load_tile(next, base + (AHEAD + 1) * span);
-            fetch_ids(base + (AHEAD + 2) * span);
+            uint8_t *const tile_next = w.tile();
+            q4_bf16x8 v[2][DB];
+            fetch_ids(base + (AHEAD + 1) * span);
+            w.reference(tops);
+            clear(next, base + span, ks, vs, s_next);
+            q4_for<QK>([&](auto x) {
+                constexpr int X = decltype(x)::value;
+                score(x, next, ks, s_next);
+                constexpr int LO = X * 8 * KB / QK, HI = (X + 1) * 8 * KB / QK;
+                q4_for<HI - LO>([&](auto y) { w.template weigh<LO + decltype(y)::value>(s, pk); });
+                if constexpr (X >= QK - DB) v[0][X - (QK - DB)] = w.v_fragment(tile, 0, X - (QK - DB));
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            q4_for<PV>([&](auto x) {
+                constexpr int X = decltype(x)::value, set = X / DB, db = X % DB;
+                w.template multiply<NP>(v[set & 1][db], set, db, pk);
+                if constexpr (set + 1 < 2 * KB) v[(set + 1) & 1][db] = w.v_fragment(tile, set + 1, db);
+                constexpr int LO = X * 8 * KB / PV, HI = (X + 1) * 8 * KB / PV;
+                q4_for<HI - LO>([&](auto y) { Wave::template raise<LO + decltype(y)::value>(tops, s_next); });
+                if constexpr (X == 0) place(next, base + (AHEAD + 1) * span);
+                if constexpr (X < KB) load_k(next, X);
+                if constexpr (X < UNITS) put_v(next, vs, tile_next, X);
+                if constexpr (X < UNITS && X % VW == VW - 1) load_v(next, X / VW);
+                __builtin_amdgcn_sched_barrier(0);
+            });
             w.staged();
         };
         int t = 0;
@@ -625,10 +645,8 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         }
         const int base = mine + (rounds - 1) * span;
         if (base + KEYS > k1) w.mask(sa, base < k1 ? (1ull << (k1 - base)) - 1 : 0);
-        q4_bf16x8 pf[NP][KB][2];
-        w.reference(sa);
-        w.weights(sa, pf);
-        w.template accumulate<NP>(w.tile(), pf);
+        w.softmax(sa, pk);
+        w.template accumulate<NP>(w.tile(), pk);
         w.stage++;
     }
 
@@ -676,10 +694,9 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)] >> (base & 63);
                 if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
             }
-            q4_bf16x8 pf[NP][KB][2];
+            uint32_t pk[NP][KB][8];
             w.mask(s, vis);
-            w.reference(s);
-            w.weights(s, pf);
+            w.softmax(s, pk);
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
                 uint8_t *const tile = w.tile();
@@ -709,20 +726,20 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 w.staged();
             };
             stage_part(0);
-            w.template accumulate<NP>(w.tile(), pf);
+            w.template accumulate<NP>(w.tile(), pk);
             w.stage++;
             if constexpr (F32) {
                 stage_part(1);
-                w.template accumulate<2>(w.tile(), pf);
+                w.template accumulate<2>(w.tile(), pk);
                 w.stage++;
                 stage_part(2);
-                w.template accumulate<1>(w.tile(), pf);
+                w.template accumulate<1>(w.tile(), pk);
                 w.stage++;
             }
         }
     }
 
-    w.l = q4_half_sum(w.l);
+    const float row_sum = q4_half_sum(w.sum[0] + w.sum[1]);
     // Values of the tree's V that are not finite were left out: added here to the rows that see them, whose outputs are then
     // not finite whatever the weight.  (The barriers also end the last reads of the V tiles.)
     __shared__ int s_ill;
@@ -748,7 +765,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     // Outputs through LDS, 64 channels at a time: the key groups of a row are joined, and rows are stored in one piece.
     float *const mine = reinterpret_cast<float *>(q4_smem) + (wave * 32 + r) * G::OUT_ROW + 4 * hh;
     float2 *const ml = reinterpret_cast<float2 *>(q4_smem + 4 * 32 * G::OUT_ROW * 4);
-    if (hh == 0) ml[wave * 32 + r] = float2{w.m, w.l};
+    if (hh == 0) ml[wave * 32 + r] = float2{w.m, row_sum};
 #pragma unroll
     for (int half = 0; half < D / 64; half++) {
         if (half) __syncthreads();
@@ -831,6 +848,7 @@ static int32_t q4_check_desc(const etv_attn_desc *h) {
     if (h->block_size % 16 != 0) return ETV_ERR_UNSUPPORTED;
     if (h->block_size > 0 && (h->max_blocks < 1 || h->num_blocks < 1)) return ETV_ERR_INVALID_ARG;
     if ((int64_t)h->Hkv * h->block_size > INT32_MAX || h->P_max > INT32_MAX - 4096) return ETV_ERR_UNSUPPORTED;
+    if ((h->block_size > 0 ? (int64_t)h->num_blocks * h->Hkv * h->block_size : (int64_t)h->B * h->Hkv * h->P_cap) > UINT32_MAX) return ETV_ERR_UNSUPPORTED;
     if (h->P_max > (h->block_size > 0 ? (int64_t)h->max_blocks * h->block_size : (int64_t)h->P_cap)) return ETV_ERR_INVALID_ARG;
     if (h->scale != 0.f && !(fabsf(h->scale) >= 1e-30f && fabsf(h->scale) <= 1e30f)) return ETV_ERR_INVALID_ARG;  // also NaN
     if ((h->flags & ~ETV_ATTN_FLAG_GENERIC) != 0) return ETV_ERR_INVALID_ARG;
