@@ -19,8 +19,7 @@ struct Q4Attn {
     void *out;
     float *lse;
     int B, T_max, Hq, Hkv, G, block_size, max_blocks, num_blocks, P_cap, P_max, words;
-    float scale_log2;  // of the scores, times log2(e); the matrix kernel: its magnitude
-    uint32_t flip;     // matrix kernel: 0x80008000 where the scale is negative (it goes into q), else 0
+    float scale_log2;  // of the scores, times log2(e)
     uint32_t inv_bs;
     // matrix kernel: a sequence's prefix in splits of `chunk` keys, one slot each, and with more than one split a slot more for
     // the tree.  Partials, if slots > 1: part_o [B * Hkv][slots][row_groups * 32 * RW][D], part_ml (reference, sum) alike.
@@ -162,7 +161,7 @@ typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
 
 // memory that no kernel writes while it is read: uniform addresses go through scalar loads
 typedef __attribute__((address_space(4))) const int32_t *const_ids;
-constexpr float kQ4Lazy = 8.0f;  // how far (log2) a maximum may pass the reference before the outputs are rescaled
+constexpr float kQ4Lazy = 1024.f;  // the largest sum of a lane's weights in a tile without a new reference
 
 // Dynamic LDS: V tiles [key groups][2][keys][D] bf16, afterwards 64 channels at a time of the
 // outputs [4][32][64 + 4] fp32.
@@ -237,8 +236,10 @@ struct Q4Wave {
     uint8_t *smem;
     int lane, r, hh, kg, wr, stage;
     q4_f32x16 o[DB];
-    float m, off, sum[2];  // reference (log2), what is added to a score; the row's sum in two chains
+    q4_f32x16 off;    // less the reference in every element: what the scores' products start from
+    float m, sum[2];  // reference (log2), -inf: none yet; the row's sum in two chains
 
+    __device__ __forceinline__ uint8_t *buffer(int x) const { return smem + kg * G::BUFS * G::TILE + x * G::TILE; }
     __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (stage & 1)) * G::TILE; }
     // Between the stores of a V tile and its reads.  Rows shared out: every wavefront has stored its part; the next tile goes to the
     // other buffer, which all have read before this barrier.  Else the tile is the wavefront's own, and LDS keeps its order.
@@ -260,44 +261,73 @@ struct Q4Wave {
             for (int i = 0; i < 16; i++) s[kb][i] = v[kb] >> (8 * (i >> 2) + (i & 3)) & 1u ? s[kb][i] : -INFINITY;
     }
 
-    // The largest score of the lane's half of a row, piece x of 8 KB.
-    template <int X>
-    __device__ __forceinline__ static void raise(float (&top)[2], const q4_f32x16 (&s)[KB]) {
-        constexpr int kb = X % KB, i = X / KB * 2;
-        float &to = top[KB == 2 ? kb : X & 1];
-        to = X < 2 ? __builtin_elementwise_maximum(s[kb][i], s[kb][i + 1]) : q4_max3(to, s[kb][i], s[kb][i + 1]);
+    // The largest score of a row.
+    __device__ __forceinline__ static float largest(const q4_f32x16 (&s)[KB]) {
+        float top[2] = {s[0][0], s[KB - 1][15]};
+#pragma unroll
+        for (int i = 0; i < 16 * KB; i += 2) top[i >> 1 & 1] = q4_max3(top[i >> 1 & 1], s[i / 16][i % 16], s[i / 16][i % 16 + 1]);
+        return q4_half_max(__builtin_elementwise_maximum(top[0], top[1]));
     }
-    // The reference of a row follows its maximum.
-    __device__ __forceinline__ void reference(const float (&tops)[2]) {
-        const float top = q4_half_max(__builtin_elementwise_maximum(tops[0], tops[1])) * p.scale_log2;
-        const bool lift = top > m + kQ4Lazy;
-        if (__any(lift)) {
-            const float next = lift ? top : m, alpha = lift ? __builtin_amdgcn_exp2f(m - next) : 1.f;
-            m = next;
-            sum[0] *= alpha;
-            sum[1] *= alpha;
+    __device__ __forceinline__ void refer_to(float reference) {
+        m = reference;
 #pragma unroll
-            for (int db = 0; db < DB; db++)
+        for (int i = 0; i < 16; i++) off[i] = -reference;
+    }
+    __device__ __forceinline__ void scale_outputs(float f) {
+        sum[0] *= f;
+        sum[1] *= f;
 #pragma unroll
-                for (int i = 0; i < 16; i++) o[db][i] *= alpha;
-        }
-        off = m == -INFINITY ? 0.f : -m;
+        for (int db = 0; db < DB; db++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[db][i] *= f;
+    }
+    __device__ __forceinline__ static void shift(q4_f32x16 (&s)[KB], float by) {
+#pragma unroll
+        for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[kb][i] -= by;
+    }
+    // Scores become relative.  A row without a reference takes the tile's largest score, and stays without one where it sees nothing.
+    __device__ __forceinline__ void enter(q4_f32x16 (&s)[KB]) {
+        const float top = largest(s);
+        const bool none = m == -INFINITY;
+        refer_to(!none ? m : fabsf(top) < INFINITY ? top : 0.f);
+        shift(s, m);
+        if (none && top == -INFINITY) m = -INFINITY;
     }
 
-    // P^T: pair x of a tile's 8 KB pairs of scores to weights.
+    // P^T: pair x of a tile's 8 KB pairs of relative scores to weights, and their part of the row's sum.
     template <int X>
-    __device__ __forceinline__ void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8]) {
+    __device__ __forceinline__ static void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
         constexpr int kb = X / 8, i = X % 8;
-        const float a = __builtin_amdgcn_exp2f(fmaf(s[kb][2 * i], p.scale_log2, off)), b = __builtin_amdgcn_exp2f(fmaf(s[kb][2 * i + 1], p.scale_log2, off));
+        const float a = __builtin_amdgcn_exp2f(s[kb][2 * i]), b = __builtin_amdgcn_exp2f(s[kb][2 * i + 1]);
         if constexpr (F32) {
             q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
-            sum[X & 1] += a + b;
+            part[X & 1] = X < 2 ? a + b : part[X & 1] + (a + b);
         } else {
             // the weights rounded to bf16 are the weights: the sum takes them as the product does
             pk[0][kb][i] = q4_pair(a, b);
-            sum[X & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i]), __builtin_bit_cast(q4_bf16x2, 0x3f803f80u),
-                                                         sum[X & 1], false);
+            part[X & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i]), __builtin_bit_cast(q4_bf16x2, 0x3f803f80u),
+                                                          X < 2 ? 0.f : part[X & 1], false);
         }
+    }
+    __device__ __forceinline__ static void weigh_all(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
+        q4_for<8 * KB>([&](auto x) { weigh<decltype(x)::value>(s, pk, part); });
+    }
+    // A tile whose sum shows that its scores have left the reference behind gives the rows a new one; only then is the maximum
+    // looked for.  s_next: scores of the next tile, relative to the old one.  (A NaN keeps its row coming here.)
+    template <bool NEXT>
+    __device__ __forceinline__ void settle(q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
+        if (__builtin_expect(__any(!(part[0] + part[1] <= kQ4Lazy)), 0)) {
+            const float top = largest(s), lift = top > 0.f && top < INFINITY ? top : 0.f;
+            scale_outputs(__builtin_amdgcn_exp2f(-lift));
+            shift(s, lift);
+            if (NEXT) shift(s_next, lift);
+            refer_to(m + lift);
+            weigh_all(s, pk, part);
+        }
+        sum[0] += part[0];
+        sum[1] += part[1];
     }
 
     // V^T of 16 keys (16 x of the tile) and 32 channels (32 db ..)
@@ -319,12 +349,6 @@ struct Q4Wave {
         }
     }
     // The same one after the other, where there is nothing to do meanwhile.
-    __device__ __forceinline__ void softmax(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8]) {
-        float tops[2];
-        q4_for<8 * KB>([&](auto x) { raise<decltype(x)::value>(tops, s); });
-        reference(tops);
-        q4_for<8 * KB>([&](auto x) { weigh<decltype(x)::value>(s, pk); });
-    }
     template <int PARTS>
     __device__ __forceinline__ void accumulate(const uint8_t *v, const uint32_t (&pk)[NP][KB][8]) {
 #pragma unroll
@@ -335,18 +359,13 @@ struct Q4Wave {
 };
 
 // Eight consecutive channels of an unquantised row as NP bf16 parts.
-__device__ __forceinline__ void q4_eight(const uint16_t *p, uint32_t flip, uint4 (&part)[1]) {
-    const uint4 w = *reinterpret_cast<const uint4 *>(p);
-    part[0] = uint4{w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
-}
-__device__ __forceinline__ void q4_eight(const float *p, uint32_t flip, uint4 (&part)[3]) {
+__device__ __forceinline__ void q4_eight(const uint16_t *p, uint4 (&part)[1]) { part[0] = *reinterpret_cast<const uint4 *>(p); }
+__device__ __forceinline__ void q4_eight(const float *p, uint4 (&part)[3]) {
     const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    const uint32_t f = flip & 0x80000000u;
-    const auto fl = [f](float x) { return __uint_as_float(__float_as_uint(x) ^ f); };
-    q4_split(fl(a.x), fl(a.y), part[0].x, part[1].x, part[2].x);
-    q4_split(fl(a.z), fl(a.w), part[0].y, part[1].y, part[2].y);
-    q4_split(fl(b.x), fl(b.y), part[0].z, part[1].z, part[2].z);
-    q4_split(fl(b.z), fl(b.w), part[0].w, part[1].w, part[2].w);
+    q4_split(a.x, a.y, part[0].x, part[1].x, part[2].x);
+    q4_split(a.z, a.w, part[0].y, part[1].y, part[2].y);
+    q4_split(b.x, b.y, part[0].z, part[1].z, part[2].z);
+    q4_split(b.z, b.w, part[0].w, part[1].w, part[2].w);
 }
 // the values that are not finite out of eight bf16 (first parts); true if there were any
 __device__ __forceinline__ bool q4_take_out(uint4 &w) {
@@ -360,7 +379,8 @@ __device__ __forceinline__ bool q4_take_out(uint4 &w) {
 // One row's eight channels from its sums, and its lse by the first of the threads.
 template <typename T>
 __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int head, int piece, int D, bool node, float ref, float sum, const float (&acc)[8]) {
-    const float inv = node && sum != 0.f ? 1.f / sum : 0.f;  // a NaN sum stays one
+    // no weight at all: zeros; an infinite score or a NaN among them: NaN
+    const float inv = !node || sum == 0.f ? 0.f : sum < INFINITY ? 1.f / sum : NAN;
     T *const dst = static_cast<T *>(p.out) + (((size_t)b * p.T_max + t) * p.Hq + head) * D + 8 * piece;
     if constexpr (sizeof(T) == 4) {
         const float4 a = inv == 0.f ? float4{0, 0, 0, 0} : float4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
@@ -371,7 +391,7 @@ __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int hea
         uint4 v = {q4_pair(acc[0] * inv, acc[1] * inv), q4_pair(acc[2] * inv, acc[3] * inv), q4_pair(acc[4] * inv, acc[5] * inv), q4_pair(acc[6] * inv, acc[7] * inv)};
         *reinterpret_cast<uint4 *>(dst) = inv == 0.f ? uint4{0, 0, 0, 0} : v;
     }
-    if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
+    if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : inv != inv ? NAN : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
 }
 
 template <int D, bool F32, int RW, bool PAGED>
@@ -391,7 +411,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     w.wr = wave % RW;
     w.stage = 0;
     w.m = -INFINITY;
-    w.off = w.sum[0] = w.sum[1] = 0.f;
+    w.sum[0] = w.sum[1] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; db++)
 #pragma unroll
@@ -440,7 +460,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             uint32_t top = 0;
 #pragma unroll
             for (int c = 0; c < 32; c++) {
-                x[c] = __uint_as_float(__float_as_uint(x[c]) ^ (p.flip & 0x80000000u));
+                x[c] *= p.scale_log2;
                 top = max(top, __float_as_uint(x[c]) & 0x7fffffffu);
             }
             const uint32_t e = max(top >> 23, 4 * NQ + 2u) - 2;  // every part's scale byte is at least 1
@@ -567,17 +587,15 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         constexpr int QK = NQ * KM * KB, PV = 2 * KB * DB, UNITS = VC * VW;
         const auto score = [&](auto x, const Codes &from, const uint32_t (&ks)[KB], q4_f32x16 (&s)[KB]) {
             constexpr int X = decltype(x)::value, kb = X % KB, i = X / KB % KM, y = X / (KB * KM);
-            s[kb] = q4_scores<2 * i, y & 3>(from.kc[kb][i], qp[y][i], s[kb], ks[kb], qs[y >> 2][i]);
+            s[kb] = q4_scores<2 * i, y & 3>(from.kc[kb][i], qp[y][i], X < KB ? w.off : s[kb], ks[kb], qs[y >> 2][i]);
         };
         // a lane's groups in bytes 0 and 2 of the scales; V's keys that weigh nothing have to be numbers
-        const auto clear = [&](const Codes &from, int base, uint32_t (&ks)[KB], uint32_t (&vs)[KB], q4_f32x16 (&s)[KB]) {
+        const auto ready = [&](const Codes &from, int base, uint32_t (&ks)[KB], uint32_t (&vs)[KB]) {
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
                 ks[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
                 const uint32_t none = from.bad[kb] | (uint32_t)((k1 - 1 - (base + 32 * kb + r)) >> 31);
                 vs[kb] = (from.vs[kb] >> (8 * hh) & ~none) | (0x7f7f7f7fu & none);
-#pragma unroll
-                for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
             }
         };
 
@@ -595,36 +613,42 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             load_tile(ahead[x], mine + (x + 1) * span);
         }
         uint32_t ks[KB], vs[KB], pk[NP][KB][8];
-        float tops[2];
-        clear(start, mine, ks, vs, sa);
+        float part[2];
+        w.refer_to(0.f);
+        ready(start, mine, ks, vs);
 #pragma unroll
         for (int u = 0; u < UNITS; u++) put_v(start, vs, w.tile(), u);
         q4_for<QK>([&](auto x) { score(x, start, ks, sa); });
-        q4_for<8 * KB>([&](auto x) { Wave::template raise<decltype(x)::value>(tops, sa); });
+        // the last round alone may have tiles that are not whole
+        const int last = mine + (rounds - 1) * span;
+        const auto cut = [&] {
+            if (last + KEYS > k1) w.mask(sa, last < k1 ? (1ull << (k1 - last)) - 1 : 0);
+        };
+        if (rounds == 1) cut();
+        w.enter(sa);
+        if (rounds > 1 && w.m == -INFINITY) w.m = 0.f;  // what `off` says
         w.staged();
-        const auto step = [&](int t, Codes &next, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
+        const auto step = [&](auto buffer, int t, Codes &next, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
             const int base = mine + t * span;
-            const uint8_t *const tile = w.tile();
-            w.stage++;
-            uint8_t *const tile_next = w.tile();
-            q4_bf16x8 v[2][DB];
+            uint8_t *const tile = w.buffer(decltype(buffer)::value), *const tile_next = w.buffer(1 - decltype(buffer)::value);
+            constexpr int FLY = 3;  // fragments of V on their way from LDS
+            q4_bf16x8 v[FLY + 1];
             fetch_ids(base + (AHEAD + 1) * span);
-            w.reference(tops);
-            clear(next, base + span, ks, vs, s_next);
+            ready(next, base + span, ks, vs);
             q4_for<QK>([&](auto x) {
                 constexpr int X = decltype(x)::value;
                 score(x, next, ks, s_next);
                 constexpr int LO = X * 8 * KB / QK, HI = (X + 1) * 8 * KB / QK;
-                q4_for<HI - LO>([&](auto y) { w.template weigh<LO + decltype(y)::value>(s, pk); });
-                if constexpr (X >= QK - DB) v[0][X - (QK - DB)] = w.v_fragment(tile, 0, X - (QK - DB));
+                q4_for<HI - LO>([&](auto y) { Wave::template weigh<LO + decltype(y)::value>(s, pk, part); });
+                if constexpr (false && X >= QK - FLY) v[X - (QK - FLY)] = w.v_fragment(tile, (X - (QK - FLY)) / DB, (X - (QK - FLY)) % DB);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            w.template settle<true>(s, s_next, pk, part);
+            if constexpr (true) q4_for<FLY>([&](auto x) { v[decltype(x)::value] = w.v_fragment(tile, decltype(x)::value / DB, decltype(x)::value % DB); });
             q4_for<PV>([&](auto x) {
-                constexpr int X = decltype(x)::value, set = X / DB, db = X % DB;
-                w.template multiply<NP>(v[set & 1][db], set, db, pk);
-                if constexpr (set + 1 < 2 * KB) v[(set + 1) & 1][db] = w.v_fragment(tile, set + 1, db);
-                constexpr int LO = X * 8 * KB / PV, HI = (X + 1) * 8 * KB / PV;
-                q4_for<HI - LO>([&](auto y) { Wave::template raise<LO + decltype(y)::value>(tops, s_next); });
+                constexpr int X = decltype(x)::value, Y = X + FLY;
+                if constexpr (Y < PV) v[Y % (FLY + 1)] = w.v_fragment(tile, Y / DB, Y % DB);
+                w.template multiply<NP>(v[X % (FLY + 1)], X / DB, X % DB, pk);
                 if constexpr (X == 0) place(next, base + (AHEAD + 1) * span);
                 if constexpr (X < KB) load_k(next, X);
                 if constexpr (X < UNITS) put_v(next, vs, tile_next, X);
@@ -635,17 +659,18 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         };
         int t = 0;
         for (; t + 2 < rounds; t += 2) {
-            step(t, ahead[0], sa, sb);
-            step(t + 1, ahead[AHEAD - 1], sb, sa);
+            step(std::integral_constant<int, 0>{}, t, ahead[0], sa, sb);
+            step(std::integral_constant<int, 1>{}, t + 1, ahead[AHEAD - 1], sb, sa);
         }
         if (t + 1 < rounds) {
-            step(t, ahead[0], sa, sb);
+            step(std::integral_constant<int, 0>{}, t, ahead[0], sa, sb);
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) sa[kb] = sb[kb];
         }
-        const int base = mine + (rounds - 1) * span;
-        if (base + KEYS > k1) w.mask(sa, base < k1 ? (1ull << (k1 - base)) - 1 : 0);
-        w.softmax(sa, pk);
+        w.stage = rounds - 1;
+        if (rounds > 1) cut();
+        Wave::weigh_all(sa, pk, part);
+        w.template settle<false>(sa, sb, pk, part);
         w.template accumulate<NP>(w.tile(), pk);
         w.stage++;
     }
@@ -655,7 +680,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         const T *const kt = static_cast<const T *>(p.kt), *const vt = static_cast<const T *>(p.vt);
         uint4 qf[D / 16][NP];
 #pragma unroll
-        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, p.flip, qf[kk]);
+        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, qf[kk]);
         for (int first = 0; first < n; first += KEYS * KW) {  // the same number of rounds for every wavefront
             const int base = first + KEYS * w.kg;
             q4_f32x16 s[KB];
@@ -669,7 +694,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
 #pragma unroll
                 for (int kk = 0; kk < D / 16; kk++) {
                     uint4 kf[NP];
-                    q4_eight(row + 16 * kk, 0, kf);
+                    q4_eight(row + 16 * kk, kf);
                     if constexpr (F32) bad |= q4_take_out(kf[0]);  // the products of its parts would be NaN
 #pragma unroll
                     for (int x = 0; x < NP; x++)
@@ -685,7 +710,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                             const T *const kr = kt + (((size_t)b * p.T_max + j) * p.Hkv + kvh) * D, *const qr = static_cast<const T *>(p.q) + q_row;
                             float sum = 0.f;
                             for (int c = 0; c < D; c++) sum = fmaf(q4_elem(kr, c), q4_elem(qr, c), sum);
-                            s[kb][i] = p.flip ? -sum : sum;
+                            s[kb][i] = sum;
                         }
                     }
             }
@@ -694,16 +719,23 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
                 vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)] >> (base & 63);
                 if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
             }
-            uint32_t pk[NP][KB][8];
+#pragma unroll
+            for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[kb][i] *= p.scale_log2;
             w.mask(s, vis);
-            w.softmax(s, pk);
+            w.enter(s);
+            uint32_t pk[NP][KB][8];
+            float part[2];
+            Wave::weigh_all(s, pk, part);
+            w.template settle<false>(s, s, pk, part);
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
                 uint8_t *const tile = w.tile();
                 for (int c = w.lane + 64 * w.wr; c < KEYS * D / 8; c += 64 * RW) {
                     const int key = c / (D / 8), piece = c % (D / 8);
                     uint4 vf[NP];
-                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, 0, vf);
+                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, vf);
                     if constexpr (F32) {
                         uint4 first_part = vf[0];
                         const bool bad = q4_take_out(first_part);
@@ -962,8 +994,6 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
         else hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 128>), grid, dim3(64), 0, st, p);
         return etv::check_launch();
     }
-    p.flip = p.scale_log2 < 0 ? 0x80008000u : 0;
-    p.scale_log2 = fabsf(p.scale_log2);
     p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.units = (int)pl.units;
     p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_seqs = etv::fast_div_inv(p.B * p.Hkv);
     p.inv_groups = etv::fast_div_inv(p.row_groups);
