@@ -21,12 +21,14 @@ struct Q4Attn {
     int B, T_max, Hq, Hkv, G, block_size, max_blocks, num_blocks, P_cap, P_max, words;
     float scale_log2;  // of the scores, times log2(e)
     uint32_t inv_bs;
-    // matrix kernel: a sequence's prefix in splits of `chunk` keys, one slot each, and with more than one split a slot more for
-    // the tree.  Partials, if slots > 1: part_o [B * Hkv][slots][row_groups * 32 * RW][D], part_ml (reference, sum) alike.
-    int chunk, nsplit, slots, row_groups, units;
-    uint32_t inv_g, inv_hkv, inv_seqs, inv_groups;
+    // matrix kernel: prefixes in splits, B * nsplit slots for them and, where there is more than one each (slots > B), B more for
+    // the trees.  chunk: keys of a split, or 0: worked out on the device, where the lengths are (B <= 64).
+    // Partials, if slots > B: part_o [Hkv][slots][rows_padded][D], part_ml (reference, sum) alike; split_tab [B] first slot, slots.
+    int chunk, nsplit, slots, row_groups, rows_padded, units, span;
+    uint32_t inv_g, inv_hkv, inv_groups, inv_nsplit;
     float *part_o;
     float2 *part_ml;
+    int2 *split_tab;
 };
 
 constexpr float kQ4Ln2 = 0.6931471805599453f;
@@ -167,8 +169,8 @@ constexpr float kQ4Lazy = 1024.f;  // the largest sum of a lane's weights in a t
 // outputs [4][32][64 + 4] fp32.
 template <int D, int RW>
 struct Q4Geo {
-    static constexpr int KB = RW == 1 ? 1 : 2, KEYS = 32 * KB;  // key blocks and keys of a tile
-    static constexpr int AHEAD = RW == 1 ? 2 : 1;                // tiles whose codes are on their way besides the next one's
+    static constexpr int KB = RW == 4 ? 2 : 1, KEYS = 32 * KB;  // key blocks and keys of a tile
+    static constexpr int AHEAD = RW == 4 ? 1 : 2;                // tiles whose codes are on their way besides the next one's
     static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = 2;
     static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
     static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
@@ -394,8 +396,38 @@ __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int hea
     if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : inv != inv ? NAN : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
 }
 
+// Which keys of which sequence a prefix slot stands for.  All splits of a call are of one size c (in rounds of `span` keys), the
+// smallest for which the slots suffice: nearly so where c = ceil(rounds / slots) works out, and with c = ceil(rounds / (slots - B))
+// always, a sequence's last split being the only one that is not full.  So a short sequence has few splits and the long ones of a
+// ragged batch share the rest.  Every wavefront works it out for itself, a lane per sequence.
+struct Q4Share {
+    int b, k0, k1, first, count;  // count 0: nobody's slot.  first, count: the sequence's slots
+};
+__device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane) {
+    const bool in = lane < p.B;
+    const int P = in ? clampi(p.prefix_len[in ? lane : 0], 0, p.P_max) : 0;
+    const int rounds = P > 0 && p.n_nodes[in ? lane : 0] > 0 ? (P + p.span - 1) / p.span : 0, slots = p.B * p.nsplit;
+    const int total = __builtin_amdgcn_readlane(wave_scan_sum(rounds), 63);
+    int c = p.chunk > 0 ? p.chunk / p.span : max(1, (total + slots - 1) / slots);
+    int count = (rounds + c - 1) / c, upto = wave_scan_sum(count);
+    if (__builtin_amdgcn_readlane(upto, 63) > slots) {
+        c = (total + slots - p.B - 1) / (slots - p.B);
+        count = (rounds + c - 1) / c;
+        upto = wave_scan_sum(count);
+    }
+    const int b = __popcll(__ballot(upto <= slot));  // sequences that end before the slot; lanes behind the last repeat its end
+    Q4Share r{};
+    if (b >= p.B) return r;
+    r.b = b;
+    r.count = __builtin_amdgcn_readlane(count, b);
+    r.first = __builtin_amdgcn_readlane(upto, b) - r.count;
+    r.k0 = (slot - r.first) * c * p.span;
+    r.k1 = min(r.k0 + c * p.span, __builtin_amdgcn_readlane(P, b));
+    return r;
+}
+
 template <int D, bool F32, int RW, bool PAGED>
-__global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
+__global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
     using G = Q4Geo<D, RW>;
@@ -418,21 +450,39 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
         for (int i = 0; i < 16; i++) w.o[db][i] = 0.f;
     const int r = w.r, hh = w.hh;
 
-    // The row groups of a unit read the same keys: their workgroups are eight apart, on one of the eight XCDs.
-    uint32_t group, slot, kvh;
+    // The row groups of a unit read the same keys: their workgroups are eight apart, on one of the eight XCDs.  The trees' units,
+    // which are short, come last.
+    uint32_t group, kvh, rem;
     const uint32_t unit = fast_div(blockIdx.x >> 3, (uint32_t)p.row_groups, p.inv_groups, group) * 8 + (blockIdx.x & 7);
     if (unit >= (uint32_t)p.units) return;
-    uint32_t bh;
-    slot = fast_div(unit, (uint32_t)(p.B * p.Hkv), p.inv_seqs, bh);  // the trees' workgroups, which are short, come last
-    const int b = (int)fast_div(bh, (uint32_t)p.Hkv, p.inv_hkv, kvh);
-    const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max);
-    const bool whole = p.slots == 1, tree_here = whole || (int)slot == p.nsplit;
-    const int k0 = whole ? 0 : tree_here ? P : min(P, (int)slot * p.chunk), k1 = whole || tree_here ? P : min(P, k0 + p.chunk);
-    if (!tree_here && k0 >= k1) return;
+    const int slot = (int)fast_div(unit, (uint32_t)p.Hkv, p.inv_hkv, kvh);
+    const bool whole = p.slots == p.B, tree_here = whole || slot >= p.B * p.nsplit;
+    int b = 0, k0 = 0, k1 = 0;
+    if (tree_here) {
+        b = whole ? slot : slot - p.B * p.nsplit;
+        k1 = whole ? clampi(p.prefix_len[b], 0, p.P_max) : 0;
+    } else if (p.B <= 64) {
+        const Q4Share share = q4_share(p, slot, w.lane);
+        if (share.count == 0) return;
+        b = share.b;
+        k0 = share.k0;
+        k1 = share.k1;
+        if (slot == share.first && kvh == 0 && group == 0 && tid == 0) p.split_tab[b] = int2{share.first, share.count};
+    } else {
+        b = (int)fast_div((uint32_t)slot, (uint32_t)p.nsplit, p.inv_nsplit, rem);
+        const int P = clampi(p.prefix_len[b], 0, p.P_max);
+        k0 = (int)min((int64_t)P, (int64_t)rem * p.chunk);
+        k1 = (int)min((int64_t)P, (int64_t)k0 + p.chunk);
+        if (rem == 0 && kvh == 0 && group == 0 && tid == 0) p.split_tab[b] = int2{slot, (P + p.chunk - 1) / p.chunk};
+        if (k0 >= k1) return;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    k0 = __builtin_amdgcn_readfirstlane(k0);
+    k1 = __builtin_amdgcn_readfirstlane(k1);
+    const int n = clampi(p.n_nodes[b], 0, p.T_max);
     uint32_t g;
     const int t = (int)fast_div(group * 32 * RW + 32 * w.wr + r, (uint32_t)p.G, p.inv_g, g);
     const size_t q_row = (((size_t)b * p.T_max + min(t, p.T_max - 1)) * p.Hq + kvh * p.G + g) * D;
-    uint32_t rem;
     const bool live = (int)fast_div(group * 32 * RW, (uint32_t)p.G, p.inv_g, rem) < n;  // has the workgroup a row?
     if (!live && !whole) return;
     bool ill = false;  // the tree's V holds values that are not finite
@@ -829,7 +879,7 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
             }
             if (!whole) {
                 if (tt >= n) continue;
-                const size_t at = ((size_t)bh * p.slots + slot) * (size_t)(p.row_groups * 32 * RW) + packed;
+                const size_t at = ((size_t)kvh * p.slots + slot) * (size_t)p.rows_padded + packed;
                 float4 *const dst = reinterpret_cast<float4 *>(p.part_o + at * D + 64 * half + 8 * piece);
                 dst[0] = float4{acc[0], acc[1], acc[2], acc[3]};
                 dst[1] = float4{acc[4], acc[5], acc[6], acc[7]};
@@ -842,31 +892,63 @@ __global__ void __launch_bounds__(256, 2) attn_q4_kernel(Q4Attn p) {
     }
 }
 
-// The partials of a row joined, split by split and the tree's last.  A thread has eight channels; grid (ceil(T_max * Hq / (2048 / D)), B).
+// The partials of a row joined, a wavefront per row: its lanes have eight channels each, and the 512 / D of them that have the
+// same ones share out the splits.  grid (ceil(T_max * Hq / 4), B).
 template <int D, bool F32>
-__global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p, int rows_padded) {
+__global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
-    const int b = blockIdx.y, piece = threadIdx.x % (D / 8), x = blockIdx.x * (2048 / D) + threadIdx.x / (D / 8);
+    constexpr int PIECES = D / 8, WORKERS = 64 / PIECES, BATCH = 4;
+    const int b = blockIdx.y, lane = threadIdx.x & 63, piece = lane % PIECES, worker = lane / PIECES;
+    const int x = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (x >= p.T_max * p.Hq) return;
     const int t = x / p.Hq, head = x % p.Hq, kvh = head / p.G;
-    const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max), used = (P + p.chunk - 1) / p.chunk;
+    const int n = clampi(p.n_nodes[b], 0, p.T_max);
     float ref = -INFINITY, sum = 0.f, acc[8] = {};
     if (t < n) {
-        const size_t row0 = ((size_t)(b * p.Hkv + kvh) * p.slots) * rows_padded + (size_t)t * p.G + head % p.G;
-        const auto slot_of = [&](int s) { return s == used ? p.nsplit : s; };
-        for (int s = 0; s <= used; s++) ref = fmaxf(ref, p.part_ml[row0 + (size_t)slot_of(s) * rows_padded].x);
-        const float zero = ref == -INFINITY ? 0.f : ref;
-        for (int s = 0; s <= used; s++) {
-            const size_t at = row0 + (size_t)slot_of(s) * rows_padded;
-            const float2 ml = p.part_ml[at];
-            const float f = __builtin_amdgcn_exp2f(ml.x - zero);
-            const float4 a = reinterpret_cast<const float4 *>(p.part_o + at * D + 8 * piece)[0], c = reinterpret_cast<const float4 *>(p.part_o + at * D + 8 * piece)[1];
-            sum += f * ml.y;
-            acc[0] += f * a.x; acc[1] += f * a.y; acc[2] += f * a.z; acc[3] += f * a.w;
-            acc[4] += f * c.x; acc[5] += f * c.y; acc[6] += f * c.z; acc[7] += f * c.w;
+        const int P = clampi(p.prefix_len[b], 0, p.P_max);
+        const int2 tab = P > 0 ? p.split_tab[b] : int2{0, 0};
+        const size_t row0 = (size_t)kvh * p.slots * p.rows_padded + (size_t)t * p.G + head % p.G;
+        // entry 0 is the tree's, the others the splits'
+        const int entries = tab.y + 1, tree = p.B * p.nsplit + b;
+        const auto at = [&](int e) { return row0 + (size_t)(e == 0 ? tree : tab.x + e - 1) * p.rows_padded; };
+        for (int first = 0; first < entries; first += 64) {
+            const int e = first + lane;
+            const float2 ml = e < entries ? p.part_ml[at(e)] : float2{-INFINITY, 0.f};
+            float top = ml.x;
+            for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+            const float next = fmaxf(ref, top), zero = next == -INFINITY ? 0.f : next;
+            const float f = e < entries ? __builtin_amdgcn_exp2f(ml.x - zero) : 0.f, old = __builtin_amdgcn_exp2f(ref - zero);
+            ref = next;
+            float part = f * ml.y;
+            for (int o = 32; o; o >>= 1) part += __shfl_xor(part, o);
+            sum = sum * old + part;
+            for (int j = 0; j < 8; j++) acc[j] *= old;
+            const int here = min(64, entries - first);
+            for (int j = worker; j < here; j += WORKERS * BATCH) {
+                float4 v[BATCH][2];
+                float g[BATCH];
+#pragma unroll
+                for (int u = 0; u < BATCH; u++) {
+                    const int k = min(j + u * WORKERS, here - 1);
+                    const float4 *const src = reinterpret_cast<const float4 *>(p.part_o + at(first + k) * D + 8 * piece);
+                    v[u][0] = src[0];
+                    v[u][1] = src[1];
+                }
+#pragma unroll
+                for (int u = 0; u < BATCH; u++) {
+                    const int k = j + u * WORKERS;
+                    g[u] = __shfl(f, min(k, here - 1));
+                    if (k < here) {
+                        acc[0] += g[u] * v[u][0].x; acc[1] += g[u] * v[u][0].y; acc[2] += g[u] * v[u][0].z; acc[3] += g[u] * v[u][0].w;
+                        acc[4] += g[u] * v[u][1].x; acc[5] += g[u] * v[u][1].y; acc[6] += g[u] * v[u][1].z; acc[7] += g[u] * v[u][1].w;
+                    }
+                }
+            }
         }
+        for (int j = 0; j < 8; j++)
+            for (int o = PIECES; o < 64; o <<= 1) acc[j] += __shfl_xor(acc[j], o);
     }
-    q4_finish<T>(p, b, t, head, piece, D, t < n, ref, sum, acc);
+    if (worker == 0) q4_finish<T>(p, b, t, head, piece, D, t < n, ref, sum, acc);
 }
 
 // What is wrong with a descriptor by itself.
@@ -888,39 +970,41 @@ static int32_t q4_check_desc(const etv_attn_desc *h) {
 }
 
 struct Q4Plan {
-    int rw, row_groups, chunk, nsplit, slots;
+    int rw, row_groups, chunk, nsplit, slots, span;
     int64_t units;
-    size_t rows() const { return (size_t)units * row_groups * 32 * rw; }
-    size_t workspace(int d) const { return slots == 1 ? 256 : rows() * ((size_t)d * 4 + 8) + 256; }
+    int rows_padded() const { return row_groups * 32 * rw; }
+    size_t rows() const { return (size_t)units * rows_padded(); }
+    size_t workspace(const etv_attn_desc *h) const { return nsplit == 1 ? 256 : rows() * ((size_t)h->d * 4 + 8) + (size_t)h->B * 8 + 256; }
 };
 
 static Q4Plan q4_plan(const etv_attn_desc *h) {
     Q4Plan pl{};
-    const int rows = h->T_max * (h->Hq / h->Hkv);
+    const int rows = h->T_max * (h->Hq / h->Hkv), B = std::max(1, h->B);
     pl.rw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     pl.row_groups = (rows + 32 * pl.rw - 1) / (32 * pl.rw);
-    const int span = (pl.rw == 1 ? 32 : 64) * (4 / pl.rw);
-    const int64_t seqs = (int64_t)std::max(1, h->B) * h->Hkv;
-    const int tiles = std::max(1, (h->P_max + span - 1) / span);  // rounds of a workgroup over the longest prefix
-    int best = 1;
+    pl.span = (pl.rw == 4 ? 64 : 32) * (4 / pl.rw);
+    const int64_t seqs = (int64_t)B * h->Hkv;
+    const int rounds = std::max(1, (h->P_max + pl.span - 1) / pl.span);  // of a workgroup over the longest prefix
+    pl.nsplit = 1;
     if (h->kv_split > 0) {
-        pl.chunk = (h->kv_split + 63) / 64 * 64;
-        best = std::max(1, (int)((h->P_max + (int64_t)pl.chunk - 1) / pl.chunk));
+        pl.chunk = (int)std::min<int64_t>((h->kv_split + (int64_t)pl.span - 1) / pl.span, rounds) * pl.span;
+        pl.nsplit = std::max(1, (h->P_max + pl.chunk - 1) / pl.chunk);
     } else {
-        // two workgroups a compute unit; a round costs 1, starting and joining a workgroup 3, the second launch 5 and a little more for
-        // every split whose rows it reads
+        // Two workgroups a compute unit.  In units of a round: starting and ending a workgroup 3, the second launch 3 and a little more
+        // for every split whose rows it reads.
         double least = 1e30;
-        for (int ns = 1; ns <= std::min(tiles, 256); ns++) {
-            const int per = (tiles + ns - 1) / ns;
-            if (ns > 1 && (tiles + per - 1) / per != ns) continue;
+        int per = rounds;
+        for (int ns = 1; ns <= std::min(rounds, 128); ns++) {
+            const int each = (rounds + ns - 1) / ns;
+            if (ns > 1 && each == per) continue;
             const double full = (double)seqs * pl.row_groups * ns / 512, turns = full < 4 ? std::ceil(full) : full + 0.5;
-            const double cost = turns * (3 + per) + (ns > 1 ? 5 + 0.1 * ns + 3e-5 * (double)seqs * rows * ns : (h->T_max + span - 1) / span);
-            if (cost < least) least = cost, best = ns, pl.chunk = per * span;
+            const double cost = turns * (3 + each) + (ns > 1 ? 3 + 0.05 * ns + 1e-5 * (double)seqs * rows * ns : (h->T_max + pl.span - 1) / pl.span);
+            if (cost < least) least = cost, pl.nsplit = ns, per = each;
         }
+        pl.chunk = B <= 64 ? 0 : per * pl.span;
     }
-    pl.nsplit = best;
-    pl.slots = best == 1 ? 1 : best + 1;
-    pl.units = seqs * pl.slots;
+    pl.slots = B * (pl.nsplit == 1 ? 1 : pl.nsplit + 1);
+    pl.units = (int64_t)pl.slots * h->Hkv;
     return pl;
 }
 
@@ -946,15 +1030,15 @@ template <int D, bool F32>
 static int32_t run_q4(const Q4Plan &pl, const Q4Attn &p, hipStream_t st) {
     const unsigned grid = (unsigned)((pl.units + 7) / 8 * 8 * pl.row_groups);
     const int32_t rc = pl.rw == 1 ? launch_q4_form<D, F32, 1>(p, grid, st) : pl.rw == 2 ? launch_q4_form<D, F32, 2>(p, grid, st) : launch_q4_form<D, F32, 4>(p, grid, st);
-    if (rc != ETV_OK || pl.slots == 1) return rc;
-    hipLaunchKernelGGL((join_q4_kernel<D, F32>), dim3((p.T_max * p.Hq + 2048 / D - 1) / (2048 / D), p.B), dim3(256), 0, st, p, pl.row_groups * 32 * pl.rw);
+    if (rc != ETV_OK || pl.nsplit == 1) return rc;
+    hipLaunchKernelGGL((join_q4_kernel<D, F32>), dim3((p.T_max * p.Hq + 3) / 4, p.B), dim3(256), 0, st, p);
     return check_launch();
 }
 
 }  // namespace etv
 
 extern "C" size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h) {
-    return etv::q4_check_desc(h) == ETV_OK ? etv::q4_plan(h).workspace(h->d) : 0;
+    return etv::q4_check_desc(h) == ETV_OK ? etv::q4_plan(h).workspace(h) : 0;
 }
 
 extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const void *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -974,7 +1058,7 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
     const etv::Q4Plan pl = etv::q4_plan(h);
     const bool generic = (h->flags & ETV_ATTN_FLAG_GENERIC) != 0;
     if (!generic && pl.units * pl.row_groups > INT32_MAX - 65536) return ETV_ERR_UNSUPPORTED;
-    if (!generic && pl.slots > 1 && (!workspace || workspace_bytes < pl.workspace(h->d))) return ETV_ERR_WORKSPACE_TOO_SMALL;
+    if (!generic && pl.nsplit > 1 && (!workspace || workspace_bytes < pl.workspace(h))) return ETV_ERR_WORKSPACE_TOO_SMALL;
     etv::Q4Attn p{};
     p.q = q; p.kt = kt; p.vt = vt;
     p.codes[0] = k_codes; p.codes[1] = v_codes; p.scales[0] = k_scales; p.scales[1] = v_scales;
@@ -994,12 +1078,14 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
         else hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 128>), grid, dim3(64), 0, st, p);
         return etv::check_launch();
     }
-    p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.units = (int)pl.units;
-    p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_seqs = etv::fast_div_inv(p.B * p.Hkv);
-    p.inv_groups = etv::fast_div_inv(p.row_groups);
-    if (pl.slots > 1) {
+    p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.rows_padded = pl.rows_padded();
+    p.units = (int)pl.units; p.span = pl.span;
+    p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_groups = etv::fast_div_inv(p.row_groups);
+    p.inv_nsplit = etv::fast_div_inv(p.nsplit);
+    if (pl.nsplit > 1) {
         p.part_o = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float2 *>(p.part_o + pl.rows() * h->d);
+        p.split_tab = reinterpret_cast<int2 *>(p.part_ml + pl.rows());
     }
     if (h->dtype == ETV_F32) return h->d == 64 ? etv::run_q4<64, true>(pl, p, st) : etv::run_q4<128, true>(pl, p, st);
     return h->d == 64 ? etv::run_q4<64, false>(pl, p, st) : etv::run_q4<128, false>(pl, p, st);
