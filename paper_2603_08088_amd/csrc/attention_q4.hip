@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
 // six (2^-26).  Six-bit and four-bit operands run at four times the bf16 rate, so three parts cost less than one bf16 product,
 // and K needs neither a conversion nor LDS.
 // fp32: P in three bf16 parts, exactly, and the tree's K, V and q likewise (products with parts below 2^-24 left out).
-// RW wavefronts of a workgroup share the keys and have rows of their own, the 4 / RW groups of them share the rows: few rows
+// RW wavefronts of a workgroup share their keys and have rows of their own; the groups of RW share the rows: few rows
 // (a token, a small tree) leave reading the cache as the work, and every wavefront reads keys of its own.
 typedef int q4_i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t q4_u32x6 __attribute__((ext_vector_type(6)));
@@ -166,14 +166,16 @@ typedef __attribute__((address_space(4))) const int32_t *const_ids;
 constexpr float kQ4Lazy = 1024.f;  // the largest sum of a lane's weights in a tile without a new reference
 
 // Dynamic LDS: V tiles [key groups][2][keys][D] bf16, afterwards 64 channels at a time of the
-// outputs [4][32][64 + 4] fp32.
-template <int D, int RW>
+// outputs [wavefronts][32][64 + 4] fp32.
+constexpr int q4_wavefronts(bool f32, int rw) { return rw == 4 || f32 ? 4 : 8; }  // of a workgroup
+template <int D, bool F32, int RW>
 struct Q4Geo {
+    static constexpr int NW = q4_wavefronts(F32, RW);
     static constexpr int KB = RW == 4 ? 2 : 1, KEYS = 32 * KB;  // key blocks and keys of a tile
     static constexpr int AHEAD = RW == 4 ? 1 : 2;                // tiles whose codes are on their way besides the next one's
-    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = 4 / RW, BUFS = 2;
+    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = NW / RW, BUFS = 2;
     static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
-    static constexpr int TILES = KW * BUFS * TILE, OUT = 4 * 32 * (OUT_ROW * 4 + 8);
+    static constexpr int TILES = KW * BUFS * TILE, OUT = NW * 32 * (OUT_ROW * 4 + 8);
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
 };
 
@@ -232,7 +234,7 @@ __device__ __forceinline__ void q4_for(F f) { q4_each(f, std::make_integer_seque
 template <int D, bool F32, int RW>
 struct Q4Wave {
     static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 3, QW = F32 ? 2 : 1;
-    using G = Q4Geo<D, RW>;
+    using G = Q4Geo<D, F32, RW>;
     static constexpr int KB = G::KB;
     const Q4Attn &p;
     uint8_t *smem;
@@ -360,15 +362,24 @@ struct Q4Wave {
     }
 };
 
-// Eight consecutive channels of an unquantised row as NP bf16 parts.
-__device__ __forceinline__ void q4_eight(const uint16_t *p, uint4 (&part)[1]) { part[0] = *reinterpret_cast<const uint4 *>(p); }
-__device__ __forceinline__ void q4_eight(const float *p, uint4 (&part)[3]) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    q4_split(a.x, a.y, part[0].x, part[1].x, part[2].x);
-    q4_split(a.z, a.w, part[0].y, part[1].y, part[2].y);
-    q4_split(b.x, b.y, part[0].z, part[1].z, part[2].z);
-    q4_split(b.z, b.w, part[0].w, part[1].w, part[2].w);
-}
+// Eight consecutive channels of an unquantised row: as they lie in memory, and as NP bf16 parts.
+template <typename T>
+struct Q4Eight {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (size_t i = 0; i < sizeof(T) / 2; i++) w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void parts(uint4 (&part)[1]) const { part[0] = w[0]; }
+    __device__ __forceinline__ void parts(uint4 (&part)[3]) const {
+        const uint4 &a = w[0], &b = w[sizeof(T) / 2 - 1];
+        const auto f = [](uint32_t x) { return __uint_as_float(x); };
+        q4_split(f(a.x), f(a.y), part[0].x, part[1].x, part[2].x);
+        q4_split(f(a.z), f(a.w), part[0].y, part[1].y, part[2].y);
+        q4_split(f(b.x), f(b.y), part[0].z, part[1].z, part[2].z);
+        q4_split(f(b.z), f(b.w), part[0].w, part[1].w, part[2].w);
+    }
+};
 // the values that are not finite out of eight bf16 (first parts); true if there were any
 __device__ __forceinline__ bool q4_take_out(uint4 &w) {
     const auto ill = [](uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
@@ -427,10 +438,10 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
 }
 
 template <int D, bool F32, int RW, bool PAGED>
-__global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q4Attn p) {
+__global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
-    using G = Q4Geo<D, RW>;
+    using G = Q4Geo<D, F32, RW>;
     constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS, AHEAD = G::AHEAD;
     extern __shared__ __attribute__((aligned(1024))) uint8_t q4_smem[];
     const int tid = threadIdx.x;
@@ -728,23 +739,45 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
     if (live && tree_here) {
         // The tree: bf16 parts throughout.  n >= 1 here.
         const T *const kt = static_cast<const T *>(p.kt), *const vt = static_cast<const T *>(p.vt);
-        uint4 qf[D / 16][NP];
+        constexpr int KK = D / 16, PIECES = KEYS * D / 8 / (64 * RW);
+        uint4 qf[KK][NP];
+        {
+            Q4Eight<T> raw[KK];
 #pragma unroll
-        for (int kk = 0; kk < D / 16; kk++) q4_eight(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh, qf[kk]);
+            for (int kk = 0; kk < KK; kk++) raw[kk].load(static_cast<const T *>(p.q) + q_row + 16 * kk + 8 * hh);
+#pragma unroll
+            for (int kk = 0; kk < KK; kk++) raw[kk].parts(qf[kk]);
+        }
         for (int first = 0; first < n; first += KEYS * KW) {  // the same number of rounds for every wavefront
             const int base = first + KEYS * w.kg;
+            // everything from memory at once: the mask, V (a wavefront's share of the tile) and K
+            uint64_t vis = p.bitmask[((size_t)b * p.T_max + min(t, p.T_max - 1)) * p.words + (min(base, n - 1) >> 6)] >> (base & 63);
+            Q4Eight<T> vraw[PIECES];
+#pragma unroll
+            for (int j = 0; j < PIECES; j++) {
+                const int c = w.lane + 64 * w.wr + 64 * RW * j, key = min(base + c / (D / 8), n - 1);
+                vraw[j].load(vt + (((size_t)b * p.T_max + key) * p.Hkv + kvh) * D + 8 * (c % (D / 8)));
+            }
+            Q4Eight<T> kraw[F32 ? 1 : KB][KK];
+            const auto load_keys = [&](int kb) {
+                const T *const row = kt + (((size_t)b * p.T_max + min(base + 32 * kb + r, n - 1)) * p.Hkv + kvh) * D + 8 * hh;
+#pragma unroll
+                for (int kk = 0; kk < KK; kk++) kraw[F32 ? 0 : kb][kk].load(row + 16 * kk);
+            };
+            if constexpr (!F32)
+#pragma unroll
+                for (int kb = 0; kb < KB; kb++) load_keys(kb);
             q4_f32x16 s[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
+                if constexpr (F32) load_keys(kb);
 #pragma unroll
                 for (int i = 0; i < 16; i++) s[kb][i] = 0.f;
-                const int key = min(base + 32 * kb + r, n - 1);
-                const T *const row = kt + (((size_t)b * p.T_max + key) * p.Hkv + kvh) * D + 8 * hh;
                 bool bad = false;
 #pragma unroll
-                for (int kk = 0; kk < D / 16; kk++) {
+                for (int kk = 0; kk < KK; kk++) {
                     uint4 kf[NP];
-                    q4_eight(row + 16 * kk, kf);
+                    kraw[F32 ? 0 : kb][kk].parts(kf);
                     if constexpr (F32) bad |= q4_take_out(kf[0]);  // the products of its parts would be NaN
 #pragma unroll
                     for (int x = 0; x < NP; x++)
@@ -764,11 +797,8 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
                         }
                     }
             }
-            uint64_t vis = 0;
-            if (base < n && t < n) {
-                vis = p.bitmask[((size_t)b * p.T_max + t) * p.words + (base >> 6)] >> (base & 63);
-                if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
-            }
+            if (base >= n || t >= n) vis = 0;
+            else if (n - base < KEYS) vis &= (1ull << (n - base)) - 1;
 #pragma unroll
             for (int kb = 0; kb < KB; kb++)
 #pragma unroll
@@ -782,10 +812,11 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
                 uint8_t *const tile = w.tile();
-                for (int c = w.lane + 64 * w.wr; c < KEYS * D / 8; c += 64 * RW) {
-                    const int key = c / (D / 8), piece = c % (D / 8);
+#pragma unroll
+                for (int j = 0; j < PIECES; j++) {
+                    const int c = w.lane + 64 * w.wr + 64 * RW * j, key = c / (D / 8), piece = c % (D / 8);
                     uint4 vf[NP];
-                    q4_eight(vt + (((size_t)b * p.T_max + min(base + key, n - 1)) * p.Hkv + kvh) * D + 8 * piece, vf);
+                    vraw[j].parts(vf);
                     if constexpr (F32) {
                         uint4 first_part = vf[0];
                         const bool bad = q4_take_out(first_part);
@@ -846,7 +877,7 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
 
     // Outputs through LDS, 64 channels at a time: the key groups of a row are joined, and rows are stored in one piece.
     float *const mine = reinterpret_cast<float *>(q4_smem) + (wave * 32 + r) * G::OUT_ROW + 4 * hh;
-    float2 *const ml = reinterpret_cast<float2 *>(q4_smem + 4 * 32 * G::OUT_ROW * 4);
+    float2 *const ml = reinterpret_cast<float2 *>(q4_smem + G::NW * 32 * G::OUT_ROW * 4);
     if (hh == 0) ml[wave * 32 + r] = float2{w.m, row_sum};
 #pragma unroll
     for (int half = 0; half < D / 64; half++) {
@@ -859,7 +890,7 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
                 *reinterpret_cast<float4 *>(mine + 32 * db + 2 * i) = float4{o[i], o[i + 1], o[i + 2], o[i + 3]};
             }
         __syncthreads();
-        for (int c = tid; c < 32 * RW * 8; c += 256) {
+        for (int c = tid; c < 32 * RW * 8; c += 64 * G::NW) {
             const int row = c >> 3, piece = c & 7, chunk = row / 32;  // chunk: the wavefront among the RW
             const uint32_t packed = group * 32 * RW + row;
             uint32_t gg;
@@ -892,14 +923,15 @@ __global__ void __launch_bounds__(256, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q
     }
 }
 
-// The partials of a row joined, a wavefront per row: its lanes have eight channels each, and the 512 / D of them that have the
-// same ones share out the splits.  grid (ceil(T_max * Hq / 4), B).
-template <int D, bool F32>
+// The partials of a row joined by WIDTH lanes: they have eight channels each, and where those are fewer than the lanes (WIDTH 64)
+// the others share out the splits.  Few rows want the latter, many rows the narrow form (15360 rows of 5 partials: 12.4 and 7.5 us;
+// 32 rows of 17: 4.6 and 11.8).  grid (ceil(T_max * Hq / (256 / WIDTH)), B).
+template <int D, bool F32, int WIDTH>
 __global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
-    constexpr int PIECES = D / 8, WORKERS = 64 / PIECES, BATCH = 4;
-    const int b = blockIdx.y, lane = threadIdx.x & 63, piece = lane % PIECES, worker = lane / PIECES;
-    const int x = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    constexpr int PIECES = D / 8, WORKERS = WIDTH / PIECES, BATCH = 4;
+    const int b = blockIdx.y, lane = threadIdx.x % WIDTH, piece = lane % PIECES, worker = lane / PIECES;
+    const int x = blockIdx.x * (256 / WIDTH) + threadIdx.x / WIDTH;
     if (x >= p.T_max * p.Hq) return;
     const int t = x / p.Hq, head = x % p.Hq, kvh = head / p.G;
     const int n = clampi(p.n_nodes[b], 0, p.T_max);
@@ -911,19 +943,19 @@ __global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
         // entry 0 is the tree's, the others the splits'
         const int entries = tab.y + 1, tree = p.B * p.nsplit + b;
         const auto at = [&](int e) { return row0 + (size_t)(e == 0 ? tree : tab.x + e - 1) * p.rows_padded; };
-        for (int first = 0; first < entries; first += 64) {
+        for (int first = 0; first < entries; first += WIDTH) {
             const int e = first + lane;
             const float2 ml = e < entries ? p.part_ml[at(e)] : float2{-INFINITY, 0.f};
             float top = ml.x;
-            for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+            for (int o = WIDTH / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
             const float next = fmaxf(ref, top), zero = next == -INFINITY ? 0.f : next;
             const float f = e < entries ? __builtin_amdgcn_exp2f(ml.x - zero) : 0.f, old = __builtin_amdgcn_exp2f(ref - zero);
             ref = next;
             float part = f * ml.y;
-            for (int o = 32; o; o >>= 1) part += __shfl_xor(part, o);
+            for (int o = WIDTH / 2; o; o >>= 1) part += __shfl_xor(part, o);
             sum = sum * old + part;
             for (int j = 0; j < 8; j++) acc[j] *= old;
-            const int here = min(64, entries - first);
+            const int here = min(WIDTH, entries - first);
             for (int j = worker; j < here; j += WORKERS * BATCH) {
                 float4 v[BATCH][2];
                 float g[BATCH];
@@ -937,7 +969,7 @@ __global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
 #pragma unroll
                 for (int u = 0; u < BATCH; u++) {
                     const int k = j + u * WORKERS;
-                    g[u] = __shfl(f, min(k, here - 1));
+                    g[u] = __shfl(f, min(k, here - 1), WIDTH);
                     if (k < here) {
                         acc[0] += g[u] * v[u][0].x; acc[1] += g[u] * v[u][0].y; acc[2] += g[u] * v[u][0].z; acc[3] += g[u] * v[u][0].w;
                         acc[4] += g[u] * v[u][1].x; acc[5] += g[u] * v[u][1].y; acc[6] += g[u] * v[u][1].z; acc[7] += g[u] * v[u][1].w;
@@ -946,7 +978,7 @@ __global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
             }
         }
         for (int j = 0; j < 8; j++)
-            for (int o = PIECES; o < 64; o <<= 1) acc[j] += __shfl_xor(acc[j], o);
+            for (int o = PIECES; o < WIDTH; o <<= 1) acc[j] += __shfl_xor(acc[j], o);
     }
     if (worker == 0) q4_finish<T>(p, b, t, head, piece, D, t < n, ref, sum, acc);
 }
@@ -982,7 +1014,8 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     const int rows = h->T_max * (h->Hq / h->Hkv), B = std::max(1, h->B);
     pl.rw = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     pl.row_groups = (rows + 32 * pl.rw - 1) / (32 * pl.rw);
-    pl.span = (pl.rw == 4 ? 64 : 32) * (4 / pl.rw);
+    const int waves = q4_wavefronts(h->dtype == ETV_F32, pl.rw);
+    pl.span = (pl.rw == 4 ? 64 : 32) * (waves / pl.rw);
     const int64_t seqs = (int64_t)B * h->Hkv;
     const int rounds = std::max(1, (h->P_max + pl.span - 1) / pl.span);  // of a workgroup over the longest prefix
     pl.nsplit = 1;
@@ -990,14 +1023,14 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
         pl.chunk = (int)std::min<int64_t>((h->kv_split + (int64_t)pl.span - 1) / pl.span, rounds) * pl.span;
         pl.nsplit = std::max(1, (h->P_max + pl.chunk - 1) / pl.chunk);
     } else {
-        // Two workgroups a compute unit.  In units of a round: starting and ending a workgroup 3, the second launch 3 and a little more
+        // Eight wavefronts a compute unit.  In units of a round: starting and ending a workgroup 3, the second launch 3 and a little more
         // for every split whose rows it reads.
         double least = 1e30;
         int per = rounds;
         for (int ns = 1; ns <= std::min(rounds, 128); ns++) {
             const int each = (rounds + ns - 1) / ns;
             if (ns > 1 && each == per) continue;
-            const double full = (double)seqs * pl.row_groups * ns / 512, turns = full < 4 ? std::ceil(full) : full + 0.5;
+            const double full = (double)seqs * pl.row_groups * ns / (2048 / waves), turns = full < 4 ? std::ceil(full) : full + 0.5;
             const double cost = turns * (3 + each) + (ns > 1 ? 3 + 0.05 * ns + 1e-5 * (double)seqs * rows * ns : (h->T_max + pl.span - 1) / pl.span);
             if (cost < least) least = cost, pl.nsplit = ns, per = each;
         }
@@ -1010,14 +1043,14 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
 
 template <int D, bool F32, int RW, bool PAGED>
 static int32_t launch_q4(const Q4Attn &p, unsigned grid, hipStream_t st) {
-    constexpr int lds = Q4Geo<D, RW>::LDS;
-    static_assert(lds <= 80 * 1024, "two workgroups a compute unit");
+    constexpr int lds = Q4Geo<D, F32, RW>::LDS;
+    static_assert(lds <= (Q4Geo<D, F32, RW>::NW == 8 ? 144 : 78) * 1024, "eight wavefronts a compute unit, and static LDS beside it");
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) {
         g_last_hip_error = (int32_t)e;
         return ETV_ERR_HIP;
     }
-    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED>), dim3(grid), dim3(256), lds, st, p);
+    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED>), dim3(grid), dim3(Q4Geo<D, F32, RW>::NW * 64), lds, st, p);
     return check_launch();
 }
 
@@ -1031,7 +1064,9 @@ static int32_t run_q4(const Q4Plan &pl, const Q4Attn &p, hipStream_t st) {
     const unsigned grid = (unsigned)((pl.units + 7) / 8 * 8 * pl.row_groups);
     const int32_t rc = pl.rw == 1 ? launch_q4_form<D, F32, 1>(p, grid, st) : pl.rw == 2 ? launch_q4_form<D, F32, 2>(p, grid, st) : launch_q4_form<D, F32, 4>(p, grid, st);
     if (rc != ETV_OK || pl.nsplit == 1) return rc;
-    hipLaunchKernelGGL((join_q4_kernel<D, F32>), dim3((p.T_max * p.Hq + 3) / 4, p.B), dim3(256), 0, st, p);
+    const int rows = p.T_max * p.Hq;
+    if ((int64_t)rows * p.B <= 2048) hipLaunchKernelGGL((join_q4_kernel<D, F32, 64>), dim3((rows + 3) / 4, p.B), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((join_q4_kernel<D, F32, D / 8>), dim3((rows + 2048 / D - 1) / (2048 / D), p.B), dim3(256), 0, st, p);
     return check_launch();
 }
 
