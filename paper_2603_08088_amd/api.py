@@ -549,55 +549,26 @@ def commit_path_indices(src_k, src_v, dst_k, dst_v, path_indices, src_len, new_l
 
 # ------------------------------------------------------------------------------------------------
 # the prefix cache in 4 bits
-def _q4_shapes(cache: KVCacheQ4, lead: int, d: int, block_table, B: int):
-    """What the C side takes on trust: four uint8 tensors of one cache's shapes, and the table's rows."""
-    shape = tuple(cache.k_codes.shape)
-    if len(shape) != lead + 4 or any(t.dtype != torch.uint8 for t in cache):
-        raise ValueError(f"codes and scales are uint8 [{'n_layers, ' if lead else ''}blocks, Hkv, block_size, d/2 or d/32]")
-    if cache.v_codes.shape != shape or any(tuple(t.shape) != shape[:-1] + (d // 32,) for t in (cache.k_scales, cache.v_scales)) or shape[-1] != d // 2:
-        raise ValueError("the codes and scales of a cache have the same rows, of d/2 and d/32 bytes")
-    if block_table is not None:
-        if block_table.dim() != 2 or block_table.shape[0] != B:
-            raise ValueError("block_table is [B, max_blocks]")
-    elif shape[lead] != B:
-        raise ValueError("a contiguous cache has one block per sequence")
-
-
-def _int32(shape, **tensors):
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape):
-            raise ValueError(f"{name} is int32 {list(shape)}")
-
-
-def _q4_desc(cache: KVCacheQ4, k, v, block_table, W: int = 0) -> Q4Desc:
-    if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("k and v are [n_layers, B, rows, Hkv, d], of one type")
-    Lyr, B, rows, Hkv, d = k.shape
-    _q4_shapes(cache, 1, d, block_table, B)
-    n, blocks, heads, size, _ = cache.k_codes.shape
-    if n != Lyr or heads != Hkv:
-        raise ValueError("the cache has other layers or heads than k and v")
-    paged = block_table is not None
-    if paged:
-        _int32((B, block_table.shape[1]), block_table=block_table)
-    # positional, in the order of Q4Desc
-    return Q4Desc(B, rows, Hkv, d, _dtype_code(k), Lyr, W, size if paged else 0, block_table.shape[1] if paged else 0,
-                  blocks if paged else 0, 0 if paged else size, 0, blocks * Hkv * size)
+def _q4_desc(fn: str, *tensors):
+    """The bytes of a Q4Desc; the binding checks types and shapes, which the C side takes on trust."""
+    dsc = _native().q4_desc(*tensors)
+    if dsc is None:
+        raise EtvError(fn, -2)
+    return dsc
 
 
 def quantize_kv_q4(k, v, cache: KVCacheQ4, prefix_len, n_rows, capacity, *, block_table=None,
                    out: Optional[Dict[str, torch.Tensor]] = None):
     """k/v [Lyr,B,rows,Hkv,d] fp32 or bf16; rows 0..n_rows[b]-1 go to positions prefix_len[b].. of the 4-bit cache, which is
     updated in place.  Returns prefix_len_out, status (int32 [B])."""
-    dsc, get = _q4_desc(cache, k, v, block_table), (out or {}).get
-    B, dev = k.shape[1], k.device
+    native, get = _native(), (out or {}).get
     plo, status = get("prefix_len_out"), get("status")
     if plo is None:
-        plo = _i32((B,), dev)
+        plo = native.empty_i32(prefix_len, len(prefix_len))
     if status is None:
-        status = _i32((B,), dev)
-    _int32((B,), prefix_len=prefix_len, n_rows=n_rows, capacity=capacity, prefix_len_out=plo, status=status)
-    rc = _native().quantize_kv_q4(dsc, k, v, *cache, block_table, prefix_len, n_rows, capacity, plo, status)
+        status = native.empty_i32(prefix_len, len(prefix_len))
+    dsc = _q4_desc("etv_quantize_kv_q4", k, v, *cache, block_table, None, None, prefix_len, n_rows, capacity, plo, status)
+    rc = native.quantize_kv_q4(dsc, k, v, *cache, block_table, prefix_len, n_rows, capacity, plo, status)
     _check("etv_quantize_kv_q4", rc)
     return dict(prefix_len_out=plo, status=status)
 
@@ -606,22 +577,18 @@ def commit_accepted_kv_q4(kt, vt, cache: KVCacheQ4, prefix_len, capacity, n_node
                           block_table=None, out: Optional[Dict[str, torch.Tensor]] = None):
     """commit_accepted_kv into a 4-bit cache: kt/vt [Lyr,B,T_max,Hkv,d] fp32 or bf16, the accepted rows are quantised as they
     are appended.  Returns prefix_len_out, slot_map, status."""
-    if acc_nodes.dim() != 2:
-        raise ValueError("acc_nodes is int32 [B, W]")
-    (B, W), dev, get = acc_nodes.shape, kt.device, (out or {}).get
-    dsc = _q4_desc(cache, kt, vt, block_table, W)
+    native, get = _native(), (out or {}).get
     plo, slot, status = get("prefix_len_out"), get("slot_map"), get("status")
     if plo is None:
-        plo = _i32((B,), dev)
+        plo = native.empty_i32(prefix_len, len(prefix_len))
     if slot is None:
-        slot = _i32((B, W), dev)
+        slot = native.empty_i32(acc_nodes, *acc_nodes.shape)
     if status is None:
-        status = _i32((B,), dev)
-    B = kt.shape[1]
-    _int32((B,), prefix_len=prefix_len, capacity=capacity, n_nodes=n_nodes, accept_len=accept_len, prefix_len_out=plo, status=status)
-    _int32((B, W), acc_nodes=acc_nodes, slot_map=slot)
-    rc = _native().commit_accepted_kv_q4(dsc, kt, vt, *cache, block_table, prefix_len, capacity, n_nodes, acc_nodes,
-                                         accept_len, plo, slot, status)
+        status = native.empty_i32(prefix_len, len(prefix_len))
+    dsc = _q4_desc("etv_commit_accepted_kv_q4", kt, vt, *cache, block_table, acc_nodes, slot, prefix_len, capacity, n_nodes,
+                   accept_len, plo, status)
+    rc = native.commit_accepted_kv_q4(dsc, kt, vt, *cache, block_table, prefix_len, capacity, n_nodes, acc_nodes, accept_len,
+                                      plo, slot, status)
     _check("etv_commit_accepted_kv_q4", rc)
     return dict(prefix_len_out=plo, slot_map=slot, status=status)
 
@@ -630,42 +597,31 @@ def dequantize_kv_q4(cache: KVCacheQ4, first, n_rows, rows: int, *, block_table=
                      out: Optional[Dict[str, torch.Tensor]] = None):
     """Positions first[b] .. first[b]+n_rows[b]-1 of the cache -> k, v [Lyr,B,rows,Hkv,d] (of `dtype`, or out["k"], out["v"]),
     zeros behind n_rows[b], and status int32 [B]."""
-    if cache.k_codes.dim() != 5:
-        raise ValueError("codes are uint8 [n_layers, blocks, Hkv, block_size, d/2]")
-    Lyr, _, Hkv, _, half = cache.k_codes.shape
-    B, dev, get = first.shape[0], first.device, (out or {}).get
-    shape = (Lyr, B, int(rows), Hkv, 2 * half)
+    native, get = _native(), (out or {}).get
     k, v, status = get("k"), get("v"), get("status")
-    if k is None:
-        k = torch.empty(shape, dtype=dtype if v is None else v.dtype, device=dev)
-    if v is None:
-        v = torch.empty(shape, dtype=k.dtype, device=dev)
+    if k is None or v is None:
+        Lyr, _, Hkv, _, half = cache.k_codes.shape
+        like = dict(dtype=dtype if k is None and v is None else (k if v is None else v).dtype, device=first.device)
+        shape = (Lyr, len(first), rows, Hkv, 2 * half)
+        k, v = (torch.empty(shape, **like) if t is None else t for t in (k, v))
     if status is None:
-        status = _i32((B,), dev)
-    if tuple(k.shape) != shape:
-        raise ValueError(f"k and v are {list(shape)}")
-    dsc = _q4_desc(cache, k, v, block_table)
-    _int32((B,), first=first, n_rows=n_rows, status=status)
-    rc = _native().dequantize_kv_q4(dsc, *cache, block_table, first, n_rows, k, v, status)
+        status = native.empty_i32(first, len(first))
+    if k.dim() == 5 and k.shape[2] != rows:
+        raise ValueError(f"k and v have {rows} rows")
+    dsc = _q4_desc("etv_dequantize_kv_q4", k, v, *cache, block_table, None, None, first, n_rows, status)
+    rc = native.dequantize_kv_q4(dsc, *cache, block_table, first, n_rows, k, v, status)
     _check("etv_dequantize_kv_q4", rc)
     return dict(k=k, v=v, status=status)
 
 
 def attn_q4_desc(q: torch.Tensor, cache: KVCacheQ4, kt: torch.Tensor, block_table: Optional[torch.Tensor], P_max: int,
                  scale: float = 0.0, kv_split: int = 0, flags: int = 0) -> AttnDesc:
-    """The descriptor of a tree_verify_attention_q4 call, which a decoding loop can keep; the shapes are checked here."""
-    if q.dim() != 4 or kt.dim() != 4 or kt.shape[:2] != q.shape[:2] or kt.shape[3] != q.shape[3] or kt.dtype != q.dtype:
-        raise ValueError("q is [B, T, Hq, d] and kt [B, T, Hkv, d], of one type")
-    B, T, Hq, d = q.shape
-    _q4_shapes(cache, 0, d, block_table, B)
-    blocks, Hkv, size, _ = cache.k_codes.shape
-    if Hkv != kt.shape[2]:
-        raise ValueError("the cache has other heads than kt")
-    paged = block_table is not None
-    if paged:
-        _int32((B, block_table.shape[1]), block_table=block_table)
-    return AttnDesc(B, T, Hq, Hkv, d, _dtype_code(q), size if paged else 0, block_table.shape[1] if paged else 0, blocks if paged else 0,
-                    0 if paged else size, int(P_max), float(scale), int(kv_split), int(flags))
+    """The descriptor of a tree_verify_attention_q4 call, which a decoding loop can keep."""
+    if q.dim() != 4 or kt.dim() != 4 or cache.k_codes.dim() != 4:
+        raise ValueError("q is [B, T, Hq, d], kt [B, T, Hkv, d], and the codes are one layer's: [blocks, Hkv, block_size, d/2]")
+    (B, T, Hq, d), (blocks, _, size, _), paged = q.shape, cache.k_codes.shape, block_table is not None
+    return AttnDesc(B, T, Hq, kt.shape[2], d, _dtype_code(q), size if paged else 0, block_table.shape[-1] if paged else 0,
+                    blocks if paged else 0, 0 if paged else size, int(P_max), float(scale), int(kv_split), int(flags))
 
 
 def tree_verify_attention_q4_workspace_bytes(dsc: AttnDesc) -> int:
@@ -677,25 +633,18 @@ def tree_verify_attention_q4(q, cache: KVCacheQ4, prefix_len, kt, vt, bitmask, n
                              workspace=None, desc: Optional[AttnDesc] = None):
     """tree_verify_attention against one layer of a 4-bit cache: q [B,T,Hq,d]; kt/vt [B,T,Hkv,d] (never quantised); cache
     codes [blocks,Hkv,block_size,d/2].  Returns (out [B,T,Hq,d] in q's dtype, lse float32 [B,Hq,T] or None).  A `desc` of
-    attn_q4_desc stands for shapes that were checked before."""
+    attn_q4_desc goes before P_max, scale, kv_split and flags."""
     dsc = _attn_desc_only(desc) if desc is not None else attn_q4_desc(q, cache, kt, block_table, P_max, scale, kv_split, flags)
-    B, T, Hq, d = q.shape
-    if desc is not None and (dsc.B, dsc.T_max, dsc.Hq, dsc.d) != (B, T, Hq, d):
-        raise ValueError("the descriptor is of other shapes")
-    if vt.shape != kt.shape or vt.dtype != kt.dtype:
-        raise ValueError("vt is like kt")
+    native = _native()
     if out is None:
         out = torch.empty_like(q)
     if lse is None and want_lse:
+        B, T, Hq, _ = q.shape
         lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+    native.q4_attn_check(dsc, q, *cache, block_table, kt, vt, prefix_len, n_nodes, bitmask, out, lse)
     if workspace is None:
         workspace = torch.empty((max(256, tree_verify_attention_q4_workspace_bytes(dsc)),), dtype=torch.uint8, device=q.device)
-    _int32((B,), prefix_len=prefix_len, n_nodes=n_nodes)
-    if bitmask.dtype != torch.int64 or tuple(bitmask.shape) != (B, T, (T + 63) // 64):
-        raise ValueError("bitmask is int64 [B, T, ceil(T / 64)]")
-    if out.shape != q.shape or out.dtype != q.dtype or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, T))):
-        raise ValueError("out is like q, lse float32 [B, Hq, T]")
-    rc = _native().tree_verify_attention_q4(dsc, q, *cache, block_table, prefix_len, kt, vt, bitmask, n_nodes, out, lse,
-                                            workspace, workspace.numel())
+    rc = native.tree_verify_attention_q4(dsc, q, *cache, block_table, prefix_len, kt, vt, bitmask, n_nodes, out, lse,
+                                         workspace, workspace.numel())
     _check("etv_tree_verify_attention_q4", rc)
     return out, lse

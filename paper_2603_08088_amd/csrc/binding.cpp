@@ -141,6 +141,130 @@ PyObject *commit_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// What the C side takes on trust in a call on a 4-bit cache.  A refusal names what was expected.
+struct Q4Shapes {
+    int64_t layers = 0, blocks = 0, heads = 0, size = 0, d = 0;
+};
+const at::Tensor &tensor_of(PyObject *o, const char *name) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: tensor expected instead of %s", name, Py_TYPE(o)->tp_name);
+        throw Refused{};
+    }
+    return THPVariable_Unpack(o);
+}
+void need(bool ok, const char *what) {
+    if (ok) return;
+    PyErr_SetString(PyExc_ValueError, what);
+    throw Refused{};
+}
+bool is_i32(const at::Tensor &t, int64_t a, int64_t b = -1) {
+    return t.scalar_type() == at::kInt && (b < 0 ? t.dim() == 1 && t.size(0) == a : t.dim() == 2 && t.size(0) == a && t.size(1) == b);
+}
+// codes and scales of K and V at args[0..3], with `lead` leading dimensions (the layers, or none), for channels d
+Q4Shapes q4_shapes(PyObject *const *args, int lead, int64_t d) {
+    const at::Tensor &k = tensor_of(args[0], "k_codes"), &ks = tensor_of(args[1], "k_scales"), &v = tensor_of(args[2], "v_codes"),
+                     &vs = tensor_of(args[3], "v_scales");
+    need(k.dim() == lead + 4, lead ? "codes and scales are uint8 [n_layers, blocks, Hkv, block_size, d/2 or d/32]"
+                                   : "codes and scales are uint8 [blocks, Hkv, block_size, d/2 or d/32]");
+    need(k.scalar_type() == at::kByte && ks.scalar_type() == at::kByte && v.scalar_type() == at::kByte && vs.scalar_type() == at::kByte,
+         "codes and scales are uint8");
+    bool same = v.sizes() == k.sizes() && ks.dim() == k.dim() && vs.sizes() == ks.sizes() && k.size(lead + 3) == d / 2 && ks.size(lead + 3) == d / 32;
+    for (int i = 0; same && i < lead + 3; i++) same = ks.size(i) == k.size(i);
+    need(same, "the codes and scales of a cache have the same rows, of d/2 and d/32 bytes");
+    return {lead ? k.size(0) : 1, k.size(lead), k.size(lead + 1), k.size(lead + 2), d};
+}
+int64_t q4_table(PyObject *o, int64_t B, const Q4Shapes &c) {  // row length of the block table, 0: contiguous
+    if (o == Py_None) {
+        need(c.blocks == B, "a contiguous cache has one block per sequence");
+        return 0;
+    }
+    const at::Tensor &t = tensor_of(o, "block_table");
+    need(t.dim() == 2 && is_i32(t, B, t.size(1)), "block_table is int32 [B, max_blocks]");
+    return t.size(1);
+}
+int32_t type_code(const at::Tensor &t) { return t.scalar_type() == at::kFloat ? ETV_F32 : t.scalar_type() == at::kBFloat16 ? ETV_BF16 : -1; }
+
+// q4_desc(k, v, k_codes, k_scales, v_codes, v_scales, block_table or None, acc_nodes or None, slot_map or None, int32 [B]...): the
+// descriptor's bytes; None where the type is neither fp32 nor bf16
+PyObject *q4_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n < 9) return PyErr_Format(PyExc_TypeError, "at least 9 arguments expected, got %zd", n);
+    try {
+        const at::Tensor &k = tensor_of(args[0], "k"), &v = tensor_of(args[1], "v");
+        need(k.dim() == 5 && v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type(), "k and v are [n_layers, B, rows, Hkv, d], of one type");
+        const Q4Shapes c = q4_shapes(args + 2, 1, k.size(4));
+        need(c.layers == k.size(0) && c.heads == k.size(3), "the cache has other layers or heads than k and v");
+        const int64_t B = k.size(1), width = q4_table(args[6], B, c);
+        int64_t W = 0;
+        if (args[7] != Py_None) {
+            const at::Tensor &acc = tensor_of(args[7], "acc_nodes");
+            need(acc.dim() == 2 && is_i32(acc, B, acc.size(1)), "acc_nodes is int32 [B, W]");
+            W = acc.size(1);
+            need(is_i32(tensor_of(args[8], "slot_map"), B, W), "slot_map is int32 [B, W]");
+        }
+        for (Py_ssize_t i = 9; i < n; i++) need(is_i32(tensor_of(args[i], "lengths"), B), "lengths, counts and status are int32 [B]");
+        etv_q4_desc d{};
+        const auto i32 = [](int64_t x) {
+            need(x >= 0 && x <= INT32_MAX, "a size does not fit 32 bits");
+            return static_cast<int32_t>(x);
+        };
+        d.B = i32(B);
+        d.rows = i32(k.size(2));
+        d.Hkv = i32(c.heads);
+        d.d = i32(c.d);
+        d.dtype = type_code(k);
+        if (d.dtype < 0) Py_RETURN_NONE;
+        d.n_layers = i32(c.layers);
+        d.W = i32(W);
+        if (width > 0 || args[6] != Py_None) {
+            d.block_size = i32(c.size);
+            d.max_blocks = i32(width);
+            d.num_blocks = i32(c.blocks);
+        } else {
+            d.P_cap = i32(c.size);
+        }
+        d.layer_rows = c.blocks * c.heads * c.size;
+        return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&d), sizeof d);
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// q4_attn_check(etv_attn_desc, q, k_codes, k_scales, v_codes, v_scales, block_table, kt, vt, prefix_len, n_nodes, bitmask, out, lse):
+// are these the tensors the descriptor speaks of?
+PyObject *q4_attn_check(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 14) return PyErr_Format(PyExc_TypeError, "14 arguments expected, got %zd", n);
+    try {
+        const etv_attn_desc &d = *arg<const etv_attn_desc *, false>(args[0]);
+        const at::Tensor &q = tensor_of(args[1], "q"), &kt = tensor_of(args[7], "kt"), &vt = tensor_of(args[8], "vt");
+        need(q.dim() == 4 && kt.dim() == 4 && vt.sizes() == kt.sizes(), "q is [B, T, Hq, d], kt and vt [B, T, Hkv, d]");
+        need(kt.scalar_type() == q.scalar_type() && vt.scalar_type() == q.scalar_type(), "q, kt and vt are of one type");
+        const Q4Shapes c = q4_shapes(args + 2, 0, q.size(3));
+        const int64_t B = q.size(0), T = q.size(1), width = q4_table(args[6], B, c);
+        need(kt.size(0) == B && kt.size(1) == T && kt.size(2) == c.heads && kt.size(3) == q.size(3), "kt and vt are [B, T, Hkv, d] with the cache's heads");
+        const bool paged = args[6] != Py_None;
+        need(d.B == B && d.T_max == T && d.Hq == q.size(2) && d.Hkv == c.heads && d.d == q.size(3) && d.dtype == type_code(q) &&
+                 d.block_size == (paged ? c.size : 0) && d.max_blocks == width && (paged ? d.num_blocks == c.blocks : d.P_cap == c.size),
+             "the descriptor is of other shapes");
+        need(is_i32(tensor_of(args[9], "prefix_len"), B) && is_i32(tensor_of(args[10], "n_nodes"), B), "prefix_len and n_nodes are int32 [B]");
+        const at::Tensor &mask = tensor_of(args[11], "bitmask"), &out = tensor_of(args[12], "out");
+        need(mask.scalar_type() == at::kLong && mask.dim() == 3 && mask.size(0) == B && mask.size(1) == T && mask.size(2) == (T + 63) / 64,
+             "bitmask is int64 [B, T, ceil(T / 64)]");
+        need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out is like q");
+        if (args[13] != Py_None) {
+            const at::Tensor &lse = tensor_of(args[13], "lse");
+            need(lse.scalar_type() == at::kFloat && lse.dim() == 3 && lse.size(0) == B && lse.size(1) == q.size(2) && lse.size(2) == T,
+                 "lse is float32 [B, Hq, T]");
+        }
+        Py_RETURN_NONE;
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
 #define ETV_METHOD(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name>, METH_FASTCALL, nullptr}
 #define ETV_METHOD_HERE(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name, true>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree), ETV_METHOD(tree_verify_attention),
@@ -150,6 +274,8 @@ PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree)
                          ETV_METHOD_HERE(quantize_kv_q4), ETV_METHOD_HERE(commit_accepted_kv_q4), ETV_METHOD_HERE(dequantize_kv_q4),
                          ETV_METHOD_HERE(tree_verify_attention_q4),
                          {"commit_desc", (PyCFunction)(void (*)(void))commit_desc, METH_FASTCALL, nullptr},
+                         {"q4_desc", (PyCFunction)(void (*)(void))q4_desc, METH_FASTCALL, nullptr},
+                         {"q4_attn_check", (PyCFunction)(void (*)(void))q4_attn_check, METH_FASTCALL, nullptr},
                          {"empty_i32", (PyCFunction)(void (*)(void))empty_i32, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
