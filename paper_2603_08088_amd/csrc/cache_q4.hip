@@ -177,34 +177,49 @@ __global__ void __launch_bounds__(256) write_rows_kernel(etv_q4_desc dsc, Q4Cach
     quantise_group(v, cache.codes[1] + row * (NG * 16) + g * 16, cache.scales[1] + row * NG + g);
 }
 
-// eight channels of a row from four bytes of codes
-__device__ __forceinline__ void put_eight(uint16_t *out, uint32_t codes, float scale) {
-    uint4 r;
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-    *reinterpret_cast<uint4 *>(out) = r;
-}
-__device__ __forceinline__ void put_eight(float *out, uint32_t codes, float scale) {
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
-    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
-    reinterpret_cast<float4 *>(out)[0] = float4{a[0], a[1], b[0], b[1]};
-    reinterpret_cast<float4 *>(out)[1] = float4{c[0], c[1], d[0], d[1]};
-}
+// Streams that this launch touches once pass the caches by.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void stream_out(void *p, u32x4 v) { __builtin_nontemporal_store(v, static_cast<u32x4 *>(p)); }
+
+// 16 bytes of a row: eight bf16 channels from four bytes of codes, or four fp32 channels from two
+template <typename T>
+struct Piece;
+template <>
+struct Piece<uint16_t> {
+    typedef uint32_t Codes;
+    static __device__ __forceinline__ void put(uint16_t *out, uint32_t codes, float scale) {
+        u32x4 r;
+        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+        stream_out(out, r);
+    }
+};
+template <>
+struct Piece<float> {
+    typedef uint16_t Codes;
+    static __device__ __forceinline__ void put(float *out, uint32_t codes, float scale) {
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+        const float4 r = {a[0], a[1], b[0], b[1]};
+        stream_out(out, __builtin_bit_cast(u32x4, r));
+    }
+};
 
 // The scale of a byte; the conversions pass a NaN on.
 __device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
 
-// grid (ceil(Hkv * rows * d/8 / (256 * U)), B, n_layers).  A thread has eight channels of K and of V of U items: its 16-byte
-// stores and its lane neighbours' are consecutive, which the wider of the two sides needs.
+// grid (ceil(Hkv * rows * pieces / (256 * U)), B, n_layers).  A thread has 16 bytes of K and of V of U items: its stores and its
+// lane neighbours' are consecutive, which the wider of the two sides needs.  The rows written are not read here: past the caches
+// they take 91 us where 138 were needed (8 x 4096 rows of 4 layers, bf16).
 constexpr int kReadItems = 4;
 template <typename T, int NG>
 __global__ void __launch_bounds__(256) read_rows_kernel(etv_q4_desc dsc, Q4Cache cache, const int32_t *__restrict__ block_table,
                                                         const int32_t *__restrict__ first, const int32_t *__restrict__ n_rows, T *__restrict__ k,
                                                         T *__restrict__ v, int32_t *__restrict__ status, uint32_t inv_bs, uint32_t inv_rows) {
     __shared__ int32_t s_status;
-    constexpr int U = kReadItems, CH = 4 * NG;  // pieces of eight channels a row
+    using P16 = Piece<T>;
+    constexpr int U = kReadItems, PER = 16 / (int)sizeof(T), CH = NG * 32 / PER;  // channels of a piece, pieces of a row
     const int b = blockIdx.y, l = blockIdx.z;
     const int32_t *const table_row = block_table + (size_t)b * dsc.max_blocks;
     const int P = first[b], n = n_rows[b];
@@ -220,22 +235,22 @@ __global__ void __launch_bounds__(256) read_rows_kernel(etv_q4_desc dsc, Q4Cache
         uint32_t i;
         const uint32_t h = fast_div(item / CH, (uint32_t)dsc.rows, inv_rows, i);
         mine[u] = h < (uint32_t)dsc.Hkv;
-        at[u] = ((((size_t)l * dsc.B + b) * dsc.rows + i) * dsc.Hkv + h) * (NG * 32) + c * 8;
+        at[u] = ((((size_t)l * dsc.B + b) * dsc.rows + i) * dsc.Hkv + h) * (NG * 32) + c * PER;
         codes[0][u] = codes[1][u] = scale[0][u] = scale[1][u] = 0;
         if (mine[u] && !st && (int)i < n) {
             const uint64_t row = (uint64_t)l * dsc.layer_rows + q4_row(dsc, table_row, inv_bs, b, (int)h, P + (int)i);
 #pragma unroll
             for (int x = 0; x < 2; x++) {
-                codes[x][u] = *reinterpret_cast<const uint32_t *>(cache.codes[x] + row * (NG * 16) + c * 4);
-                scale[x][u] = cache.scales[x][row * NG + c / 4];
+                codes[x][u] = *reinterpret_cast<const typename P16::Codes *>(cache.codes[x] + row * (NG * 16) + c * (PER / 2));
+                scale[x][u] = cache.scales[x][row * NG + c * PER / 32];
             }
         }
     }
 #pragma unroll
     for (int u = 0; u < U; u++)
         if (mine[u]) {
-            put_eight(k + at[u], codes[0][u], scale_of(scale[0][u]));
-            put_eight(v + at[u], codes[1][u], scale_of(scale[1][u]));
+            P16::put(k + at[u], codes[0][u], scale_of(scale[0][u]));
+            P16::put(v + at[u], codes[1][u], scale_of(scale[1][u]));
         }
 }
 
@@ -252,7 +267,7 @@ static int32_t check_q4(const etv_q4_desc *h, const void *k, const void *v, cons
     if (((uintptr_t)c.scales[0] | (uintptr_t)c.scales[1]) & 3) return ETV_ERR_INVALID_ARG;
     // positions and items of a sequence are counted in 31 bits
     if (h->block_size > 0 && (int64_t)h->max_blocks * h->block_size > INT32_MAX) return ETV_ERR_UNSUPPORTED;
-    if ((int64_t)h->Hkv * (commit ? h->W : h->rows) * (h->d / 8) > INT32_MAX - 1024) return ETV_ERR_UNSUPPORTED;
+    if ((int64_t)h->Hkv * (commit ? h->W : h->rows) * (h->d / 4) > INT32_MAX - 1024) return ETV_ERR_UNSUPPORTED;
     if (h->B > 65535 || h->n_layers > 65535) return ETV_ERR_UNSUPPORTED;
     return ETV_OK;
 }
@@ -314,7 +329,7 @@ extern "C" int32_t etv_dequantize_kv_q4(const etv_q4_desc *h, const uint8_t *k_c
     if (rc != ETV_OK) return rc;
     if (h->B == 0) return ETV_OK;
     const int per_block = 256 * etv::kReadItems;
-    const dim3 grid((unsigned)(((int64_t)h->Hkv * h->rows * (h->d / 8) + per_block - 1) / per_block), h->B, h->n_layers);
+    const dim3 grid((unsigned)(((int64_t)h->Hkv * h->rows * (h->d * (h->dtype == ETV_BF16 ? 2 : 4) / 16) + per_block - 1) / per_block), h->B, h->n_layers);
     const uint32_t inv_bs = h->block_size ? etv::fast_div_inv(h->block_size) : 0, inv_rows = etv::fast_div_inv(h->rows);
     const auto launch = [&](auto kernel, auto *ko, auto *vo) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, etv::as_stream(stream), *h, cache, block_table, first, n_rows, ko, vo, status, inv_bs,
