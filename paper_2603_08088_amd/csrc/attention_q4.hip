@@ -437,7 +437,7 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
     return r;
 }
 
-template <int D, bool F32, int RW, bool PAGED>
+template <int D, bool F32, int RW, bool PAGED, bool BIG>
 __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
@@ -563,21 +563,30 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             int id[KB][2];
             uint32_t off[KB][2];  // of the first of the 16 positions within its block, plus the head's rows
         } ids;
-        const auto fetch_ids = [&](int base) {  // positions are held within the split
-            if constexpr (PAGED)
+        // The walk through the table: block and offset of the next 16 positions, in scalar registers.  Behind the split it stays in the
+        // last block, whose rows exist.
+        const int span = KEYS * KW, mine = k0 + KEYS * w.kg;
+        uint32_t walk = 0, walk_off = 0, jump = 0, jump_off = 0, last_block = 0;
+        if constexpr (PAGED) {
+            walk = fast_div((uint32_t)mine, (uint32_t)p.block_size, p.inv_bs, walk_off);
+            if constexpr (KW > 1) jump = fast_div((uint32_t)(span - KEYS), (uint32_t)p.block_size, p.inv_bs, jump_off);
+            last_block = fast_div((uint32_t)(k1 - 1), (uint32_t)p.block_size, p.inv_bs, rem);
+        }
+        const auto advance = [&](uint32_t blocks, uint32_t positions) {
+            walk += blocks;
+            walk_off += positions;
+            if (walk_off >= (uint32_t)p.block_size) walk_off -= (uint32_t)p.block_size, walk++;
+        };
+        const auto fetch_ids = [&] {
+            if constexpr (PAGED) {
 #pragma unroll
-                for (int kb = 0; kb < KB; kb++)
-#pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        const int pos = min(base + 32 * kb + 16 * x, (k1 - 1) & ~15);
-                        // fast_div without conditions, which would leave the scalar unit
-                        int q = (int)__umulhi((uint32_t)pos, p.inv_bs), off = pos - q * p.block_size;
-                        const int over = (p.block_size - 1 - off) >> 31;
-                        q -= over;
-                        off -= p.block_size & over;
-                        ids.id[kb][x] = table[q];
-                        ids.off[kb][x] = (uint32_t)off + kvh * (uint32_t)p.block_size;
-                    }
+                for (int x = 0; x < 2 * KB; x++) {
+                    ids.id[x / 2][x & 1] = table[min(walk, last_block)];
+                    ids.off[x / 2][x & 1] = walk_off + kvh * (uint32_t)p.block_size;
+                    advance(0, 16);
+                }
+                if constexpr (KW > 1) advance(jump, jump_off);
+            }
         };
         // A lane's rows (of a layer, fewer than 2^32) in the cache.
         const auto place = [&](Codes &to, int base) {
@@ -599,26 +608,28 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
                 }
             }
         };
+        // Byte offsets of at most 32 bits are one register beside a scalar base (BIG: a cache of 4 GiB of codes and more).
+        using Offset = std::conditional_t<BIG, uint64_t, uint32_t>;
         const auto load_k = [&](Codes &to, int kb) {
-            const uint8_t *const codes = p.codes[0] + 16 * hh + (uint64_t)to.row[kb] * (D / 2);
+            const uint8_t *const codes = p.codes[0] + ((Offset)to.row[kb] * (D / 2) + 16 * hh);
 #pragma unroll
             for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(codes + 32 * i);
             if constexpr (D == 128) {
-                to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + (uint64_t)to.row[kb] * 4);
-                to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + (uint64_t)to.row[kb] * 4);
+                to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + (Offset)to.row[kb] * 4);
+                to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + (Offset)to.row[kb] * 4);
             } else {
-                to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + (uint64_t)to.row[kb] * 2);
-                to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + (uint64_t)to.row[kb] * 2);
+                to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + (Offset)to.row[kb] * 2);
+                to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + (Offset)to.row[kb] * 2);
             }
         };
         const auto load_v = [&](Codes &to, int j) {
             const int c = piece_of(j), kb = c / KM, i = c % KM;
-            const uint8_t *const at = p.codes[1] + 16 * hh + (uint64_t)(kb ? to.row[KB - 1] : to.row[0]) * (D / 2) + 32 * i;
+            const uint8_t *const at = p.codes[1] + ((Offset)(kb ? to.row[KB - 1] : to.row[0]) * (D / 2) + 16 * hh + 32 * i + (VW == 4 ? 0 : 8 * half));
             if constexpr (VW == 4) {
                 const uint4 v = *reinterpret_cast<const uint4 *>(at);
                 to.vc[j][0] = v.x; to.vc[j][1] = v.y; to.vc[j][VW - 2] = v.z; to.vc[j][VW - 1] = v.w;
             } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(at + 8 * half);
+                const uint2 v = *reinterpret_cast<const uint2 *>(at);
                 to.vc[j][0] = v.x; to.vc[j][1] = v.y;
             }
         };
@@ -650,27 +661,27 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             constexpr int X = decltype(x)::value, kb = X % KB, i = X / KB % KM, y = X / (KB * KM);
             s[kb] = q4_scores<2 * i, y & 3>(from.kc[kb][i], qp[y][i], X < KB ? w.off : s[kb], ks[kb], qs[y >> 2][i]);
         };
-        // a lane's groups in bytes 0 and 2 of the scales; V's keys that weigh nothing have to be numbers
+        // A lane's groups in bytes 0 and 2 of the scales.  V of keys that weigh nothing has to be numbers; a block outside the pool shows
+        // in its scores.
         const auto ready = [&](const Codes &from, int base, uint32_t (&ks)[KB], uint32_t (&vs)[KB]) {
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
-                ks[kb] = from.ks[kb] >> (8 * hh) | from.bad[kb];
-                const uint32_t none = from.bad[kb] | (uint32_t)((k1 - 1 - (base + 32 * kb + r)) >> 31);
-                vs[kb] = (from.vs[kb] >> (8 * hh) & ~none) | (0x7f7f7f7fu & none);
+                ks[kb] = from.ks[kb] >> (8 * hh) | (PAGED ? from.bad[kb] : 0u);
+                vs[kb] = r < k1 - base - 32 * kb ? from.vs[kb] >> (8 * hh) : 0x7f7f7f7fu;
             }
         };
 
         // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials, and
         // stores the next tile's V (into the other buffer) between its value products: the matrix and the vector unit are both busy
         // within one wavefront.  Codes of the tiles behind are on their way; beyond the split they are a held row's, unused.
-        const int span = KEYS * KW, mine = k0 + KEYS * w.kg, rounds = (k1 - k0 + span - 1) / span;
+        const int rounds = (k1 - k0 + span - 1) / span;
         Codes start, ahead[AHEAD];
         q4_f32x16 sa[KB], sb[KB];
-        fetch_ids(mine);
+        fetch_ids();
         load_tile(start, mine);
 #pragma unroll
         for (int x = 0; x < AHEAD; x++) {
-            fetch_ids(mine + (x + 1) * span);
+            fetch_ids();
             load_tile(ahead[x], mine + (x + 1) * span);
         }
         uint32_t ks[KB], vs[KB], pk[NP][KB][8];
@@ -694,7 +705,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             uint8_t *const tile = w.buffer(decltype(buffer)::value), *const tile_next = w.buffer(1 - decltype(buffer)::value);
             constexpr int FLY = 3;  // fragments of V on their way from LDS
             q4_bf16x8 v[FLY + 1];
-            fetch_ids(base + (AHEAD + 1) * span);
+            fetch_ids();
             ready(next, base + span, ks, vs);
             q4_for<QK>([&](auto x) {
                 constexpr int X = decltype(x)::value;
@@ -1041,22 +1052,25 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     return pl;
 }
 
-template <int D, bool F32, int RW, bool PAGED>
+template <int D, bool F32, int RW, bool PAGED, bool BIG>
 static int32_t launch_q4(const Q4Attn &p, unsigned grid, hipStream_t st) {
     constexpr int lds = Q4Geo<D, F32, RW>::LDS;
     static_assert(lds <= (Q4Geo<D, F32, RW>::NW == 8 ? 144 : 78) * 1024, "eight wavefronts a compute unit, and static LDS beside it");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED, BIG>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) {
         g_last_hip_error = (int32_t)e;
         return ETV_ERR_HIP;
     }
-    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED>), dim3(grid), dim3(Q4Geo<D, F32, RW>::NW * 64), lds, st, p);
+    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED, BIG>), dim3(grid), dim3(Q4Geo<D, F32, RW>::NW * 64), lds, st, p);
     return check_launch();
 }
 
 template <int D, bool F32, int RW>
 static int32_t launch_q4_form(const Q4Attn &p, unsigned grid, hipStream_t st) {
-    return p.block_size ? launch_q4<D, F32, RW, true>(p, grid, st) : launch_q4<D, F32, RW, false>(p, grid, st);
+    const bool paged = p.block_size != 0;
+    const uint64_t rows = paged ? (uint64_t)p.num_blocks * p.Hkv * p.block_size : (uint64_t)p.B * p.Hkv * p.P_cap;
+    if (rows * (D / 2) > UINT32_MAX) return paged ? launch_q4<D, F32, RW, true, true>(p, grid, st) : launch_q4<D, F32, RW, false, true>(p, grid, st);
+    return paged ? launch_q4<D, F32, RW, true, false>(p, grid, st) : launch_q4<D, F32, RW, false, false>(p, grid, st);
 }
 
 template <int D, bool F32>
