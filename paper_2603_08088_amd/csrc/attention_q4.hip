@@ -165,17 +165,18 @@ typedef __attribute__((address_space(3))) q4_s16x4 q4_lds_s16x4;
 typedef __attribute__((address_space(4))) const int32_t *const_ids;
 constexpr float kQ4Lazy = 1024.f;  // the largest sum of a lane's weights in a tile without a new reference
 
-// Dynamic LDS: V tiles [key groups][2][keys][D] bf16, afterwards 64 channels at a time of the
-// outputs [wavefronts][32][64 + 4] fp32.
+// Dynamic LDS, by key group: V tiles [2][keys][D] bf16, K tiles [1 or 2][keys][D/2] and their scales [keys][4]; afterwards 64
+// channels at a time of the outputs [wavefronts][32][64 + 4] fp32.
 constexpr int q4_wavefronts(bool f32, int rw) { return rw == 4 || f32 ? 4 : 8; }  // of a workgroup
 template <int D, bool F32, int RW>
 struct Q4Geo {
     static constexpr int NW = q4_wavefronts(F32, RW);
     static constexpr int KB = RW == 4 ? 2 : 1, KEYS = 32 * KB;  // key blocks and keys of a tile
-    static constexpr int AHEAD = RW == 4 ? 1 : 2;                // tiles whose codes are on their way besides the next one's
+    static constexpr int AHEAD = RW == 4 ? 1 : 2;                // tiles on their way besides those in LDS
     static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = NW / RW, BUFS = 2;
-    static constexpr int OUT_ROW = 64 + 4;  // floats; four on from a multiple of the banks
-    static constexpr int TILES = KW * BUFS * TILE, OUT = NW * 32 * (OUT_ROW * 4 + 8);
+    static constexpr int K_BUFS = RW > 1 ? 2 : 1, K_TILE = KEYS * D / 2, K_SCALES = KEYS * 4;
+    static constexpr int K_AT = KW * BUFS * TILE, K_SCALES_AT = K_AT + KW * K_BUFS * K_TILE, TILES = K_SCALES_AT + KW * K_BUFS * K_SCALES;
+    static constexpr int OUT_ROW = 64 + 4, OUT = NW * 32 * (OUT_ROW * 4 + 8);  // floats; four on from a multiple of the banks
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
 };
 
@@ -437,7 +438,7 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
     return r;
 }
 
-template <int D, bool F32, int RW, bool PAGED, bool BIG>
+template <int D, bool F32, int RW, bool PAGED>
 __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ? 1 : 2) attn_q4_kernel(Q4Attn p) {
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
@@ -544,32 +545,27 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             }
         }
 
-        // What a lane reads of a tile: of key row r of each key block the groups 2i + hh (K: all; V: pieces shared out over RW).
-        constexpr int NC = KB * KM, VC = NC < RW ? 1 : NC / RW, VW = NC < RW ? 2 : 4;  // pieces (key block, i); a wavefront's of V, their words
+        // A wavefront's pieces of a tile are 16 whole rows each, a lane having a quarter of a row of K and of V: loads of consecutive
+        // memory beside a scalar base.  (Each lane with the rows and groups that its products want costs the address unit four
+        // times as long a load, and every wavefront K's: 267 us where 16 x 8 heads of 4096 keys and 128 nodes take DUMMY now.)
+        constexpr int PC = KEYS / 16 / RW, VW = D / 32;  // pieces of a wavefront, words of a lane
         struct Codes {
-            uint4 kc[KB][KM];
-            uint32_t vc[VC][VW];
-            uint32_t ks[KB], vs[KB];  // as they lie in memory: nothing may wait for them where they are asked for
-            uint32_t bad[KB];         // all ones: a block outside the pool
-            uint32_t row[KB];
+            uint32_t k[PC][VW], v[PC][VW], ks[PC], vs[PC];  // K of a tile, V of the one before it; scales: the quarter's
         };
-        const auto piece_of = [&](int j) { return NC < RW ? w.wr / 2 : j * RW + w.wr; };  // NC < RW: half a piece each
-        const int half = NC < RW ? w.wr & 1 : 0;
-        // Blocks are multiples of 16 positions and tiles begin at multiples of 32: the lanes r < 16 of a key block share a block of the
-        // pool, and so do the others.  Ids come by scalar loads, a tile earlier than the codes.
+        struct Rows {
+            uint32_t row[PC], bad[PC];  // scalar: first row in the layer's cache; all ones: in a block outside the pool
+            int pos[PC];                // position of that row
+        };
+        const int key16 = w.lane >> 2, quarter = w.lane & 3;
+        const int span = KEYS * KW, mine = k0 + KEYS * w.kg, rounds = (k1 - k0 + span - 1) / span;
+        // The walk through the table: block and offset of the wavefront's next 16 positions, in scalar registers (blocks are multiples of
+        // 16 positions, pieces begin at multiples of 16).  Behind the split it stays in the last block, whose rows exist.
         const const_ids table = (const_ids)(uintptr_t)(PAGED ? p.block_table + (size_t)b * p.max_blocks : nullptr);
-        const uint32_t seq_row = PAGED ? 0 : ((uint32_t)b * p.Hkv + kvh) * (uint32_t)p.P_cap, block_rows = PAGED ? (uint32_t)(p.Hkv * p.block_size) : 0;
-        struct Ids {
-            int id[KB][2];
-            uint32_t off[KB][2];  // of the first of the 16 positions within its block, plus the head's rows
-        } ids;
-        // The walk through the table: block and offset of the next 16 positions, in scalar registers.  Behind the split it stays in the
-        // last block, whose rows exist.
-        const int span = KEYS * KW, mine = k0 + KEYS * w.kg;
+        const uint32_t head_rows = kvh * (uint32_t)(PAGED ? p.block_size : p.P_cap), block_rows = (uint32_t)(p.Hkv * p.block_size);
         uint32_t walk = 0, walk_off = 0, jump = 0, jump_off = 0, last_block = 0;
         if constexpr (PAGED) {
-            walk = fast_div((uint32_t)mine, (uint32_t)p.block_size, p.inv_bs, walk_off);
-            if constexpr (KW > 1) jump = fast_div((uint32_t)(span - KEYS), (uint32_t)p.block_size, p.inv_bs, jump_off);
+            walk = fast_div((uint32_t)(mine + 16 * w.wr), (uint32_t)p.block_size, p.inv_bs, walk_off);
+            jump = fast_div((uint32_t)(span - (PC - 1) * 16), (uint32_t)p.block_size, p.inv_bs, jump_off);
             last_block = fast_div((uint32_t)(k1 - 1), (uint32_t)p.block_size, p.inv_bs, rem);
         }
         const auto advance = [&](uint32_t blocks, uint32_t positions) {
@@ -577,120 +573,142 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             walk_off += positions;
             if (walk_off >= (uint32_t)p.block_size) walk_off -= (uint32_t)p.block_size, walk++;
         };
-        const auto fetch_ids = [&] {
-            if constexpr (PAGED) {
+        int ids[PC] = {};
+        uint32_t offs[PC] = {};
+        const auto fetch_ids = [&] {  // of the tile that is placed next
+            if constexpr (PAGED)
 #pragma unroll
-                for (int x = 0; x < 2 * KB; x++) {
-                    ids.id[x / 2][x & 1] = table[min(walk, last_block)];
-                    ids.off[x / 2][x & 1] = walk_off + kvh * (uint32_t)p.block_size;
-                    advance(0, 16);
+                for (int j = 0; j < PC; j++) {
+                    ids[j] = table[min(walk, last_block)];
+                    offs[j] = walk_off;
+                    advance(j + 1 < PC ? 0 : jump, j + 1 < PC ? 16 : jump_off);
                 }
-                if constexpr (KW > 1) advance(jump, jump_off);
+        };
+        const auto place = [&](Rows &to, int base) {
+#pragma unroll
+            for (int j = 0; j < PC; j++) {
+                to.pos[j] = base + 16 * (j * RW + w.wr);
+                if constexpr (PAGED) {
+                    to.bad[j] = (uint32_t)((ids[j] | (p.num_blocks - 1 - ids[j])) >> 31);  // negative or too large
+                    to.row[j] = ((uint32_t)ids[j] & ~to.bad[j]) * block_rows + head_rows + offs[j];
+                } else {
+                    to.bad[j] = 0;
+                    to.pos[j] = min(to.pos[j], (k1 - 1) & ~15);
+                    to.row[j] = (uint32_t)b * p.Hkv * (uint32_t)p.P_cap + head_rows + (uint32_t)to.pos[j];
+                }
             }
         };
-        // A lane's rows (of a layer, fewer than 2^32) in the cache.
-        const auto place = [&](Codes &to, int base) {
+        // Rows 16 on from a piece's first exist where they are a block's; in a contiguous cache they are held within the split.
+        const auto load = [&](const uint8_t *codes, const uint8_t *scales, const Rows &rows, int j, uint32_t (&c)[PC][VW], uint32_t (&sc)[PC]) {
+            const uint32_t key = PAGED ? (uint32_t)key16 : (uint32_t)min(key16, k1 - 1 - rows.pos[j]);
+            const uint8_t *const from = codes + (uint64_t)rows.row[j] * (D / 2) + (key * (D / 2) + quarter * (D / 8));
+            if constexpr (VW == 4) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                c[j][0] = x.x; c[j][1] = x.y; c[j][VW - 2] = x.z; c[j][VW - 1] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(from);
+                c[j][0] = x.x; c[j][1] = x.y;
+            }
+            sc[j] = (scales + (uint64_t)rows.row[j] * (D / 32))[key * (D / 32) + (D == 128 ? quarter : quarter >> 1)];
+        };
+        const auto load_k = [&](Codes &to, const Rows &rows, int j) {
+            load(p.codes[0], p.scales[0], rows, j, to.k, to.ks);
+        };
+        const auto load_v = [&](Codes &to, const Rows &rows, int j) {
+            load(p.codes[1], p.scales[1], rows, j, to.v, to.vs);
+        };
+        uint8_t *const k_tiles = q4_smem + G::K_AT + w.kg * G::K_BUFS * G::K_TILE, *const k_scales = q4_smem + G::K_SCALES_AT + w.kg * G::K_BUFS * G::K_SCALES;
+        // K as it came, its 16-byte pieces of a row (D 128) moved about so that eight rows' reads reach all banks; bad: NaN scales
+        const auto put_k = [&](const Codes &from, uint32_t bad, int buffer, int j) {
+            const int row = 16 * (j * RW + w.wr) + key16, x = G::K_BUFS > 1 ? buffer : 0;
+            uint8_t *const to = k_tiles + x * G::K_TILE + row * (D / 2);
+            if constexpr (VW == 4) *reinterpret_cast<uint4 *>(to + ((quarter ^ (key16 >> 2)) << 4)) = uint4{from.k[j][0], from.k[j][1], from.k[j][VW - 2], from.k[j][VW - 1]};
+            else *reinterpret_cast<uint2 *>(to + 8 * quarter) = uint2{from.k[j][0], from.k[j][1]};
+            (k_scales + x * G::K_SCALES)[row * (D / 32) + (D == 128 ? quarter : quarter >> 1)] = (uint8_t)(from.ks[j] | bad);
+        };
+        // V of a piece as bf16, eight channels of word x; keys behind the split weigh nothing and have to be numbers
+        const auto put_v = [&](const Codes &from, int pos, uint8_t *tile, int u) {
+            const int j = u / VW, x = u % VW, row = 16 * (j * RW + w.wr) + key16;
+            const float f = q4_scale(key16 < k1 - pos - 16 * (j * RW) ? from.vs[j] : 127u);
+            const uint32_t in = from.v[j][x];
+            uint4 v;
+            v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 0));
+            v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 1));
+            v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 2));
+            v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 3));
+            *reinterpret_cast<uint4 *>(tile + row * G::ROW + (((VW * quarter + x) ^ q4_swizzle<D>(row)) << 4)) = v;
+        };
+        // K of a tile as the products want it: of key row r of each key block the groups 2i + hh, the scales' bytes 0 and 2
+        const auto get_k = [&](int buffer, uint4 (&kf)[KB][KM], uint32_t (&ks)[KB]) {
+            const int x = G::K_BUFS > 1 ? buffer : 0;
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
-                if constexpr (PAGED) {
-                    uint32_t first[2], bad[2];
+                const int row = 32 * kb + r;
+                const uint8_t *const from = k_tiles + x * G::K_TILE + row * (D / 2), *const sc = k_scales + x * G::K_SCALES + row * (D / 32);
 #pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        const int id = ids.id[kb][x];
-                        bad[x] = (uint32_t)((id | (p.num_blocks - 1 - id)) >> 31);  // all ones: negative or too large
-                        first[x] = ((uint32_t)id & ~bad[x]) * block_rows + ids.off[kb][x];
-                    }
-                    to.row[kb] = (r < 16 ? first[0] : first[1]) + (uint32_t)(r & 15);  // the 16 positions are the block's throughout
-                    to.bad[kb] = r < 16 ? bad[0] : bad[1];
-                } else {
-                    to.row[kb] = seq_row + (uint32_t)min(base + 32 * kb + r, k1 - 1);
-                    to.bad[kb] = 0;
-                }
-            }
-        };
-        // Byte offsets of at most 32 bits are one register beside a scalar base (BIG: a cache of 4 GiB of codes and more).
-        using Offset = std::conditional_t<BIG, uint64_t, uint32_t>;
-        const auto load_k = [&](Codes &to, int kb) {
-            const uint8_t *const codes = p.codes[0] + ((Offset)to.row[kb] * (D / 2) + 16 * hh);
-#pragma unroll
-            for (int i = 0; i < KM; i++) to.kc[kb][i] = *reinterpret_cast<const uint4 *>(codes + 32 * i);
-            if constexpr (D == 128) {
-                to.ks[kb] = *reinterpret_cast<const uint32_t *>(p.scales[0] + (Offset)to.row[kb] * 4);
-                to.vs[kb] = *reinterpret_cast<const uint32_t *>(p.scales[1] + (Offset)to.row[kb] * 4);
-            } else {
-                to.ks[kb] = *reinterpret_cast<const uint16_t *>(p.scales[0] + (Offset)to.row[kb] * 2);
-                to.vs[kb] = *reinterpret_cast<const uint16_t *>(p.scales[1] + (Offset)to.row[kb] * 2);
-            }
-        };
-        const auto load_v = [&](Codes &to, int j) {
-            const int c = piece_of(j), kb = c / KM, i = c % KM;
-            const uint8_t *const at = p.codes[1] + ((Offset)(kb ? to.row[KB - 1] : to.row[0]) * (D / 2) + 16 * hh + 32 * i + (VW == 4 ? 0 : 8 * half));
-            if constexpr (VW == 4) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(at);
-                to.vc[j][0] = v.x; to.vc[j][1] = v.y; to.vc[j][VW - 2] = v.z; to.vc[j][VW - 1] = v.w;
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(at);
-                to.vc[j][0] = v.x; to.vc[j][1] = v.y;
-            }
-        };
-        const auto load_tile = [&](Codes &to, int base) {
-            place(to, base);
-#pragma unroll
-            for (int kb = 0; kb < KB; kb++) load_k(to, kb);
-#pragma unroll
-            for (int j = 0; j < VC; j++) load_v(to, j);
-        };
-        // V of a tile as bf16 into LDS, eight channels of unit u.
-        const auto put_v = [&](const Codes &from, const uint32_t (&vsc)[KB], uint8_t *tile, int u) {
-            {
-                const int j = u / VW, x = u % VW, c = piece_of(j), kb = c / KM, i = c % KM;
-                const uint32_t vs = kb ? vsc[KB - 1] : vsc[0];
-                const float f = q4_scale(vs >> (16 * i) & 255u);
-                const uint32_t in = from.vc[j][x];
-                uint4 v;
-                v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 0));
-                v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 1));
-                v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 2));
-                v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(in, f, 3));
-                *reinterpret_cast<uint4 *>(tile + (32 * kb + r) * G::ROW + (((4 * (2 * i + hh) + 2 * half + x) ^ q4_swizzle<D>(r)) << 4)) = v;
+                for (int i = 0; i < KM; i++) kf[kb][i] = *reinterpret_cast<const uint4 *>(from + (D == 128 ? ((2 * i + hh) ^ (r >> 2 & 3)) << 4 : 16 * hh));
+                ks[kb] = (D == 128 ? *reinterpret_cast<const uint32_t *>(sc) : (uint32_t) * reinterpret_cast<const uint16_t *>(sc)) >> (8 * hh);
             }
         };
         // Scores: product X of a tile's QK, y the part of q.
-        constexpr int QK = NQ * KM * KB, PV = 2 * KB * DB, UNITS = VC * VW;
-        const auto score = [&](auto x, const Codes &from, const uint32_t (&ks)[KB], q4_f32x16 (&s)[KB]) {
+        constexpr int QK = NQ * KM * KB, PV = 2 * KB * DB, UNITS = PC * VW;
+        const auto score = [&](auto x, const uint4 (&kf)[KB][KM], const uint32_t (&ks)[KB], q4_f32x16 (&s)[KB]) {
             constexpr int X = decltype(x)::value, kb = X % KB, i = X / KB % KM, y = X / (KB * KM);
-            s[kb] = q4_scores<2 * i, y & 3>(from.kc[kb][i], qp[y][i], X < KB ? w.off : s[kb], ks[kb], qs[y >> 2][i]);
-        };
-        // A lane's groups in bytes 0 and 2 of the scales.  V of keys that weigh nothing has to be numbers; a block outside the pool shows
-        // in its scores.
-        const auto ready = [&](const Codes &from, int base, uint32_t (&ks)[KB], uint32_t (&vs)[KB]) {
-#pragma unroll
-            for (int kb = 0; kb < KB; kb++) {
-                ks[kb] = from.ks[kb] >> (8 * hh) | (PAGED ? from.bad[kb] : 0u);
-                vs[kb] = r < k1 - base - 32 * kb ? from.vs[kb] >> (8 * hh) : 0x7f7f7f7fu;
-            }
+            s[kb] = q4_scores<2 * i, y & 3>(kf[kb][i], qp[y][i], X < KB ? w.off : s[kb], ks[kb], qs[y >> 2][i]);
         };
 
-        // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials, and
-        // stores the next tile's V (into the other buffer) between its value products: the matrix and the vector unit are both busy
-        // within one wavefront.  Codes of the tiles behind are on their way; beyond the split they are a held row's, unused.
-        const int rounds = (k1 - k0 + span - 1) / span;
-        Codes start, ahead[AHEAD];
+        // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials; between its
+        // value products it stores the next tile's V and the K of the one after into LDS: the matrix and the vector unit are both busy
+        // within one wavefront.  What is stored was asked for a step (AHEAD: two) before.
+        Codes start, second, ahead[AHEAD];
+        Rows rows, newer;  // of the tile whose K was asked for last, and of the next one
+        uint32_t bad[AHEAD][PC];
         q4_f32x16 sa[KB], sb[KB];
         fetch_ids();
-        load_tile(start, mine);
+        place(rows, mine);
+#pragma unroll
+        for (int j = 0; j < PC; j++) {
+            load_k(start, rows, j);
+            load_v(start, rows, j);
+        }
+        fetch_ids();
+        place(newer, mine + span);
+#pragma unroll
+        for (int j = 0; j < PC; j++) load_k(second, newer, j);
+        uint32_t first_bad[2][PC];
+#pragma unroll
+        for (int j = 0; j < PC; j++) first_bad[0][j] = rows.bad[j], first_bad[1][j] = newer.bad[j];
+        rows = newer;
 #pragma unroll
         for (int x = 0; x < AHEAD; x++) {
             fetch_ids();
-            load_tile(ahead[x], mine + (x + 1) * span);
+            place(newer, mine + (x + 2) * span);
+#pragma unroll
+            for (int j = 0; j < PC; j++) {
+                load_v(ahead[x], rows, j);
+                load_k(ahead[x], newer, j);
+                bad[x][j] = newer.bad[j];
+            }
+            rows = newer;
         }
-        uint32_t ks[KB], vs[KB], pk[NP][KB][8];
+        uint4 kf[KB][KM];
+        uint32_t ks[KB], pk[NP][KB][8];
         float part[2];
         w.refer_to(0.f);
-        ready(start, mine, ks, vs);
 #pragma unroll
-        for (int u = 0; u < UNITS; u++) put_v(start, vs, w.tile(), u);
-        q4_for<QK>([&](auto x) { score(x, start, ks, sa); });
+        for (int j = 0; j < PC; j++) put_k(start, first_bad[0][j], 0, j);
+#pragma unroll
+        for (int u = 0; u < UNITS; u++) put_v(start, mine + 16 * w.wr, w.buffer(0), u);
+        if constexpr (G::K_BUFS == 1) {
+            asm volatile("" ::: "memory");
+            get_k(0, kf, ks);
+            asm volatile("" ::: "memory");
+        }
+#pragma unroll
+        for (int j = 0; j < PC; j++) put_k(second, first_bad[1][j], 1, j);
+        w.staged();
+        if constexpr (G::K_BUFS > 1) get_k(0, kf, ks);
+        q4_for<QK>([&](auto x) { score(x, kf, ks, sa); });
         // the last round alone may have tiles that are not whole
         const int last = mine + (rounds - 1) * span;
         const auto cut = [&] {
@@ -700,42 +718,47 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         w.enter(sa);
         if (rounds > 1 && w.m == -INFINITY) w.m = 0.f;  // what `off` says
         w.staged();
-        const auto step = [&](auto buffer, int t, Codes &next, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
+        const auto step = [&](auto buffer, int t, Codes &codes, uint32_t (&bad_k)[PC], q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
+            constexpr int NOW = decltype(buffer)::value, FLY = 3;  // fragments of V on their way from LDS
             const int base = mine + t * span;
-            uint8_t *const tile = w.buffer(decltype(buffer)::value), *const tile_next = w.buffer(1 - decltype(buffer)::value);
-            constexpr int FLY = 3;  // fragments of V on their way from LDS
+            uint8_t *const tile = w.buffer(NOW), *const tile_next = w.buffer(1 - NOW);
             q4_bf16x8 v[FLY + 1];
             fetch_ids();
-            ready(next, base + span, ks, vs);
+            get_k(1 - NOW, kf, ks);
             q4_for<QK>([&](auto x) {
                 constexpr int X = decltype(x)::value;
-                score(x, next, ks, s_next);
+                score(x, kf, ks, s_next);
                 constexpr int LO = X * 8 * KB / QK, HI = (X + 1) * 8 * KB / QK;
                 q4_for<HI - LO>([&](auto y) { Wave::template weigh<LO + decltype(y)::value>(s, pk, part); });
-                if constexpr (false && X >= QK - FLY) v[X - (QK - FLY)] = w.v_fragment(tile, (X - (QK - FLY)) / DB, (X - (QK - FLY)) % DB);
                 __builtin_amdgcn_sched_barrier(0);
             });
             w.template settle<true>(s, s_next, pk, part);
-            if constexpr (true) q4_for<FLY>([&](auto x) { v[decltype(x)::value] = w.v_fragment(tile, decltype(x)::value / DB, decltype(x)::value % DB); });
+            q4_for<FLY>([&](auto x) { v[decltype(x)::value] = w.v_fragment(tile, decltype(x)::value / DB, decltype(x)::value % DB); });
             q4_for<PV>([&](auto x) {
                 constexpr int X = decltype(x)::value, Y = X + FLY;
                 if constexpr (Y < PV) v[Y % (FLY + 1)] = w.v_fragment(tile, Y / DB, Y % DB);
                 w.template multiply<NP>(v[X % (FLY + 1)], X / DB, X % DB, pk);
-                if constexpr (X == 0) place(next, base + (AHEAD + 1) * span);
-                if constexpr (X < KB) load_k(next, X);
-                if constexpr (X < UNITS) put_v(next, vs, tile_next, X);
-                if constexpr (X < UNITS && X % VW == VW - 1) load_v(next, X / VW);
+                if constexpr (X == 0) place(newer, base + (AHEAD + 2) * span);
+                if constexpr (X < UNITS) put_v(codes, base + span + 16 * w.wr, tile_next, X);
+                if constexpr (X < UNITS && X % VW == VW - 1) {
+                    constexpr int J = X / VW;
+                    put_k(codes, bad_k[J], NOW, J);
+                    bad_k[J] = newer.bad[J];
+                    load_v(codes, rows, J);
+                    load_k(codes, newer, J);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             });
+            rows = newer;
             w.staged();
         };
         int t = 0;
         for (; t + 2 < rounds; t += 2) {
-            step(std::integral_constant<int, 0>{}, t, ahead[0], sa, sb);
-            step(std::integral_constant<int, 1>{}, t + 1, ahead[AHEAD - 1], sb, sa);
+            step(std::integral_constant<int, 0>{}, t, ahead[0], bad[0], sa, sb);
+            step(std::integral_constant<int, 1>{}, t + 1, ahead[AHEAD - 1], bad[AHEAD - 1], sb, sa);
         }
         if (t + 1 < rounds) {
-            step(std::integral_constant<int, 0>{}, t, ahead[0], sa, sb);
+            step(std::integral_constant<int, 0>{}, t, ahead[0], bad[0], sa, sb);
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) sa[kb] = sb[kb];
         }
@@ -1052,25 +1075,22 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     return pl;
 }
 
-template <int D, bool F32, int RW, bool PAGED, bool BIG>
+template <int D, bool F32, int RW, bool PAGED>
 static int32_t launch_q4(const Q4Attn &p, unsigned grid, hipStream_t st) {
     constexpr int lds = Q4Geo<D, F32, RW>::LDS;
-    static_assert(lds <= (Q4Geo<D, F32, RW>::NW == 8 ? 144 : 78) * 1024, "eight wavefronts a compute unit, and static LDS beside it");
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED, BIG>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static_assert(lds <= (Q4Geo<D, F32, RW>::NW == 8 ? 150 : 78) * 1024, "eight wavefronts a compute unit, and static LDS beside it");
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_q4_kernel<D, F32, RW, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) {
         g_last_hip_error = (int32_t)e;
         return ETV_ERR_HIP;
     }
-    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED, BIG>), dim3(grid), dim3(Q4Geo<D, F32, RW>::NW * 64), lds, st, p);
+    hipLaunchKernelGGL((attn_q4_kernel<D, F32, RW, PAGED>), dim3(grid), dim3(Q4Geo<D, F32, RW>::NW * 64), lds, st, p);
     return check_launch();
 }
 
 template <int D, bool F32, int RW>
 static int32_t launch_q4_form(const Q4Attn &p, unsigned grid, hipStream_t st) {
-    const bool paged = p.block_size != 0;
-    const uint64_t rows = paged ? (uint64_t)p.num_blocks * p.Hkv * p.block_size : (uint64_t)p.B * p.Hkv * p.P_cap;
-    if (rows * (D / 2) > UINT32_MAX) return paged ? launch_q4<D, F32, RW, true, true>(p, grid, st) : launch_q4<D, F32, RW, false, true>(p, grid, st);
-    return paged ? launch_q4<D, F32, RW, true, false>(p, grid, st) : launch_q4<D, F32, RW, false, false>(p, grid, st);
+    return p.block_size ? launch_q4<D, F32, RW, true>(p, grid, st) : launch_q4<D, F32, RW, false>(p, grid, st);
 }
 
 template <int D, bool F32>
