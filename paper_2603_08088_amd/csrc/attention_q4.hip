@@ -172,7 +172,6 @@ template <int D, bool F32, int RW>
 struct Q4Geo {
     static constexpr int NW = q4_wavefronts(F32, RW);
     static constexpr int KB = RW == 4 ? 2 : 1, KEYS = 32 * KB;  // key blocks and keys of a tile
-    static constexpr int AHEAD = RW == 4 ? 1 : 2;                // tiles on their way besides those in LDS
     static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = NW / RW, BUFS = 2;
     static constexpr int K_BUFS = RW > 1 ? 2 : 1, K_TILE = KEYS * D / 2, K_SCALES = KEYS * 4;
     static constexpr int K_AT = KW * BUFS * TILE, K_SCALES_AT = K_AT + KW * K_BUFS * K_TILE, TILES = K_SCALES_AT + KW * K_BUFS * K_SCALES;
@@ -408,10 +407,10 @@ __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int hea
     if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : inv != inv ? NAN : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
 }
 
-// Which keys of which sequence a prefix slot stands for.  All splits of a call are of one size c (in rounds of `span` keys), the
-// smallest for which the slots suffice: nearly so where c = ceil(rounds / slots) works out, and with c = ceil(rounds / (slots - B))
-// always, a sequence's last split being the only one that is not full.  So a short sequence has few splits and the long ones of a
-// ragged batch share the rest.  Every wavefront works it out for itself, a lane per sequence.
+// Which keys of which sequence a prefix slot stands for.  All splits of a call are of one size c (in rounds of `span` keys), about the
+// smallest for which the slots suffice: not before c = ceil(rounds / slots), and with c = ceil(rounds / (slots - B)) always, a
+// sequence's last split being the only one that is not full.  So a short sequence has few splits and the long ones of a ragged
+// batch share the rest.  Every wavefront works it out for itself, a lane per sequence.
 struct Q4Share {
     int b, k0, k1, first, count;  // count 0: nobody's slot.  first, count: the sequence's slots
 };
@@ -422,8 +421,9 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
     const int total = __builtin_amdgcn_readlane(wave_scan_sum(rounds), 63);
     int c = p.chunk > 0 ? p.chunk / p.span : max(1, (total + slots - 1) / slots);
     int count = (rounds + c - 1) / c, upto = wave_scan_sum(count);
-    if (__builtin_amdgcn_readlane(upto, 63) > slots) {
-        c = (total + slots - p.B - 1) / (slots - p.B);
+    const int enough = p.chunk > 0 ? c : (total + slots - p.B - 1) / max(1, slots - p.B);
+    while (c < enough && __builtin_amdgcn_readlane(upto, 63) > slots) {
+        c = min(c + 1 + c / 16, enough);
         count = (rounds + c - 1) / c;
         upto = wave_scan_sum(count);
     }
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
     using T = std::conditional_t<F32, float, uint16_t>;
     using Wave = Q4Wave<D, F32, RW>;
     using G = Q4Geo<D, F32, RW>;
-    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS, AHEAD = G::AHEAD;
+    constexpr int KM = Wave::KM, DB = Wave::DB, NP = Wave::NP, NQ = Wave::NQ, QW = Wave::QW, KW = G::KW, KB = G::KB, KEYS = G::KEYS;
     extern __shared__ __attribute__((aligned(1024))) uint8_t q4_smem[];
     const int tid = threadIdx.x;
     Wave w{p, q4_smem};
@@ -546,8 +546,8 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         }
 
         // A wavefront's pieces of a tile are 16 whole rows each, a lane having a quarter of a row of K and of V: loads of consecutive
-        // memory beside a scalar base.  (Each lane with the rows and groups that its products want costs the address unit four
-        // times as long a load, and every wavefront K's: 267 us where 16 x 8 heads of 4096 keys and 128 nodes take DUMMY now.)
+        // memory beside a scalar base.  (A lane that loads the rows and groups its products want takes the address unit four times as
+        // long, and K would be loaded by every wavefront: 268 us for 32 x 8 heads of 4096 keys and 128 nodes, 245 this way.)
         constexpr int PC = KEYS / 16 / RW, VW = D / 32;  // pieces of a wavefront, words of a lane
         struct Codes {
             uint32_t k[PC][VW], v[PC][VW], ks[PC], vs[PC];  // K of a tile, V of the one before it; scales: the quarter's
@@ -659,44 +659,37 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
 
         // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials; between its
         // value products it stores the next tile's V and the K of the one after into LDS: the matrix and the vector unit are both busy
-        // within one wavefront.  What is stored was asked for a step (AHEAD: two) before.
-        Codes start, second, ahead[AHEAD];
-        Rows rows, newer;  // of the tile whose K was asked for last, and of the next one
-        uint32_t bad[AHEAD][PC];
+        // within one wavefront.  What is stored was asked for a step before (two steps ahead took 38.6 us instead of 35.7 where 32 x 8
+        // heads of 4096 keys and 8 nodes leave the reading: more registers and a longer start).
+        Codes start, second, codes;
+        Rows first, rows, newer;  // rows, newer: of the tile whose K was asked for last, and of the next one
+        uint32_t bad[PC];         // of the K in `codes`
         q4_f32x16 sa[KB], sb[KB];
         fetch_ids();
-        place(rows, mine);
+        place(first, mine);
 #pragma unroll
         for (int j = 0; j < PC; j++) {
-            load_k(start, rows, j);
-            load_v(start, rows, j);
+            load_k(start, first, j);
+            load_v(start, first, j);
         }
         fetch_ids();
-        place(newer, mine + span);
+        place(rows, mine + span);
 #pragma unroll
-        for (int j = 0; j < PC; j++) load_k(second, newer, j);
-        uint32_t first_bad[2][PC];
+        for (int j = 0; j < PC; j++) load_k(second, rows, j);
+        fetch_ids();
+        place(newer, mine + 2 * span);
 #pragma unroll
-        for (int j = 0; j < PC; j++) first_bad[0][j] = rows.bad[j], first_bad[1][j] = newer.bad[j];
-        rows = newer;
-#pragma unroll
-        for (int x = 0; x < AHEAD; x++) {
-            fetch_ids();
-            place(newer, mine + (x + 2) * span);
-#pragma unroll
-            for (int j = 0; j < PC; j++) {
-                load_v(ahead[x], rows, j);
-                load_k(ahead[x], newer, j);
-                bad[x][j] = newer.bad[j];
-            }
-            rows = newer;
+        for (int j = 0; j < PC; j++) {
+            load_v(codes, rows, j);
+            load_k(codes, newer, j);
+            bad[j] = newer.bad[j];
         }
         uint4 kf[KB][KM];
         uint32_t ks[KB], pk[NP][KB][8];
         float part[2];
         w.refer_to(0.f);
 #pragma unroll
-        for (int j = 0; j < PC; j++) put_k(start, first_bad[0][j], 0, j);
+        for (int j = 0; j < PC; j++) put_k(start, first.bad[j], 0, j);
 #pragma unroll
         for (int u = 0; u < UNITS; u++) put_v(start, mine + 16 * w.wr, w.buffer(0), u);
         if constexpr (G::K_BUFS == 1) {
@@ -705,7 +698,8 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             asm volatile("" ::: "memory");
         }
 #pragma unroll
-        for (int j = 0; j < PC; j++) put_k(second, first_bad[1][j], 1, j);
+        for (int j = 0; j < PC; j++) put_k(second, rows.bad[j], 1, j);
+        rows = newer;
         w.staged();
         if constexpr (G::K_BUFS > 1) get_k(0, kf, ks);
         q4_for<QK>([&](auto x) { score(x, kf, ks, sa); });
@@ -718,7 +712,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         w.enter(sa);
         if (rounds > 1 && w.m == -INFINITY) w.m = 0.f;  // what `off` says
         w.staged();
-        const auto step = [&](auto buffer, int t, Codes &codes, uint32_t (&bad_k)[PC], q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
+        const auto step = [&](auto buffer, int t, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
             constexpr int NOW = decltype(buffer)::value, FLY = 3;  // fragments of V on their way from LDS
             const int base = mine + t * span;
             uint8_t *const tile = w.buffer(NOW), *const tile_next = w.buffer(1 - NOW);
@@ -738,12 +732,12 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
                 constexpr int X = decltype(x)::value, Y = X + FLY;
                 if constexpr (Y < PV) v[Y % (FLY + 1)] = w.v_fragment(tile, Y / DB, Y % DB);
                 w.template multiply<NP>(v[X % (FLY + 1)], X / DB, X % DB, pk);
-                if constexpr (X == 0) place(newer, base + (AHEAD + 2) * span);
+                if constexpr (X == 0) place(newer, base + 3 * span);
                 if constexpr (X < UNITS) put_v(codes, base + span + 16 * w.wr, tile_next, X);
                 if constexpr (X < UNITS && X % VW == VW - 1) {
                     constexpr int J = X / VW;
-                    put_k(codes, bad_k[J], NOW, J);
-                    bad_k[J] = newer.bad[J];
+                    put_k(codes, bad[J], NOW, J);
+                    bad[J] = newer.bad[J];
                     load_v(codes, rows, J);
                     load_k(codes, newer, J);
                 }
@@ -754,11 +748,11 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         };
         int t = 0;
         for (; t + 2 < rounds; t += 2) {
-            step(std::integral_constant<int, 0>{}, t, ahead[0], bad[0], sa, sb);
-            step(std::integral_constant<int, 1>{}, t + 1, ahead[AHEAD - 1], bad[AHEAD - 1], sb, sa);
+            step(std::integral_constant<int, 0>{}, t, sa, sb);
+            step(std::integral_constant<int, 1>{}, t + 1, sb, sa);
         }
         if (t + 1 < rounds) {
-            step(std::integral_constant<int, 0>{}, t, ahead[0], bad[0], sa, sb);
+            step(std::integral_constant<int, 0>{}, t, sa, sb);
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) sa[kb] = sb[kb];
         }
