@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
 //   O^T[d, r]   += V^T P^T   bf16: V is converted (exactly) into an LDS tile and comes back through the transpose read; P stays
 //                            in registers as the product's B operand
 // The parts of q: with e the exponent of its group's maximum, part x is q less the parts before it, rounded to e2m3 at scale
-// 2^(e - 2 - 4x).  Three parts leave at most 2^-14 of the group's maximum, which is half a unit of the bf16 there; fp32 takes
-// six (2^-26).  Six-bit and four-bit operands run at four times the bf16 rate, so three parts cost less than one bf16 product,
-// and K needs neither a conversion nor LDS.
+// 2^(e - 2 - 4x).  Four parts leave at most 2^-18 of the group's maximum, fp32 takes six (2^-26).  (Three, 2^-14, are enough for
+// outputs rounded to bf16, but show in lse.)  Six-bit and four-bit operands run at four times the bf16 rate: four parts cost what
+// one bf16 product would, and K needs no conversion.
 // fp32: P in three bf16 parts, exactly, and the tree's K, V and q likewise (products with parts below 2^-24 left out).
 // RW wavefronts of a workgroup share their keys and have rows of their own; the groups of RW share the rows: few rows
 // (a token, a small tree) leave reading the cache as the work, and every wavefront reads keys of its own.
@@ -175,6 +175,9 @@ struct Q4Geo {
     static constexpr int ROW = 2 * D, TILE = KEYS * ROW, KW = NW / RW, BUFS = 2;
     static constexpr int K_BUFS = RW > 1 ? 2 : 1, K_TILE = KEYS * D / 2, K_SCALES = KEYS * 4;
     static constexpr int K_AT = KW * BUFS * TILE, K_SCALES_AT = K_AT + KW * K_BUFS * K_TILE, TILES = K_SCALES_AT + KW * K_BUFS * K_SCALES;
+    // Do the scores' products start from less the reference (16 registers, all alike), or is it taken off each score?  The former
+    // saves 32 instructions a tile; where registers are short it costs more in spills (32 x 8 heads of 4096 keys, 128 nodes: 468 us, 279 the other way).
+    static constexpr bool RELATIVE = !(RW == 4 && D == 128 && !F32);
     static constexpr int OUT_ROW = 64 + 4, OUT = NW * 32 * (OUT_ROW * 4 + 8);  // floats; four on from a multiple of the banks
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
 };
@@ -233,7 +236,7 @@ __device__ __forceinline__ void q4_for(F f) { q4_each(f, std::make_integer_seque
 
 template <int D, bool F32, int RW>
 struct Q4Wave {
-    static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 3, QW = F32 ? 2 : 1;
+    static constexpr int KM = D / 64, DB = D / 32, NP = F32 ? 3 : 1, NQ = F32 ? 6 : 4, QW = (NQ + 3) / 4;
     using G = Q4Geo<D, F32, RW>;
     static constexpr int KB = G::KB;
     const Q4Attn &p;
@@ -241,7 +244,7 @@ struct Q4Wave {
     int lane, r, hh, kg, wr, stage;
     q4_f32x16 o[DB];
     q4_f32x16 off;    // less the reference in every element: what the scores' products start from
-    float m, sum[2];  // reference (log2), -inf: none yet; the row's sum in two chains
+    float m, taken, sum[2];  // reference (log2), -inf: none yet; the same as scores lose it; the row's sum in two chains
 
     __device__ __forceinline__ uint8_t *buffer(int x) const { return smem + kg * G::BUFS * G::TILE + x * G::TILE; }
     __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (stage & 1)) * G::TILE; }
@@ -273,9 +276,9 @@ struct Q4Wave {
         return q4_half_max(__builtin_elementwise_maximum(top[0], top[1]));
     }
     __device__ __forceinline__ void refer_to(float reference) {
-        m = reference;
+        m = taken = reference;
 #pragma unroll
-        for (int i = 0; i < 16; i++) off[i] = -reference;
+        for (int i = 0; i < 16; i++) off[i] = G::RELATIVE ? -reference : 0.f;
     }
     __device__ __forceinline__ void scale_outputs(float f) {
         sum[0] *= f;
@@ -296,26 +299,21 @@ struct Q4Wave {
         const float top = largest(s);
         const bool none = m == -INFINITY;
         refer_to(!none ? m : fabsf(top) < INFINITY ? top : 0.f);
-        shift(s, m);
+        if (G::RELATIVE) shift(s, m);
         if (none && top == -INFINITY) m = -INFINITY;
     }
 
     // P^T: pair x of a tile's 8 KB pairs of relative scores to weights, and their part of the row's sum.
     template <int X>
-    __device__ __forceinline__ static void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
+    __device__ __forceinline__ void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) const {
         constexpr int kb = X / 8, i = X % 8;
-        const float a = __builtin_amdgcn_exp2f(s[kb][2 * i]), b = __builtin_amdgcn_exp2f(s[kb][2 * i + 1]);
-        if constexpr (F32) {
-            q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
-            part[X & 1] = X < 2 ? a + b : part[X & 1] + (a + b);
-        } else {
-            // the weights rounded to bf16 are the weights: the sum takes them as the product does
-            pk[0][kb][i] = q4_pair(a, b);
-            part[X & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(q4_bf16x2, pk[0][kb][i]), __builtin_bit_cast(q4_bf16x2, 0x3f803f80u),
-                                                          X < 2 ? 0.f : part[X & 1], false);
-        }
+        const float by = G::RELATIVE ? 0.f : taken;
+        const float a = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i] : s[kb][2 * i] - by), b = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i + 1] : s[kb][2 * i + 1] - by);
+        if constexpr (F32) q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
+        else pk[0][kb][i] = q4_pair(a, b);  // the value product takes them rounded to bf16, the sum (and lse) does not
+        part[X & 1] = X < 2 ? a + b : part[X & 1] + (a + b);
     }
-    __device__ __forceinline__ static void weigh_all(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
+    __device__ __forceinline__ void weigh_all(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) const {
         q4_for<8 * KB>([&](auto x) { weigh<decltype(x)::value>(s, pk, part); });
     }
     // A tile whose sum shows that its scores have left the reference behind gives the rows a new one; only then is the maximum
@@ -323,11 +321,13 @@ struct Q4Wave {
     template <bool NEXT>
     __device__ __forceinline__ void settle(q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
         if (__builtin_expect(__any(!(part[0] + part[1] <= kQ4Lazy)), 0)) {
-            const float top = largest(s), lift = top > 0.f && top < INFINITY ? top : 0.f;
+            const float top = G::RELATIVE ? largest(s) : largest(s) - taken, lift = top > 0.f && top < INFINITY ? top : 0.f;
             scale_outputs(__builtin_amdgcn_exp2f(-lift));
-            shift(s, lift);
-            if (NEXT) shift(s_next, lift);
-            refer_to(m + lift);
+            if (G::RELATIVE) shift(s, lift);
+            if (G::RELATIVE && NEXT) shift(s_next, lift);
+            const bool none = m == -INFINITY;
+            refer_to(taken + lift);
+            if (none) m = -INFINITY;
             weigh_all(s, pk, part);
         }
         sum[0] += part[0];
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             }
             const uint32_t e = max(top >> 23, 4 * NQ + 2u) - 2;  // every part's scale byte is at least 1
             qs[0][i] = e | (e - 4) << 8 | (e - 8) << 16 | (NQ > 3 ? (e - 12) << 24 : 0u);
-            if constexpr (NQ > 3) qs[QW - 1][i] = (e - 16) | (e - 20) << 8;
+            if constexpr (NQ > 4) qs[QW - 1][i] = (e - 16) | (e - 20) << 8;
             if (top >= 0x7f800000u)
                 for (int j = 0; j < QW; j++) qs[j][i] = 0xffffffffu;
 #pragma unroll
@@ -639,26 +639,25 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             *reinterpret_cast<uint4 *>(tile + row * G::ROW + (((VW * quarter + x) ^ q4_swizzle<D>(row)) << 4)) = v;
         };
         // K of a tile as the products want it: of key row r of each key block the groups 2i + hh, the scales' bytes 0 and 2
-        const auto get_k = [&](int buffer, uint4 (&kf)[KB][KM], uint32_t (&ks)[KB]) {
+        const auto get_k = [&](int buffer, int i, uint4 (&kf)[KB][KM], uint32_t (&ks)[KB]) {
             const int x = G::K_BUFS > 1 ? buffer : 0;
 #pragma unroll
             for (int kb = 0; kb < KB; kb++) {
                 const int row = 32 * kb + r;
                 const uint8_t *const from = k_tiles + x * G::K_TILE + row * (D / 2), *const sc = k_scales + x * G::K_SCALES + row * (D / 32);
-#pragma unroll
-                for (int i = 0; i < KM; i++) kf[kb][i] = *reinterpret_cast<const uint4 *>(from + (D == 128 ? ((2 * i + hh) ^ (r >> 2 & 3)) << 4 : 16 * hh));
-                ks[kb] = (D == 128 ? *reinterpret_cast<const uint32_t *>(sc) : (uint32_t) * reinterpret_cast<const uint16_t *>(sc)) >> (8 * hh);
+                kf[kb][i] = *reinterpret_cast<const uint4 *>(from + (D == 128 ? ((2 * i + hh) ^ (r >> 2 & 3)) << 4 : 16 * hh));
+                if (i == 0) ks[kb] = (D == 128 ? *reinterpret_cast<const uint32_t *>(sc) : (uint32_t) * reinterpret_cast<const uint16_t *>(sc)) >> (8 * hh);
             }
         };
         // Scores: product X of a tile's QK, y the part of q.
         constexpr int QK = NQ * KM * KB, PV = 2 * KB * DB, UNITS = PC * VW;
         const auto score = [&](auto x, const uint4 (&kf)[KB][KM], const uint32_t (&ks)[KB], q4_f32x16 (&s)[KB]) {
-            constexpr int X = decltype(x)::value, kb = X % KB, i = X / KB % KM, y = X / (KB * KM);
+            constexpr int X = decltype(x)::value, kb = X % KB, y = X / KB % NQ, i = X / (KB * NQ);
             s[kb] = q4_scores<2 * i, y & 3>(kf[kb][i], qp[y][i], X < KB ? w.off : s[kb], ks[kb], qs[y >> 2][i]);
         };
 
-        // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials; between its
-        // value products it stores the next tile's V and the K of the one after into LDS: the matrix and the vector unit are both busy
+        // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials (or, where
+        // they are not relative, before its value products); between those it stores the next tile's V and the K of the one after into LDS: the matrix and the vector unit are both busy
         // within one wavefront.  What is stored was asked for a step before (two steps ahead took 38.6 us instead of 35.7 where 32 x 8
         // heads of 4096 keys and 8 nodes leave the reading: more registers and a longer start).
         Codes start, second, codes;
@@ -694,14 +693,14 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         for (int u = 0; u < UNITS; u++) put_v(start, mine + 16 * w.wr, w.buffer(0), u);
         if constexpr (G::K_BUFS == 1) {
             asm volatile("" ::: "memory");
-            get_k(0, kf, ks);
+            q4_for<KM>([&](auto i) { get_k(0, decltype(i)::value, kf, ks); });
             asm volatile("" ::: "memory");
         }
 #pragma unroll
         for (int j = 0; j < PC; j++) put_k(second, rows.bad[j], 1, j);
         rows = newer;
         w.staged();
-        if constexpr (G::K_BUFS > 1) get_k(0, kf, ks);
+        if constexpr (G::K_BUFS > 1) q4_for<KM>([&](auto i) { get_k(0, decltype(i)::value, kf, ks); });
         q4_for<QK>([&](auto x) { score(x, kf, ks, sa); });
         // the last round alone may have tiles that are not whole
         const int last = mine + (rounds - 1) * span;
@@ -718,12 +717,13 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             uint8_t *const tile = w.buffer(NOW), *const tile_next = w.buffer(1 - NOW);
             q4_bf16x8 v[FLY + 1];
             fetch_ids();
-            get_k(1 - NOW, kf, ks);
+            get_k(1 - NOW, 0, kf, ks);
             q4_for<QK>([&](auto x) {
                 constexpr int X = decltype(x)::value;
+                if constexpr (KM == 2 && X == KB * NQ - 3) get_k(1 - NOW, KM - 1, kf, ks);  // no earlier: registers
                 score(x, kf, ks, s_next);
                 constexpr int LO = X * 8 * KB / QK, HI = (X + 1) * 8 * KB / QK;
-                q4_for<HI - LO>([&](auto y) { Wave::template weigh<LO + decltype(y)::value>(s, pk, part); });
+                q4_for<HI - LO>([&](auto y) { w.template weigh<LO + decltype(y)::value>(s, pk, part); });
                 __builtin_amdgcn_sched_barrier(0);
             });
             w.template settle<true>(s, s_next, pk, part);
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         }
         w.stage = rounds - 1;
         if (rounds > 1) cut();
-        Wave::weigh_all(sa, pk, part);
+        w.weigh_all(sa, pk, part);
         w.template settle<false>(sa, sb, pk, part);
         w.template accumulate<NP>(w.tile(), pk);
         w.stage++;
@@ -835,7 +835,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             w.enter(s);
             uint32_t pk[NP][KB][8];
             float part[2];
-            Wave::weigh_all(s, pk, part);
+            w.weigh_all(s, pk, part);
             w.template settle<false>(s, s, pk, part);
             // V, one bf16 part of it at a time
             const auto stage_part = [&](int part) {
@@ -984,7 +984,8 @@ __global__ void __launch_bounds__(256) join_q4_kernel(Q4Attn p) {
             sum = sum * old + part;
             for (int j = 0; j < 8; j++) acc[j] *= old;
             const int here = min(WIDTH, entries - first);
-            for (int j = worker; j < here; j += WORKERS * BATCH) {
+            for (int j0 = 0; j0 < here; j0 += WORKERS * BATCH) {  // all lanes stay: the shuffles need them
+                const int j = j0 + worker;
                 float4 v[BATCH][2];
                 float g[BATCH];
 #pragma unroll

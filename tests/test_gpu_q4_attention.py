@@ -46,6 +46,47 @@ def test_generic_kernel_against_float64(shape):
     c.check(*c.run(flags=api.ATTN_FLAG_GENERIC))
 
 
+@pytest.mark.parametrize("splits", [2, 9, 16, 17, 31, 33, 64, 65, 130])
+@pytest.mark.parametrize("T,Hq,Hkv,d,dtype", [(1, 8, 2, 128, "bf16"), (17, 2, 1, 64, "bf16"), (40, 4, 2, 128, "f32"), (80, 32, 16, 64, "bf16")])
+def test_every_number_of_splits_is_joined(T, Hq, Hkv, d, dtype, splits):
+    """Fewer and more partials than the lanes of a row take at once, few and many rows, lengths that leave the last split short."""
+    step = 512                                       # of the largest round of a workgroup
+    Ps = [splits * step - 37, splits * step // 3]
+    c = Case(splits, 2, T, Hq, Hkv, d, dtype, [1, 1], 0)
+    c.Ps, c.P_max, c.size = Ps, max(Ps), max(Ps)
+    rng, shape = c.rng, (2, Hkv, max(Ps))
+    c.codes = [rng.integers(0, 256, shape + (d // 2,)).astype(np.uint8) for _ in range(2)]
+    c.scales = [rng.integers(122, 127, shape + (d // 32,)).astype(np.uint8) for _ in range(2)]
+    want, want_lse = c.run(flags=api.ATTN_FLAG_GENERIC)
+    got, lse = c.run(kv_split=step)
+    # two roundings to the type in either, weights and result, and 2^-13 for scores and sums in another order
+    tol = (4 * torch.finfo(c.dtype).eps / 2 + 2.0 ** -13) * want.float().abs().max().item()
+    assert (got.float() - want.float()).abs().max().item() <= tol and (lse - want_lse).abs().max().item() <= 2.0 ** -13
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,d,kv_split", [(70, 3, 8, 2, 128, 0), (66, 1, 4, 4, 64, 128), (33, 40, 8, 2, 128, 256), (5, 90, 8, 1, 128, 0)])
+def test_large_batches_of_ragged_sequences(B, T, Hq, Hkv, d, kv_split):
+    """More sequences than a wavefront has lanes, sequences without a prefix and without nodes; against the generic kernel."""
+    rng = np.random.default_rng(B)
+    Ps, ns = [int(x) for x in rng.integers(0, 900, B)], [int(x) for x in rng.integers(0, T + 1, B)]
+    Ps[1], Ps[2], ns[3], ns[0], Ps[0] = 0, 899, 0, T, 700
+    c = Case(B, B, T, Hq, Hkv, d, "bf16", Ps, 16, ns)
+    want, want_lse = c.run(flags=api.ATTN_FLAG_GENERIC)
+    got, lse = c.run(kv_split=kv_split)
+    assert (got.float() - want.float()).abs().max().item() <= (4 * 2.0 ** -8 + 2.0 ** -13) * want.float().abs().max().item()
+    assert torch.equal(torch.isinf(lse), torch.isinf(want_lse)) and torch.nan_to_num(lse - want_lse).abs().max().item() <= 2.0 ** -13
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,Hq,P", [(2, 8, 60), (20, 8, 300), (50, 8, 200)])
+def test_lse_keeps_fp32(dtype, T, Hq, P):
+    """The sum is over unrounded weights, of scores that are right to 2^-18 of q's maximum."""
+    c = Case(15, 1, T, Hq, 2, 128, dtype, [P], 16, [T])
+    _, lse = c.run()
+    want = c.plain()[1]
+    assert np.abs(lse.double().cpu().numpy() - want).max() <= c.score_slack() / 8 + 2.0 ** -20
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [1.0, -0.09, 2.0])
 def test_scales_of_either_sign_and_peaked_rows(dtype, scale):
