@@ -532,6 +532,7 @@ ETV_API int32_t etv_dequantize_kv_q4(const etv_q4_desc *h_desc, const uint8_t *k
  * zeros and lse = -inf.  A key in a block outside [0, num_blocks) counts as NaN.
  * h_desc: block_size 0 or a multiple of 16, num_blocks used when paged; flags: ETV_ATTN_FLAG_GENERIC or 0; scale 0
  * or of a magnitude within 1e-30 .. 1e30, of either sign.
+ * h_desc->kv_split is rounded up to whole rounds of a workgroup (64 to 256 keys).
  * workspace: etv_tree_verify_attention_q4_workspace_bytes(h_desc) bytes, 256-byte aligned.
  * Supported: dtype F32 or BF16, d in {64, 128}, Hq % Hkv == 0, 1 <= T_max <= ETV_ATTN_MAX_TREE. */
 ETV_API size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h_desc);

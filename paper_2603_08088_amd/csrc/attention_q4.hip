@@ -176,7 +176,7 @@ struct Q4Geo {
     static constexpr int K_BUFS = RW > 1 ? 2 : 1, K_TILE = KEYS * D / 2, K_SCALES = KEYS * 4;
     static constexpr int K_AT = KW * BUFS * TILE, K_SCALES_AT = K_AT + KW * K_BUFS * K_TILE, TILES = K_SCALES_AT + KW * K_BUFS * K_SCALES;
     // Do the scores' products start from less the reference (16 registers, all alike), or is it taken off each score?  The former
-    // saves 32 instructions a tile; where registers are short it costs more in spills (32 x 8 heads of 4096 keys, 128 nodes: 468 us, 279 the other way).
+    // saves 32 instructions a tile; where registers are short it costs more in spills (32 x 8 heads of 4096 keys, 128 nodes: 468 us, 279 to 296 the other way).
     static constexpr bool RELATIVE = !(RW == 4 && D == 128 && !F32);
     static constexpr int OUT_ROW = 64 + 4, OUT = NW * 32 * (OUT_ROW * 4 + 8);  // floats; four on from a multiple of the banks
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
@@ -547,7 +547,8 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
 
         // A wavefront's pieces of a tile are 16 whole rows each, a lane having a quarter of a row of K and of V: loads of consecutive
         // memory beside a scalar base.  (A lane that loads the rows and groups its products want takes the address unit four times as
-        // long, and K would be loaded by every wavefront: 268 us for 32 x 8 heads of 4096 keys and 128 nodes, 245 this way.)
+        // long, and K would be loaded by every wavefront: 268 us for 32 x 8 heads of 4096 keys and 128 nodes, 250 this way, with q in
+        // three parts.)
         constexpr int PC = KEYS / 16 / RW, VW = D / 32;  // pieces of a wavefront, words of a lane
         struct Codes {
             uint32_t k[PC][VW], v[PC][VW], ks[PC], vs[PC];  // K of a tile, V of the one before it; scales: the quarter's

