@@ -134,7 +134,7 @@ class Case:
 
     def score_slack(self, scale=0.0):
         """How far a score may be off: the products of a row are exact or rounded to fp32 and added in fp32 (d + 8 roundings of at
-        most 2^-24 of the sum of their magnitudes); q may enter them as a fixed-point number of 2^-14 (fp32: 2^-26) of its group's maximum."""
+        most 2^-24 of the sum of their magnitudes); q may enter them as a fixed-point number of 2^-18 (fp32: 2^-26) of its group's maximum."""
         G, sc = self.Hq // self.Hkv, abs(scale) or 1 / math.sqrt(self.d)
         q = np.abs(self.q.double().numpy())
         top = q.reshape(*q.shape[:-1], -1, 32).max(-1).repeat(32, -1)
@@ -144,7 +144,7 @@ class Case:
             for h in range(self.Hq):
                 keys = np.concatenate((K[:, h // G], np.nan_to_num(np.abs(self.kt[b, :, h // G].double().numpy()), posinf=0)))
                 if len(keys):
-                    exactness = 2.0 ** (-14 if self.dtype == torch.bfloat16 else -26)
+                    exactness = 2.0 ** (-18 if self.dtype == torch.bfloat16 else -26)
                     worst = max(worst, float((keys @ (top[b, :, h] * exactness + q[b, :, h] * (self.d + 8) * 2.0 ** -24).T).max()))
         return worst * sc
 
