@@ -145,10 +145,12 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
 //   P^T          = exp2(S^T * scale - reference)   a lane has 32 keys of one row; the reference follows the maximum lazily
 //   O^T[d, r]   += V^T P^T   bf16: V is converted (exactly) into an LDS tile and comes back through the transpose read; P stays
 //                            in registers as the product's B operand
-// The parts of q: with e the exponent of its group's maximum, part x is q less the parts before it, rounded to e2m3 at scale
-// 2^(e - 2 - 4x).  Four parts leave at most 2^-18 of the group's maximum, fp32 takes six (2^-26).  (Three, 2^-14, are enough for
-// outputs rounded to bf16, but show in lse.)  Six-bit and four-bit operands run at four times the bf16 rate: four parts cost what
-// one bf16 product would, and K needs no conversion.
+// The parts of q: part x is q less the parts before it, rounded to e2m3 at scale 2^(e - 2 - 4x), e being the exponent of its group's
+// maximum, one up where that comes within 1/16 of the next power of two: so the first part is never held at 7.5, the largest value
+// there is (a value just under 8 would leave the next part one just under 8 again, and so on: 2^-16 of it after four), and of the
+// maximum, at least 3.875 at that scale, no more than 2^-16 / 3.875 is left.  That is 2^-17.95 after four parts; fp32 takes six
+// (2^-25.95).  (Three, 2^-13.95, are enough for outputs rounded to bf16, but show in lse.)  Six-bit and four-bit operands run at four
+// times the bf16 rate: four parts cost what one bf16 product would, and K needs no conversion.
 // fp32: P in three bf16 parts, exactly, and the tree's K, V and q likewise (products with parts below 2^-24 left out).
 // RW wavefronts of a workgroup share their keys and have rows of their own; the groups of RW share the rows: few rows
 // (a token, a small tree) leave reading the cache as the work, and every wavefront reads keys of its own.
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
                 x[c] *= p.scale_log2;
                 top = max(top, __float_as_uint(x[c]) & 0x7fffffffu);
             }
-            const uint32_t e = max(top >> 23, 4 * NQ + 2u) - 2;  // every part's scale byte is at least 1
+            const uint32_t e = max((top + 0x80000u) >> 23, 4 * NQ + 2u) - 2;  // every part's scale byte is at least 1
             qs[0][i] = e | (e - 4) << 8 | (e - 8) << 16 | (NQ > 3 ? (e - 12) << 24 : 0u);
             if constexpr (NQ > 4) qs[QW - 1][i] = (e - 16) | (e - 20) << 8;
             if (top >= 0x7f800000u)

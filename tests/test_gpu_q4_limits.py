@@ -1,0 +1,56 @@
+"""tree_verify_attention_q4 on the GPU at the limits of what it takes: scores, lengths, layouts and every form of its kernel."""
+import copy
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_08088_amd import api
+from q4_plain import Case, place, quantise
+
+pytestmark = pytest.mark.gpu
+
+
+def call(c, cache, **kw):
+    """The call of Case.run on a cache of the caller's (one layer)."""
+    return api.tree_verify_attention_q4(c.q.cuda(), cache, c.ints(c.Ps), c.kt.cuda(), c.vt.cuda(), torch.from_numpy(c.words()).cuda(),
+                                        c.ints(c.ns), P_max=c.P_max, block_table=c.tables(), **kw)
+
+
+def hold(c, x, b, lo, rows):
+    """Rows [n, Hkv, d] of K (x = 0) or V (1) into positions lo .. of sequence b."""
+    codes, scales = quantise(rows)
+    for i in range(len(rows)):
+        page, off = place(c.table, c.size, b, lo + i)
+        c.codes[x][page, :, off], c.scales[x][page, :, off] = codes[i], scales[i]
+
+
+def scale_for(log2_scale):
+    """The largest float32 whose product with log2(e) in float32 is `log2_scale`."""
+    one, s = np.float32(1.4426950408889634), np.float32(log2_scale * math.log(2) * (1 + 2.0 ** -20))
+    while s * one > np.float32(log2_scale):
+        s = np.nextafter(s, np.float32(0))
+    assert s * one == np.float32(log2_scale)
+    return float(s)
+
+
+@pytest.mark.parametrize("d,T,Hq", [(64, 16, 2), (128, 16, 2), (64, 128, 2), (128, 128, 4)])
+@pytest.mark.parametrize("log2_scale", [2 - 2.0 ** -22, 0.125 - 2.0 ** -26, 2 - 2.0 ** -13, 1.0, 0.18])
+def test_queries_just_under_a_power_of_two_keep_their_bits(d, T, Hq, log2_scale):
+    """One key, one channel of q: lse is the score.  q comes as a number of four digits, off by at most 2^-17.95 of it; beside that
+    are some twelve fp32 roundings (the scale's two, q's, one a product, the logarithm's)."""
+    scale = scale_for(np.float32(log2_scale)) if log2_scale != 0.18 else 0.18 * math.log(2)
+    for part in range(0, 128, T):
+        c = Case(1, 1, T, Hq, 2, d, "bf16", [1], 0)
+        c.vis[:] = False                             # the tree's keys are not seen
+        c.q[:] = 0
+        mantissas = 1 + torch.arange(part, part + T) / 128
+        c.q[0, :, :, d - 3] = mantissas[:, None].to(torch.bfloat16)
+        row = np.zeros((1, 2, d))
+        row[0, :, d - 3] = 96
+        hold(c, 0, 0, 0, row)
+        _, lse = c.run(scale=scale)
+        want = mantissas.double()[None, None] * 96 * float(np.float32(scale))
+        off = ((lse.double().cpu() - want).abs() / want).max().item()
+        assert off <= 2.0 ** -17.95 + 12 * 2.0 ** -24, off

@@ -1,0 +1,44 @@
+"""The 4-bit prefix cache at the limits of its calls: what the host decides, and the digits of q; needs no GPU."""
+import ctypes as C
+
+import numpy as np
+
+from paper_2603_08088_amd import api
+
+A = 1 << 20      # an aligned address that nobody follows
+
+
+def attn_desc(**kw):
+    return api.AttnDesc(**{**dict(B=1, T_max=8, Hq=8, Hkv=2, d=128, dtype=api.BF16, block_size=16, max_blocks=9, num_blocks=9, P_cap=0, P_max=100),
+                           **kw})
+
+
+def attend(d, ks=A, vs=A, ws=A, size=1 << 40):
+    return api.lib().etv_tree_verify_attention_q4(C.byref(d), A, A, ks, A, vs, A, A, A, A, A, A, A, None, ws, size, None)
+
+
+def six_bits(x):
+    """To the nearest e2m3 (ties to the even mantissa), beyond 7.5 to 7.5."""
+    a = np.abs(x)
+    step = np.exp2(np.clip(np.floor(np.log2(np.maximum(a, 1e-30))), 0, 2) - 3)
+    return np.copysign(np.minimum(np.rint(a / step) * step, 7.5), x)
+
+
+def left(x, top, parts):
+    """What `parts` six-bit digits of x leave, in units of the group's maximum: the exponent is that of the maximum, one up
+    where it comes within 1/16 of the next power of two."""
+    e = np.floor(np.log2(top)) + (top / np.exp2(np.floor(np.log2(top))) >= 1.9375)
+    y = x / np.exp2(e - 2)
+    for _ in range(parts):
+        y = 16 * (y - six_bits(y))
+    return np.abs(y) / 16.0 ** parts * np.exp2(e - 2) / top
+
+
+def test_what_the_digits_of_q_leave():
+    """2^-17.95 of the group's maximum after four, 2^-25.95 after six, for any value up to that maximum."""
+    rng = np.random.default_rng(0)
+    tops = np.concatenate((1 + np.arange(1 << 16) / 65536, 2 - 2.0 ** -np.arange(1, 24), 1.9375 + np.array([-1, 0, 1]) * 2.0 ** -23))
+    for top in (tops, tops * rng.uniform(1, 1.5, tops.shape)):
+        for x in (top, -top, top * rng.uniform(0, 1, top.shape), top * 2.0 ** -rng.uniform(0, 18, top.shape)):
+            assert left(x, top, 4).max() <= 2.0 ** -17.95 and left(x, top, 6).max() <= 2.0 ** -25.95
+    assert left(tops, tops, 4).max() > 2.0 ** -18.1
