@@ -477,7 +477,8 @@ ETV_API int32_t etv_commit_path_indices(const etv_cache_desc *h_desc, const void
  * Row order, codes and scales alike, K and V in tensors of their own; layer l starts layer_rows rows after layer l-1:
  *   contiguous (block_size == 0)  [B, Hkv, P_cap]: position p of head h of sequence b is row (b * Hkv + h) * P_cap + p
  *   paged (multiple of 16)        [num_blocks, Hkv, block_size], blocks by block_table as in attention
- * codes are 16-byte aligned, scales 4-byte aligned.  d is 64 or 128; the unquantised side is fp32 or bf16.
+ * codes are 16-byte aligned, scales 4-byte aligned (one layer's, as attention takes it: d/32 bytes, wherever the layer starts).
+ * d is 64 or 128; the unquantised side is fp32 or bf16.
  * ------------------------------------------------------------------------- */
 typedef struct etv_q4_desc {
     int32_t B;

@@ -1120,7 +1120,8 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
     if (h->P_max > 0 && (!k_codes || !k_scales || !v_codes || !v_scales)) return ETV_ERR_INVALID_ARG;
     const uintptr_t align = (uintptr_t)q | (uintptr_t)kt | (uintptr_t)vt | (uintptr_t)out | (uintptr_t)k_codes | (uintptr_t)v_codes |
                             (uintptr_t)workspace;
-    if (align & 15 || ((uintptr_t)k_scales | (uintptr_t)v_scales) & 3) return ETV_ERR_INVALID_ARG;
+    // scales: whole rows.  (A layer of a contiguous cache, heads of 64, starts at a multiple of two bytes; they are read byte by byte.)
+    if (align & 15 || ((uintptr_t)k_scales | (uintptr_t)v_scales) & (uintptr_t)(h->d / 32 - 1)) return ETV_ERR_INVALID_ARG;
     if (h->B == 0) return ETV_OK;
     const etv::Q4Plan pl = etv::q4_plan(h);
     const bool generic = (h->flags & ETV_ATTN_FLAG_GENERIC) != 0;

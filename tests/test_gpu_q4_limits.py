@@ -54,3 +54,15 @@ def test_queries_just_under_a_power_of_two_keep_their_bits(d, T, Hq, log2_scale)
         want = mantissas.double()[None, None] * 96 * float(np.float32(scale))
         off = ((lse.double().cpu() - want).abs() / want).max().item()
         assert off <= 2.0 ** -17.95 + 12 * 2.0 ** -24, off
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_layer_of_a_cache_of_odd_rows(dtype):
+    """Scales of heads of 64 are two bytes a row: the second layer of 1003 rows starts at an odd pair."""
+    c = Case(2, 1, 3, 4, 1, 64, dtype, [998], 0)
+    assert c.size == 1003
+    cache = c.cache(layers=3)
+    assert cache.layer(1).k_scales.data_ptr() % 4 == 2
+    for layer in range(3):
+        for kw in (dict(), dict(kv_split=128), dict(flags=api.ATTN_FLAG_GENERIC)):
+            c.check(*call(c, cache.layer(layer), **kw))

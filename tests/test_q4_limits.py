@@ -17,6 +17,14 @@ def attend(d, ks=A, vs=A, ws=A, size=1 << 40):
     return api.lib().etv_tree_verify_attention_q4(C.byref(d), A, A, ks, A, vs, A, A, A, A, A, A, A, None, ws, size, None)
 
 
+def test_scales_of_one_layer_are_aligned_to_their_rows():
+    """B = 0 has nothing to launch: what is left are the checks."""
+    for d, unit in ((64, 2), (128, 4)):
+        desc = attn_desc(B=0, d=d)
+        assert attend(desc, ks=A + unit) == attend(desc, vs=A + 3 * unit) == 0
+        assert attend(desc, ks=A + unit // 2) == attend(desc, vs=A + unit // 2) == attend(desc, ks=A + unit + 1) == -1
+
+
 def six_bits(x):
     """To the nearest e2m3 (ties to the even mantissa), beyond 7.5 to 7.5."""
     a = np.abs(x)
