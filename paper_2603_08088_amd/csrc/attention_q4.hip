@@ -69,6 +69,7 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
     const int n = clampi(p.n_nodes[b], 0, p.T_max), P = clampi(p.prefix_len[b], 0, p.P_max);
     const size_t orow = (((size_t)b * p.T_max + k) * p.Hq + h) * D;
     float m = -INFINITY, l = 0.f, acc[C];
+    bool sees = false;
     for (int c = 0; c < C; c++) acc[c] = 0.f;
     if (k < n) {
         for (int c = 0; c < C; c++) sq[lane + 64 * c] = q4_elem(static_cast<const T *>(p.q), orow + lane + 64 * c);
@@ -111,6 +112,7 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
             sp[lane] = e;
             __syncthreads();
             const uint64_t seen = __ballot(see);
+            sees = sees || seen != 0;
             for (int x = 0; x < count; x++) {
                 if (!(seen >> x & 1)) continue;
                 const int jj = base + x - (tree ? P : 0);
@@ -132,9 +134,9 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
             }
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = !sees ? 0.f : l == 0.f ? NAN : 1.f / l;  // nothing but scores of -inf: NaN
     for (int c = 0; c < C; c++) q4_store(static_cast<T *>(p.out), orow + C * lane + c, acc[c] * inv);
-    if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.T_max + k] = l == 0.f ? -INFINITY : (m + log2f(l)) * kQ4Ln2;
+    if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.T_max + k] = !sees ? -INFINITY : l == 0.f ? NAN : (m + log2f(l)) * kQ4Ln2;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -391,11 +393,22 @@ __device__ __forceinline__ bool q4_take_out(uint4 &w) {
     return any;
 }
 
+// Does a node see a key?  Asked only where its weights add up to nothing.
+__device__ __forceinline__ bool q4_sees(const int32_t *prefix_len, const uint64_t *mask, int P_max, int n) {
+    bool any = min(*prefix_len, P_max) > 0;
+    for (int w = 0; 64 * w < n; w++) any = any || (n - 64 * w < 64 ? mask[w] & ((1ull << (n - 64 * w)) - 1) : mask[w]) != 0;
+    return any;
+}
+
 // One row's eight channels from its sums, and its lse by the first of the threads.
 template <typename T>
 __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int head, int piece, int D, bool node, float ref, float sum, const float (&acc)[8]) {
-    // no weight at all: zeros; an infinite score or a NaN among them: NaN
-    const float inv = !node || sum == 0.f ? 0.f : sum < INFINITY ? 1.f / sum : NAN;
+    // no key: zeros; keys, but no weight (scores of -inf alone), an infinite score or a NaN among them: NaN
+    if (node && sum == 0.f) {
+        node = q4_sees(p.prefix_len + b, p.bitmask + ((size_t)b * p.T_max + t) * p.words, p.P_max, clampi(p.n_nodes[b], 0, p.T_max));
+        sum = NAN;
+    }
+    const float inv = !node ? 0.f : sum < INFINITY ? 1.f / sum : NAN;
     T *const dst = static_cast<T *>(p.out) + (((size_t)b * p.T_max + t) * p.Hq + head) * D + 8 * piece;
     if constexpr (sizeof(T) == 4) {
         const float4 a = inv == 0.f ? float4{0, 0, 0, 0} : float4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};

@@ -66,3 +66,19 @@ def test_every_layer_of_a_cache_of_odd_rows(dtype):
     for layer in range(3):
         for kw in (dict(), dict(kv_split=128), dict(flags=api.ATTN_FLAG_GENERIC)):
             c.check(*call(c, cache.layer(layer), **kw))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,Ps,kw", [(6, [0], {}), (70, [0], {}), (6, [0, 600], dict(kv_split=64)), (40, [0, 600], dict(kv_split=64)),
+                                     (40, [0, 600], dict(flags=api.ATTN_FLAG_GENERIC))])
+def test_rows_that_see_only_a_score_of_minus_infinity(dtype, T, Ps, kw):
+    """They see a key, so they are NaN, as the definition's quotient is; a row that sees none is zeros and -inf."""
+    c = Case(3, len(Ps), T, 8, 2, 64, dtype, Ps, 16)
+    c.vis[0] = False
+    c.vis[0, 3:, 4] = True                           # rows 0 .. 2 see nothing, the others this key
+    c.kt[0, 4, 0, 9], c.kt[0, 4, 1, 9] = float("inf"), float("-inf")
+    c.q[0, :, :4, 9], c.q[0, :, 4:, 9] = -1, 2
+    out, lse = c.run(**kw)
+    assert (out[0, :3] == 0).all() and torch.isneginf(lse[0, :, :3]).all()
+    assert torch.isnan(out[0, 3:]).all() and torch.isnan(lse[0, :, 3:]).all()
+    assert torch.isfinite(out[1:]).all()
