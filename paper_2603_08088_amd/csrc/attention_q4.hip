@@ -180,8 +180,9 @@ struct Q4Geo {
     static constexpr int K_BUFS = RW > 1 ? 2 : 1, K_TILE = KEYS * D / 2, K_SCALES = KEYS * 4;
     static constexpr int K_AT = KW * BUFS * TILE, K_SCALES_AT = K_AT + KW * K_BUFS * K_TILE, TILES = K_SCALES_AT + KW * K_BUFS * K_SCALES;
     // Do the scores' products start from less the reference (16 registers, all alike), or is it taken off each score?  The former
-    // saves 32 instructions a tile; where registers are short it costs more in spills (32 x 8 heads of 4096 keys, 128 nodes: 468 us, 279 to 296 the other way).
-    static constexpr bool RELATIVE = !(RW == 4 && D == 128 && !F32);
+    // saves 16 instructions a key block; where registers are short it costs more in spills, whose reloads wait for every load on its
+    // way (32 x 8 heads of 4096 keys, 8 nodes: 51.6 us, 39.4 the other way; 128 nodes: 468 and 275).
+    static constexpr bool RELATIVE = !(RW != 2 && D == 128 && !F32);
     static constexpr int OUT_ROW = 64 + 4, OUT = NW * 32 * (OUT_ROW * 4 + 8);  // floats; four on from a multiple of the banks
     static constexpr int LDS = TILES > OUT ? TILES : OUT;
 };
@@ -248,7 +249,7 @@ struct Q4Wave {
     int lane, r, hh, kg, wr, stage;
     q4_f32x16 o[DB];
     q4_f32x16 off;    // less the reference in every element: what the scores' products start from
-    float m, taken, sum[2];  // reference (log2), -inf: none yet; the same as scores lose it; the row's sum in two chains
+    float ref, sum[2];  // reference (log2); the row's sum in two chains: zero while nothing has been weighed, and no reference holds
 
     __device__ __forceinline__ uint8_t *buffer(int x) const { return smem + kg * G::BUFS * G::TILE + x * G::TILE; }
     __device__ __forceinline__ uint8_t *tile() const { return smem + (kg * G::BUFS + (stage & 1)) * G::TILE; }
@@ -280,7 +281,7 @@ struct Q4Wave {
         return q4_half_max(__builtin_elementwise_maximum(top[0], top[1]));
     }
     __device__ __forceinline__ void refer_to(float reference) {
-        m = taken = reference;
+        ref = reference;
 #pragma unroll
         for (int i = 0; i < 16; i++) off[i] = G::RELATIVE ? -reference : 0.f;
     }
@@ -298,20 +299,20 @@ struct Q4Wave {
 #pragma unroll
             for (int i = 0; i < 16; i++) s[kb][i] -= by;
     }
-    // Scores become relative.  A row without a reference takes the tile's largest score, and stays without one where it sees nothing.
-    __device__ __forceinline__ void enter(q4_f32x16 (&s)[KB]) {
+    // Has the row a weight so far?  A reference's own key weighs 1, so a sum never falls back to zero.
+    __device__ __forceinline__ float row_sum() const { return q4_half_sum(sum[0] + sum[1]); }
+    // Scores become relative.  A row without a reference (`none`) takes the tile's largest score, if it sees any.
+    __device__ __forceinline__ void enter(q4_f32x16 (&s)[KB], bool none) {
         const float top = largest(s);
-        const bool none = m == -INFINITY;
-        refer_to(!none ? m : fabsf(top) < INFINITY ? top : 0.f);
-        if (G::RELATIVE) shift(s, m);
-        if (none && top == -INFINITY) m = -INFINITY;
+        refer_to(!none ? ref : fabsf(top) < INFINITY ? top : 0.f);
+        if (G::RELATIVE) shift(s, ref);
     }
 
     // P^T: pair x of a tile's 8 KB pairs of relative scores to weights, and their part of the row's sum.
     template <int X>
     __device__ __forceinline__ void weigh(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) const {
         constexpr int kb = X / 8, i = X % 8;
-        const float by = G::RELATIVE ? 0.f : taken;
+        const float by = G::RELATIVE ? 0.f : ref;
         const float a = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i] : s[kb][2 * i] - by), b = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i + 1] : s[kb][2 * i + 1] - by);
         if constexpr (F32) q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
         else pk[0][kb][i] = q4_pair(a, b);  // the value product takes them rounded to bf16, the sum (and lse) does not
@@ -325,13 +326,11 @@ struct Q4Wave {
     template <bool NEXT>
     __device__ __forceinline__ void settle(q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) {
         if (__builtin_expect(__any(!(part[0] + part[1] <= kQ4Lazy)), 0)) {
-            const float top = G::RELATIVE ? largest(s) : largest(s) - taken, lift = top > 0.f && top < INFINITY ? top : 0.f;
+            const float top = G::RELATIVE ? largest(s) : largest(s) - ref, lift = top > 0.f && top < INFINITY ? top : 0.f;
             scale_outputs(__builtin_amdgcn_exp2f(-lift));
             if (G::RELATIVE) shift(s, lift);
             if (G::RELATIVE && NEXT) shift(s_next, lift);
-            const bool none = m == -INFINITY;
-            refer_to(taken + lift);
-            if (none) m = -INFINITY;
+            refer_to(ref + lift);
             weigh_all(s, pk, part);
         }
         sum[0] += part[0];
@@ -469,7 +468,6 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
     w.kg = wave / RW;
     w.wr = wave % RW;
     w.stage = 0;
-    w.m = -INFINITY;
     w.sum[0] = w.sum[1] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; db++)
@@ -702,7 +700,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         uint4 kf[KB][KM];
         uint32_t ks[KB], pk[NP][KB][8];
         float part[2];
-        w.refer_to(0.f);
+        w.refer_to(0.f);  // what the first scores start from; that tile brings the reference
 #pragma unroll
         for (int j = 0; j < PC; j++) put_k(start, first.bad[j], 0, j);
 #pragma unroll
@@ -724,8 +722,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             if (last + KEYS > k1) w.mask(sa, last < k1 ? (1ull << (k1 - last)) - 1 : 0);
         };
         if (rounds == 1) cut();
-        w.enter(sa);
-        if (rounds > 1 && w.m == -INFINITY) w.m = 0.f;  // what `off` says
+        w.enter(sa, true);
         w.staged();
         const auto step = [&](auto buffer, int t, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
             constexpr int NOW = decltype(buffer)::value, FLY = 3;  // fragments of V on their way from LDS
@@ -848,7 +845,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
 #pragma unroll
                 for (int i = 0; i < 16; i++) s[kb][i] *= p.scale_log2;
             w.mask(s, vis);
-            w.enter(s);
+            w.enter(s, w.row_sum() == 0.f);
             uint32_t pk[NP][KB][8];
             float part[2];
             w.weigh_all(s, pk, part);
@@ -896,7 +893,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         }
     }
 
-    const float row_sum = q4_half_sum(w.sum[0] + w.sum[1]);
+    const float row_sum = w.row_sum();
     // Values of the tree's V that are not finite were left out: added here to the rows that see them, whose outputs are then
     // not finite whatever the weight.  (The barriers also end the last reads of the V tiles.)
     __shared__ int s_ill;
@@ -922,7 +919,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
     // Outputs through LDS, 64 channels at a time: the key groups of a row are joined, and rows are stored in one piece.
     float *const mine = reinterpret_cast<float *>(q4_smem) + (wave * 32 + r) * G::OUT_ROW + 4 * hh;
     float2 *const ml = reinterpret_cast<float2 *>(q4_smem + G::NW * 32 * G::OUT_ROW * 4);
-    if (hh == 0) ml[wave * 32 + r] = float2{w.m, row_sum};
+    if (hh == 0) ml[wave * 32 + r] = float2{row_sum == 0.f ? -INFINITY : w.ref, row_sum};
 #pragma unroll
     for (int half = 0; half < D / 64; half++) {
         if (half) __syncthreads();

@@ -82,3 +82,21 @@ def test_rows_that_see_only_a_score_of_minus_infinity(dtype, T, Ps, kw):
     assert (out[0, :3] == 0).all() and torch.isneginf(lse[0, :, :3]).all()
     assert torch.isnan(out[0, 3:]).all() and torch.isnan(lse[0, :, 3:]).all()
     assert torch.isfinite(out[1:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,Hq,d", [(1, 8, 128), (5, 8, 64), (13, 8, 128), (40, 8, 128), (40, 8, 64)])
+@pytest.mark.parametrize("P,low,tree_low", [(20, -200, -200), (300, -90, -90), (700, -200, -200), (700, -5000, -4990), (700, -150, -700), (40, -400, 30)])
+def test_rows_whose_scores_are_all_far_below_zero(dtype, T, Hq, d, P, low, tree_low):
+    """A softmax does not change when all scores fall by the same amount: those of the prefix about `low`, the tree's about `tree_low`;
+    whole and in splits, where wavefronts and splits without keys stand beside those with."""
+    c = Case(8, 2, T, Hq, 2, d, dtype, [P, P // 2], 16)
+    K = c.rng.standard_normal((P, 2, d))
+    K[:, :, d - 32:] = 0
+    K[:, :, d - 1] = low / 4
+    c.q[..., d - 32:], c.q[..., d - 1] = 0, 4 * math.sqrt(d)
+    c.kt[..., d - 32:], c.kt[..., d - 1] = 0, tree_low / 4
+    for b in range(2):
+        hold(c, 0, b, 0, K[:c.Ps[b]])
+    for kv_split in (4096, 128):
+        c.check(*c.run(kv_split=kv_split))
