@@ -531,6 +531,7 @@ ETV_API int32_t etv_dequantize_kv_q4(const etv_q4_desc *h_desc, const uint8_t *k
  * plain decoding.  q, out, kt, vt, bitmask, n_nodes, lse and the result are as there, h_desc->dtype being the type of
  * q, kt, vt and out; the tree rows are never quantised and always in a buffer of their own.  A row that sees no key gives
  * zeros and lse = -inf, one that sees nothing but scores of -inf NaN.  A key in a block outside [0, num_blocks) counts as NaN.
+ * A prefix key whose product with q leaves the range of fp32 scores an infinity of either sign or NaN (q is multiplied in parts).
  * h_desc: block_size 0 or a multiple of 16, num_blocks used when paged; flags: ETV_ATTN_FLAG_GENERIC or 0; scale 0
  * or of a magnitude within 1e-30 .. 1e30, of either sign.
  * h_desc->kv_split is rounded up to whole rounds of a workgroup (64 to 256 keys).

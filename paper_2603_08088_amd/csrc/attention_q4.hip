@@ -301,11 +301,12 @@ struct Q4Wave {
     }
     // Has the row a weight so far?  A reference's own key weighs 1, so a sum never falls back to zero.
     __device__ __forceinline__ float row_sum() const { return q4_half_sum(sum[0] + sum[1]); }
-    // Scores become relative.  A row without a reference (`none`) takes the tile's largest score, if it sees any.
-    __device__ __forceinline__ void enter(q4_f32x16 (&s)[KB], bool none) {
+    // Scores become relative.  A row without a reference (`none`) takes the tile's largest score, if it sees any.  Returns the latter.
+    __device__ __forceinline__ float enter(q4_f32x16 (&s)[KB], bool none) {
         const float top = largest(s);
         refer_to(!none ? ref : fabsf(top) < INFINITY ? top : 0.f);
         if (G::RELATIVE) shift(s, ref);
+        return top;
     }
 
     // P^T: pair x of a tile's 8 KB pairs of relative scores to weights, and their part of the row's sum.
@@ -419,6 +420,31 @@ __device__ __forceinline__ void q4_finish(const Q4Attn &p, int b, int t, int hea
         *reinterpret_cast<uint4 *>(dst) = inv == 0.f ? uint4{0, 0, 0, 0} : v;
     }
     if (p.lse && piece == 0) p.lse[((size_t)b * p.Hq + head) * p.T_max + t] = inv == 0.f ? -INFINITY : inv != inv ? NAN : (ref + __builtin_amdgcn_logf(sum)) * kQ4Ln2;
+}
+
+// The largest finite score (log2) that a row has among the keys of the wavefront's first tile to have one, from position `from` on;
+// -inf: none.  Asked only by rows whose first tile scores -inf throughout (products beyond the fp32 range): their reference.
+// Vector arithmetic, a lane per row and every other key.
+template <typename T, int D>
+__device__ __forceinline__ float q4_some_score(const Q4Attn &p, const T *q, bool wanted, int b, int kvh, int from, int keys, int step, int to, int hh) {
+    float best = -INFINITY;
+    for (int base = from; base < to && __any(wanted && best == -INFINITY); base += step) {  // uniform
+        float top = -INFINITY;
+        for (int j = base + hh; j < min(base + keys, to); j += 2) {
+            bool known;
+            const uint64_t row = q4_prefix_row(p, b, kvh, j, known);
+            float s = known ? 0.f : NAN;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 2) {
+                const q4_f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)p.codes[0][row * (D / 2) + c / 2], q4_scale(p.scales[0][row * (D / 32) + c / 32]), 0);
+                s = fmaf(q4_elem(q, c) * p.scale_log2, x[0], fmaf(q4_elem(q, c + 1) * p.scale_log2, x[1], s));
+            }
+            if (fabsf(s) < INFINITY) top = fmaxf(top, s);
+        }
+        top = q4_half_max(top);
+        if (wanted && best == -INFINITY) best = top;
+    }
+    return best;
 }
 
 // Which keys of which sequence a prefix slot stands for.  All splits of a call are of one size c (in rounds of `span` keys), about the
@@ -722,7 +748,11 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
             if (last + KEYS > k1) w.mask(sa, last < k1 ? (1ull << (k1 - last)) - 1 : 0);
         };
         if (rounds == 1) cut();
-        w.enter(sa, true);
+        const float top = w.enter(sa, true);
+        if (rounds > 1 && __builtin_expect(__any(top == -INFINITY), 0)) {
+            const float some = q4_some_score<T, D>(p, static_cast<const T *>(p.q) + q_row, top == -INFINITY, b, kvh, mine + span, KEYS, span, k1, hh);
+            if (some != -INFINITY) w.refer_to(some);
+        }
         w.staged();
         const auto step = [&](auto buffer, int t, q4_f32x16 (&s)[KB], q4_f32x16 (&s_next)[KB]) {
             constexpr int NOW = decltype(buffer)::value, FLY = 3;  // fragments of V on their way from LDS

@@ -100,3 +100,22 @@ def test_rows_whose_scores_are_all_far_below_zero(dtype, T, Hq, d, P, low, tree_
         hold(c, 0, b, 0, K[:c.Ps[b]])
     for kv_split in (4096, 128):
         c.check(*c.run(kv_split=kv_split))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,Hq,d", [(5, 8, 128), (13, 8, 64), (40, 8, 128), (40, 8, 64)])
+@pytest.mark.parametrize("none,P,kv_split", [(300, 700, 4096), (300, 700, 512), (300, 300, 4096), (257, 1200, 4096)])
+def test_tiles_whose_scores_overflow_to_minus_infinity_weigh_nothing(dtype, T, Hq, d, none, P, kv_split):
+    """The first keys score -inf for every row, the others 2^-384: such keys weigh nothing, wherever a wavefront meets them.
+    The scale is a power of two in base 2 and q's large value one too, so that its lower digits are zero."""
+    c, scale = Case(4, 1, T, Hq, 2, d, dtype, [P], 16), scale_for(0.125)
+    K = c.rng.standard_normal((P, 2, d))
+    K[:, :, :32], K[:, :, 40], c.kt[..., :32], c.kt[..., 40] = 0, -384, 0, -384
+    hold(c, 0, 0, 0, K)
+    small = copy.deepcopy(c)                         # for the tolerance: without the keys that weigh nothing
+    K[:none, :, 3] = -1e38
+    hold(c, 0, 0, 0, K)
+    for x in (c, small):
+        x.q[..., :32], x.q[..., 3], x.q[..., 40] = 0, 2.0 ** 126, 8
+    small.plain = c.plain
+    small.check(*c.run(scale=scale, kv_split=kv_split), scale=scale)
