@@ -458,10 +458,11 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
     const bool in = lane < p.B;
     const int P = in ? clampi(p.prefix_len[in ? lane : 0], 0, p.P_max) : 0;
     const int rounds = P > 0 && p.n_nodes[in ? lane : 0] > 0 ? (P + p.span - 1) / p.span : 0, slots = p.B * p.nsplit;
-    const int total = __builtin_amdgcn_readlane(wave_scan_sum(rounds), 63);
-    int c = p.chunk > 0 ? p.chunk / p.span : max(1, (total + slots - 1) / slots);
+    // 64 prefixes of almost 2^31 positions are almost 2^31 rounds: the sums of rounds are unsigned
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane(wave_scan_sum(rounds), 63);
+    int c = p.chunk > 0 ? p.chunk / p.span : max(1, (int)((total + slots - 1) / (uint32_t)slots));
     int count = (rounds + c - 1) / c, upto = wave_scan_sum(count);
-    const int enough = p.chunk > 0 ? c : (total + slots - p.B - 1) / max(1, slots - p.B);
+    const int enough = p.chunk > 0 ? c : (int)((total + (uint32_t)(slots - p.B) - 1) / (uint32_t)max(1, slots - p.B));
     while (c < enough && __builtin_amdgcn_readlane(upto, 63) > slots) {
         c = min(c + 1 + c / 16, enough);
         count = (rounds + c - 1) / c;
@@ -474,7 +475,7 @@ __device__ __forceinline__ Q4Share q4_share(const Q4Attn &p, int slot, int lane)
     r.count = __builtin_amdgcn_readlane(count, b);
     r.first = __builtin_amdgcn_readlane(upto, b) - r.count;
     r.k0 = (slot - r.first) * c * p.span;
-    r.k1 = min(r.k0 + c * p.span, __builtin_amdgcn_readlane(P, b));
+    r.k1 = r.k0 + min(c * p.span, __builtin_amdgcn_readlane(P, b) - r.k0);  // k0 + c * span may pass 2^31
     return r;
 }
 
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
         const int P = clampi(p.prefix_len[b], 0, p.P_max);
         k0 = (int)min((int64_t)P, (int64_t)rem * p.chunk);
         k1 = (int)min((int64_t)P, (int64_t)k0 + p.chunk);
-        if (rem == 0 && kvh == 0 && group == 0 && tid == 0) p.split_tab[b] = int2{slot, (P + p.chunk - 1) / p.chunk};
+        if (rem == 0 && kvh == 0 && group == 0 && tid == 0) p.split_tab[b] = int2{slot, (int)(((uint32_t)P + (uint32_t)p.chunk - 1) / (uint32_t)p.chunk)};
         if (k0 >= k1) return;
     }
     b = __builtin_amdgcn_readfirstlane(b);
@@ -1093,7 +1094,7 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
     pl.nsplit = 1;
     if (h->kv_split > 0) {
         pl.chunk = (int)std::min<int64_t>((h->kv_split + (int64_t)pl.span - 1) / pl.span, rounds) * pl.span;
-        pl.nsplit = std::max(1, (h->P_max + pl.chunk - 1) / pl.chunk);
+        pl.nsplit = std::max(1, (int)(((int64_t)h->P_max + pl.chunk - 1) / pl.chunk));
     } else {
         // Eight wavefronts a compute unit.  In units of a round: starting and ending a workgroup 3, the second launch 3 and a little more
         // for every split whose rows it reads.

@@ -119,3 +119,25 @@ def test_tiles_whose_scores_overflow_to_minus_infinity_weigh_nothing(dtype, T, H
         x.q[..., :32], x.q[..., 3], x.q[..., 40] = 0, 2.0 ** 126, 8
     small.plain = c.plain
     small.check(*c.run(scale=scale, kv_split=kv_split), scale=scale)
+
+
+@pytest.mark.parametrize("B,kv_split", [(1, 0), (1, 1 << 24), (65, 0)])
+def test_prefixes_up_to_the_longest(B, kv_split):
+    """2^31 - 4097 positions, all but the last 2^20 - 4097 in one block, which weighs nothing: what is out comes from those."""
+    d, size, width = 64, 1 << 20, 2048
+    P = 2 ** 31 - 4097
+    kc, ks, vc, vs = (torch.zeros((2, 1, size, w), dtype=torch.uint8, device="cuda") for w in (d // 2, d // 32, d // 2, d // 32))
+    kc[0], ks[:], vs[:] = 0xff, 127 + 3, 127                         # K: -48 throughout; V: 0
+    vc[1] = 0x22                                                     # V: 1
+    table = torch.zeros((B, width), dtype=torch.int32, device="cuda")
+    table[:, -1] = 1
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    lens[B // 2] = P
+    q, kt = torch.ones((B, 1, 1, d), dtype=torch.bfloat16, device="cuda"), torch.full((B, 1, 1, d), -48.0, dtype=torch.bfloat16, device="cuda")
+    mask, n = torch.ones((B, 1, 1), dtype=torch.int64, device="cuda"), torch.ones(B, dtype=torch.int32, device="cuda")
+    out, lse = api.tree_verify_attention_q4(q, api.KVCacheQ4(kc, ks, vc, vs), lens, kt, torch.full_like(kt, 3), mask, n, P_max=P, block_table=table,
+                                            kv_split=kv_split)
+    # sums and outputs of equal weights are whole numbers below 2^24 a lane
+    assert torch.equal(out[B // 2], torch.ones_like(out[0])) and abs(lse[B // 2].item() - math.log(2 ** 20 - 4097)) <= 2.0 ** -20 * 14
+    others = torch.arange(B, device="cuda") != B // 2
+    assert (out[others] == 3).all() and (lse[others] + 48 * 8).abs().le(2.0 ** -10).all()

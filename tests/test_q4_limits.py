@@ -25,6 +25,12 @@ def test_scales_of_one_layer_are_aligned_to_their_rows():
         assert attend(desc, ks=A + unit // 2) == attend(desc, vs=A + unit // 2) == attend(desc, ks=A + unit + 1) == -1
 
 
+def test_the_longest_prefixes_are_split():
+    """Splits are counted beyond 31 bits: 128 of 2^24 keys."""
+    d = attn_desc(T_max=1, Hq=1, Hkv=1, d=64, block_size=1 << 20, max_blocks=2048, num_blocks=2, P_max=2 ** 31 - 4097, kv_split=1 << 24)
+    assert api.tree_verify_attention_q4_workspace_bytes(d) >= 129 * 32 * 64 * 4
+
+
 def six_bits(x):
     """To the nearest e2m3 (ties to the even mantissa), beyond 7.5 to 7.5."""
     a = np.abs(x)
