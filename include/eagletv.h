@@ -534,7 +534,8 @@ ETV_API int32_t etv_dequantize_kv_q4(const etv_q4_desc *h_desc, const uint8_t *k
  * A prefix key whose product with q leaves the range of fp32 scores an infinity of either sign or NaN (q is multiplied in parts).
  * h_desc: block_size 0 or a multiple of 16, num_blocks used when paged; flags: ETV_ATTN_FLAG_GENERIC or 0; scale 0
  * or of a magnitude within 1e-30 .. 1e30, of either sign.
- * h_desc->kv_split is rounded up to whole rounds of a workgroup (64 to 256 keys).
+ * h_desc->kv_split is rounded up to whole rounds of a workgroup (64 to 256 keys); one that gives 2^31 workgroups or more is
+ * ETV_ERR_UNSUPPORTED (and its workspace 0).
  * workspace: etv_tree_verify_attention_q4_workspace_bytes(h_desc) bytes, 256-byte aligned.
  * Supported: dtype F32 or BF16, d in {64, 128}, Hq % Hkv == 0, 1 <= T_max <= ETV_ATTN_MAX_TREE. */
 ETV_API size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h_desc);

@@ -1075,8 +1075,9 @@ static int32_t q4_check_desc(const etv_attn_desc *h) {
 }
 
 struct Q4Plan {
-    int rw, row_groups, chunk, nsplit, slots, span;
-    int64_t units;
+    int rw, row_groups, chunk, nsplit, span;
+    int64_t slots, units;
+    bool fits() const { return units * row_groups <= INT32_MAX - 65536; }  // in a grid, and every count of the kernel in 31 bits
     int rows_padded() const { return row_groups * 32 * rw; }
     size_t rows() const { return (size_t)units * rows_padded(); }
     size_t workspace(const etv_attn_desc *h) const { return nsplit == 1 ? 256 : rows() * ((size_t)h->d * 4 + 8) + (size_t)h->B * 8 + 256; }
@@ -1109,8 +1110,8 @@ static Q4Plan q4_plan(const etv_attn_desc *h) {
         }
         pl.chunk = B <= 64 ? 0 : per * pl.span;
     }
-    pl.slots = B * (pl.nsplit == 1 ? 1 : pl.nsplit + 1);
-    pl.units = (int64_t)pl.slots * h->Hkv;
+    pl.slots = (int64_t)B * (pl.nsplit == 1 ? 1 : pl.nsplit + 1);
+    pl.units = pl.slots * h->Hkv;
     return pl;
 }
 
@@ -1146,7 +1147,9 @@ static int32_t run_q4(const Q4Plan &pl, const Q4Attn &p, hipStream_t st) {
 }  // namespace etv
 
 extern "C" size_t etv_tree_verify_attention_q4_workspace_bytes(const etv_attn_desc *h) {
-    return etv::q4_check_desc(h) == ETV_OK ? etv::q4_plan(h).workspace(h) : 0;
+    if (etv::q4_check_desc(h) != ETV_OK) return 0;
+    const etv::Q4Plan pl = etv::q4_plan(h);
+    return pl.fits() ? pl.workspace(h) : (h->flags & ETV_ATTN_FLAG_GENERIC) != 0 ? 256 : 0;
 }
 
 extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const void *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -1166,7 +1169,7 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
     if (h->B == 0) return ETV_OK;
     const etv::Q4Plan pl = etv::q4_plan(h);
     const bool generic = (h->flags & ETV_ATTN_FLAG_GENERIC) != 0;
-    if (!generic && pl.units * pl.row_groups > INT32_MAX - 65536) return ETV_ERR_UNSUPPORTED;
+    if (!generic && !pl.fits()) return ETV_ERR_UNSUPPORTED;
     if (!generic && pl.nsplit > 1 && (!workspace || workspace_bytes < pl.workspace(h))) return ETV_ERR_WORKSPACE_TOO_SMALL;
     etv::Q4Attn p{};
     p.q = q; p.kt = kt; p.vt = vt;
@@ -1187,7 +1190,7 @@ extern "C" int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h, const vo
         else hipLaunchKernelGGL((etv::attn_q4_generic_kernel<uint16_t, 128>), grid, dim3(64), 0, st, p);
         return etv::check_launch();
     }
-    p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = pl.slots; p.row_groups = pl.row_groups; p.rows_padded = pl.rows_padded();
+    p.chunk = pl.chunk; p.nsplit = pl.nsplit; p.slots = (int)pl.slots; p.row_groups = pl.row_groups; p.rows_padded = pl.rows_padded();
     p.units = (int)pl.units; p.span = pl.span;
     p.inv_g = etv::fast_div_inv(p.G); p.inv_hkv = etv::fast_div_inv(p.Hkv); p.inv_groups = etv::fast_div_inv(p.row_groups);
     p.inv_nsplit = etv::fast_div_inv(p.nsplit);

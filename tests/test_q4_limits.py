@@ -25,10 +25,26 @@ def test_scales_of_one_layer_are_aligned_to_their_rows():
         assert attend(desc, ks=A + unit // 2) == attend(desc, vs=A + unit // 2) == attend(desc, ks=A + unit + 1) == -1
 
 
+def test_a_split_call_needs_its_workspace():
+    d = attn_desc(P_max=8192, max_blocks=512, kv_split=64)
+    need = api.tree_verify_attention_q4_workspace_bytes(d)
+    assert need > 256
+    assert attend(d, size=need - 1) == attend(d, ws=None) == -3
+
+
 def test_the_longest_prefixes_are_split():
     """Splits are counted beyond 31 bits: 128 of 2^24 keys."""
     d = attn_desc(T_max=1, Hq=1, Hkv=1, d=64, block_size=1 << 20, max_blocks=2048, num_blocks=2, P_max=2 ** 31 - 4097, kv_split=1 << 24)
     assert api.tree_verify_attention_q4_workspace_bytes(d) >= 129 * 32 * 64 * 4
+
+
+def test_more_splits_than_can_be_counted_are_refused():
+    """4097 sequences of 1048320 splits of 64 keys: their partials are 2^32 + 3841.  No launch, and no workspace that would do."""
+    d = attn_desc(B=4097, T_max=1, Hq=1, Hkv=1, d=64, dtype=api.F32, block_size=1 << 20, max_blocks=128, num_blocks=128, P_max=1048320 * 128, kv_split=128)
+    assert api.tree_verify_attention_q4_workspace_bytes(d) == 0
+    assert attend(d) == -2
+    d.kv_split = 1 << 16
+    assert api.tree_verify_attention_q4_workspace_bytes(d) > 4097 * 2047 * 32 * 64 * 4
 
 
 def six_bits(x):
