@@ -141,3 +141,49 @@ def test_prefixes_up_to_the_longest(B, kv_split):
     assert torch.equal(out[B // 2], torch.ones_like(out[0])) and abs(lse[B // 2].item() - math.log(2 ** 20 - 4097)) <= 2.0 ** -20 * 14
     others = torch.arange(B, device="cuda") != B // 2
     assert (out[others] == 3).all() and (lse[others] + 48 * 8).abs().le(2.0 ** -10).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [3, 10, 40])
+@pytest.mark.parametrize("rising", [False, True])
+def test_references_move_in_the_middle_of_long_prefixes(dtype, d, T, rising):
+    """Scores far apart, met at random or each tile far above the one before: rows get a new reference tile after tile."""
+    c = Case(5, 1, T, 8, 2, d, dtype, [3000], 16, q_scale=12.0)
+    if rising:
+        K = c.rng.standard_normal((3000, 2, d))
+        K[:, :, 7] = np.arange(3000)[:, None] / 8
+        hold(c, 0, 0, 0, K)
+        c.q[..., 7] = 16 * d / 64
+    for kv_split in (4096, 1024):
+        c.check(*c.run(kv_split=kv_split))
+
+
+@pytest.mark.parametrize("kv_split", [4096, 256])
+@pytest.mark.parametrize("block", [0, 48])
+@pytest.mark.parametrize("T", [5, 13, 33])            # rows of one, two and four wavefronts
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_form_of_the_kernel_reads_a_prefix(d, dtype, T, block, kv_split):
+    """Both head sizes and types, rows of one, two and four wavefronts, either layout, split and whole; prefixes end inside a tile."""
+    c = Case(6, 3, T, 8, 2, d, dtype, [523, 70, 257], block, [T, T - 1, T])
+    c.check(*c.run(kv_split=kv_split))
+
+
+@pytest.mark.parametrize("T,Hq,d", [(6, 8, 128), (14, 8, 64), (40, 8, 128), (40, 4, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_finite_rows_beside_values_that_are_not(dtype, T, Hq, d):
+    """Infinities and NaN in tree K and V that some rows see: the other rows, and the other columns, keep their precision."""
+    c = Case(7, 1, T, Hq, 2, d, dtype, [37], 16)
+    c.kt[0, 1, 0, 9], c.kt[0, 3, 1, d - 1] = float("nan"), float("inf")
+    c.vt[0, 2, 0, 33], c.vt[0, 2, 1, 3], c.vt[0, 4, 1, 5] = float("inf"), float("nan"), float("-inf")
+    c.vis[0] = c.rng.random((T, T)) < 0.3
+    out, _ = c.run()
+    want, _, spread = c.plain()
+    got, fine = out.double().cpu().numpy(), np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isposinf(got), np.isposinf(want)) and fine.any() and not fine.all()
+    # the bound of Case.check
+    ds, half = c.score_slack(), torch.finfo(c.dtype).eps / 2
+    weight = math.expm1(2 * ds) + (2 * half if dtype == "bf16" else 8 * 2.0 ** -24) + (37 + T + 64) * 2.0 ** -24
+    off = np.abs(got[fine] - want[fine]) - weight * (spread[fine] + np.abs(want[fine])) - half * np.abs(want[fine]) * 1.01
+    assert off.max() <= 1e-30, off.max()
