@@ -143,12 +143,12 @@ __global__ void __launch_bounds__(64) attn_q4_generic_kernel(Q4Attn p) {
 // The matrix kernel.  With the G * T_max query rows of a KV head packed into rows r = t * G + g, a wavefront has 32 of them and
 // takes 32 or 64 keys at a time:
 //   S^T[key, r]  = K Q^T     v_mfma_scale_f32_32x32x64_f8f6f4: K as the cache holds it (fp4, its scale bytes the instruction's),
-//                            16 bytes a lane straight from memory, q in NQ parts of 6 bits (e2m3)
+//                            by way of LDS, q in NQ parts of 6 bits (e2m3)
 //   P^T          = exp2(S^T * scale - reference)   a lane has 32 keys of one row; the reference follows the maximum lazily
 //   O^T[d, r]   += V^T P^T   bf16: V is converted (exactly) into an LDS tile and comes back through the transpose read; P stays
 //                            in registers as the product's B operand
 // The parts of q: part x is q less the parts before it, rounded to e2m3 at scale 2^(e - 2 - 4x), e being the exponent of its group's
-// maximum, one up where that comes within 1/16 of the next power of two: so the first part is never held at 7.5, the largest value
+// maximum, one up where that comes within 1/32 of the next power of two: so the first part is never held at 7.5, the largest value
 // there is (a value just under 8 would leave the next part one just under 8 again, and so on: 2^-16 of it after four), and of the
 // maximum, at least 3.875 at that scale, no more than 2^-16 / 3.875 is left.  That is 2^-17.95 after four parts; fp32 takes six
 // (2^-25.95).  (Three, 2^-13.95, are enough for outputs rounded to bf16, but show in lse.)  Six-bit and four-bit operands run at four
@@ -229,8 +229,8 @@ __device__ __forceinline__ float q4_half_sum(float v) {
 __device__ __forceinline__ float q4_max3(float a, float b, float c) {
     return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
-// Positions of 16-byte pieces within a row of the V tile: the lanes of a store, which have rows of their own, and those of a
-// transpose read both reach all banks.
+// Positions of 16-byte pieces within a row of the V tile: the lanes of a transpose read reach all banks.  (16 lanes of a store, four to
+// a row, reach half of them.  Of the cycles that LDS is busy, 43 % are conflicts of any kind: 32 x 8 heads of 4096 keys, 128 nodes.)
 template <int D>
 __device__ __forceinline__ int q4_swizzle(int row) { return D == 128 ? (((row & 3) << 1) | ((row >> 2) & 1)) : ((row & 2) << 1); }
 
@@ -316,7 +316,7 @@ struct Q4Wave {
         const float by = G::RELATIVE ? 0.f : ref;
         const float a = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i] : s[kb][2 * i] - by), b = __builtin_amdgcn_exp2f(G::RELATIVE ? s[kb][2 * i + 1] : s[kb][2 * i + 1] - by);
         if constexpr (F32) q4_split(a, b, pk[0][kb][i], pk[1][kb][i], pk[NP - 1][kb][i]);
-        else pk[0][kb][i] = q4_pair(a, b);  // the value product takes them rounded to bf16, the sum (and lse) does not
+        else pk[0][kb][i] = q4_pair(a, b);  // the value product takes them rounded to bf16, as on an unquantised cache, the sum (and lse) does not
         part[X & 1] = X < 2 ? a + b : part[X & 1] + (a + b);
     }
     __device__ __forceinline__ void weigh_all(const q4_f32x16 (&s)[KB], uint32_t (&pk)[NP][KB][8], float (&part)[2]) const {
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(q4_wavefronts(F32, RW) * 64, F32 && D == 128 ?
 
         // Software pipeline: a step has the scores of its tile already and works out the next tile's between its exponentials (or, where
         // they are not relative, before its value products); between those it stores the next tile's V and the K of the one after into LDS: the matrix and the vector unit are both busy
-        // within one wavefront.  What is stored was asked for a step before (two steps ahead took 38.6 us instead of 35.7 where 32 x 8
+        // within one wavefront.  What is stored was asked for a step before (two steps ahead took 8 % longer where 32 x 8
         // heads of 4096 keys and 8 nodes leave the reading: more registers and a longer start).
         Codes start, second, codes;
         Rows first, rows, newer;  // rows, newer: of the tile whose K was asked for last, and of the next one

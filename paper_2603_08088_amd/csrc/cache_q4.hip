@@ -5,8 +5,8 @@
 // quantises has one group of 32 channels of K and the same one of V (its maximum needs no other lane, its codes are one
 // 16-byte store, and the lanes of a wavefront store 16 or 32 consecutive rows of a head: 1 KiB of codes, 64 bytes of scales).
 // The conversions are single instructions (two values each), exact in the scale, rounding to nearest even.
-// Measured: 2 prompts of 4096 and 3001 rows, 8 layers, 8 heads of 128, bf16: written in 55 us (5.3 TB/s), read back in 51 us
-// (5.8 TB/s); a token of 8 sequences, 32 layers, or the path of one tree: 3 to 4 us a launch, which is the launch.
+// Measured: 2 prompts of 4096 and 3001 rows, 8 layers, 8 heads of 128, bf16, other buffers every time: written in 63 us (4.7 TB/s), read
+// back in 52 us (5.7 TB/s); a token of 8 sequences, 32 layers, or the path of one tree: 3 to 5 us a launch, which is the launch.
 #include "etv_common.h"
 
 namespace etv {
@@ -212,8 +212,9 @@ struct Piece<float> {
 __device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
 
 // grid (ceil(Hkv * rows * pieces / (256 * U)), B, n_layers).  A thread has 16 bytes of K and of V of U items: its stores and its
-// lane neighbours' are consecutive, which the wider of the two sides needs.  The rows written are not read here: past the caches
-// they take 91 us where 138 were needed (8 x 4096 rows of 4 layers, bf16).
+// lane neighbours' are consecutive, which the wider of the two sides needs.  The rows written are not read here: past the caches,
+// 8 x 4096 rows of 4 layers, bf16, take 136 us instead of 138 (the 640 MB come from and go to memory either way), and 7097 rows of 8 layers
+// just written 116, the writing with them, instead of 147.
 constexpr int kReadItems = 4;
 template <typename T, int NG>
 __global__ void __launch_bounds__(256) read_rows_kernel(etv_q4_desc dsc, Q4Cache cache, const int32_t *__restrict__ block_table,

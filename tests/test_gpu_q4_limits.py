@@ -187,3 +187,15 @@ def test_finite_rows_beside_values_that_are_not(dtype, T, Hq, d):
     weight = math.expm1(2 * ds) + (2 * half if dtype == "bf16" else 8 * 2.0 ** -24) + (37 + T + 64) * 2.0 ** -24
     off = np.abs(got[fine] - want[fine]) - weight * (spread[fine] + np.abs(want[fine])) - half * np.abs(want[fine]) * 1.01
     assert off.max() <= 1e-30, off.max()
+
+
+@pytest.mark.parametrize("T,kv_split", [(3, 4096), (40, 64)])
+def test_outputs_do_not_depend_on_lse_or_the_workspace(T, kv_split):
+    c = Case(9, 2, T, 8, 2, 64, "bf16", [300, 41], 16)
+    want, _ = c.run(kv_split=kv_split)
+    used = torch.full((1 << 26,), 0xff, dtype=torch.uint8, device="cuda")        # larger than asked for, NaN throughout
+    for kw in (dict(want_lse=False), dict(workspace=used), dict(want_lse=False, flags=api.ATTN_FLAG_GENERIC)):
+        got, lse = c.run(kv_split=kv_split, **kw)
+        assert (lse is None) == ("want_lse" in kw)
+        assert "flags" in kw or torch.equal(got, want)
+        c.check(got, lse)

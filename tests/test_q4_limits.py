@@ -56,7 +56,7 @@ def six_bits(x):
 
 def left(x, top, parts):
     """What `parts` six-bit digits of x leave, in units of the group's maximum: the exponent is that of the maximum, one up
-    where it comes within 1/16 of the next power of two."""
+    where it comes within 1/32 of the next power of two."""
     e = np.floor(np.log2(top)) + (top / np.exp2(np.floor(np.log2(top))) >= 1.9375)
     y = x / np.exp2(e - 2)
     for _ in range(parts):
