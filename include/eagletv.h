@@ -546,6 +546,146 @@ ETV_API int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h_desc, const 
                                      const uint64_t *bitmask, const int32_t *n_nodes, void *out, float *lse, void *workspace,
                                      size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Beam decoding over a paged cache -- the candidates of Section 2.3's draft trees, or of a beam search, come from the best
+ * continuations of every frontier node or beam; each of them goes on with the cache of its parent (Section 3.1, branches that share
+ * the committed prefix).  One step is a run of the calls below around the attention: etv_beam_select, etv_reorder_beams,
+ * etv_resize_block_tables, etv_rotary_write_kv.
+ *
+ * The free blocks of a pool are a ring: free_blocks int32 [num_blocks] and free_state int32 [2] = (first, count), all on the
+ * device; the free ones are free_blocks[(first + i) % num_blocks], 0 <= i < count.  A call takes blocks from the front and puts
+ * blocks behind the end; what it puts there it does not take itself.  The state is read from free_state and written to
+ * free_state_out (which must not alias it).  A state outside 0 <= first < num_blocks, 0 <= count <= num_blocks counts as an empty
+ * ring that takes nothing back, and stays as it is.
+ * ------------------------------------------------------------------------- */
+#define ETV_MAX_BEAMS 64 /* largest number of beams of one request, before and after a step */
+
+/* resize_block_tables -- the block tables of sequences whose lengths change from len to new_len, and the slots of the rows that
+ * are new.  With old = ceil(len / block_size) and want = ceil(new_len / block_size):
+ *   want > old: entries old .. want-1 get the ring's next blocks, sequences in order, ascending within a sequence;
+ *   want < old: entries want .. old-1 go behind the ring's end in the same order.  The table keeps them, as stale entries.
+ *   slot_map[b, i] = physical slot (block * block_size + offset) of position len[b] + i, -1 for i >= new_len[b] - len[b].
+ *   len_out[b] = new_len[b]; for a refused sequence len[b], its table row is left as it was and its slots are -1.
+ * Every entry of `block_table` belongs to one sequence alone (beams that share blocks give them back by etv_reorder_beams).
+ *   Status bits: ETV_COMMIT_BAD_LEN (a negative length, or more than S new rows), ETV_COMMIT_CAPACITY (a length beyond the table row),
+ *   ETV_BRANCH_NO_BLOCKS (the blocks of this and all sequences before it are more than the ring holds), ETV_COMMIT_BAD_BLOCK (the
+ *   entry new rows go on in, or one to give back, is outside the pool), ETV_BRANCH_BAD_FREE (a ring entry to take is outside the pool,
+ *   or the ring has no room for the blocks given back by this and the sequences before it).
+ *   The accounting of taken blocks follows the lengths alone: a sequence refused for what a table or the ring holds keeps its
+ *   share of the ring, unused.
+ *
+ *  len, new_len  in  int32 [B];  block_table in/out int32 [B, max_blocks];  free_blocks in/out, free_state in, free_state_out out
+ *  len_out int32 [B] (must alias neither length);  slot_map int32 [B, S]  nullable;  status int32 [B]
+ * Requires B * S and num_blocks * block_size below 2^31. */
+typedef struct etv_pages_desc {
+    int32_t B;
+    int32_t S;          /* row length of slot_map, and the most rows a sequence may grow by; at least 1 */
+    int32_t block_size; /* any positive number */
+    int32_t max_blocks;
+    int32_t num_blocks;
+    int32_t reserved;
+} etv_pages_desc;
+
+ETV_API int32_t etv_resize_block_tables(const etv_pages_desc *h_desc, const int32_t *len, const int32_t *new_len, int32_t *block_table,
+                                int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out, int32_t *len_out,
+                                int32_t *slot_map, int32_t *status, void *stream);
+
+/* rotary_write_kv -- rotary position encoding of q and k by positions on one or several axes (time, height, width), and the write
+ * of k and v into the cache, in one pass.  Channel pair i (i < rot_dim / 2) of every head turns with axis a = axis_of[i]:
+ *   angle = positions[a, b, t] * inv_freq[i] (the product, its sine and cosine good to fp32 at any 32-bit position)
+ *   (x, y) -> scale * (x cos - y sin, y cos + x sin)
+ * where (x, y) are channels (i, i + rot_dim/2), or (2i, 2i+1) with ETV_ROTARY_INTERLEAVED; channels from rot_dim on are copied.
+ * ETV_ROTARY_INVERSE turns by -angle: the gradient of the call, and the way back to unencoded rows.
+ * Rows t >= n_rows[b] are padding: nothing is read or written for them.
+ * A row of k and v goes to slot slot_map[b, t] of the cache (as etv_resize_block_tables writes them; contiguous: b * P_cap + p), unless
+ * that is outside [0, cache_rows).  Two rows of a call must not have one slot.
+ *
+ *  q [B, T, Hq, d], k, v [B, T, Hkv, d] in, q_out, k_out, v_out out: heads and channels are contiguous, the strides of sequences and
+ *            tokens are h_desc's, in elements (multiples of 16 bytes; pointers 16-byte aligned).  q and q_out NULL with Hq == 0; k, v
+ *            NULL with Hkv == 0, v also alone; k_out, v_out nullable.  An output may be its input (same pointer and strides).
+ *  positions int32 [n_axes, B, T];  inv_freq float [rot_dim / 2];  n_rows int32 [B]  nullable (=> T)
+ *  slot_map  int32 [B, T], k_cache, v_cache one layer in the layouts of the attention; all three or none
+ * Supported: dtype F32 or BF16 (fp32 arithmetic, rounded once), d and rot_dim multiples of 16, 16 <= rot_dim <= d <= 256. */
+#define ETV_ROTARY_INTERLEAVED 1
+#define ETV_ROTARY_INVERSE 2
+
+typedef struct etv_rotary_desc {
+    int32_t B, T, Hq, Hkv, d, dtype;
+    int32_t rot_dim, n_axes, flags;
+    int32_t block_size;     /* the cache's: 0 contiguous, > 0 paged */
+    int64_t cache_rows;     /* its slots: num_blocks * block_size or B * P_cap */
+    float scale;            /* 0 => 1 */
+    int32_t reserved;
+    int64_t strides[12];    /* (sequence, token) of q, k, v, q_out, k_out, v_out */
+    uint8_t axis_of[128];   /* axis of each pair, below n_axes */
+} etv_rotary_desc;
+
+ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q, const void *k, const void *v, const int32_t *positions,
+                            const float *inv_freq, const int32_t *n_rows, void *q_out, void *k_out, void *v_out,
+                            const int32_t *slot_map, void *k_cache, void *v_cache, void *stream);
+
+/* beam_select -- the M best continuations of a request over its K beams (or frontier nodes) and the vocabulary:
+ *   total[k, v] = scores[b, k] + logits[b, k, v] - log sum_v' exp(logits[b, k, v'])
+ * the M largest in descending order, ties to the lower k, then the lower v.  A beam with finished[b, k] != 0 offers (k, end_token) at
+ * scores[b, k] and nothing else.  Beams k >= n_beams[b], scores of -inf and logits of -inf offer nothing.  Where fewer than M are
+ * offered the rest is parent = token = -1 with a score of -inf.  Totals are formed and compared in 64 bits (the sum over the
+ * vocabulary is good to about 1e-8), and rounded once.
+ *   finished_out[b, m] = 1 if the parent was finished or the token is end_token, else 0
+ *   Status bits: ETV_BEAM_BAD_LOGITS (a live beam's logits hold NaN or +inf: that beam offers nothing), ETV_BEAM_BAD_SCORE (a beam's
+ *   score is NaN or +inf: the same), ETV_BEAM_SHORT (fewer than M are offered).
+ *
+ *  logits in [B, K, V], rows contiguous, strides in elements from h_desc;  scores in float [B, K]
+ *  n_beams in int32 [B] nullable (=> K);  finished in uint8 [B, K] nullable
+ *  out_scores float [B, M]; parent, token int32 [B, M]; finished_out uint8 [B, M] nullable; status int32 [B]
+ *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.
+ * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V. */
+#define ETV_BEAM_BAD_LOGITS 1
+#define ETV_BEAM_BAD_SCORE 2
+#define ETV_BEAM_SHORT 4
+
+typedef struct etv_beam_desc {
+    int32_t B, K, V, M, dtype;
+    int32_t end_token;      /* -1: none (and then no finished beams) */
+    int64_t batch_stride, row_stride;
+} etv_beam_desc;
+
+ETV_API size_t etv_beam_select_workspace_bytes(const etv_beam_desc *h_desc);
+
+ETV_API int32_t etv_beam_select(const etv_beam_desc *h_desc, const void *logits, const float *scores, const int32_t *n_beams,
+                        const uint8_t *finished, float *out_scores, int32_t *parent, int32_t *token, uint8_t *finished_out,
+                        int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* reorder_beams -- the cache after a step: new beam i of request b goes on from old beam parent[b, i] (-1: there is none).  All beams of
+ * a request have the length len[b], and share blocks only among themselves and at the same place in their tables.
+ *   Blocks wholly inside the length are shared: table_out[b, i, j] = block_table[b, parent[b, i], j].
+ *   The block that is being filled (len[b] % block_size rows) belongs to one beam: of the new beams that come from one such block the first
+ *   keeps it, every other gets the ring's next block -- requests in order, beams in order -- with the rows copied, K and V, in all layers.
+ *   Blocks of old beams that no new beam refers to go behind the ring's end, in the order of request, place in the table, old beam.
+ *   Entries behind the length are -1, and so are rows without a parent.  M != K starts (one beam becomes several) or ends a search.
+ *   Status bits: ETV_COMMIT_BAD_LEN (negative length), ETV_COMMIT_CAPACITY (length beyond the table row), ETV_COMMIT_BAD_NODE (a parent
+ *   outside [-1, K)), ETV_COMMIT_BAD_BLOCK (a needed entry of a parent is outside the pool), ETV_BRANCH_NO_BLOCKS (as above),
+ *   ETV_BRANCH_BAD_FREE (the ring has no room for what this request and those before it give back).  A refused request's rows of table_out
+ *   are -1; its old tables and their blocks stay as they were and nothing is taken or given back for it (with ETV_BRANCH_BAD_FREE its
+ *   share of the ring is lost).  ETV_BRANCH_BAD_FREE is also set where a ring entry to take is outside the pool; then only the
+ *   row of the beam that it was for is -1.
+ *
+ *  k_cache, v_cache in/out; block_table in int32 [B, K, max_blocks]; len in int32 [B]; parent in int32 [B, M]
+ *  table_out out int32 [B, M, max_blocks] (must not alias block_table); status out int32 [B]
+ *  workspace: etv_reorder_beams_workspace_bytes(B, K, M, max_blocks) bytes, 16-byte aligned.
+ * Requires 1 <= K, M <= ETV_MAX_BEAMS, a paged cache (ETV_ERR_UNIMPLEMENTED otherwise) and d * elem_bytes % 16 == 0. */
+ETV_API size_t etv_reorder_beams_workspace_bytes(int32_t B, int32_t K, int32_t M, int32_t max_blocks);
+
+ETV_API int32_t etv_reorder_beams(const etv_cache_desc *h_desc, void *k_cache, void *v_cache, const int32_t *block_table, const int32_t *len,
+                          int32_t K, const int32_t *parent, int32_t M, int32_t *free_blocks, const int32_t *free_state,
+                          int32_t *table_out, int32_t *free_state_out, int32_t *status, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/* reorder_beams_q4 -- the same over a 4-bit cache (rows, dtype and W of the descriptor are not used). */
+ETV_API int32_t etv_reorder_beams_q4(const etv_q4_desc *h_desc, uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales,
+                             const int32_t *block_table, const int32_t *len, int32_t K, const int32_t *parent, int32_t M,
+                             int32_t *free_blocks, const int32_t *free_state, int32_t *table_out, int32_t *free_state_out,
+                             int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

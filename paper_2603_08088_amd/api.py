@@ -33,7 +33,9 @@ ATTN_FLAG_UNIFORM_SPLITS = 32
 ATTN_FLAG_KEY_BLOCKS = 64
 ATTN_FLAG_WIDE = 128
 ATTN_KERNELS = ("generic", "f32", "tile", "wide", "key_blocks")   # by ETV_ATTN_KERNEL_*
-MAX_TREE, ATTN_MAX_TREE = 256, 256
+BEAM_BAD_LOGITS, BEAM_BAD_SCORE, BEAM_SHORT = 1, 2, 4
+ROTARY_INTERLEAVED, ROTARY_INVERSE = 1, 2
+MAX_TREE, ATTN_MAX_TREE, MAX_BEAMS = 256, 256, 64
 ATTN_STATIC_WORKSPACE_BYTES = 64 << 20
 
 EXPORTS = ("etv_status_string", "etv_version", "etv_last_hip_error", "etv_build_tree_mask",
@@ -44,7 +46,9 @@ EXPORTS = ("etv_status_string", "etv_version", "etv_last_hip_error", "etv_build_
            "etv_verify_epilogue", "etv_lm_head_argmax_workspace_bytes", "etv_lm_head_argmax",
            "etv_lm_head_packed_bytes", "etv_pack_lm_head", "etv_replicate_branches", "etv_commit_path_indices",
            "etv_quantize_kv_q4", "etv_commit_accepted_kv_q4", "etv_dequantize_kv_q4",
-           "etv_tree_verify_attention_q4_workspace_bytes", "etv_tree_verify_attention_q4")
+           "etv_tree_verify_attention_q4_workspace_bytes", "etv_tree_verify_attention_q4",
+           "etv_resize_block_tables", "etv_rotary_write_kv", "etv_beam_select_workspace_bytes", "etv_beam_select",
+           "etv_reorder_beams_workspace_bytes", "etv_reorder_beams", "etv_reorder_beams_q4")
 
 
 class AttnDesc(C.Structure):
@@ -72,6 +76,19 @@ class CacheDesc(C.Structure):
 class Q4Desc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "rows", "Hkv", "d", "dtype", "n_layers", "W", "block_size", "max_blocks",
                                          "num_blocks", "P_cap", "reserved")] + [("layer_rows", C.c_int64)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "S", "block_size", "max_blocks", "num_blocks", "reserved")]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "T", "Hq", "Hkv", "d", "dtype", "rot_dim", "n_axes", "flags", "block_size")] + \
+               [("cache_rows", C.c_int64), ("scale", C.c_float), ("reserved", C.c_int32), ("strides", C.c_int64 * 12), ("axis_of", C.c_uint8 * 128)]
+
+
+class BeamDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "K", "V", "M", "dtype", "end_token")] + [("batch_stride", C.c_int64), ("row_stride", C.c_int64)]
 
 
 class KVCacheQ4(NamedTuple):
@@ -160,6 +177,21 @@ def lib():
         l.etv_tree_verify_attention_q4_workspace_bytes.argtypes = [C.POINTER(AttnDesc)]
         l.etv_tree_verify_attention_q4.restype = i32
         l.etv_tree_verify_attention_q4.argtypes = [C.POINTER(AttnDesc), vp] + q4 + [vp] * 8 + [sz, vp]
+        l.etv_resize_block_tables.restype = i32
+        l.etv_resize_block_tables.argtypes = [C.POINTER(PagesDesc)] + [vp] * 10
+        l.etv_rotary_write_kv.restype = i32
+        l.etv_rotary_write_kv.argtypes = [C.POINTER(RotaryDesc)] + [vp] * 13
+        l.etv_beam_select_workspace_bytes.restype = sz
+        l.etv_beam_select_workspace_bytes.argtypes = [C.POINTER(BeamDesc)]
+        l.etv_beam_select.restype = i32
+        l.etv_beam_select.argtypes = [C.POINTER(BeamDesc)] + [vp] * 10 + [sz, vp]
+        l.etv_reorder_beams_workspace_bytes.restype = sz
+        l.etv_reorder_beams_workspace_bytes.argtypes = [i32] * 4
+        beams = [vp, vp, i32, vp, i32] + [vp] * 6 + [sz, vp]     # block table, len, K, parent, M ... workspace, stream
+        l.etv_reorder_beams.restype = i32
+        l.etv_reorder_beams.argtypes = [C.POINTER(CacheDesc), vp, vp] + beams
+        l.etv_reorder_beams_q4.restype = i32
+        l.etv_reorder_beams_q4.argtypes = [C.POINTER(Q4Desc)] + [vp] * 4 + beams
         _lib = l
     return _lib
 
@@ -648,3 +680,149 @@ def tree_verify_attention_q4(q, cache: KVCacheQ4, prefix_len, kt, vt, bitmask, n
                                          workspace, workspace.numel())
     _check("etv_tree_verify_attention_q4", rc)
     return out, lse
+
+
+# ------------------------------------------------------------------------------------------------
+# beam decoding over a paged cache
+class FreeBlocks(NamedTuple):
+    """The free blocks of a pool, a ring on the device: blocks int32 [num_blocks] and state int32 [2] = (first, count).  The calls write
+    blocks in place and the new state into a tensor of its own: ``free = free.after(result)``."""
+    blocks: torch.Tensor
+    state: torch.Tensor
+
+    @classmethod
+    def all(cls, num_blocks: int, device="cuda") -> "FreeBlocks":
+        """Every block of a pool is free."""
+        return cls(torch.arange(num_blocks, dtype=torch.int32, device=device), torch.tensor([0, num_blocks], dtype=torch.int32, device=device))
+
+    def after(self, result: Dict[str, torch.Tensor]) -> "FreeBlocks":
+        return self._replace(state=result["free_state"])
+
+
+def resize_block_tables(block_table, length, new_length, free: FreeBlocks, block_size: int, S: int, *, want_slots: bool = True,
+                        out: Optional[Dict[str, torch.Tensor]] = None):
+    """block_table int32 [B, max_blocks] (updated in place); length, new_length int32 [B]; S: the most rows a sequence may grow by.
+    Sequences that grow take blocks of the ring, those that shrink give theirs back.  Returns free_state [2], length [B], slot_map [B, S]
+    (the new rows' slots, -1 behind them; None without want_slots) and status [B]."""
+    native, get = _native(), (out or {}).get
+    state, plo, slots, status = get("free_state"), get("length"), get("slot_map"), get("status")
+    if state is None:
+        state = native.empty_i32(length, 2)
+    if plo is None:
+        plo = native.empty_i32(length, len(length))
+    if status is None:
+        status = native.empty_i32(length, len(length))
+    if slots is None and want_slots:
+        slots = native.empty_i32(length, len(length), S)
+    dsc = native.pages_desc(block_table, length, new_length, free.blocks, free.state, state, plo, slots, status, block_size, S)
+    rc = native.resize_block_tables(dsc, length, new_length, block_table, free.blocks, free.state, state, plo, slots, status)
+    _check("etv_resize_block_tables", rc)
+    return dict(free_state=state, length=plo, slot_map=slots, status=status)
+
+
+class Rotary:
+    """A rotary encoding, as a model keeps it: inv_freq float32 [rot_dim / 2] on the device, the axis of each channel pair (none: all 0; three
+    axes: ``[0] * 16 + [1] * 24 + [2] * 24``), pairs of neighbours or of halves, and a factor on the result."""
+
+    def __init__(self, inv_freq: torch.Tensor, *, axis_of=None, interleaved: bool = False, scale: float = 1.0):
+        pairs = inv_freq.numel()
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float32 or not 0 < pairs <= 128:
+            raise ValueError("inv_freq is float32 [rot_dim / 2], of at most 128 pairs")
+        axis_of = [0] * pairs if axis_of is None else [int(a) for a in axis_of]
+        if len(axis_of) != pairs or not all(0 <= a < 128 for a in axis_of):
+            raise ValueError("axis_of names an axis for every channel pair")
+        if not 0 < abs(scale) < float("inf"):
+            raise ValueError("scale is a finite number other than 0")
+        self.inv_freq, flags = inv_freq, ROTARY_INTERLEAVED if interleaved else 0
+        self._desc, self._back = (bytes(RotaryDesc(rot_dim=2 * pairs, flags=f, scale=scale, axis_of=(C.c_uint8 * 128)(*axis_of)))
+                                  for f in (flags, flags | ROTARY_INVERSE))
+
+
+def rotary_write_kv(q, k, v, positions, rotary: Rotary, *, n_rows=None, slot_map=None, k_cache=None, v_cache=None, paged: bool = True,
+                    inverse: bool = False, out: Optional[Dict[str, torch.Tensor]] = None):
+    """q [B,T,Hq,d], k/v [B,T,Hkv,d] (each may be None; views of one projection's output are fine); positions int32 [n_axes,B,T] or [B,T].
+    Rotated q, and k and v written to slot_map int32 [B,T] of one layer's cache (paged [nb,Hkv,bs,d], else [B,P_cap,Hkv,d]).  Outputs may be
+    passed in `out`, the inputs among them; without a cache rotated k is returned too, v only where out["v"] is given.  inverse: turned
+    back (the gradient).  Rows from n_rows[b] on are left as they were.  Returns q, k, v (None: not asked for)."""
+    native, get = _native(), (out or {}).get
+    qo, ko, vo = get("q"), get("k"), get("v")
+    if qo is None and q is not None:
+        qo = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if ko is None and k is not None and k_cache is None:
+        ko = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    dsc = native.rotary_desc(rotary._back if inverse else rotary._desc, q, k, v, positions, rotary.inv_freq, n_rows, qo, ko, vo, slot_map,
+                             k_cache, v_cache, paged)
+    if dsc is None:
+        raise EtvError("etv_rotary_write_kv", -2)
+    rc = native.rotary_write_kv(dsc, q, k, v, positions, rotary.inv_freq, n_rows, qo, ko, vo, slot_map, k_cache, v_cache)
+    _check("etv_rotary_write_kv", rc)
+    return dict(q=qo, k=ko, v=vo)
+
+
+def beam_select_workspace_bytes(B: int, K: int, V: int, M: int, dtype=torch.float32) -> int:
+    code = F32 if dtype == torch.float32 else BF16
+    return int(lib().etv_beam_select_workspace_bytes(C.byref(BeamDesc(B, K, V, M, code, -1, K * V, V))))
+
+
+def beam_select(logits, scores, M: int, *, n_beams=None, finished=None, end_token: int = -1,
+                out: Optional[Dict[str, torch.Tensor]] = None, workspace=None):
+    """logits [B,K,V] fp32 or bf16 (rows may be padded), scores float32 [B,K] -> the M best continuations: scores float32, parent and token
+    int32, finished uint8, each [B,M] (-inf, -1, -1, 0 where fewer are offered), and status int32 [B].  finished uint8 or bool [B,K]: beams
+    that offer end_token at their own score alone."""
+    B, K, V = logits.shape
+    native, get = _native(), (out or {}).get
+    best, parent, token, ended, status = get("scores"), get("parent"), get("token"), get("finished"), get("status")
+    if best is None:
+        best = torch.empty((B, M), dtype=torch.float32, device=logits.device)
+    if parent is None:
+        parent = native.empty_i32(logits, B, M)
+    if token is None:
+        token = native.empty_i32(logits, B, M)
+    if ended is None:
+        ended = torch.empty((B, M), dtype=torch.uint8, device=logits.device)
+    if status is None:
+        status = native.empty_i32(logits, B)
+    dsc = native.beam_desc(logits, scores, n_beams, finished, best, parent, token, ended, status, M, end_token)
+    if dsc is None:
+        raise EtvError("etv_beam_select", -2)
+    if workspace is None:
+        workspace = torch.empty((max(256, beam_select_workspace_bytes(B, K, V, M, logits.dtype)),), dtype=torch.uint8, device=logits.device)
+    rc = native.beam_select(dsc, logits, scores, n_beams, finished, best, parent, token, ended, status, workspace, workspace.numel())
+    _check("etv_beam_select", rc)
+    return dict(scores=best, parent=parent, token=token, finished=ended, status=status)
+
+
+def reorder_beams_workspace_bytes(B: int, K: int, M: int, max_blocks: int) -> int:
+    return int(lib().etv_reorder_beams_workspace_bytes(B, K, M, max_blocks))
+
+
+def _reorder_beams(fn: str, call, parts, block_table, length, parent, free: FreeBlocks, out, workspace):
+    native, get = _native(), (out or {}).get
+    if block_table.dim() != 3 or parent.dim() != 2:
+        raise ValueError("block_table is int32 [B, K, max_blocks], parent int32 [B, M]")
+    (B, K, width), M = block_table.shape, parent.shape[1]
+    table, state, status = get("block_table"), get("free_state"), get("status")
+    if table is None:
+        table = native.empty_i32(block_table, B, M, width)
+    if state is None:
+        state = native.empty_i32(block_table, 2)
+    if status is None:
+        status = native.empty_i32(block_table, B)
+    dsc = native.reorder_desc(*parts, block_table, length, parent, free.blocks, free.state, table, state, status)
+    if dsc is None:
+        raise EtvError(fn, -2)
+    if workspace is None:
+        workspace = torch.empty((max(256, reorder_beams_workspace_bytes(B, K, M, width)),), dtype=torch.uint8, device=block_table.device)
+    _check(fn, call(dsc, *parts, block_table, length, K, parent, M, free.blocks, free.state, table, state, status, workspace, workspace.numel()))
+    return dict(block_table=table, free_state=state, status=status)
+
+
+def reorder_beams(k_cache, v_cache, block_table, length, parent, free: FreeBlocks, *, out: Optional[Dict[str, torch.Tensor]] = None, workspace=None):
+    """Caches [Lyr,nb,Hkv,bs,d] (half-filled blocks are copied where beams part); block_table int32 [B,K,max_blocks]; length int32 [B]; parent int32
+    [B,M], -1 for none -> block_table [B,M,max_blocks], free_state [2], status [B]."""
+    return _reorder_beams("etv_reorder_beams", _native().reorder_beams, (k_cache, v_cache), block_table, length, parent, free, out, workspace)
+
+
+def reorder_beams_q4(cache: KVCacheQ4, block_table, length, parent, free: FreeBlocks, *, out: Optional[Dict[str, torch.Tensor]] = None, workspace=None):
+    """reorder_beams over a 4-bit cache."""
+    return _reorder_beams("etv_reorder_beams_q4", _native().reorder_beams_q4, tuple(cache), block_table, length, parent, free, out, workspace)

@@ -3,7 +3,8 @@
 // 9 us per attention call: longer than the kernel.  Here one template turns the arguments into those of the C prototype in
 // eagletv.h: a pointer parameter takes a device-resident contiguous tensor or None, a descriptor any object with the buffer
 // of that struct, an integer an int or what has __index__ (numpy's integers, tensors of one); the trailing stream is the
-// current one.  The GIL is released around the call.  HERE: the tensors must be on the device whose stream that is.
+// current one.  The GIL is released around the call.  HERE: the tensors must be on the device whose stream that is.  Bit i of STRIDED: the
+// descriptor holds the strides of argument i.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -23,9 +24,11 @@ struct Refused {};  // a Python exception is set
 
 template <class T>
 constexpr bool is_desc = std::is_same_v<T, const etv_attn_desc *> || std::is_same_v<T, const etv_commit_desc *> ||
-                         std::is_same_v<T, const etv_cache_desc *> || std::is_same_v<T, const etv_q4_desc *>;
+                         std::is_same_v<T, const etv_cache_desc *> || std::is_same_v<T, const etv_q4_desc *> ||
+                         std::is_same_v<T, const etv_pages_desc *> || std::is_same_v<T, const etv_rotary_desc *> ||
+                         std::is_same_v<T, const etv_beam_desc *>;
 
-template <class T, bool HERE>
+template <class T, bool HERE, bool STRIDED = false>
 T arg(PyObject *o) {
     if constexpr (std::is_integral_v<T>) {
         if (!PyIndex_Check(o)) {
@@ -55,7 +58,7 @@ T arg(PyObject *o) {
             throw Refused{};
         }
         const at::Tensor &t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || !t.is_contiguous()) {
+        if (!t.is_cuda() || !(STRIDED || t.is_contiguous())) {
             PyErr_SetString(PyExc_AssertionError, "device-resident contiguous tensors only");
             throw Refused{};
         }
@@ -67,10 +70,10 @@ T arg(PyObject *o) {
     }
 }
 
-template <bool HERE, class... A, std::size_t... I>
+template <bool HERE, unsigned STRIDED, class... A, std::size_t... I>
 int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I...>) {
     std::tuple<A...> v;
-    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>, HERE>(args[I])), ...);  // left to right; the stream is last
+    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>, HERE, (STRIDED >> I & 1) != 0>(args[I])), ...);  // left to right; the stream is last
     std::get<sizeof...(A) - 1>(v) = c10::hip::getCurrentHIPStream().stream();
     int32_t rc;
     Py_BEGIN_ALLOW_THREADS;
@@ -82,13 +85,13 @@ int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I..
 template <class... A>
 constexpr Py_ssize_t arity(int32_t (*)(A...)) { return sizeof...(A) - 1; }
 
-template <auto F, bool HERE = false>
+template <auto F, bool HERE = false, unsigned STRIDED = 0>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     constexpr Py_ssize_t want = arity(F);
     if (n != want) return PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
     try {
-        return PyLong_FromLong(apply<HERE>(F, args, std::make_index_sequence<want>{}));
+        return PyLong_FromLong(apply<HERE, STRIDED>(F, args, std::make_index_sequence<want>{}));
     } catch (const Refused &) {
         return nullptr;
     }
@@ -265,6 +268,199 @@ PyObject *q4_attn_check(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Beam decoding.  What the C side takes on trust, checked; the descriptor's bytes, or None where a type is neither fp32 nor bf16.
+template <class D>
+PyObject *bytes_of(const D &d) { return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&d), sizeof d); }
+int32_t fit32(int64_t x) {
+    need(x >= 0 && x <= INT32_MAX, "a size does not fit 32 bits");
+    return static_cast<int32_t>(x);
+}
+int64_t int_of(PyObject *o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Refused{};
+    return v;
+}
+const at::Tensor *maybe(PyObject *o, const char *name) { return o == Py_None ? nullptr : &tensor_of(o, name); }
+int64_t ring_blocks(PyObject *blocks, PyObject *state, PyObject *state_out) {
+    const at::Tensor &r = tensor_of(blocks, "free.blocks");
+    need(r.dim() == 1 && is_i32(r, r.size(0)), "free.blocks is int32 [num_blocks]");
+    need(is_i32(tensor_of(state, "free.state"), 2) && is_i32(tensor_of(state_out, "free_state"), 2), "the state of the free blocks is int32 [2]");
+    return r.size(0);
+}
+
+// pages_desc(block_table, length, new_length, free_blocks, free_state, free_state_out, length_out, slot_map or None, status, block_size, S)
+PyObject *pages_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "11 arguments expected, got %zd", n);
+    try {
+        const at::Tensor &table = tensor_of(args[0], "block_table");
+        need(table.dim() == 2 && is_i32(table, table.size(0), table.size(1)), "block_table is int32 [B, max_blocks]");
+        const int64_t B = table.size(0), S = int_of(args[10]);
+        etv_pages_desc d{};
+        d.num_blocks = fit32(ring_blocks(args[3], args[4], args[5]));
+        for (int i : {1, 2, 6, 8}) need(is_i32(tensor_of(args[i], "lengths"), B), "lengths and status are int32 [B]");
+        if (const at::Tensor *slots = maybe(args[7], "slot_map")) need(is_i32(*slots, B, S), "slot_map is int32 [B, S]");
+        d.B = fit32(B);
+        d.S = fit32(S);
+        d.block_size = fit32(int_of(args[9]));
+        d.max_blocks = fit32(table.size(1));
+        return bytes_of(d);
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// rotary_desc(descriptor of the encoding, q, k, v, positions, inv_freq, n_rows, q_out, k_out, v_out, slot_map, k_cache, v_cache, paged)
+PyObject *rotary_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 14) return PyErr_Format(PyExc_TypeError, "14 arguments expected, got %zd", n);
+    try {
+        etv_rotary_desc d = *arg<const etv_rotary_desc *, false>(args[0]);
+        const at::Tensor *rows[6], *first = nullptr;
+        const char *names[6] = {"q", "k", "v", "out[\"q\"]", "out[\"k\"]", "out[\"v\"]"};
+        for (int i = 0; i < 6; i++) {
+            rows[i] = maybe(args[i < 3 ? 1 + i : 4 + i], names[i]);
+            if (rows[i] && !first) first = rows[i];
+        }
+        need(first && first->dim() == 4, "q, k and v are [B, T, heads, d]");
+        const int64_t B = first->size(0), T = first->size(1), width = first->size(3);
+        int64_t heads[3] = {0, 0, 0};
+        for (int i = 0; i < 6; i++) {
+            if (!rows[i]) continue;
+            const at::Tensor &t = *rows[i];
+            need(t.dim() == 4 && t.size(0) == B && t.size(1) == T && t.size(3) == width && t.scalar_type() == first->scalar_type(),
+                 "q, k, v and their outputs are [B, T, heads, d], of one type");
+            need(t.numel() == 0 || ((t.size(3) == 1 || t.stride(3) == 1) && (t.size(2) == 1 || t.stride(2) == width)), "heads and channels are contiguous");
+            if (i < 3) heads[i] = t.size(2);
+            else need(rows[i - 3] && t.size(2) == heads[i - 3], "an output has the shape of its input");
+            d.strides[2 * i] = t.stride(0);
+            d.strides[2 * i + 1] = t.stride(1);
+        }
+        need(!rows[2] || (rows[1] && heads[2] == heads[1]), "v has the heads of k");
+        const at::Tensor &pos = tensor_of(args[4], "positions"), &freq = tensor_of(args[5], "inv_freq");
+        need(pos.scalar_type() == at::kInt && (pos.dim() == 2 || pos.dim() == 3) && pos.size(-2) == B && pos.size(-1) == T, "positions are int32 [n_axes, B, T] or [B, T]");
+        need(freq.scalar_type() == at::kFloat && freq.dim() == 1 && freq.size(0) * 2 == d.rot_dim, "inv_freq is float32 [rot_dim / 2]");
+        d.n_axes = pos.dim() == 2 ? 1 : fit32(pos.size(0));
+        if (const at::Tensor *rows_of = maybe(args[6], "n_rows")) need(is_i32(*rows_of, B), "n_rows is int32 [B]");
+        d.block_size = 0, d.cache_rows = 0;
+        if (const at::Tensor *slots = maybe(args[10], "slot_map")) {
+            need(is_i32(*slots, B, T), "slot_map is int32 [B, T]");
+            const int paged = PyObject_IsTrue(args[13]);
+            for (int i = 11; i < 13; i++) {
+                const at::Tensor &c = tensor_of(args[i], "k_cache and v_cache");
+                need(c.dim() == 4 && c.size(3) == width && c.size(paged ? 1 : 2) == heads[1] && c.scalar_type() == first->scalar_type() &&
+                         c.sizes() == tensor_of(args[11], "k_cache").sizes(),
+                     paged ? "a paged cache is [num_blocks, Hkv, block_size, d], of q's type" : "a contiguous cache is [B, P_cap, Hkv, d], of q's type");
+                need(paged || c.size(0) == B, "a contiguous cache has B sequences");
+                d.cache_rows = c.size(0) * c.size(paged ? 2 : 1);
+                d.block_size = paged ? fit32(c.size(2)) : 0;
+                need(!paged || d.block_size > 0, "blocks of no rows");
+            }
+        } else {
+            need(args[11] == Py_None && args[12] == Py_None, "a cache needs a slot_map");
+        }
+        d.B = fit32(B);
+        d.T = fit32(T);
+        d.Hq = fit32(heads[0]);
+        d.Hkv = fit32(heads[1]);
+        d.d = fit32(width);
+        d.dtype = type_code(*first);
+        if (d.dtype < 0) Py_RETURN_NONE;
+        return bytes_of(d);
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// beam_desc(logits, scores, n_beams, finished, scores_out, parent, token, finished_out, status, M, end_token)
+PyObject *beam_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 11) return PyErr_Format(PyExc_TypeError, "11 arguments expected, got %zd", n);
+    try {
+        const at::Tensor &x = tensor_of(args[0], "logits"), &scores = tensor_of(args[1], "scores"), &best = tensor_of(args[4], "out[\"scores\"]");
+        need(x.dim() == 3 && (x.size(2) == 1 || x.stride(2) == 1), "logits are [B, K, V], the vocabulary contiguous");
+        const int64_t B = x.size(0), K = x.size(1), M = int_of(args[9]);
+        need(scores.scalar_type() == at::kFloat && scores.dim() == 2 && scores.size(0) == B && scores.size(1) == K, "scores are float32 [B, K]");
+        need(best.scalar_type() == at::kFloat && best.dim() == 2 && best.size(0) == B && best.size(1) == M, "out[\"scores\"] is float32 [B, M]");
+        if (const at::Tensor *t = maybe(args[2], "n_beams")) need(is_i32(*t, B), "n_beams is int32 [B]");
+        if (const at::Tensor *t = maybe(args[3], "finished"))
+            need((t->scalar_type() == at::kByte || t->scalar_type() == at::kBool) && t->dim() == 2 && t->size(0) == B && t->size(1) == K, "finished is uint8 [B, K]");
+        need(is_i32(tensor_of(args[5], "parent"), B, M) && is_i32(tensor_of(args[6], "token"), B, M), "parent and token are int32 [B, M]");
+        if (const at::Tensor *t = maybe(args[7], "out[\"finished\"]"))
+            need((t->scalar_type() == at::kByte || t->scalar_type() == at::kBool) && t->dim() == 2 && t->size(0) == B && t->size(1) == M, "out[\"finished\"] is uint8 [B, M]");
+        need(is_i32(tensor_of(args[8], "status"), B), "status is int32 [B]");
+        etv_beam_desc d{};
+        d.B = fit32(B);
+        d.K = fit32(K);
+        d.V = fit32(x.size(2));
+        d.M = fit32(M);
+        d.dtype = type_code(x);
+        const int64_t end = int_of(args[10]);
+        need(end >= -1 && end < x.size(2), "end_token is outside the vocabulary");
+        d.end_token = static_cast<int32_t>(end);
+        d.batch_stride = x.stride(0);
+        d.row_stride = x.stride(1);
+        if (d.dtype < 0) Py_RETURN_NONE;
+        return bytes_of(d);
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// reorder_desc(parts of the cache (2, or codes and scales of K and V: 4)..., block_table, length, parent, free_blocks, free_state, table_out,
+// free_state_out, status): an etv_cache_desc or etv_q4_desc
+PyObject *reorder_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10 && n != 12) return PyErr_Format(PyExc_TypeError, "10 or 12 arguments expected, got %zd", n);
+    try {
+        const bool q4 = n == 12;
+        PyObject *const *rest = args + (q4 ? 4 : 2);
+        const at::Tensor &table = tensor_of(rest[0], "block_table"), &parent = tensor_of(rest[2], "parent"), &out = tensor_of(rest[5], "out[\"block_table\"]");
+        need(table.scalar_type() == at::kInt && table.dim() == 3, "block_table is int32 [B, K, max_blocks]");
+        const int64_t B = table.size(0);
+        need(parent.dim() == 2 && is_i32(parent, B, parent.size(1)), "parent is int32 [B, M]");
+        need(out.scalar_type() == at::kInt && out.dim() == 3 && out.size(0) == B && out.size(1) == parent.size(1) && out.size(2) == table.size(2),
+             "out[\"block_table\"] is int32 [B, M, max_blocks]");
+        need(is_i32(tensor_of(rest[1], "length"), B) && is_i32(tensor_of(rest[7], "status"), B), "length and status are int32 [B]");
+        const at::Tensor &k = tensor_of(args[0], "k_cache"), &v = tensor_of(args[q4 ? 2 : 1], "v_cache");
+        need(k.dim() == 5 && v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type(), "a cache is [n_layers, num_blocks, Hkv, block_size, ...]");
+        need(k.size(1) == ring_blocks(rest[3], rest[4], rest[6]), "free.blocks has an entry for every block of the cache");
+        need(k.size(3) > 0, "blocks of no rows");
+        if (q4) {
+            const Q4Shapes c = q4_shapes(args, 1, k.size(4) * 2);
+            etv_q4_desc d{};
+            d.B = fit32(B);
+            d.rows = 1;
+            d.Hkv = fit32(c.heads);
+            d.d = fit32(c.d);
+            d.n_layers = fit32(c.layers);
+            d.block_size = fit32(c.size);
+            d.max_blocks = fit32(table.size(2));
+            d.num_blocks = fit32(c.blocks);
+            d.layer_rows = c.blocks * c.heads * c.size;
+            return bytes_of(d);
+        }
+        if (type_code(k) < 0) Py_RETURN_NONE;
+        etv_cache_desc d{};
+        d.B = fit32(B);
+        d.Hkv = fit32(k.size(2));
+        d.d = fit32(k.size(4));
+        d.elem_bytes = static_cast<int32_t>(k.element_size());
+        d.n_layers = fit32(k.size(0));
+        d.block_size = fit32(k.size(3));
+        d.max_blocks = fit32(table.size(2));
+        d.num_blocks = fit32(k.size(1));
+        d.cache_layer_stride = k.numel() / (k.size(0) > 0 ? k.size(0) : 1);
+        return bytes_of(d);
+    } catch (const Refused &) {
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
 #define ETV_METHOD(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name>, METH_FASTCALL, nullptr}
 #define ETV_METHOD_HERE(name) {#name, (PyCFunction)(void (*)(void))call<&etv_##name, true>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree), ETV_METHOD(tree_verify_attention),
@@ -273,6 +469,13 @@ PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree)
                          ETV_METHOD(pack_lm_head), ETV_METHOD(replicate_branches), ETV_METHOD(commit_path_indices),
                          ETV_METHOD_HERE(quantize_kv_q4), ETV_METHOD_HERE(commit_accepted_kv_q4), ETV_METHOD_HERE(dequantize_kv_q4),
                          ETV_METHOD_HERE(tree_verify_attention_q4),
+                         ETV_METHOD_HERE(resize_block_tables), ETV_METHOD_HERE(reorder_beams), ETV_METHOD_HERE(reorder_beams_q4),
+                         {"rotary_write_kv", (PyCFunction)(void (*)(void))call<&etv_rotary_write_kv, true, 0x38e>, METH_FASTCALL, nullptr},
+                         {"beam_select", (PyCFunction)(void (*)(void))call<&etv_beam_select, true, 0x2>, METH_FASTCALL, nullptr},
+                         {"pages_desc", (PyCFunction)(void (*)(void))pages_desc, METH_FASTCALL, nullptr},
+                         {"rotary_desc", (PyCFunction)(void (*)(void))rotary_desc, METH_FASTCALL, nullptr},
+                         {"beam_desc", (PyCFunction)(void (*)(void))beam_desc, METH_FASTCALL, nullptr},
+                         {"reorder_desc", (PyCFunction)(void (*)(void))reorder_desc, METH_FASTCALL, nullptr},
                          {"commit_desc", (PyCFunction)(void (*)(void))commit_desc, METH_FASTCALL, nullptr},
                          {"q4_desc", (PyCFunction)(void (*)(void))q4_desc, METH_FASTCALL, nullptr},
                          {"q4_attn_check", (PyCFunction)(void (*)(void))q4_attn_check, METH_FASTCALL, nullptr},

@@ -1,0 +1,165 @@
+// Block tables and slot maps from the sequences' lengths: blocks taken from and given back to a ring of free ones, in one launch.
+#include "etv_common.h"
+#include "free_ring.h"
+
+namespace etv {
+
+constexpr int kSlotsPerWg = 1024;  // elements of slot_map that a workgroup writes
+constexpr int kMaxRow = 1 << 22;   // longest table row: 256 of them are counted in 31 bits
+
+// What the lengths alone say of a sequence.
+struct PagePlan {
+    int32_t st;  // ETV_COMMIT_BAD_LEN / ETV_COMMIT_CAPACITY or 0
+    int old, want;
+    __device__ int take() const { return st == 0 && want > old ? want - old : 0; }
+    __device__ int give() const { return st == 0 && want < old ? old - want : 0; }
+};
+__device__ __forceinline__ PagePlan page_plan(const etv_pages_desc &dsc, uint32_t inv_bs, int len, int new_len) {
+    PagePlan p{0, 0, 0};
+    if (len < 0 || new_len < 0 || (long)new_len - len > dsc.S) {
+        p.st = ETV_COMMIT_BAD_LEN;
+        return p;
+    }
+    uint32_t rem;
+    p.old = (int)fast_div((uint32_t)len + (uint32_t)(dsc.block_size - 1), dsc.block_size, inv_bs, rem);
+    p.want = (int)fast_div((uint32_t)new_len + (uint32_t)(dsc.block_size - 1), dsc.block_size, inv_bs, rem);
+    if (p.old > dsc.max_blocks || p.want > dsc.max_blocks) p.st = ETV_COMMIT_CAPACITY;
+    return p;
+}
+
+// Workgroup 0: what is given back, and the ring's new state.  256 sequences at a time; a wavefront walks the table entries of one.
+__device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int32_t *len, const int32_t *new_len, const int32_t *block_table,
+                          int32_t *free_blocks, const Ring &ring, int32_t *free_state_out, int32_t *len_out, int32_t *slot_map, int32_t *status) {
+    __shared__ int s_first[256], s_give[256], s_bad[256];
+    __shared__ long s_at[256], s_most[2];
+    const int t = threadIdx.x, lane = t & 63;
+    if (t < 2) s_most[t] = 0;
+    long taken = 0, given = 0;
+    const long room = ring.room();
+    for (int b0 = 0; b0 < dsc.B; b0 += 256) {
+        const int b = b0 + t;
+        PagePlan p{0, 0, 0};
+        if (b < dsc.B) p = page_plan(dsc, inv_bs, len[b], new_len[b]);
+        s_first[t] = p.want;
+        s_give[t] = p.give();
+        s_bad[t] = 0;
+        const int take = p.take();
+        const long t_end = block_scan_sum(take, taken);
+        if (take > 0 && t_end <= ring.count) atomicMax((unsigned long long *)&s_most[0], (unsigned long long)t_end);
+        __syncthreads();
+        for (int s = t >> 6; s < 256; s += 4) {
+            const int32_t *row = block_table + (size_t)(b0 + s) * dsc.max_blocks + s_first[s];
+            int bad = 0;
+            for (int j = lane; j < s_give[s]; j += 64) bad |= (uint32_t)row[j] >= (uint32_t)dsc.num_blocks;
+            if (bad) s_bad[s] = 1;
+        }
+        __syncthreads();
+        const int give = s_bad[t] ? 0 : s_give[t];
+        const long g_end = block_scan_sum(give, given);
+        int32_t st = s_bad[t] ? ETV_COMMIT_BAD_BLOCK : give > 0 && g_end > room ? ETV_BRANCH_BAD_FREE : 0;
+        if (give > 0 && !st) atomicMax((unsigned long long *)&s_most[1], (unsigned long long)g_end);
+        s_at[t] = g_end - give;
+        if (st) s_give[t] = 0;
+        if (b < dsc.B && p.give() > 0) {
+            status[b] = st;
+            len_out[b] = st ? len[b] : new_len[b];
+        }
+        __syncthreads();
+        for (int s = t >> 6; s < 256; s += 4) {
+            const int32_t *row = block_table + (size_t)(b0 + s) * dsc.max_blocks + s_first[s];
+            for (int j = lane; j < s_give[s]; j += 64) free_blocks[ring.place(ring.count + s_at[s] + j)] = row[j];
+        }
+        __syncthreads();
+    }
+    __syncthreads();
+    if (t == 0) ring.leave(free_state_out, s_most[0], s_most[1]);
+}
+
+// Workgroups 1 ..: kSlotsPerWg elements of the slot map each, and the new table entries, lengths and status of the sequences that start in
+// them.  Every workgroup adds up the blocks of the sequences before its own; the sequences' table rows and the ring's entries that
+// are read here are written by nobody.
+__device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S, const int32_t *len, const int32_t *new_len, int32_t *block_table,
+                     const int32_t *free_blocks, const Ring &ring, int32_t *len_out, int32_t *slot_map, int32_t *status) {
+    __shared__ int s_len[kSlotsPerWg], s_rows[kSlotsPerWg], s_old[kSlotsPerWg], s_tail[kSlotsPerWg];
+    __shared__ long s_base[kSlotsPerWg];
+    const int t = threadIdx.x;
+    const uint32_t e0 = (blockIdx.x - 1) * kSlotsPerWg, last = (uint32_t)(dsc.B * dsc.S - 1);
+    uint32_t rem;
+    const int b_lo = (int)fast_div(e0, dsc.S, inv_S, rem), b_hi = (int)fast_div(min(e0 + kSlotsPerWg - 1, last), dsc.S, inv_S, rem);
+    const int nb = b_hi - b_lo + 1;
+    long mine = 0;
+    for (int b = t; b < b_lo; b += 256) mine += page_plan(dsc, inv_bs, len[b], new_len[b]).take();
+    long base = block_sum(mine);
+    for (int s0 = 0; s0 < nb; s0 += 256) {
+        const int s = s0 + t, b = b_lo + s;
+        PagePlan p{0, 0, 0};
+        int L = 0, N = 0;
+        if (s < nb) {
+            L = len[b], N = new_len[b];
+            p = page_plan(dsc, inv_bs, L, N);
+        }
+        const int take = p.take();
+        const long end = block_scan_sum(take, base);
+        if (s >= nb) continue;
+        int32_t st = p.st, tail = 0;
+        const int rows = st ? 0 : N - L;
+        if (!st && take > 0 && end > ring.count) st = ETV_BRANCH_NO_BLOCKS;
+        if (rows > 0 && (long)p.old * dsc.block_size != L) {  // the new rows begin in a block that is there
+            tail = block_table[(size_t)b * dsc.max_blocks + p.old - 1];
+            if (!st && (uint32_t)tail >= (uint32_t)dsc.num_blocks) st = ETV_COMMIT_BAD_BLOCK;
+        }
+        if (!st)
+            for (int j = 0; j < take; j++)
+                if ((uint32_t)free_blocks[ring.place(end - take + j)] >= (uint32_t)dsc.num_blocks) st = ETV_BRANCH_BAD_FREE;
+        s_len[s] = L;
+        s_rows[s] = st ? 0 : max(rows, 0);
+        s_old[s] = p.old;
+        s_tail[s] = tail;
+        s_base[s] = end - take;
+        const bool starts = (uint32_t)b * dsc.S >= e0;
+        if (starts && p.give() == 0) {
+            status[b] = st;
+            len_out[b] = st ? L : N;
+        }
+    }
+    __syncthreads();
+    for (int r = t; r < kSlotsPerWg; r += 256) {
+        const uint32_t e = e0 + r;
+        if (e > last) break;
+        uint32_t i;
+        const int b = (int)fast_div(e, dsc.S, inv_S, i), s = b - b_lo;
+        int32_t slot = -1;
+        if ((int)i < s_rows[s]) {
+            uint32_t off;
+            const int j = (int)fast_div((uint32_t)s_len[s] + i, dsc.block_size, inv_bs, off);
+            const int block = j < s_old[s] ? s_tail[s] : free_blocks[ring.place(s_base[s] + j - s_old[s])];
+            slot = block * dsc.block_size + (int)off;
+            if (j >= s_old[s] && off == 0) block_table[(size_t)b * dsc.max_blocks + j] = block;
+        }
+        if (slot_map) slot_map[e] = slot;
+    }
+}
+
+__global__ void __launch_bounds__(256) resize_tables_kernel(etv_pages_desc dsc, uint32_t inv_bs, uint32_t inv_S, const int32_t *len, const int32_t *new_len,
+                                                            int32_t *block_table, int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out,
+                                                            int32_t *len_out, int32_t *slot_map, int32_t *status) {
+    const Ring ring(free_state, dsc.num_blocks);
+    if (blockIdx.x == 0) give_back(dsc, inv_bs, len, new_len, block_table, free_blocks, ring, free_state_out, len_out, slot_map, status);
+    else grow(dsc, inv_bs, inv_S, len, new_len, block_table, free_blocks, ring, len_out, slot_map, status);
+}
+
+}  // namespace etv
+
+extern "C" int32_t etv_resize_block_tables(const etv_pages_desc *h, const int32_t *len, const int32_t *new_len, int32_t *block_table,
+                                           int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out, int32_t *len_out,
+                                           int32_t *slot_map, int32_t *status, void *stream) {
+    if (!h || h->B < 0 || h->S < 1 || h->block_size < 1 || h->max_blocks < 1 || h->num_blocks < 1) return ETV_ERR_INVALID_ARG;
+    if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
+    if (h->B > 0 && (!len || !new_len || !block_table || !len_out || !status || len_out == len || len_out == new_len)) return ETV_ERR_INVALID_ARG;
+    if ((int64_t)h->B * h->S > INT32_MAX - etv::kSlotsPerWg || (int64_t)h->num_blocks * h->block_size > INT32_MAX || h->max_blocks > etv::kMaxRow)
+        return ETV_ERR_UNSUPPORTED;
+    const unsigned wgs = 1 + (unsigned)(((int64_t)h->B * h->S + etv::kSlotsPerWg - 1) / etv::kSlotsPerWg);
+    hipLaunchKernelGGL(etv::resize_tables_kernel, dim3(wgs), dim3(256), 0, etv::as_stream(stream), *h, etv::fast_div_inv(h->block_size),
+                       etv::fast_div_inv(h->S), len, new_len, block_table, free_blocks, free_state, free_state_out, len_out, slot_map, status);
+    return etv::check_launch();
+}

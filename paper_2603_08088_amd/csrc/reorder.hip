@@ -1,0 +1,305 @@
+// The beams' block tables after a step: gathered from the parents', with blocks shared, the half-filled block copied where several beams go on
+// from it, and the blocks that nobody refers to any more put back into the ring.  Two launches: the tables and what they need and
+// give back, then -- every workgroup adding up what the requests before its own need -- the copies.
+#include "etv_common.h"
+#include "free_ring.h"
+
+namespace etv {
+
+constexpr int kCols = 128;  // columns of the tables of one request that a workgroup takes
+
+struct ReorderShape {
+    int B, K, M, max_blocks, num_blocks, block_size, chunks;
+};
+// What the first launch finds in one chunk of a request's columns.
+struct ChunkRecord {
+    int32_t st;    // status bits
+    int32_t need;  // blocks to copy into (the chunk that holds the half-filled block)
+    int32_t give;  // blocks given back; their ids follow in the chunk's list
+    int32_t pad;
+};
+struct ReorderWorkspace {
+    ChunkRecord *records;  // [B][chunks]
+    int32_t *from;         // [B][M]: the block to copy from, -1: none
+    int32_t *give;         // [B][chunks][kCols * K]
+};
+
+__device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len) {
+    if (len < 0) return ETV_COMMIT_BAD_LEN;
+    return ((long)len + sh.block_size - 1) / sh.block_size > sh.max_blocks ? ETV_COMMIT_CAPACITY : 0;
+}
+
+// grid (chunks, B), 128 threads: a thread per column of the table.
+__global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
+                                                               int32_t *table_out, ReorderWorkspace ws) {
+    extern __shared__ int32_t s_table[];  // [K][kCols]
+    __shared__ int s_parent[ETV_MAX_BEAMS];
+    __shared__ unsigned int s_alive[2];
+    const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 63, col = c * kCols + t;
+    int32_t st = length_status(sh, len[b]);
+    const int L = st ? 0 : len[b], full = L / sh.block_size, cols = (int)(((long)L + sh.block_size - 1) / sh.block_size);
+    if (t < 2) s_alive[t] = 0;
+    __syncthreads();
+    int bad = 0;
+    if (t < sh.M) {
+        const int p = parent[(size_t)b * sh.M + t];
+        const bool ok = p >= 0 && p < sh.K;
+        bad = !ok && p != -1;
+        s_parent[t] = ok ? p : -1;
+        if (ok) atomicOr(&s_alive[p >> 5], 1u << (p & 31));
+    }
+    if (__syncthreads_or(bad)) st |= ETV_COMMIT_BAD_NODE;
+    const uint64_t alive = s_alive[0] | (uint64_t)s_alive[1] << 32;
+    const int32_t *src = block_table + (size_t)b * sh.K * sh.max_blocks;
+    bad = 0;
+    for (int k = 0; k < sh.K; k++) {
+        const int32_t id = col < cols ? src[(size_t)k * sh.max_blocks + col] : -1;
+        s_table[k * kCols + t] = id;
+        if (col < cols && alive >> k & 1) bad |= (uint32_t)id >= (uint32_t)sh.num_blocks;
+    }
+    if (__syncthreads_or(bad)) st |= ETV_COMMIT_BAD_BLOCK;
+    if (col < sh.max_blocks)
+        for (int i = 0; i < sh.M; i++) {
+            const int p = s_parent[i];
+            table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && p >= 0 && col < cols ? s_table[p * kCols + t] : -1;
+        }
+    // blocks of beams without a child that neither a parent nor an earlier such beam has
+    uint64_t gone = 0;
+    if (col < cols && !st)
+        for (int k = 0; k < sh.K; k++) {
+            if (alive >> k & 1) continue;
+            const int32_t id = s_table[k * kCols + t];
+            bool mine = (uint32_t)id < (uint32_t)sh.num_blocks;
+            for (int j = 0; j < sh.K && mine; j++) mine = !((alive >> j & 1 || j < k) && s_table[j * kCols + t] == id);
+            if (mine) gone |= 1ull << k;
+        }
+    __shared__ int s_wave[2];
+    const int count = __popcll(gone);
+    const int upto = wave_scan_sum(count);
+    if (lane == 63) s_wave[t >> 6] = upto;
+    __syncthreads();
+    int32_t *list = ws.give + ((size_t)b * sh.chunks + c) * kCols * sh.K;
+    int at = upto - count + (t >= 64 ? s_wave[0] : 0);
+    for (; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kCols + t];
+    // the half-filled block: its first child keeps it
+    const bool here = !st && L % sh.block_size != 0 && full / kCols == c;
+    int need = 0;
+    if (t < 64) {
+        const int p = lane < sh.M ? s_parent[lane] : -1;
+        const int32_t id = here && p >= 0 ? s_table[p * kCols + full % kCols] : -1;
+        bool later = false;
+        for (int j = 0; j < sh.M; j++) {
+            const int32_t other = __shfl(id, j);
+            later |= j < lane && other == id;
+        }
+        later = later && id >= 0;
+        need = __popcll(__ballot(later));
+        if (here && lane < sh.M) ws.from[(size_t)b * sh.M + lane] = later ? id : -1;
+    }
+    if (t == 0) ws.records[(size_t)b * sh.chunks + c] = {st, need, s_wave[0] + s_wave[1], 0};
+}
+
+// What all chunks of a request say.
+__device__ __forceinline__ ChunkRecord request(const ReorderShape &sh, const ReorderWorkspace &ws, int b) {
+    ChunkRecord r{0, 0, 0, 0};
+    for (int c = 0; c < sh.chunks; c++) {
+        const ChunkRecord x = ws.records[(size_t)b * sh.chunks + c];
+        r.st |= x.st;
+        r.need += x.need;
+        r.give += x.give;
+    }
+    if (r.st) r.need = r.give = 0;
+    return r;
+}
+
+struct CacheParts {
+    uint8_t *base[4];
+    size_t layer_bytes[4];
+    int row_bytes[4];
+    int parts, Hkv, n_layers;
+};
+
+// The rows of a half-filled block: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is shorter.
+template <class U>
+__device__ __forceinline__ void copy_rows(uint8_t *layer, int src, int dst, int Hkv, int block_size, int row_bytes, int rows) {
+    const int units = rows * row_bytes / (int)sizeof(U);
+    for (int h = threadIdx.x >> 6; h < Hkv; h += 4) {
+        const U *from = reinterpret_cast<const U *>(layer + ((size_t)src * Hkv + h) * block_size * row_bytes);
+        U *to = reinterpret_cast<U *>(layer + ((size_t)dst * Hkv + h) * block_size * row_bytes);
+        for (int u = threadIdx.x & 63; u < units; u += 64) to[u] = from[u];
+    }
+}
+
+// Workgroups 0 .. B-1: status, the table entries of the copies and the ring.  Then B * n_layers * parts * G workgroups that copy.
+__global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, CacheParts cache, int G, const int32_t *len, int32_t *free_blocks,
+                                                           const int32_t *free_state, int32_t *table_out, int32_t *free_state_out, int32_t *status,
+                                                           ReorderWorkspace ws) {
+    const Ring ring(free_state, sh.num_blocks);
+    const int t = threadIdx.x, lane = t & 63;
+    if ((int)blockIdx.x >= sh.B) {
+        int x = blockIdx.x - sh.B;
+        const int g = x % G;
+        x /= G;
+        const int part = x % cache.parts;
+        x /= cache.parts;
+        const int l = x % cache.n_layers, b = x / cache.n_layers;
+        const int need = request(sh, ws, b).need;
+        if (g >= need) return;
+        long before = 0;
+        for (int o = t; o < b; o += 256) before += request(sh, ws, o).need;
+        before = block_sum(before);
+        if (before + need > ring.count) return;
+        const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
+        const int rows = len[b] % sh.block_size;
+        uint8_t *layer = cache.base[part] + (size_t)l * cache.layer_bytes[part];
+        uint64_t todo = __ballot(from >= 0);
+        for (int i = 0; i < need; i++, todo &= todo - 1) {
+            if (i % G != g) continue;
+            const int src = __shfl(from, __builtin_ctzll(todo)), dst = free_blocks[ring.place(before + i)];
+            if ((uint32_t)dst >= (uint32_t)sh.num_blocks) continue;
+            if (cache.row_bytes[part] % 16 == 0) copy_rows<uint4>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+            else copy_rows<uint16_t>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+        }
+        return;
+    }
+    __shared__ long s_need, s_give, s_taken, s_given;
+    __shared__ int s_st, s_any;
+    const int b = blockIdx.x;
+    if (t == 0) s_taken = s_given = 0;
+    long needs = 0, gives = 0;
+    for (int b0 = 0; b0 <= b; b0 += 256) {
+        const int o = b0 + t;
+        ChunkRecord r{0, 0, 0, 0};
+        if (o <= b) r = request(sh, ws, o);
+        const long need_end = block_scan_sum(r.need, needs);
+        int32_t st = r.st;
+        if (!st && r.need > 0 && need_end > ring.count) st = ETV_BRANCH_NO_BLOCKS, r.give = 0;
+        else if (r.need > 0) atomicMax((unsigned long long *)&s_taken, (unsigned long long)need_end);
+        const long give_end = block_scan_sum(r.give, gives);
+        if (r.give > 0) {
+            if (give_end > ring.room()) st |= ETV_BRANCH_BAD_FREE;
+            else atomicMax((unsigned long long *)&s_given, (unsigned long long)give_end);
+        }
+        if (o == b) s_st = st, s_need = need_end - r.need, s_give = give_end - r.give, s_any = r.need;
+    }
+    __syncthreads();
+    int32_t st = s_st;
+    if (b == sh.B - 1 && t == 0) ring.leave(free_state_out, s_taken, s_given);
+    const int L = len[b];
+    const long give_at = s_give;
+    if (st) {
+        for (size_t i = t; i < (size_t)sh.M * sh.max_blocks; i += 256) table_out[(size_t)b * sh.M * sh.max_blocks + i] = -1;
+    } else {
+        if (s_any) {
+            const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
+            uint64_t todo = __ballot(from >= 0);
+            for (long i = s_need; todo; i++, todo &= todo - 1) {
+                const int32_t dst = free_blocks[ring.place(i)];
+                int32_t *row = table_out + ((size_t)b * sh.M + __builtin_ctzll(todo)) * sh.max_blocks;
+                if ((uint32_t)dst < (uint32_t)sh.num_blocks) {
+                    if (t == 0) row[L / sh.block_size] = dst;
+                } else {
+                    st |= ETV_BRANCH_BAD_FREE;
+                    for (int j = t; j < sh.max_blocks; j += 256) row[j] = -1;
+                }
+            }
+        }
+        long at = ring.count + give_at;
+        for (int c = 0; c < sh.chunks; c++) {
+            const int n = ws.records[(size_t)b * sh.chunks + c].give;
+            const int32_t *list = ws.give + ((size_t)b * sh.chunks + c) * kCols * sh.K;
+            for (int i = t; i < n; i += 256) free_blocks[ring.place(at + i)] = list[i];
+            at += n;
+        }
+    }
+    if (t == 0) status[b] = st;
+}
+
+// An empty batch takes and gives nothing.
+__global__ void ring_copy_kernel(const int32_t *free_state, int32_t *free_state_out) { free_state_out[threadIdx.x] = free_state[threadIdx.x]; }
+
+static int reorder_chunks(int max_blocks) { return (max_blocks + kCols - 1) / kCols; }
+
+static size_t reorder_bytes(int64_t B, int64_t K, int64_t M, int max_blocks) {
+    const size_t lists = (size_t)B * reorder_chunks(max_blocks);
+    return lists * sizeof(ChunkRecord) + (size_t)B * M * 4 + lists * kCols * K * 4;
+}
+
+static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const int32_t *block_table, const int32_t *len, const int32_t *parent,
+                       int32_t *free_blocks, const int32_t *free_state, int32_t *table_out, int32_t *free_state_out, int32_t *status, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+    const ReorderShape sh = shape;
+    if (sh.B < 0 || sh.K < 1 || sh.M < 1 || sh.max_blocks < 1 || sh.num_blocks < 1 || cache.n_layers < 1 || cache.Hkv < 1) return ETV_ERR_INVALID_ARG;
+    if (sh.K > ETV_MAX_BEAMS || sh.M > ETV_MAX_BEAMS || sh.B > 65535 || sh.max_blocks > (1 << 22) || (int64_t)sh.num_blocks * sh.block_size > INT32_MAX)
+        return ETV_ERR_UNSUPPORTED;
+    if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
+    hipStream_t s = as_stream(stream);
+    if (sh.B == 0) {
+        hipLaunchKernelGGL(ring_copy_kernel, dim3(1), dim3(2), 0, s, free_state, free_state_out);
+        return check_launch();
+    }
+    if (!block_table || !len || !parent || !table_out || !status || table_out == block_table) return ETV_ERR_INVALID_ARG;
+    for (int i = 0; i < cache.parts; i++)
+        if (!cache.base[i] || (uintptr_t)cache.base[i] % (cache.row_bytes[i] % 16 ? 2 : 16)) return ETV_ERR_INVALID_ARG;
+    if ((uintptr_t)workspace & 15) return ETV_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < reorder_bytes(sh.B, sh.K, sh.M, sh.max_blocks)) return ETV_ERR_WORKSPACE_TOO_SMALL;
+    ReorderWorkspace ws;
+    ws.records = static_cast<ChunkRecord *>(workspace);
+    ws.from = reinterpret_cast<int32_t *>(ws.records + (size_t)sh.B * sh.chunks);
+    ws.give = ws.from + (size_t)sh.B * sh.M;
+    // a workgroup per copy while they are few, a loop over a request's copies beyond
+    const int64_t one = (int64_t)sh.B * cache.n_layers * cache.parts;
+    int64_t G = 2048 / one;
+    G = G < 1 ? 1 : G > sh.M ? sh.M : G;
+    if (sh.B + one * G > INT32_MAX) return ETV_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(reorder_tables_kernel, dim3(sh.chunks, sh.B), dim3(kCols), sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
+    const int32_t rc = check_launch();
+    if (rc != ETV_OK) return rc;
+    hipLaunchKernelGGL(reorder_copy_kernel, dim3((unsigned)(sh.B + one * G)), dim3(256), 0, s, sh, cache, (int)G, len, free_blocks, free_state, table_out,
+                       free_state_out, status, ws);
+    return check_launch();
+}
+
+}  // namespace etv
+
+extern "C" size_t etv_reorder_beams_workspace_bytes(int32_t B, int32_t K, int32_t M, int32_t max_blocks) {
+    if (B < 0 || K < 1 || M < 1 || K > ETV_MAX_BEAMS || M > ETV_MAX_BEAMS || B > 65535 || max_blocks < 1 || max_blocks > (1 << 22)) return 0;
+    return etv::reorder_bytes(B, K, M, max_blocks);
+}
+
+extern "C" int32_t etv_reorder_beams(const etv_cache_desc *h, void *k_cache, void *v_cache, const int32_t *block_table, const int32_t *len, int32_t K,
+                                     const int32_t *parent, int32_t M, int32_t *free_blocks, const int32_t *free_state, int32_t *table_out,
+                                     int32_t *free_state_out, int32_t *status, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!h || h->block_size < 0 || h->d < 1 || h->cache_layer_stride < 0) return ETV_ERR_INVALID_ARG;
+    if (h->block_size == 0) return ETV_ERR_UNIMPLEMENTED;
+    if ((h->elem_bytes != 2 && h->elem_bytes != 4) || (int64_t)h->d * h->elem_bytes % 16 || h->d > (1 << 16)) return ETV_ERR_UNSUPPORTED;
+    const etv::ReorderShape sh{h->B, K, M, h->max_blocks, h->num_blocks, h->block_size, etv::reorder_chunks(h->max_blocks)};
+    etv::CacheParts cache{};
+    cache.parts = 2, cache.Hkv = h->Hkv, cache.n_layers = h->n_layers;
+    for (int i = 0; i < 2; i++) {
+        cache.base[i] = static_cast<uint8_t *>(i ? v_cache : k_cache);
+        cache.layer_bytes[i] = (size_t)h->cache_layer_stride * h->elem_bytes;
+        cache.row_bytes[i] = h->d * h->elem_bytes;
+    }
+    if (h->n_layers > 1 && cache.layer_bytes[0] % 16) return ETV_ERR_UNSUPPORTED;
+    return etv::reorder(sh, cache, block_table, len, parent, free_blocks, free_state, table_out, free_state_out, status, workspace, workspace_bytes, stream);
+}
+
+extern "C" int32_t etv_reorder_beams_q4(const etv_q4_desc *h, uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales,
+                                        const int32_t *block_table, const int32_t *len, int32_t K, const int32_t *parent, int32_t M, int32_t *free_blocks,
+                                        const int32_t *free_state, int32_t *table_out, int32_t *free_state_out, int32_t *status, void *workspace,
+                                        size_t workspace_bytes, void *stream) {
+    if (!h || h->block_size < 0 || h->layer_rows < 0) return ETV_ERR_INVALID_ARG;
+    if (h->block_size == 0) return ETV_ERR_UNIMPLEMENTED;
+    if (h->block_size % 16 || (h->d != 64 && h->d != 128)) return ETV_ERR_UNSUPPORTED;
+    const etv::ReorderShape sh{h->B, K, M, h->max_blocks, h->num_blocks, h->block_size, etv::reorder_chunks(h->max_blocks)};
+    etv::CacheParts cache{};
+    cache.parts = 4, cache.Hkv = h->Hkv, cache.n_layers = h->n_layers;
+    uint8_t *base[4] = {k_codes, v_codes, k_scales, v_scales};
+    for (int i = 0; i < 4; i++) {
+        cache.base[i] = base[i];
+        cache.row_bytes[i] = h->d / (i < 2 ? 2 : 32);
+        cache.layer_bytes[i] = (size_t)h->layer_rows * cache.row_bytes[i];
+    }
+    return etv::reorder(sh, cache, block_table, len, parent, free_blocks, free_state, table_out, free_state_out, status, workspace, workspace_bytes, stream);
+}

@@ -1,0 +1,138 @@
+"""beam_select on the GPU against its definition in 64 bits: the choices exactly, the scores to their rounding."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import beam_plain
+from paper_2603_08088_amd import api
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def dev(a, dtype=np.int32):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=dtype)).cuda()
+
+
+def check(logits, scores, M, n_beams=None, finished=None, end=-1, **kw):
+    """logits: a host tensor [B, K, V]."""
+    r = api.beam_select(kw.pop("on", None) if "on" in kw else logits.cuda(), dev(scores, np.float32), M, n_beams=None if n_beams is None else dev(n_beams),
+                        finished=None if finished is None else dev(finished, np.uint8), end_token=end, **kw)
+    with np.errstate(invalid="ignore"):
+        best, parent, token, ended, status = beam_plain.select(logits.double().numpy(), np.asarray(scores, dtype=np.float32), M, n_beams, finished, end)
+    assert np.array_equal(r["parent"].cpu().numpy(), parent) and np.array_equal(r["token"].cpu().numpy(), token)
+    assert np.array_equal(r["finished"].cpu().numpy(), ended) and r["status"].tolist() == status
+    got = r["scores"].double().cpu().numpy()
+    fine = np.isfinite(best)
+    assert np.array_equal(got[~fine], best[~fine])
+    # the sum's relative error of 1e-8 is the total's absolute one; then a rounding to fp32
+    assert (np.abs(got[fine] - best[fine]) <= 1e-8 + 2.0 ** -24 * np.abs(best[fine]) * (1 + 1e-6)).all()
+    return r
+
+
+def normal(rng, shape, dtype, spread=2.0):
+    return torch.from_numpy((spread * rng.standard_normal(shape)).astype(np.float32)).to(DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,K,M,V", [(1, 1, 1, 1), (1, 1, 8, 5), (2, 3, 4, 7), (1, 4, 4, 1000), (3, 8, 8, 4097), (2, 10, 10, 32000), (1, 64, 64, 3001), (4, 5, 64, 8192),
+                                     (1, 1, 60, 50021), (70, 2, 3, 300), (2, 64, 1, 2048)])
+def test_the_best_continuations(B, K, M, V, dtype):
+    rng = np.random.default_rng(V + M)
+    check(normal(rng, (B, K, V), dtype), -5 * rng.random((B, K)), M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad", [0, 1, 3, 8])
+def test_rows_apart_and_odd_vocabularies(dtype, pad):
+    """Rows that begin at any element; what lies between them is not looked at."""
+    rng = np.random.default_rng(pad)
+    B, K, V = 3, 5, 5003
+    whole = torch.full((B + 1, K + 1, V + pad), float("nan"), dtype=DT[dtype])
+    x = normal(rng, (B, K, V), dtype)
+    whole[1:, 1:, :V] = x
+    check(x, -rng.random((B, K)), 7, on=whole.cuda()[1:, 1:, :V])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 4, 33, 64])
+def test_ties_go_to_the_lowest(dtype, M):
+    """Equal logits everywhere, few different values, equal beams: the lower beam, then the lower token."""
+    rng = np.random.default_rng(M)
+    check(torch.zeros((2, 3, 9001), dtype=DT[dtype]), np.zeros((2, 3)), M)
+    check(torch.from_numpy(rng.integers(0, 3, (2, 4, 8193)).astype(np.float32)).to(DT[dtype]), -np.tile(rng.integers(0, 2, (2, 1)), (1, 4)), M)
+    x = normal(rng, (2, 1, 5001), dtype).expand(2, 6, 5001).contiguous()      # six beams alike, each row at another alignment
+    check(x, np.full((2, 6), -1.25), M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masked_logits_finished_and_missing_beams(dtype):
+    rng = np.random.default_rng(9)
+    B, K, V, M = 6, 7, 6007, 9
+    x = normal(rng, (B, K, V), dtype)
+    x[torch.from_numpy(rng.random((B, K, V)) < 0.995)] = -math.inf
+    x[0, 2] = x[1] = -math.inf                                        # beams that offer nothing, a request that does not
+    x[2, 1, :], x[2, 1, 4000] = -math.inf, 3.0                        # one token, of probability 1
+    x[3, 0, 17] = torch.finfo(DT[dtype]).min                          # lowest value: an offer like any other
+    n, done = rng.integers(0, K + 1, B), (rng.random((B, K)) < 0.3).astype(np.uint8)
+    n[2], done[2, 1], scores = K, 0, -4 * rng.random((B, K))
+    scores[4, :3] = -math.inf
+    check(x, scores, M, n, done, 4000)
+    check(x, scores, M, n, None, 4000)
+    check(x, scores, M, None, done, 0)
+    check(x, scores, M, [0] * B, done, 0)
+    check(x, scores, M, None, np.ones((B, K), dtype=np.uint8), V - 1)
+    lone = torch.full((1, 2, 5000), torch.finfo(DT[dtype]).min, dtype=DT[dtype])
+    check(lone, [[0.0, -1.0]], 5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+def test_beams_that_are_not_finite_offer_nothing_and_are_reported(dtype, what):
+    rng = np.random.default_rng(11)
+    for at in (0, 4095, 4096, 8999):
+        x = normal(rng, (3, 4, 9000), dtype)
+        x[0, 1, at] = x[1, 3, at] = what
+        x[2, 2, at] = what                                            # a finished beam's logits do not matter
+        scores = -rng.random((3, 4))
+        scores[1, 0] = what
+        r = check(x, scores, 6, None, np.array([[0, 0, 0, 0], [0, 0, 0, 0], [0, 0, 1, 0]]), 7)
+        assert r["status"].tolist() == [1, 3, 0]
+
+
+@pytest.mark.parametrize("spread", [0.0, 0.3, 30.0, 1e4])
+def test_totals_far_apart_and_close_together(spread):
+    rng = np.random.default_rng(12)
+    for dtype in DT:
+        check(normal(rng, (2, 6, 20011), dtype, spread), -100 * rng.random((2, 6)), 16)
+    big = torch.from_numpy((3e38 * rng.uniform(-1, 1, (1, 2, 5000))).astype(np.float32))
+    check(big, [[0.0, -1.0]], 8)
+
+
+def test_close_calls_between_beams():
+    """Totals of different beams that differ by a few 1e-8: decided as in 64 bits."""
+    rng = np.random.default_rng(13)
+    x = normal(rng, (4, 2, 30000), "f32", 3.0)
+    f = x.double().numpy()
+    lse = np.log(np.exp(f).sum(-1))
+    top = f.max(-1) - lse
+    # scores in fp32 that make the beams' best totals nearly equal; the nearest are some 1e-7 apart
+    scores = np.stack((-top[:, 0] - 6, -top[:, 1] - 6), 1).astype(np.float32)
+    totals = np.sort(top + scores, 1)
+    gap = totals[:, 1] - totals[:, 0]
+    assert (gap < 1e-6).all()
+    if (gap > 2e-8).all():
+        check(x, scores, 2)
+
+
+def test_the_workspace_may_hold_anything():
+    rng = np.random.default_rng(14)
+    x = normal(rng, (3, 4, 7000), "bf16")
+    n = api.beam_select_workspace_bytes(3, 4, 7000, 5, torch.bfloat16)
+    for fill in (0, 255):
+        ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+        check(x, -rng.random((3, 4)), 5, [4, 0, 2], workspace=ws)
+    r = api.beam_select(x.cuda()[:0], dev(np.zeros((0, 4)), np.float32), 5)
+    assert r["parent"].shape == (0, 5)
