@@ -18,18 +18,18 @@ struct Candidate {
     float x;
     int32_t v;
 };
-constexpr int kScanCap = 384;    // candidates a segment collects before it falls back on one round per candidate
 constexpr int kMaxSteps = 8;     // steps of a segment
-constexpr int kMergeCap = 1024;  // candidates a request collects, as in a segment
+constexpr int kMergeThreads = 512;
+constexpr int kMergeCap = 2048;  // candidates a request collects, as in a segment
 
 // What a beam offers: nothing, its end token, or its row of logits.
 enum { kBeamNone, kBeamDone, kBeamLive, kBeamBad };
 __device__ __forceinline__ int beam_state(const etv_beam_desc &dsc, const float *scores, const int32_t *n_beams, const uint8_t *finished, int b, int k) {
-    if (n_beams && k >= n_beams[b]) return kBeamNone;
+    // asked for together
+    const int beams = n_beams ? n_beams[b] : dsc.K;
     const float s = scores[(size_t)b * dsc.K + k];
-    if (!(s < INFINITY)) return kBeamBad;
-    if (s == -INFINITY) return kBeamNone;
-    return finished && finished[(size_t)b * dsc.K + k] ? kBeamDone : kBeamLive;
+    const int done = finished ? finished[(size_t)b * dsc.K + k] : 0;
+    return k >= beams || s == -INFINITY ? kBeamNone : !(s < INFINITY) ? kBeamBad : done ? kBeamDone : kBeamLive;
 }
 
 // Sixteen bytes of a row of logits, which begins at any element; `get` makes them fp32 where they are used, which keeps bf16 in half the registers.
@@ -42,7 +42,10 @@ struct Logits<float> {
     typedef float vec_at __attribute__((ext_vector_type(4), aligned(4)));
     static __device__ float get(const vec &u, int i) { return u[i]; }
     static __device__ void set(vec &u, int i, float x) { u[i] = x; }
-    static __device__ float none() { return -INFINITY; }
+    // the first n are not there
+    static __device__ void drop(vec &u, int n) {
+        for (int i = 0; i < 4; i++) u[i] = i < n ? -INFINITY : u[i];
+    }
     static __device__ float one(float x) { return x; }
 };
 template <>
@@ -52,7 +55,9 @@ struct Logits<uint16_t> {
     typedef unsigned int vec_at __attribute__((ext_vector_type(4), aligned(2)));
     static __device__ float get(const vec &u, int i) { return __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16); }
     static __device__ void set(vec &u, int i, uint16_t x) { u[i / 2] = i & 1 ? (u[i / 2] & 0xffffu) | (uint32_t)x << 16 : (u[i / 2] & 0xffff0000u) | x; }
-    static __device__ uint16_t none() { return 0xff80; }
+    static __device__ void drop(vec &u, int n) {
+        for (int i = 0; i < 4; i++) u[i] = 2 * i + 1 < n ? 0xff80ff80u : 2 * i < n ? (u[i] & 0xffff0000u) | 0xff80u : u[i];
+    }
     static __device__ float one(uint16_t x) { return bf16_bits_to_float(x); }
 };
 
@@ -69,36 +74,58 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// A number that at least R of the wavefront's 64 values of x reach, none below -FLT_MAX: the R-th largest with the low 16 of its 32 bits cut off,
-// found bit by bit.
-__device__ __forceinline__ float reached_by(float x, int R) {
-    const uint32_t key = order_of(x) >> 16;
+// A number that at least R values reach, none below -FLT_MAX: the R-th largest with the low 16 of its 32 bits cut off, found bit by bit.  `count` tells how
+// many have a key of at least its argument.
+template <int UNROLL = 16, class F>
+__device__ __forceinline__ float reached_by(F count, int R) {
     uint32_t cut = 0;
-#pragma unroll
+#pragma unroll UNROLL
     for (int bit = 15; bit >= 0; bit--) {
         const uint32_t trial = cut | 1u << bit;
-        if (__popcll(__ballot(key >= trial)) >= R) cut = trial;
+        if (count(trial) >= R) cut = trial;
     }
     if (cut <= 0x007fu) return -FLT_MAX;  // the order of -inf
     const uint32_t full = cut << 16;
     return __uint_as_float(full & 0x80000000u ? full ^ 0x80000000u : ~full);
 }
 
+// The largest, and the sum, over 2^width neighbouring lanes, in each of them: within a row of sixteen by lane moves of the vector unit.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)); }
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, false));
+}
+template <class V, class F>
+__device__ __forceinline__ V lanes_join(V v, int width, F f) {
+    if (width > 0) v = f(v, moved<0xb1>(v));   // the neighbour: quads (1, 0, 3, 2)
+    if (width > 1) v = f(v, moved<0x4e>(v));   // the other pair: quads (2, 3, 0, 1)
+    if (width > 2) v = f(v, moved<0x141>(v));  // the other quad, whose lanes are alike: halves of a row mirrored
+    if (width > 3) v = f(v, moved<0x140>(v));  // the other half: rows mirrored
+    if (width > 4) v = f(v, __shfl_xor(v, 16));
+    if (width > 5) v = f(v, __shfl_xor(v, 32));
+    return v;
+}
+__device__ __forceinline__ float lanes_sum(float v, int width) { return lanes_join(v, width, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float lanes_best(float v, int width) { return lanes_join(v, width, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ double lanes_sum(double v, int width) { return lanes_join(v, width, [](double a, double b) { return a + b; }); }
+
 __device__ __forceinline__ double block_sum(double v) {
-    __shared__ double s_part[4];
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+    __shared__ double s_part[kMergeThreads / 64];
+    v = lanes_sum(v, 6);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (s_part[0] + s_part[1]) + (s_part[2] + s_part[3]);
+    v = 0;
+    for (int w = 0; w < kMergeThreads / 64; w++) v += s_part[w];
+    return v;
 }
 
 // The largest key, of equal ones that with the lowest place, over the workgroup.
 template <class K, class P>
 __device__ __forceinline__ void block_best(K &key, P &place) {
-    __shared__ K s_key[4];
-    __shared__ P s_place[4];
+    __shared__ K s_key[kMergeThreads / 64];
+    __shared__ P s_place[kMergeThreads / 64];
     const auto take = [&](K k, P p) {
         if (k > key || (k == key && p < place)) key = k, place = p;
     };
@@ -110,12 +137,12 @@ __device__ __forceinline__ void block_best(K &key, P &place) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) s_key[threadIdx.x >> 6] = key, s_place[threadIdx.x >> 6] = place;
     __syncthreads();
-    for (int w = 0; w < 4; w++) take(s_key[w], s_place[w]);
+    for (int w = 0; w < kMergeThreads / 64; w++) take(s_key[w], s_place[w]);
 }
 
 constexpr double kLog2e = 1.4426950408889634;
 
-// 2^z for -1000 <= z <= 0, to 1.9e-9 of itself: a whole number n, taken off by a sum whose last bit is a one, and a polynomial in what is left (the
+// 2^z for |z| <= 1000, to 1.9e-9 of itself: a whole number n, taken off by a sum whose last bit is a one, and a polynomial in what is left (the
 // smallest relative error on [-1/2, 1/2] at its degree, by Remez's exchange); n goes into the exponent.
 __device__ __forceinline__ double exp2_fast(double z) {
     const double shifted = z + 6755399441055744.0;  // 1.5 * 2^52
@@ -136,20 +163,22 @@ __device__ __forceinline__ float term(float t) { return __builtin_amdgcn_exp2f(f
 constexpr double kTermMean = 1 + 3.4e-9;
 
 // A segment of one row of logits by one wavefront: `steps` times 64 lanes' four vectors, the next step's on their way while one is worked on.  Every
-// logit takes part in the running sum; of the order only the largest of each lane's sixteen or thirty-two is kept.  Those bound the M-th best of
-// the segment from below (a number that M lanes reach), and the few vectors that reach the bound are read again, from the caches, for
-// the candidates, which are ranked by counting.
-template <class T>
+// logit takes part in the running sum; of the order only the largest of every two vectors is kept, the best two of them for each lane.  Those bound the
+// M-th best of the segment from below (a number that M of them reach), and the few vectors that reach the bound are read again, from the
+// caches, for the candidates, which are ranked by counting.  TINY: fewer logits than a vector holds.
+template <class T, bool TINY>
 __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
-                                                       const uint8_t *finished, int splits, int steps, int list, ScanHead *heads, Candidate *cands) {
+                                                       const uint8_t *finished, int splits, uint32_t inv_splits, uint32_t inv_K, int steps, int list, int room,
+                                                       ScanHead *heads, Candidate *cands) {
     constexpr int N = Logits<T>::N, G = 4, E = G * N;
     __shared__ float s_most[kMaxSteps * 64];
-    __shared__ Candidate s_cand[kScanCap];
+    extern __shared__ __attribute__((aligned(16))) Candidate s_cand[];  // [room + 8]
     __shared__ int s_n;
-    const int row = blockIdx.x / splits, split = blockIdx.x - row * splits, b = row / dsc.K, k = row - b * dsc.K, t = threadIdx.x;
-    if (beam_state(dsc, scores, n_beams, finished, b, k) != kBeamLive) return;
+    uint32_t split, k;
+    const int t = threadIdx.x;
+    const uint32_t row = fast_div(blockIdx.x, splits, inv_splits, split), b = fast_div(row, dsc.K, inv_K, k);
     const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
-    const int V = dsc.V, v_begin = split * (64 * E * steps), v_end = min(V, v_begin + 64 * E * steps);
+    const int V = dsc.V, v_begin = (int)split * (64 * E * steps), v_end = min(V, v_begin + 64 * E * steps);
     // Vector g of a step begins at place(): the row's last N logits stand in for a vector that would leave the row, without those of
     // them that belong to the vectors before.
     const auto place = [&](int step, int g) { return v_begin + (step * G + g) * 64 * N + t * N; };
@@ -158,37 +187,36 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 #pragma unroll
         for (int g = 0; g < G; g++) {
             const int v = place(step, g), at = min(v, V - N);
-            raw[g] = vec{};
-            if (V >= N) raw[g] = *reinterpret_cast<const typename Logits<T>::vec_at *>(x + at);
-            else
-                for (int j = 0; j < V; j++) Logits<T>::set(raw[g], j + N - V, x[j]);
+            if (!TINY) raw[g] = *reinterpret_cast<const typename Logits<T>::vec_at *>(x + at);
+            else {
+                raw[g] = vec{};
+#pragma unroll
+                for (int j = 0; j < N; j++) Logits<T>::set(raw[g], j, x[max(at + j, 0)]);
+            }
         }
     };
     const auto mask = [&](vec *raw, int step) {  // only where a step reaches behind the row
 #pragma unroll
-        for (int g = 0; g < G; g++) {
-            const int v = place(step, g), at = min(v, V - N);
-#pragma unroll
-            for (int j = 0; j < N; j++)
-                if (at + j < v) Logits<T>::set(raw[g], j, Logits<T>::none());
-        }
+        for (int g = 0; g < G; g++) Logits<T>::drop(raw[g], place(step, g) - min(place(step, g), V - N));
     };
     if (t == 0) s_n = 0;
     vec raw[G];
     load(raw, 0);
-    float ref = -INFINITY, best = -INFINITY;
+    if (beam_state(dsc, scores, n_beams, finished, b, k) != kBeamLive) return;
+    float ref = -INFINITY, best = -INFINITY, second = -INFINITY;
     double s = 0;
-    int step = 0;
-    for (; step < steps && place(step, 0) - t * N < v_end; step++) {
-        vec next[G];
-        if (step + 1 < steps) load(next, step + 1);
-        if (place(step + 1, 0) - t * N > V) mask(raw, step);
-        float r[E], most = -INFINITY;
+    const auto work = [&](const vec *raw, int step) {
+        float r[E], half[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < E; i++) r[i] = Logits<T>::get(raw[i / N], i % N);
 #pragma unroll
-        for (int i = 0; i < E; i += 2) most = max3(r[i], r[i + 1], most);
+        for (int i = 0; i < E / 2; i += 2) {
+            half[0] = max3(r[i], r[i + 1], half[0]);
+            half[1] = max3(r[E / 2 + i], r[E / 2 + i + 1], half[1]);
+        }
+        const float most = fmaxf(half[0], half[1]);
         s_most[step * 64 + t] = most;
+        second = fmaxf(fmaxf(second, fminf(half[0], half[1])), fminf(best, most));
         best = fmaxf(best, most);
         const float top = wave_best(most, [](float p, float q) { return fmaxf(p, q); });
         if (top > ref) {
@@ -201,40 +229,97 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 #pragma unroll
         for (int i = 0; i < E; i++) part[i % 4] += term(r[i] - from);
         s += (double)(part[0] + part[1]) + (double)(part[2] + part[3]);
+    };
+    const int count = (v_end - v_begin + 64 * E - 1) / (64 * E);
+    // a step ahead: the loop's loads are counted, so that it waits for the older ones alone
+    for (int step = 0; step + 1 < count; step++) {
+        vec next[G];
+        load(next, step + 1);
+        work(raw, step);
 #pragma unroll
         for (int g = 0; g < G; g++) raw[g] = next[g];
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off);
-    s *= kTermMean;
-    const float cut = reached_by(best, dsc.M);
+    const bool reaches_behind = v_begin + count * (64 * E) > V;
+    if (reaches_behind) mask(raw, count - 1);
+    work(raw, count - 1);
+    s = lanes_sum(s, 6) * kTermMean;
+    const uint32_t key = order_of(best) >> 16, key2 = order_of(second) >> 16;
+    const float cut = reached_by([&](uint32_t c) { return __popcll(__ballot(key >= c)) + __popcll(__ballot(key2 >= c)); }, dsc.M);
     uint32_t todo = 0;
-    for (int i = 0; i < step; i++) todo |= (s_most[i * 64 + t] >= cut) << i;
+    for (int i = 0; i < count; i++) todo |= (s_most[i * 64 + t] >= cut) << i;
     while (todo) {
         const int i = __builtin_ctz(todo);
         todo &= todo - 1;
-        load(raw, i);
-        mask(raw, i);
+        if (count > 1) load(raw, i);  // a single step's are still here
+        if (reaches_behind) mask(raw, i);
+        uint32_t hits = 0;
 #pragma unroll
-        for (int j = 0; j < E; j++) {
-            const float y = Logits<T>::get(raw[j / N], j % N);
-            if (y >= cut) {
-                const int at = atomicAdd(&s_n, 1);
-                if (at < kScanCap) s_cand[at] = {y, min(place(i, j / N), V - N) + j % N};
-            }
+        for (int j = 0; j < E; j++) hits |= (uint32_t)(Logits<T>::get(raw[j / N], j % N) >= cut) << j;
+        while (hits) {
+            const int j = __builtin_ctz(hits);
+            hits &= hits - 1;
+            const int v = min(place(i, j / N), V - N) + j % N, at = atomicAdd(&s_n, 1);
+            if (at < room) s_cand[at] = {Logits<T>::one(x[v]), v};
         }
     }
     __syncthreads();
     Candidate *out = cands + (size_t)blockIdx.x * list;
     int n = s_n;
-    if (n <= kScanCap) {
+    if (n > room) {  // large ones side by side in a few lanes: a bound from all logits
+        const auto all = [&](auto f) {
+            for (int v = v_begin + t; v < v_end; v += 64) f(v, Logits<T>::one(x[v]));
+        };
+        const float closer = reached_by<1>(
+            [&](uint32_t c) {
+                int mine = 0;
+                all([&](int, float y) { mine += order_of(y) >> 16 >= c; });
+                return (int)lanes_sum((float)mine, 6);
+            },
+            dsc.M);
+        __syncthreads();
+        if (t == 0) s_n = 0;
+        __syncthreads();
+        all([&](int v, float y) {
+            if (!(y >= closer)) return;
+            const int at = atomicAdd(&s_n, 1);
+            if (at < room) s_cand[at] = {y, v};
+        });
+        __syncthreads();
+        n = s_n;
+    }
+    if (n <= room && n > 2 * dsc.M + 64) {  // ranking takes n^2 steps: first those below a closer bound go
+        const float closer = reached_by<1>(
+            [&](uint32_t c) {
+                int all = 0;
+                for (int i0 = 0; i0 < n; i0 += 64) all += __popcll(__ballot(i0 + t < n && order_of(s_cand[min(i0 + t, n - 1)].x) >> 16 >= c));
+                return all;
+            },
+            dsc.M);
+        int kept = 0;
+        for (int i0 = 0; i0 < n; i0 += 64) {  // closing up behind the reads
+            const Candidate own = s_cand[min(i0 + t, n - 1)];
+            const bool keep = i0 + t < n && own.x >= closer;
+            const uint64_t lanes = __ballot(keep);
+            __syncthreads();
+            if (keep) s_cand[kept + __popcll(lanes & ((1ull << t) - 1))] = own;
+            kept += __popcll(lanes);
+        }
+        n = kept;
+        __syncthreads();
+    }
+    if (n <= room) {
+        if (t < 8) s_cand[n + t] = {-INFINITY, INT32_MAX};  // to a multiple of eight
+        __syncthreads();
         for (int i = t; i < n; i += 64) {
             const Candidate own = s_cand[i];
             int rank = 0;
-            for (int j = 0; j < n; j++) {
-                const Candidate o = s_cand[j];
-                rank += o.x > own.x || (o.x == own.x && o.v < own.v);
-            }
+#pragma unroll 1
+            for (int j0 = 0; j0 < n; j0 += 8)
+#pragma unroll
+                for (int j = j0; j < j0 + 8; j++) {
+                    const Candidate o = s_cand[j];
+                    rank += (o.x > own.x) | ((o.x == own.x) & (o.v < own.v));
+                }
             if (rank < dsc.M) out[rank] = own;
         }
     } else {  // many equal ones: the next best after the last, a round each
@@ -263,54 +348,63 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
 // other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them.
 template <class T>
-__global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
-                                                         const uint8_t *finished, int splits, int list, const ScanHead *heads, const Candidate *cands,
+__global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
+                                                         const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list, const ScanHead *heads, const Candidate *cands,
                                                          float *out_scores, int32_t *parent, int32_t *token, uint8_t *finished_out, int32_t *status) {
     constexpr double kClose = 0x1p-22;
     __shared__ double s_base[ETV_MAX_BEAMS], s_max[ETV_MAX_BEAMS];
     __shared__ int s_state[ETV_MAX_BEAMS], s_status, s_n;
-    __shared__ float s_cut[4];
-    __shared__ double s_total[kMergeCap], s_best[ETV_MAX_BEAMS];
-    __shared__ long s_place[kMergeCap], s_best_place[ETV_MAX_BEAMS];
+    __shared__ float s_cut[kMergeThreads / 64];
+    __shared__ int s_part[2][kMergeThreads / 64];
+    struct Total {
+        double x;
+        long place;
+    };
+    __shared__ Total s_total[kMergeCap + 4], s_best[ETV_MAX_BEAMS];
     __shared__ unsigned int s_again[2];
     const int b = blockIdx.x, t = threadIdx.x;
-    const long V = dsc.V;
     const int lists = dsc.K * splits, M = dsc.M;
     heads += (size_t)b * lists;
     cands += (size_t)b * lists * list;
     if (t == 0) s_status = 0;
     if (t < 2) s_again[t] = 0;
     __syncthreads();
-    // as many lanes a beam as it has segments, up to a wavefront
-    const int width = splits > 32 ? 64 : splits > 16 ? 32 : splits > 8 ? 16 : splits > 4 ? 8 : splits > 2 ? 4 : splits;
-    for (int k0 = 0; k0 < dsc.K; k0 += 256 / width) {
-        const int k = k0 + t / width, lane = t % width;
+    // a thread's first list, on its way while the sums are joined: how many, and the first two
+    int head_n = 0;
+    int4 head = {};
+    if (t < lists) {
+        head_n = heads[t].n;
+        head = *reinterpret_cast<const int4 *>(cands + (size_t)t * list);
+    }
+    // 2^width lanes a beam
+    for (int k0 = 0; k0 < dsc.K; k0 += kMergeThreads >> width) {
+        const int k = k0 + (t >> width), lane = t & ((1 << width) - 1);
+        ScanHead first = {-INFINITY, 0, 0};
+        if (k < dsc.K && lane < splits) first = heads[k * splits + lane];  // of a beam that is not live: anything
         int state = k < dsc.K ? beam_state(dsc, scores, n_beams, finished, b, k) : kBeamNone;
-        double base = 0, most = 0;
-        float m = -INFINITY;
-        double s = 0;
+        float m = first.m;
+        double s = first.s;
         const auto scale = [](float from, float to) { return from > -INFINITY && from != to ? exp2_fast(fmax(((double)from - (double)to) * kLog2e, -1000.0)) : 1.0; };
         if (state == kBeamLive)
-            for (int i = lane; i < splits; i += width) {  // running: the sum is relative to the largest so far
+            for (int i = lane + (1 << width); i < splits; i += 1 << width) {  // running: the sum is relative to the largest so far
                 const ScanHead h = heads[k * splits + i];
                 const float top = fmaxf(m, h.m);
                 s = s * scale(m, top) + h.s * scale(h.m, top);  // without a logit: 0, or NaN
                 m = top;
             }
-        for (int off = 1; off < width; off <<= 1) {
-            const float om = __shfl_xor(m, off), top = fmaxf(m, om);
-            const double os = __shfl_xor(s, off) * scale(om, top), is = s * scale(m, top);
-            s = t & off ? os + is : is + os;
-            m = top;
-        }
+        const float own = m;
+        m = lanes_best(m, width);
+        s = lanes_sum(s * scale(own, m), width);
         if (k < dsc.K && lane == 0) {
-            base = scores[(size_t)b * dsc.K + k];
+            double base = scores[(size_t)b * dsc.K + k], most = 0;
             if (state == kBeamLive) {
                 if (!(s < INFINITY)) {
                     atomicOr(&s_status, ETV_BEAM_BAD_LOGITS);
                     state = kBeamNone;
                 }
-                base -= log(s);
+                // from an fp32 logarithm: s = 2^l (1 + d) with |d| < 2^-20
+                const double l = __builtin_amdgcn_logf((float)s);
+                base -= l * 0.6931471805599453 + fma(s, exp2_fast(-l), -1.0);
                 most = m;
             } else if (state == kBeamBad) {
                 atomicOr(&s_status, ETV_BEAM_BAD_SCORE);
@@ -320,58 +414,140 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
         }
     }
     __syncthreads();
-    // entry i of list l
-    const auto entries = [&](int l) {
-        const int state = s_state[l / splits];
-        return state == kBeamLive ? heads[l].n : state == kBeamDone && l % splits == 0 ? 1 : 0;
+    // entry i of list l, of beam k; places order as (beam, token) do
+    const auto value = [&](const Candidate &c, int k, double &x, long &place) {
+        x = ((double)c.x - s_max[k]) + s_base[k];
+        place = (long)k << 32 | (uint32_t)c.v;
     };
-    const auto entry = [&](int l, int i, double &x, long &place) {
-        const int k = l / splits;
+    const auto entry = [&](int l, int k, int i, double &x, long &place) {
         if (s_state[k] == kBeamLive) {
-            const Candidate c = cands[(size_t)l * list + i];
-            x = ((double)c.x - s_max[k]) + s_base[k];
-            place = k * V + c.v;
+            Candidate c = {__int_as_float(i ? head.z : head.x), i ? head.w : head.y};
+            if (l != t || i > 1) c = cands[(size_t)l * list + i];
+            value(c, k, x, place);
         } else {
             x = s_base[k];
-            place = k * V + dsc.end_token;
+            place = (long)k << 32 | (uint32_t)dsc.end_token;
         }
+    };
+    const auto entries = [&](int l, int &k) {
+        uint32_t rest;
+        k = (int)fast_div(l, splits, inv_splits, rest);
+        const int state = s_state[k];
+        return state == kBeamLive ? l == t ? head_n : heads[l].n : state == kBeamDone && rest == 0 ? 1 : 0;
     };
     int n;
     for (int round = 0;; round++) {
         float top = -INFINITY;
-        for (int l = t; l < lists; l += 256)
-            if (entries(l) > 0) {
+        for (int l = t; l < lists; l += kMergeThreads) {
+            int k;
+            if (entries(l, k) > 0) {
                 double x;
                 long place;
-                entry(l, 0, x, place);
+                entry(l, k, 0, x, place);
                 top = fmaxf(top, (float)x);
             }
-        const float mine = reached_by(top, M);
+        }
+        const uint32_t key = order_of(top) >> 16;
         if (t == 0) s_n = 0;
-        if ((t & 63) == 0) s_cut[t >> 6] = mine;
-        __syncthreads();
-        float cut = fmaxf(fmaxf(s_cut[0], s_cut[1]), fmaxf(s_cut[2], s_cut[3]));
-        cut = fmaxf(cut - fmaxf(fabsf(cut) * 0x1p-21f, 0x1p-20f), -FLT_MAX);  // and those too close to it
-        for (int l = t; l < lists; l += 256) {
-            const int have = entries(l);
-            for (int i = 0; i < have; i++) {
-                double x;
-                long place;
-                entry(l, i, x, place);
-                if (!((float)x >= cut)) break;
-                const int at = atomicAdd(&s_n, 1);
-                if (at < kMergeCap) s_total[at] = x, s_place[at] = place;
+        if (M > 16) {
+            // samples of all lists: where lists are few several threads look into one, `apart` entries from each other
+            int share = 0;
+            while (lists << (share + 1) <= kMergeThreads) share++;
+            const int apart = (M + (1 << share) - 1) >> share, deep = t & ((1 << share) - 1);
+            uint32_t sample = key;
+            if (share) {
+                int k;
+                const int l = t >> share;
+                sample = 0;
+                if (l < lists && deep * apart < entries(l, k)) {
+                    double x;
+                    long place;
+                    entry(l, k, deep * apart, x, place);
+                    sample = order_of((float)x) >> 16;
+                }
             }
+            // a first sample stands for one entry, each further one for `apart`; the parts of a count alternate between two places, for one barrier each
+            int turn = 0;
+            const float all = reached_by<1>(
+                [&](uint32_t c) {
+                    const int part = __popcll(__ballot(!deep && sample >= c)) + apart * __popcll(__ballot(deep && sample >= c));
+                    turn ^= 1;
+                    if ((t & 63) == 0) s_part[turn][t >> 6] = part;
+                    __syncthreads();
+                    int sum = 0;
+#pragma unroll
+                    for (int w = 0; w < kMergeThreads / 64; w++) sum += s_part[turn][w];
+                    return sum;
+                },
+                M);
+            if ((t & 63) == 0) s_cut[t >> 6] = all;
+        } else {       // those of one wavefront are enough: six times as fast
+            const float mine = reached_by([&](uint32_t c) { return __popcll(__ballot(key >= c)); }, M);
+            if ((t & 63) == 0) s_cut[t >> 6] = mine;
         }
         __syncthreads();
-        const int found = s_n;
+        float cut = s_cut[0];
+#pragma unroll
+        for (int w = 1; w < kMergeThreads / 64; w++) cut = fmaxf(cut, s_cut[w]);
+        int found;
+        for (bool counted = false;; counted = true) {
+            cut = fmaxf(cut - fmaxf(fabsf(cut) * 0x1p-21f, 0x1p-20f), -FLT_MAX);  // and those too close to it
+            for (int l = t; l < lists; l += kMergeThreads) {
+                int k;
+                const int have = entries(l, k);
+                const auto collect = [&](int i) {
+                    double x;
+                    long place;
+                    entry(l, k, i, x, place);
+                    if (!((float)x >= cut)) return false;
+                    const int at = atomicAdd(&s_n, 1);
+                    if (at < kMergeCap) s_total[at] = {x, place};
+                    return true;
+                };
+                if (have > 0 && collect(0) && have > 1 && collect(1))
+                    for (int i = 2; i < have && collect(i); i++) {
+                    }
+            }
+            __syncthreads();
+            found = s_n;
+            if (found <= kMergeCap || counted) break;
+            // too many: a bound from all entries, counted in the lists by bisection
+            cut = reached_by<1>(
+                [&](uint32_t c) {
+                    int n = 0;
+                    for (int l = t; l < lists; l += kMergeThreads) {
+                        int k, lo = 0, hi = entries(l, k);
+                        while (lo < hi) {
+                            const int i = (lo + hi) >> 1;
+                            double x;
+                            long place;
+                            entry(l, k, i, x, place);
+                            if (order_of((float)x) >> 16 >= c) lo = i + 1;
+                            else hi = i;
+                        }
+                        n += lo;
+                    }
+                    return (int)block_sum((double)n);
+                },
+                M);
+            __syncthreads();
+            if (t == 0) s_n = 0;
+            __syncthreads();
+        }
         if (found <= kMergeCap) {
-            for (int i = t; i < found; i += 256) {
-                const double x = s_total[i];
-                const long place = s_place[i];
+            if (t < 4) s_total[found + t] = {-INFINITY, INT64_MAX};  // to a multiple of four
+            __syncthreads();
+            for (int i = t; i < found; i += kMergeThreads) {
+                const Total own = s_total[i];
                 int rank = 0;
-                for (int j = 0; j < found; j++) rank += s_total[j] > x || (s_total[j] == x && s_place[j] < place);
-                if (rank < M) s_best[rank] = x, s_best_place[rank] = place;
+#pragma unroll 1
+                for (int j0 = 0; j0 < found; j0 += 4)
+#pragma unroll
+                    for (int j = j0; j < j0 + 4; j++) {
+                        const Total o = s_total[j];
+                        rank += (o.x > own.x) | ((o.x == own.x) & (o.place < own.place));
+                    }
+                if (rank < M) s_best[rank] = own;
             }
             n = min(found, M);
         } else {
@@ -380,12 +556,13 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
             for (n = 0; n < M; n++) {
                 double best = -INFINITY;
                 long at = INT64_MAX;
-                for (int l = t; l < lists; l += 256) {
-                    const int have = entries(l);
+                for (int l = t; l < lists; l += kMergeThreads) {
+                    int k;
+                    const int have = entries(l, k);
                     for (int i = 0; i < have; i++) {
                         double x;
                         long place;
-                        entry(l, i, x, place);
+                        entry(l, k, i, x, place);
                         if ((x < last || (x == last && place > last_place)) && (x > best || (x == best && place < at))) {
                             best = x, at = place;
                             break;  // a list is in order
@@ -394,7 +571,7 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
                 }
                 block_best(best, at);
                 if (best == -INFINITY) break;
-                if (t == 0) s_best[n] = best, s_best_place[n] = at;
+                if (t == 0) s_best[n] = {best, at};
                 last = best, last_place = at;
             }
         }
@@ -402,24 +579,25 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
         if (round) break;
         // Two totals of different beams too close to call: neighbours of the M best, or the last of them and one left out.  (Equal ones are those of
         // equal rows.)
-        const auto call = [&](double x, long place, double y, long other) {
-            const int k = (int)(place / V), k1 = (int)(other / V);
-            if (k != k1 && x > y && x - y < kClose) {
+        const auto call = [&](const Total &a, const Total &o) {
+            const int k = (int)(a.place >> 32), k1 = (int)(o.place >> 32);
+            if (k != k1 && a.x > o.x && a.x - o.x < kClose) {
                 atomicOr(&s_again[k >> 5], 1u << (k & 31));
                 atomicOr(&s_again[k1 >> 5], 1u << (k1 & 31));
             }
         };
-        if (t + 1 < n) call(s_best[t], s_best_place[t], s_best[t + 1], s_best_place[t + 1]);
+        if (t + 1 < n) call(s_best[t], s_best[t + 1]);
         if (n == M && found <= kMergeCap) {
-            for (int i = t; i < found; i += 256) call(s_best[M - 1], s_best_place[M - 1], s_total[i], s_place[i]);
+            for (int i = t; i < found; i += kMergeThreads) call(s_best[M - 1], s_total[i]);
         } else if (n == M) {
-            for (int l = t; l < lists; l += 256) {
-                const int have = entries(l);
+            for (int l = t; l < lists; l += kMergeThreads) {
+                int k;
+                const int have = entries(l, k);
                 for (int i = 0; i < have; i++) {
                     double x;
                     long place;
-                    entry(l, i, x, place);
-                    call(s_best[M - 1], s_best_place[M - 1], x, place);
+                    entry(l, k, i, x, place);
+                    call(s_best[M - 1], {x, place});
                 }
             }
         }
@@ -431,7 +609,7 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
             if (s_state[k] != kBeamLive) continue;
             const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
             double s = 0;
-            for (int v = t; v < dsc.V; v += 256) s += exp2_fast(fmax(((double)Logits<T>::one(x[v]) - s_max[k]) * kLog2e, -1000.0));
+            for (int v = t; v < dsc.V; v += kMergeThreads) s += exp2_fast(fmax(((double)Logits<T>::one(x[v]) - s_max[k]) * kLog2e, -1000.0));
             s = block_sum(s);
             // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
             if (t == 0) s_base[k] = rint(((double)scores[(size_t)b * dsc.K + k] - log(s)) * 0x1p40) * 0x1p-40;
@@ -440,10 +618,10 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
     }
     if (t < M) {
         const bool found = t < n;
-        const long place = found ? s_best_place[t] : 0;
-        const int k = (int)(place / V), v = (int)(place - k * V);
+        const long place = found ? s_best[t].place : 0;
+        const int k = (int)(place >> 32), v = (int)place;
         const size_t o = (size_t)b * M + t;
-        out_scores[o] = found ? (float)s_best[t] : -INFINITY;
+        out_scores[o] = found ? (float)s_best[t].x : -INFINITY;
         parent[o] = found ? k : -1;
         token[o] = found ? v : -1;
         if (finished_out) finished_out[o] = found && (s_state[k] == kBeamDone || v == dsc.end_token);
@@ -452,11 +630,12 @@ __global__ void __launch_bounds__(256) beam_merge_kernel(etv_beam_desc dsc, cons
 }
 
 // Steps of a wavefront's segment: more of them mean fewer lists to merge, fewer more wavefronts.
+constexpr int kFullWaves = 4096;
 static int beam_step(const etv_beam_desc *h) { return 64 * (h->dtype == ETV_BF16 ? 32 : 16); }
 static int beam_steps(const etv_beam_desc *h) {
     const int64_t rows = (int64_t)h->B * h->K, all = (h->V + beam_step(h) - 1) / beam_step(h);
     int n = 1;
-    while (n < kMaxSteps && rows * ((all + 2 * n - 1) / (2 * n)) >= 4096) n *= 2;
+    while (n < kMaxSteps && rows * ((all + 2 * n - 1) / (2 * n)) >= kFullWaves) n *= 2;
     return n;
 }
 static int beam_splits(const etv_beam_desc *h) {
@@ -464,7 +643,7 @@ static int beam_splits(const etv_beam_desc *h) {
     return (int)((h->V + segment - 1) / segment);
 }
 
-static int beam_list(const etv_beam_desc *h) { return (h->M + 3) & ~3; }
+static int beam_list(const etv_beam_desc *h) { return (h->M + 1) & ~1; }
 
 static int32_t check_beam(const etv_beam_desc *h) {
     if (!h || h->B < 0 || h->K < 1 || h->M < 1 || h->V < 1 || h->end_token < -1 || h->end_token >= h->V) return ETV_ERR_INVALID_ARG;
@@ -500,10 +679,17 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
     hipStream_t s = etv::as_stream(stream);
     const auto run = [&](auto *x) {
         using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
-        hipLaunchKernelGGL(etv::beam_scan_kernel<T>, dim3(lists), dim3(64), 0, s, *h, x, scores, n_beams, finished, splits, steps, list, heads, cands);
+        const auto scan = h->V < etv::Logits<T>::N ? etv::beam_scan_kernel<T, true> : etv::beam_scan_kernel<T, false>;
+        const uint32_t inv_splits = etv::fast_div_inv(splits);
+        // room for the candidates: some times M where lists are short against the lanes, more of it fewer wavefronts at a time
+        const int room = h->M <= 16 ? 256 : h->M <= 32 ? 512 : 1024;
+        hipLaunchKernelGGL(scan, dim3(lists), dim3(64), (room + 8) * sizeof(etv::Candidate), s, *h, x, scores, n_beams, finished, splits, inv_splits,
+                           etv::fast_div_inv(h->K), steps, list, room, heads, cands);
         const int32_t rc = etv::check_launch();
         if (rc != ETV_OK) return rc;
-        hipLaunchKernelGGL(etv::beam_merge_kernel<T>, dim3(h->B), dim3(256), 0, s, *h, x, scores, n_beams, finished, splits, list, heads, cands, out_scores,
+        int width = 0;  // as many lanes a beam as it has segments, up to a wavefront
+        while (width < 6 && (1 << width) < splits) width++;
+        hipLaunchKernelGGL(etv::beam_merge_kernel<T>, dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits, width, list, heads, cands, out_scores,
                            parent, token, finished_out, status);
         return etv::check_launch();
     };
