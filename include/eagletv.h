@@ -596,7 +596,7 @@ ETV_API int32_t etv_resize_block_tables(const etv_pages_desc *h_desc, const int3
  *   (x, y) -> scale * (x cos - y sin, y cos + x sin)
  * where (x, y) are channels (i, i + rot_dim/2), or (2i, 2i+1) with ETV_ROTARY_INTERLEAVED; channels from rot_dim on are copied.
  * ETV_ROTARY_INVERSE turns by -angle: the gradient of the call, and the way back to unencoded rows.
- * Rows t >= n_rows[b] are padding: nothing is read or written for them.
+ * Rows t >= n_rows[b] are padding: nothing is written for them.
  * A row of k and v goes to slot slot_map[b, t] of the cache (as etv_resize_block_tables writes them; contiguous: b * P_cap + p), unless
  * that is outside [0, cache_rows).  Two rows of a call must not have one slot.
  *

@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     };
     const auto entry = [&](int l, int k, int i, double &x, long &place) {
         if (s_state[k] == kBeamLive) {
-            Candidate c = {__int_as_float(i ? head.z : head.x), i ? head.w : head.y};
+            Candidate c = {__int_as_float(i ? +head.z : +head.x), i ? +head.w : +head.y};
             if (l != t || i > 1) c = cands[(size_t)l * list + i];
             value(c, k, x, place);
         } else {

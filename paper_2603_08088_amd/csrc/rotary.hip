@@ -48,77 +48,98 @@ struct Vec<uint16_t> {
         }
     }
     static __device__ u32x4 store(const float *x) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
         u32x4 u;
-        for (int i = 0; i < 4; i++) u[i] = float_to_bf16_bits(x[2 * i]) | (uint32_t)float_to_bf16_bits(x[2 * i + 1]) << 16;
+        for (int i = 0; i < 4; i++) u[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector((f2){x[2 * i], x[2 * i + 1]}, b2));
         return u;
     }
 };
 
-// One token a workgroup: its sines and cosines once, in LDS, for all heads; then 16-byte vectors in pairs, both members of a channel pair with one lane.
-template <class T>
+// One token a workgroup.  A thread has the same place in every head it comes to -- two 16-byte vectors, both members of a channel pair among them -- so
+// that its sines and cosines, worked out once for the token and passed around by LDS, stay in its registers.  What bounds it is memory,
+// and for few tokens the chain of loads: what the arguments alone say the place of is asked for before the angles are worked out, the first
+// head's vectors among it, and every further head's before the one before it is finished.
+template <class T, bool INTER>
 __global__ void __launch_bounds__(256) rotary_kernel(etv_rotary_desc dsc, RotaryPtrs p, const int32_t *positions, const float *inv_freq,
-                                                     const int32_t *n_rows, const int32_t *slot_map, uint32_t inv_T) {
+                                                     const int32_t *n_rows, const int32_t *slot_map, uint32_t inv_T, uint32_t inv_upr, uint32_t inv_bs) {
     constexpr int N = Vec<T>::N;
     __shared__ float2 s_turn[128];
-    const int t = threadIdx.x, half = dsc.rot_dim / 2;
-    uint32_t row;
+    const int t = threadIdx.x, half = dsc.rot_dim / 2, upr = dsc.d / (2 * N), turning = half / N;
+    uint32_t row, u32;
     const uint32_t b = fast_div(blockIdx.x, dsc.T, inv_T, row);
-    if (n_rows && (int)row >= n_rows[b]) return;
-    for (int i = t; i < half; i += 256)
-        s_turn[i] = turn_of(positions[((size_t)dsc.axis_of[i] * dsc.B + b) * dsc.T + row], inv_freq[i], dsc.scale, dsc.flags & ETV_ROTARY_INVERSE);
-    __syncthreads();
+    const int first = (int)fast_div(t, upr, inv_upr, u32), u = (int)u32, step = (int)fast_div(256, upr, inv_upr, u32);
+    const bool turns = u < turning;
+    const int at = !turns ? dsc.rot_dim + (u - turning) * 2 * N : (INTER ? 2 : 1) * u * N, gap = turns && !INTER ? half : N;
+    // heads of q, then of k, then of v; the remainder of the 256 threads has none
+    const int heads = first < step ? dsc.Hq + dsc.Hkv + (p.v ? dsc.Hkv : 0) : 0;
+    const auto rows_of = [&](const void *base, int i) { return static_cast<const T *>(base) + b * dsc.strides[2 * i] + row * dsc.strides[2 * i + 1]; };
+    const T *src[3] = {rows_of(p.q, 0), rows_of(p.k, 1), rows_of(p.v, 2)};
+    const auto pick = [&](int head, const auto &q, const auto &k, const auto &v, int &h) {
+        const bool not_q = head >= dsc.Hq, is_v = head >= dsc.Hq + dsc.Hkv;
+        h = head - (not_q ? dsc.Hq : 0) - (is_v ? dsc.Hkv : 0);
+        return is_v ? v : not_q ? k : q;
+    };
+    const auto load = [&](int head, u32x4 &ra, u32x4 &rb) {
+        int h;
+        const T *from = pick(head, +src[0], +src[1], +src[2], h) + h * dsc.d + at;
+        ra = *reinterpret_cast<const u32x4 *>(from);
+        rb = *reinterpret_cast<const u32x4 *>(from + gap);
+    };
+    u32x4 ra = {}, rb = {};
+    if (first < heads) load(first, ra, rb);
+    const int rows = n_rows ? n_rows[b] : dsc.T;
     long slot = slot_map ? slot_map[blockIdx.x] : -1;
+    if (t < half) {
+        const float f = inv_freq[t];
+        s_turn[t] = turn_of(positions[((size_t)dsc.axis_of[t] * dsc.B + b) * dsc.T + row], f, dsc.scale, dsc.flags & ETV_ROTARY_INVERSE);
+    }
+    __syncthreads();
+    if ((int)row >= rows) return;
     if (slot >= dsc.cache_rows) slot = -1;
-    const int upr = dsc.d / (2 * N), turning = half / N, units = (dsc.Hq + 2 * dsc.Hkv) * upr;
-    for (int x = t; x < units; x += 256) {
-        const int head = x / upr, u = x - head * upr;
-        const int which = head < dsc.Hq ? 0 : head < dsc.Hq + dsc.Hkv ? 1 : 2;
-        const int h = head - (which == 0 ? 0 : which == 1 ? dsc.Hq : dsc.Hq + dsc.Hkv);
-        const T *src = static_cast<const T *>(which == 0 ? p.q : which == 1 ? p.k : p.v);
-        T *out = static_cast<T *>(which == 0 ? p.q_out : which == 1 ? p.k_out : p.v_out);
-        T *cache = static_cast<T *>(which == 0 ? nullptr : which == 1 ? p.k_cache : p.v_cache);
-        if (!src) continue;
-        const int at = dsc.flags & ETV_ROTARY_INTERLEAVED || u >= turning ? (u < turning ? 2 * u * N : dsc.rot_dim + (u - turning) * 2 * N) : u * N;
-        const int gap = dsc.flags & ETV_ROTARY_INTERLEAVED || u >= turning ? N : half;
-        src += b * dsc.strides[2 * which] + row * dsc.strides[2 * which + 1] + h * dsc.d + at;
-        u32x4 ra = *reinterpret_cast<const u32x4 *>(src), rb = *reinterpret_cast<const u32x4 *>(src + gap);
-        if (which < 2 && u < turning) {
+    uint32_t off = 0;
+    const uint32_t block = slot >= 0 && dsc.block_size > 0 ? fast_div((uint32_t)slot, dsc.block_size, inv_bs, off) : 0;
+    // where head 0 of the slot lies, and how far apart heads are
+    const long cache_at = (dsc.block_size ? (long)block * dsc.Hkv * dsc.block_size + off : slot * dsc.Hkv) * dsc.d + at;
+    const long cache_head = (long)(dsc.block_size ? dsc.block_size : 1) * dsc.d;
+    T *out[3] = {const_cast<T *>(rows_of(p.q_out, 3)), const_cast<T *>(rows_of(p.k_out, 4)), const_cast<T *>(rows_of(p.v_out, 5))};
+    float2 turn[N];
+#pragma unroll
+    for (int j = 0; j < N; j++) turn[j] = turns ? s_turn[u * N + j] : make_float2(1, 0);
+    for (int head = first; head < heads; head += step) {
+        u32x4 na = {}, nb = {};
+        if (head + step < heads) load(head + step, na, nb);
+        int h;
+        const int which = pick(head, 0, 1, 2, h);
+        if (turns && which < 2) {
             float xa[N], xb[N];
             Vec<T>::load(ra, xa);
             Vec<T>::load(rb, xb);
-            if (dsc.flags & ETV_ROTARY_INTERLEAVED) {
+            const auto rotate = [](float &x, float &y, const float2 &c) {
+                const float was = x;
+                x = was * c.x - y * c.y;
+                y = y * c.x + was * c.y;
+            };
 #pragma unroll
-                for (int j = 0; j < N; j += 2) {
-                    const float2 ca = s_turn[u * N + j / 2], cb = s_turn[u * N + N / 2 + j / 2];
-                    const float a0 = xa[j], b0 = xb[j];
-                    xa[j] = a0 * ca.x - xa[j + 1] * ca.y;
-                    xa[j + 1] = xa[j + 1] * ca.x + a0 * ca.y;
-                    xb[j] = b0 * cb.x - xb[j + 1] * cb.y;
-                    xb[j + 1] = xb[j + 1] * cb.x + b0 * cb.y;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; j++) {
-                    const float2 c = s_turn[u * N + j];
-                    const float a0 = xa[j];
-                    xa[j] = a0 * c.x - xb[j] * c.y;
-                    xb[j] = xb[j] * c.x + a0 * c.y;
-                }
+            for (int j = 0; j < N; j++) {
+                if (!INTER) rotate(xa[j], xb[j], turn[j]);
+                else if (j < N / 2) rotate(xa[2 * j], xa[2 * j + 1], turn[j]);
+                else rotate(xb[2 * j - N], xb[2 * j - N + 1], turn[j]);
             }
             ra = Vec<T>::store(xa);
             rb = Vec<T>::store(xb);
         }
-        if (out) {
-            out += b * dsc.strides[6 + 2 * which] + row * dsc.strides[7 + 2 * which] + h * dsc.d + at;
-            *reinterpret_cast<u32x4 *>(out) = ra;
-            *reinterpret_cast<u32x4 *>(out + gap) = rb;
+        if (pick(head, p.q_out, p.k_out, p.v_out, h)) {
+            T *to = pick(head, +out[0], +out[1], +out[2], h) + h * dsc.d + at;
+            *reinterpret_cast<u32x4 *>(to) = ra;
+            *reinterpret_cast<u32x4 *>(to + gap) = rb;
         }
-        if (cache && slot >= 0) {
-            const long bs = dsc.block_size;
-            cache += (bs ? ((slot / bs * dsc.Hkv + h) * bs + slot % bs) : slot * dsc.Hkv + h) * dsc.d + at;
-            *reinterpret_cast<u32x4 *>(cache) = ra;
-            *reinterpret_cast<u32x4 *>(cache + gap) = rb;
+        if (slot >= 0 && which > 0) {
+            T *to = static_cast<T *>(which == 1 ? p.k_cache : p.v_cache) + cache_at + h * cache_head;
+            *reinterpret_cast<u32x4 *>(to) = ra;
+            *reinterpret_cast<u32x4 *>(to + gap) = rb;
         }
+        ra = na, rb = nb;
     }
 }
 
@@ -151,8 +172,10 @@ extern "C" int32_t etv_rotary_write_kv(const etv_rotary_desc *h, const void *q, 
     etv_rotary_desc d = *h;
     if (d.scale == 0) d.scale = 1;
     const etv::RotaryPtrs p{q, k, v, q_out, k_out, v_out, k_cache, v_cache};
-    const auto kernel = d.dtype == ETV_BF16 ? etv::rotary_kernel<uint16_t> : etv::rotary_kernel<float>;
+    const bool inter = d.flags & ETV_ROTARY_INTERLEAVED;
+    const auto kernel = d.dtype == ETV_BF16 ? (inter ? etv::rotary_kernel<uint16_t, true> : etv::rotary_kernel<uint16_t, false>)
+                                            : (inter ? etv::rotary_kernel<float, true> : etv::rotary_kernel<float, false>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(d.B * d.T)), dim3(256), 0, etv::as_stream(stream), d, p, positions, inv_freq, n_rows, slot_map,
-                       etv::fast_div_inv(d.T));
+                       etv::fast_div_inv(d.T), etv::fast_div_inv(d.d * (d.dtype == ETV_BF16 ? 2 : 4) / 32), d.block_size ? etv::fast_div_inv(d.block_size) : 0);
     return etv::check_launch();
 }
