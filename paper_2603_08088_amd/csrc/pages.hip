@@ -5,6 +5,7 @@
 namespace etv {
 
 constexpr int kSlotsPerWg = 1024;  // elements of slot_map that a workgroup writes
+constexpr int kFewRows = 64;       // up to so many new rows a thread checks the blocks of a sequence by itself
 constexpr int kMaxRow = 1 << 22;   // longest table row: 256 of them are counted in 31 bits
 
 // What the lengths alone say of a sequence.
@@ -27,52 +28,65 @@ __device__ __forceinline__ PagePlan page_plan(const etv_pages_desc &dsc, uint32_
     return p;
 }
 
-// Workgroup 0: what is given back, and the ring's new state.  256 sequences at a time; a wavefront walks the table entries of one.
+// Workgroup 0: what is given back, and the ring's new state.  256 sequences at a time; those that give are put in a list, whose sequences the
+// wavefronts share out among themselves.
 __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int32_t *len, const int32_t *new_len, const int32_t *block_table,
-                          int32_t *free_blocks, const Ring &ring, int32_t *free_state_out, int32_t *len_out, int32_t *slot_map, int32_t *status) {
-    __shared__ int s_first[256], s_give[256], s_bad[256];
-    __shared__ long s_at[256], s_most[2];
+                          int32_t *free_blocks, const Ring &ring, int32_t *free_state_out, int32_t *len_out, int32_t *status) {
+    struct Giver {
+        int b, first, n, bad;
+        long at;
+    };
+    __shared__ Giver s_giver[256];
+    __shared__ unsigned long long s_most[2];
     const int t = threadIdx.x, lane = t & 63;
     if (t < 2) s_most[t] = 0;
     long taken = 0, given = 0;
-    const long room = ring.room();
     for (int b0 = 0; b0 < dsc.B; b0 += 256) {
         const int b = b0 + t;
+        int L = 0, N = 0;
         PagePlan p{0, 0, 0};
-        if (b < dsc.B) p = page_plan(dsc, inv_bs, len[b], new_len[b]);
-        s_first[t] = p.want;
-        s_give[t] = p.give();
-        s_bad[t] = 0;
-        const int take = p.take();
-        const long t_end = block_scan_sum(take, taken);
-        if (take > 0 && t_end <= ring.count) atomicMax((unsigned long long *)&s_most[0], (unsigned long long)t_end);
+        if (b < dsc.B) {
+            L = len[b], N = new_len[b];
+            p = page_plan(dsc, inv_bs, L, N);
+        }
+        const int take = p.take(), give = p.give();
+        const long t_end = block_scan_sum(take, taken);  // a barrier, too: s_most is set
+        if (take > 0 && t_end <= ring.count) atomicMax(&s_most[0], (unsigned long long)t_end);
+        if (!__syncthreads_or(give)) continue;
+        long before = 0;
+        const int place = (int)block_scan_sum(give > 0, before) - 1, n = (int)before;
+        if (give > 0) s_giver[place] = {b, p.want, give, 0, 0};
         __syncthreads();
-        for (int s = t >> 6; s < 256; s += 4) {
-            const int32_t *row = block_table + (size_t)(b0 + s) * dsc.max_blocks + s_first[s];
+        for (int s = t >> 6; s < n; s += 4) {
+            const int32_t *row = block_table + (size_t)s_giver[s].b * dsc.max_blocks + s_giver[s].first;
             int bad = 0;
-            for (int j = lane; j < s_give[s]; j += 64) bad |= (uint32_t)row[j] >= (uint32_t)dsc.num_blocks;
-            if (bad) s_bad[s] = 1;
+#pragma unroll 4
+            for (int j = lane; j < s_giver[s].n; j += 64) bad |= (uint32_t)row[j] >= (uint32_t)dsc.num_blocks;
+            if (bad) s_giver[s].bad = 1;
         }
         __syncthreads();
-        const int give = s_bad[t] ? 0 : s_give[t];
-        const long g_end = block_scan_sum(give, given);
-        int32_t st = s_bad[t] ? ETV_COMMIT_BAD_BLOCK : give > 0 && g_end > room ? ETV_BRANCH_BAD_FREE : 0;
-        if (give > 0 && !st) atomicMax((unsigned long long *)&s_most[1], (unsigned long long)g_end);
-        s_at[t] = g_end - give;
-        if (st) s_give[t] = 0;
-        if (b < dsc.B && p.give() > 0) {
+        // in the order of the sequences, which is that of the list
+        const int good = give > 0 && !s_giver[place].bad ? give : 0;
+        const long g_end = block_scan_sum(good, given);
+        if (give > 0) {
+            const int32_t st = !good ? ETV_COMMIT_BAD_BLOCK : g_end > ring.room() ? ETV_BRANCH_BAD_FREE : 0;
+            if (!st) atomicMax(&s_most[1], (unsigned long long)g_end);
+            s_giver[place].at = ring.count + g_end - good;
+            if (st) s_giver[place].n = 0;
             status[b] = st;
-            len_out[b] = st ? len[b] : new_len[b];
+            len_out[b] = st ? L : N;
         }
         __syncthreads();
-        for (int s = t >> 6; s < 256; s += 4) {
-            const int32_t *row = block_table + (size_t)(b0 + s) * dsc.max_blocks + s_first[s];
-            for (int j = lane; j < s_give[s]; j += 64) free_blocks[ring.place(ring.count + s_at[s] + j)] = row[j];
+        for (int s = t >> 6; s < n; s += 4) {
+            const Giver g = s_giver[s];
+            const int32_t *row = block_table + (size_t)g.b * dsc.max_blocks + g.first;
+#pragma unroll 4
+            for (int j = lane; j < g.n; j += 64) free_blocks[ring.place(g.at + j)] = row[j];
         }
         __syncthreads();
     }
     __syncthreads();
-    if (t == 0) ring.leave(free_state_out, s_most[0], s_most[1]);
+    if (t == 0) ring.leave(free_state_out, (long)s_most[0], (long)s_most[1]);
 }
 
 // Workgroups 1 ..: kSlotsPerWg elements of the slot map each, and the new table entries, lengths and status of the sequences that start in
@@ -89,7 +103,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
     const int nb = b_hi - b_lo + 1;
     long mine = 0;
     for (int b = t; b < b_lo; b += 256) mine += page_plan(dsc, inv_bs, len[b], new_len[b]).take();
-    long base = block_sum(mine);
+    long base = b_lo > 0 ? block_sum(mine) : 0;
     for (int s0 = 0; s0 < nb; s0 += 256) {
         const int s = s0 + t, b = b_lo + s;
         PagePlan p{0, 0, 0};
@@ -108,7 +122,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
             tail = block_table[(size_t)b * dsc.max_blocks + p.old - 1];
             if (!st && (uint32_t)tail >= (uint32_t)dsc.num_blocks) st = ETV_COMMIT_BAD_BLOCK;
         }
-        if (!st)
+        if (!st && dsc.S <= kFewRows)
             for (int j = 0; j < take; j++)
                 if ((uint32_t)free_blocks[ring.place(end - take + j)] >= (uint32_t)dsc.num_blocks) st = ETV_BRANCH_BAD_FREE;
         s_len[s] = L;
@@ -117,15 +131,36 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
         s_tail[s] = tail;
         s_base[s] = end - take;
         const bool starts = (uint32_t)b * dsc.S >= e0;
-        if (starts && p.give() == 0) {
+        if (starts && p.give() == 0 && (st || take == 0 || dsc.S <= kFewRows)) {
             status[b] = st;
             len_out[b] = st ? L : N;
         }
     }
     __syncthreads();
+    if (dsc.S > kFewRows) {  // few sequences with many blocks each: every workgroup of a sequence checks all of its share of the ring
+        for (int s = 0; s < nb; s++) {
+            const int rows = s_rows[s], b = b_lo + s;
+            if (rows <= 0) continue;
+            uint32_t off;
+            const int take = (int)fast_div((uint32_t)s_len[s] + rows + dsc.block_size - 1, dsc.block_size, inv_bs, off) - s_old[s];
+            int bad = 0;
+#pragma unroll 4
+            for (int j = t; j < take; j += 256) bad |= (uint32_t)free_blocks[ring.place(s_base[s] + j)] >= (uint32_t)dsc.num_blocks;
+            bad = __syncthreads_or(bad);
+            if (t == 0) {
+                if (bad) s_rows[s] = 0;
+                if (take > 0 && (uint32_t)b * dsc.S >= e0) {
+                    status[b] = bad ? ETV_BRANCH_BAD_FREE : 0;
+                    len_out[b] = s_len[s] + (bad ? 0 : rows);
+                }
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll 4
     for (int r = t; r < kSlotsPerWg; r += 256) {
         const uint32_t e = e0 + r;
-        if (e > last) break;
+        if (e > last) continue;
         uint32_t i;
         const int b = (int)fast_div(e, dsc.S, inv_S, i), s = b - b_lo;
         int32_t slot = -1;
@@ -144,7 +179,7 @@ __global__ void __launch_bounds__(256) resize_tables_kernel(etv_pages_desc dsc, 
                                                             int32_t *block_table, int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out,
                                                             int32_t *len_out, int32_t *slot_map, int32_t *status) {
     const Ring ring(free_state, dsc.num_blocks);
-    if (blockIdx.x == 0) give_back(dsc, inv_bs, len, new_len, block_table, free_blocks, ring, free_state_out, len_out, slot_map, status);
+    if (blockIdx.x == 0) give_back(dsc, inv_bs, len, new_len, block_table, free_blocks, ring, free_state_out, len_out, status);
     else grow(dsc, inv_bs, inv_S, len, new_len, block_table, free_blocks, ring, len_out, slot_map, status);
 }
 
