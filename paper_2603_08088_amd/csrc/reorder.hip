@@ -29,50 +29,75 @@ __device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len
     return ((long)len + sh.block_size - 1) / sh.block_size > sh.max_blocks ? ETV_COMMIT_CAPACITY : 0;
 }
 
-// grid (chunks, B), 128 threads: a thread per column of the table.
+// grid (chunks, B), 128 threads: a thread per column of the table.  The old beams' entries of its column are asked for eight at a time; FEW: they
+// are eight at most and stay in its registers.
+template <bool FEW>
 __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
                                                                int32_t *table_out, ReorderWorkspace ws) {
     extern __shared__ int32_t s_table[];  // [K][kCols]
     __shared__ int s_parent[ETV_MAX_BEAMS];
     __shared__ unsigned int s_alive[2];
     const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 63, col = c * kCols + t;
+    const int32_t *src = block_table + (size_t)b * sh.K * sh.max_blocks + min(col, sh.max_blocks - 1);
+    if (t < 2) s_alive[t] = 0;
+    const int p = t < sh.M ? parent[(size_t)b * sh.M + t] : -1;
+    int32_t id[8];
+    for (int k0 = 0; k0 < sh.K; k0 += 8) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) id[i] = src[(size_t)min(k0 + i, sh.K - 1) * sh.max_blocks];
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (k0 + i < sh.K) s_table[(k0 + i) * kCols + t] = id[i];
+        if (FEW) break;
+    }
     int32_t st = length_status(sh, len[b]);
     const int L = st ? 0 : len[b], full = L / sh.block_size, cols = (int)(((long)L + sh.block_size - 1) / sh.block_size);
-    if (t < 2) s_alive[t] = 0;
     __syncthreads();
-    int bad = 0;
-    if (t < sh.M) {
-        const int p = parent[(size_t)b * sh.M + t];
-        const bool ok = p >= 0 && p < sh.K;
-        bad = !ok && p != -1;
-        s_parent[t] = ok ? p : -1;
-        if (ok) atomicOr(&s_alive[p >> 5], 1u << (p & 31));
-    }
-    if (__syncthreads_or(bad)) st |= ETV_COMMIT_BAD_NODE;
+    const bool ok = p >= 0 && p < sh.K;
+    if (t < sh.M) s_parent[t] = ok ? p : -1;
+    if (ok) atomicOr(&s_alive[p >> 5], 1u << (p & 31));
+    if (__syncthreads_or(!ok && p != -1)) st |= ETV_COMMIT_BAD_NODE;
     const uint64_t alive = s_alive[0] | (uint64_t)s_alive[1] << 32;
-    const int32_t *src = block_table + (size_t)b * sh.K * sh.max_blocks;
-    bad = 0;
-    for (int k = 0; k < sh.K; k++) {
-        const int32_t id = col < cols ? src[(size_t)k * sh.max_blocks + col] : -1;
-        s_table[k * kCols + t] = id;
-        if (col < cols && alive >> k & 1) bad |= (uint32_t)id >= (uint32_t)sh.num_blocks;
+    const auto outside = [&](int32_t x) { return (uint32_t)x >= (uint32_t)sh.num_blocks; };
+    int bad = 0;
+    if (col < cols) {
+        if (FEW) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) bad |= (alive >> k & 1) && outside(id[k]);
+        } else {
+            for (int k = 0; k < sh.K; k++) bad |= (alive >> k & 1) && outside(s_table[k * kCols + t]);
+        }
     }
     if (__syncthreads_or(bad)) st |= ETV_COMMIT_BAD_BLOCK;
     if (col < sh.max_blocks)
+#pragma unroll 4
         for (int i = 0; i < sh.M; i++) {
-            const int p = s_parent[i];
-            table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && p >= 0 && col < cols ? s_table[p * kCols + t] : -1;
+            const int from = s_parent[i];
+            table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && from >= 0 && col < cols ? s_table[from * kCols + t] : -1;
         }
     // blocks of beams without a child that neither a parent nor an earlier such beam has
     uint64_t gone = 0;
-    if (col < cols && !st)
-        for (int k = 0; k < sh.K; k++) {
-            if (alive >> k & 1) continue;
-            const int32_t id = s_table[k * kCols + t];
-            bool mine = (uint32_t)id < (uint32_t)sh.num_blocks;
-            for (int j = 0; j < sh.K && mine; j++) mine = !((alive >> j & 1 || j < k) && s_table[j * kCols + t] == id);
-            if (mine) gone |= 1ull << k;
+    if (col < cols && !st) {
+        if (FEW) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                bool mine = k < sh.K && !(alive >> k & 1) && !outside(id[k]);
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    if (j != k) mine &= !((j < k || (alive >> j & 1)) && id[j] == id[k]);
+                gone |= (uint64_t)mine << k;
+            }
+        } else {
+            for (uint64_t dead = ~alive & (~0ull >> (64 - sh.K)); dead; dead &= dead - 1) {
+                const int k = __builtin_ctzll(dead);
+                const int32_t x = s_table[k * kCols + t];
+                bool mine = !outside(x);
+#pragma unroll 8
+                for (int j = 0; j < sh.K; j++) mine &= !((j < k || (alive >> j & 1)) && j != k && s_table[j * kCols + t] == x);
+                gone |= (uint64_t)mine << k;
+            }
         }
+    }
     __shared__ int s_wave[2];
     const int count = __popcll(gone);
     const int upto = wave_scan_sum(count);
@@ -85,16 +110,13 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
     const bool here = !st && L % sh.block_size != 0 && full / kCols == c;
     int need = 0;
     if (t < 64) {
-        const int p = lane < sh.M ? s_parent[lane] : -1;
-        const int32_t id = here && p >= 0 ? s_table[p * kCols + full % kCols] : -1;
+        const int from = lane < sh.M ? s_parent[lane] : -1;
+        const int32_t own = here && from >= 0 ? s_table[from * kCols + full % kCols] : -1;
         bool later = false;
-        for (int j = 0; j < sh.M; j++) {
-            const int32_t other = __shfl(id, j);
-            later |= j < lane && other == id;
-        }
-        later = later && id >= 0;
+        for (int j = 0; j < sh.M; j++) later |= j < lane && __builtin_amdgcn_readlane(own, j) == own;
+        later = later && own >= 0;
         need = __popcll(__ballot(later));
-        if (here && lane < sh.M) ws.from[(size_t)b * sh.M + lane] = later ? id : -1;
+        if (here && lane < sh.M) ws.from[(size_t)b * sh.M + lane] = later ? own : -1;
     }
     if (t == 0) ws.records[(size_t)b * sh.chunks + c] = {st, need, s_wave[0] + s_wave[1], 0};
 }
@@ -146,8 +168,10 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         const int need = request(sh, ws, b).need;
         if (g >= need) return;
         long before = 0;
-        for (int o = t; o < b; o += 256) before += request(sh, ws, o).need;
-        before = block_sum(before);
+        if (b > 0) {
+            for (int o = t; o < b; o += 256) before += request(sh, ws, o).need;
+            before = block_sum(before);
+        }
         if (before + need > ring.count) return;
         const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
         const int rows = len[b] % sh.block_size;
@@ -252,7 +276,7 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
     int64_t G = 2048 / one;
     G = G < 1 ? 1 : G > sh.M ? sh.M : G;
     if (sh.B + one * G > INT32_MAX) return ETV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(reorder_tables_kernel, dim3(sh.chunks, sh.B), dim3(kCols), sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
+    hipLaunchKernelGGL(sh.K <= 8 ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(kCols), sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
     const int32_t rc = check_launch();
     if (rc != ETV_OK) return rc;
     hipLaunchKernelGGL(reorder_copy_kernel, dim3((unsigned)(sh.B + one * G)), dim3(256), 0, s, sh, cache, (int)G, len, free_blocks, free_state, table_out,
