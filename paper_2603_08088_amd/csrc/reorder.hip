@@ -8,6 +8,8 @@ namespace etv {
 
 constexpr int kCols = 128;  // columns of the tables of one request that a workgroup takes
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
 struct ReorderShape {
     int B, K, M, max_blocks, num_blocks, block_size, chunks;
 };
@@ -141,14 +143,43 @@ struct CacheParts {
     int parts, Hkv, n_layers;
 };
 
-// The rows of a half-filled block: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is shorter.
-template <class U>
+// Blocks to copy into for requests [from, to), by one wavefront; `st` collects their status.
+__device__ __forceinline__ int needs(const ReorderShape &sh, const ReorderWorkspace &ws, int from, int to, int &st) {
+    int sum = 0, any = 0;
+    for (int i = from * sh.chunks + (threadIdx.x & 63); i < to * sh.chunks; i += 64) {
+        const ChunkRecord r = ws.records[i];
+        sum += r.need;
+        any |= r.st;
+    }
+    st = __ballot(any) != 0;
+    if (st && to - from > 1) {  // a refused request needs none
+        sum = 0;
+        for (int o = from + (threadIdx.x & 63); o < to; o += 64) sum += request(sh, ws, o).need;
+    }
+    return __builtin_amdgcn_readlane(wave_scan_sum(sum), 63);
+}
+
+// The rows of a half-filled block: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is shorter; AHEAD a
+// thread on their way.  (A block of one layer has less than 2^32 bytes.)
+template <class U, int AHEAD>
 __device__ __forceinline__ void copy_rows(uint8_t *layer, int src, int dst, int Hkv, int block_size, int row_bytes, int rows) {
-    const int units = rows * row_bytes / (int)sizeof(U);
-    for (int h = threadIdx.x >> 6; h < Hkv; h += 4) {
-        const U *from = reinterpret_cast<const U *>(layer + ((size_t)src * Hkv + h) * block_size * row_bytes);
-        U *to = reinterpret_cast<U *>(layer + ((size_t)dst * Hkv + h) * block_size * row_bytes);
-        for (int u = threadIdx.x & 63; u < units; u += 64) to[u] = from[u];
+    const uint32_t per_head = (uint32_t)(rows * row_bytes) / sizeof(U), all = per_head * Hkv, inv = per_head == 1 ? 0xffffffffu : 0xffffffffu / per_head;
+    const uint32_t head = (uint32_t)block_size * row_bytes;
+    const uint8_t *from = layer + (size_t)src * Hkv * head;
+    uint8_t *to = layer + (size_t)dst * Hkv * head;
+    for (uint32_t u0 = threadIdx.x; u0 < all; u0 += AHEAD * 256) {
+        U x[AHEAD];
+        uint32_t at[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) {
+            uint32_t unit;
+            const uint32_t h = fast_div(min(u0 + i * 256, all - 1), per_head, inv, unit);
+            at[i] = h * head + unit * (uint32_t)sizeof(U);
+            x[i] = *reinterpret_cast<const U *>(from + at[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++)
+            if (u0 + i * 256 < all) *reinterpret_cast<U *>(to + at[i]) = x[i];
     }
 }
 
@@ -165,24 +196,21 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         const int part = x % cache.parts;
         x /= cache.parts;
         const int l = x % cache.n_layers, b = x / cache.n_layers;
-        const int need = request(sh, ws, b).need;
-        if (g >= need) return;
-        long before = 0;
-        if (b > 0) {
-            for (int o = t; o < b; o += 256) before += request(sh, ws, o).need;
-            before = block_sum(before);
-        }
-        if (before + need > ring.count) return;
+        int st, others;
         const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
-        const int rows = len[b] % sh.block_size;
+        const int rows = (int)((uint32_t)len[b] % (uint32_t)sh.block_size);
+        const int need = needs(sh, ws, b, b + 1, st);
+        if (st || g >= need) return;
+        const long before = needs(sh, ws, 0, b, others);
+        if (before + need > ring.count) return;
         uint8_t *layer = cache.base[part] + (size_t)l * cache.layer_bytes[part];
         uint64_t todo = __ballot(from >= 0);
         for (int i = 0; i < need; i++, todo &= todo - 1) {
             if (i % G != g) continue;
             const int src = __shfl(from, __builtin_ctzll(todo)), dst = free_blocks[ring.place(before + i)];
             if ((uint32_t)dst >= (uint32_t)sh.num_blocks) continue;
-            if (cache.row_bytes[part] % 16 == 0) copy_rows<uint4>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
-            else copy_rows<uint16_t>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+            if (cache.row_bytes[part] % 16 == 0) copy_rows<u32x4, 8>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+            else copy_rows<uint16_t, 2>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
         }
         return;
     }
@@ -263,6 +291,8 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
         return check_launch();
     }
     if (!block_table || !len || !parent || !table_out || !status || table_out == block_table) return ETV_ERR_INVALID_ARG;
+    for (int i = 0; i < cache.parts; i++)
+        if ((double)cache.Hkv * sh.block_size * cache.row_bytes[i] >= 0x1p32) return ETV_ERR_UNSUPPORTED;
     for (int i = 0; i < cache.parts; i++)
         if (!cache.base[i] || (uintptr_t)cache.base[i] % (cache.row_bytes[i] % 16 ? 2 : 16)) return ETV_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 15) return ETV_ERR_INVALID_ARG;
