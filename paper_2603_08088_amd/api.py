@@ -714,9 +714,7 @@ def resize_block_tables(block_table, length, new_length, free: FreeBlocks, block
         status = native.empty_i32(length, len(length))
     if slots is None and want_slots:
         slots = native.empty_i32(length, len(length), S)
-    dsc = native.pages_desc(block_table, length, new_length, free.blocks, free.state, state, plo, slots, status, block_size, S)
-    rc = native.resize_block_tables(dsc, length, new_length, block_table, free.blocks, free.state, state, plo, slots, status)
-    _check("etv_resize_block_tables", rc)
+    _check("etv_resize_block_tables", native.resize_block_tables(block_table, length, new_length, free.blocks, free.state, state, plo, slots, status, block_size, S))
     return dict(free_state=state, length=plo, slot_map=slots, status=status)
 
 
@@ -750,11 +748,8 @@ def rotary_write_kv(q, k, v, positions, rotary: Rotary, *, n_rows=None, slot_map
         qo = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if ko is None and k is not None and k_cache is None:
         ko = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dsc = native.rotary_desc(rotary._back if inverse else rotary._desc, q, k, v, positions, rotary.inv_freq, n_rows, qo, ko, vo, slot_map,
-                             k_cache, v_cache, paged)
-    if dsc is None:
-        raise EtvError("etv_rotary_write_kv", -2)
-    rc = native.rotary_write_kv(dsc, q, k, v, positions, rotary.inv_freq, n_rows, qo, ko, vo, slot_map, k_cache, v_cache)
+    rc = native.rotary_write_kv(rotary._back if inverse else rotary._desc, q, k, v, positions, rotary.inv_freq, n_rows, qo, ko, vo, slot_map, k_cache,
+                                v_cache, paged)
     _check("etv_rotary_write_kv", rc)
     return dict(q=qo, k=ko, v=vo)
 
@@ -769,7 +764,7 @@ def beam_select(logits, scores, M: int, *, n_beams=None, finished=None, end_toke
     """logits [B,K,V] fp32 or bf16 (rows may be padded), scores float32 [B,K] -> the M best continuations: scores float32, parent and token
     int32, finished uint8, each [B,M] (-inf, -1, -1, 0 where fewer are offered), and status int32 [B].  finished uint8 or bool [B,K]: beams
     that offer end_token at their own score alone."""
-    B, K, V = logits.shape
+    B = logits.shape[0]
     native, get = _native(), (out or {}).get
     best, parent, token, ended, status = get("scores"), get("parent"), get("token"), get("finished"), get("status")
     if best is None:
@@ -782,13 +777,7 @@ def beam_select(logits, scores, M: int, *, n_beams=None, finished=None, end_toke
         ended = torch.empty((B, M), dtype=torch.uint8, device=logits.device)
     if status is None:
         status = native.empty_i32(logits, B)
-    dsc = native.beam_desc(logits, scores, n_beams, finished, best, parent, token, ended, status, M, end_token)
-    if dsc is None:
-        raise EtvError("etv_beam_select", -2)
-    if workspace is None:
-        workspace = torch.empty((max(256, beam_select_workspace_bytes(B, K, V, M, logits.dtype)),), dtype=torch.uint8, device=logits.device)
-    rc = native.beam_select(dsc, logits, scores, n_beams, finished, best, parent, token, ended, status, workspace, workspace.numel())
-    _check("etv_beam_select", rc)
+    _check("etv_beam_select", native.beam_select(logits, scores, n_beams, finished, best, parent, token, ended, status, M, end_token, workspace))
     return dict(scores=best, parent=parent, token=token, finished=ended, status=status)
 
 
@@ -796,33 +785,27 @@ def reorder_beams_workspace_bytes(B: int, K: int, M: int, max_blocks: int) -> in
     return int(lib().etv_reorder_beams_workspace_bytes(B, K, M, max_blocks))
 
 
-def _reorder_beams(fn: str, call, parts, block_table, length, parent, free: FreeBlocks, out, workspace):
+def _reorder_beams(fn: str, parts, block_table, length, parent, free: FreeBlocks, out, workspace):
     native, get = _native(), (out or {}).get
-    if block_table.dim() != 3 or parent.dim() != 2:
-        raise ValueError("block_table is int32 [B, K, max_blocks], parent int32 [B, M]")
-    (B, K, width), M = block_table.shape, parent.shape[1]
     table, state, status = get("block_table"), get("free_state"), get("status")
     if table is None:
-        table = native.empty_i32(block_table, B, M, width)
+        if block_table.dim() != 3 or parent.dim() != 2:
+            raise ValueError("block_table is int32 [B, K, max_blocks], parent int32 [B, M]")
+        table = native.empty_i32(block_table, len(block_table), parent.shape[1], block_table.shape[2])
     if state is None:
-        state = native.empty_i32(block_table, 2)
+        state = native.empty_i32(length, 2)
     if status is None:
-        status = native.empty_i32(block_table, B)
-    dsc = native.reorder_desc(*parts, block_table, length, parent, free.blocks, free.state, table, state, status)
-    if dsc is None:
-        raise EtvError(fn, -2)
-    if workspace is None:
-        workspace = torch.empty((max(256, reorder_beams_workspace_bytes(B, K, M, width)),), dtype=torch.uint8, device=block_table.device)
-    _check(fn, call(dsc, *parts, block_table, length, K, parent, M, free.blocks, free.state, table, state, status, workspace, workspace.numel()))
+        status = native.empty_i32(length, len(length))
+    _check(fn, native.reorder_beams(*parts, block_table, length, parent, free.blocks, free.state, table, state, status, workspace))
     return dict(block_table=table, free_state=state, status=status)
 
 
 def reorder_beams(k_cache, v_cache, block_table, length, parent, free: FreeBlocks, *, out: Optional[Dict[str, torch.Tensor]] = None, workspace=None):
     """Caches [Lyr,nb,Hkv,bs,d] (half-filled blocks are copied where beams part); block_table int32 [B,K,max_blocks]; length int32 [B]; parent int32
     [B,M], -1 for none -> block_table [B,M,max_blocks], free_state [2], status [B]."""
-    return _reorder_beams("etv_reorder_beams", _native().reorder_beams, (k_cache, v_cache), block_table, length, parent, free, out, workspace)
+    return _reorder_beams("etv_reorder_beams", (k_cache, v_cache), block_table, length, parent, free, out, workspace)
 
 
 def reorder_beams_q4(cache: KVCacheQ4, block_table, length, parent, free: FreeBlocks, *, out: Optional[Dict[str, torch.Tensor]] = None, workspace=None):
     """reorder_beams over a 4-bit cache."""
-    return _reorder_beams("etv_reorder_beams_q4", _native().reorder_beams_q4, tuple(cache), block_table, length, parent, free, out, workspace)
+    return _reorder_beams("etv_reorder_beams_q4", cache, block_table, length, parent, free, out, workspace)

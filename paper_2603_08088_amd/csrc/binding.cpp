@@ -3,8 +3,8 @@
 // 9 us per attention call: longer than the kernel.  Here one template turns the arguments into those of the C prototype in
 // eagletv.h: a pointer parameter takes a device-resident contiguous tensor or None, a descriptor any object with the buffer
 // of that struct, an integer an int or what has __index__ (numpy's integers, tensors of one); the trailing stream is the
-// current one.  The GIL is released around the call.  HERE: the tensors must be on the device whose stream that is.  Bit i of STRIDED: the
-// descriptor holds the strides of argument i.
+// current one.  The GIL is released around the call.  HERE: the tensors must be on the device whose stream that is.  STRIDED: the
+// descriptor holds the strides of the tensor.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -70,10 +70,10 @@ T arg(PyObject *o) {
     }
 }
 
-template <bool HERE, unsigned STRIDED, class... A, std::size_t... I>
+template <bool HERE, class... A, std::size_t... I>
 int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I...>) {
     std::tuple<A...> v;
-    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>, HERE, (STRIDED >> I & 1) != 0>(args[I])), ...);  // left to right; the stream is last
+    ((std::get<I>(v) = arg<std::tuple_element_t<I, std::tuple<A...>>, HERE>(args[I])), ...);  // left to right; the stream is last
     std::get<sizeof...(A) - 1>(v) = c10::hip::getCurrentHIPStream().stream();
     int32_t rc;
     Py_BEGIN_ALLOW_THREADS;
@@ -85,13 +85,13 @@ int32_t apply(int32_t (*f)(A...), PyObject *const *args, std::index_sequence<I..
 template <class... A>
 constexpr Py_ssize_t arity(int32_t (*)(A...)) { return sizeof...(A) - 1; }
 
-template <auto F, bool HERE = false, unsigned STRIDED = 0>
+template <auto F, bool HERE = false>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     constexpr Py_ssize_t want = arity(F);
     if (n != want) return PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
     try {
-        return PyLong_FromLong(apply<HERE, STRIDED>(F, args, std::make_index_sequence<want>{}));
+        return PyLong_FromLong(apply<HERE>(F, args, std::make_index_sequence<want>{}));
     } catch (const Refused &) {
         return nullptr;
     }
@@ -268,9 +268,34 @@ PyObject *q4_attn_check(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// Beam decoding.  What the C side takes on trust, checked; the descriptor's bytes, or None where a type is neither fp32 nor bf16.
-template <class D>
-PyObject *bytes_of(const D &d) { return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&d), sizeof d); }
+// Beam decoding: one call checks what the C side takes on trust, fills in the descriptor and launches -- the kernels are shorter than a second way
+// through Python.  Arguments of f come as Python objects, which are converted as above, or as themselves.
+template <class T, bool STRIDED, class V>
+T given(const V &v) {
+    if constexpr (std::is_same_v<V, PyObject *>) return arg<T, true, STRIDED>(v);
+    else return static_cast<T>(v);
+}
+template <unsigned STRIDED, class... A, class... V, std::size_t... I>
+PyObject *launch_with(int32_t (*f)(A...), std::index_sequence<I...>, const V &...vs) {
+    std::tuple<A...> v;
+    ((std::get<I>(v) = given<std::tuple_element_t<I, std::tuple<A...>>, (STRIDED >> I & 1) != 0>(vs)), ...);
+    std::get<sizeof...(A) - 1>(v) = c10::hip::getCurrentHIPStream().stream();
+    int32_t rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = std::apply(f, v);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+}
+template <unsigned STRIDED = 0, class... A, class... V>
+PyObject *launch(int32_t (*f)(A...), const V &...vs) {
+    static_assert(sizeof...(A) == sizeof...(V) + 1, "all arguments but the stream");
+    return launch_with<STRIDED>(f, std::make_index_sequence<sizeof...(V)>{}, vs...);
+}
+at::Tensor workspace_for(size_t bytes, const at::Tensor &like) {
+    return at::empty({static_cast<int64_t>(bytes < 256 ? 256 : bytes)}, at::TensorOptions().dtype(at::kByte).device(like.device()));
+}
+PyObject *unsupported() { return PyLong_FromLong(ETV_ERR_UNSUPPORTED); }
+int64_t bytes_in(const at::Tensor &t) { return t.numel() * t.element_size(); }
 int32_t fit32(int64_t x) {
     need(x >= 0 && x <= INT32_MAX, "a size does not fit 32 bits");
     return static_cast<int32_t>(x);
@@ -288,8 +313,8 @@ int64_t ring_blocks(PyObject *blocks, PyObject *state, PyObject *state_out) {
     return r.size(0);
 }
 
-// pages_desc(block_table, length, new_length, free_blocks, free_state, free_state_out, length_out, slot_map or None, status, block_size, S)
-PyObject *pages_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// resize_block_tables(block_table, length, new_length, free_blocks, free_state, free_state_out, length_out, slot_map or None, status, block_size, S)
+PyObject *resize_block_tables(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 11) return PyErr_Format(PyExc_TypeError, "11 arguments expected, got %zd", n);
     try {
@@ -304,15 +329,15 @@ PyObject *pages_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
         d.S = fit32(S);
         d.block_size = fit32(int_of(args[9]));
         d.max_blocks = fit32(table.size(1));
-        return bytes_of(d);
+        return launch(&etv_resize_block_tables, &d, args[1], args[2], args[0], args[3], args[4], args[5], args[6], args[7], args[8]);
     } catch (const Refused &) {
         return nullptr;
     }
     END_HANDLE_TH_ERRORS
 }
 
-// rotary_desc(descriptor of the encoding, q, k, v, positions, inv_freq, n_rows, q_out, k_out, v_out, slot_map, k_cache, v_cache, paged)
-PyObject *rotary_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// rotary_write_kv(descriptor of the encoding, q, k, v, positions, inv_freq, n_rows, q_out, k_out, v_out, slot_map, k_cache, v_cache, paged)
+PyObject *rotary_write_kv(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 14) return PyErr_Format(PyExc_TypeError, "14 arguments expected, got %zd", n);
     try {
@@ -366,18 +391,18 @@ PyObject *rotary_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
         d.Hkv = fit32(heads[1]);
         d.d = fit32(width);
         d.dtype = type_code(*first);
-        if (d.dtype < 0) Py_RETURN_NONE;
-        return bytes_of(d);
+        if (d.dtype < 0) return unsupported();
+        return launch<0x38e>(&etv_rotary_write_kv, &d, args[1], args[2], args[3], args[4], args[5], args[6], args[7], args[8], args[9], args[10], args[11], args[12]);
     } catch (const Refused &) {
         return nullptr;
     }
     END_HANDLE_TH_ERRORS
 }
 
-// beam_desc(logits, scores, n_beams, finished, scores_out, parent, token, finished_out, status, M, end_token)
-PyObject *beam_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// beam_select(logits, scores, n_beams, finished, scores_out, parent, token, finished_out, status, M, end_token, workspace or None): None allocates
+PyObject *beam_select(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 11) return PyErr_Format(PyExc_TypeError, "11 arguments expected, got %zd", n);
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "12 arguments expected, got %zd", n);
     try {
         const at::Tensor &x = tensor_of(args[0], "logits"), &scores = tensor_of(args[1], "scores"), &best = tensor_of(args[4], "out[\"scores\"]");
         need(x.dim() == 3 && (x.size(2) == 1 || x.stride(2) == 1), "logits are [B, K, V], the vocabulary contiguous");
@@ -402,21 +427,25 @@ PyObject *beam_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
         d.end_token = static_cast<int32_t>(end);
         d.batch_stride = x.stride(0);
         d.row_stride = x.stride(1);
-        if (d.dtype < 0) Py_RETURN_NONE;
-        return bytes_of(d);
+        if (d.dtype < 0) return unsupported();
+        at::Tensor own;
+        const at::Tensor *ws = maybe(args[11], "workspace");
+        if (!ws) ws = &(own = workspace_for(etv_beam_select_workspace_bytes(&d), x));
+        need(ws->is_contiguous() && ws->device() == x.device(), "the workspace is contiguous and on the logits' device");
+        return launch<0x2>(&etv_beam_select, &d, args[0], args[1], args[2], args[3], args[4], args[5], args[6], args[7], args[8], ws->data_ptr(), bytes_in(*ws));
     } catch (const Refused &) {
         return nullptr;
     }
     END_HANDLE_TH_ERRORS
 }
 
-// reorder_desc(parts of the cache (2, or codes and scales of K and V: 4)..., block_table, length, parent, free_blocks, free_state, table_out,
-// free_state_out, status): an etv_cache_desc or etv_q4_desc
-PyObject *reorder_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// reorder_beams(parts of the cache (2, or codes and scales of K and V: 4)..., block_table, length, parent, free_blocks, free_state, table_out,
+// free_state_out, status, workspace or None)
+PyObject *reorder_beams(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 10 && n != 12) return PyErr_Format(PyExc_TypeError, "10 or 12 arguments expected, got %zd", n);
+    if (n != 11 && n != 13) return PyErr_Format(PyExc_TypeError, "11 or 13 arguments expected, got %zd", n);
     try {
-        const bool q4 = n == 12;
+        const bool q4 = n == 13;
         PyObject *const *rest = args + (q4 ? 4 : 2);
         const at::Tensor &table = tensor_of(rest[0], "block_table"), &parent = tensor_of(rest[2], "parent"), &out = tensor_of(rest[5], "out[\"block_table\"]");
         need(table.scalar_type() == at::kInt && table.dim() == 3, "block_table is int32 [B, K, max_blocks]");
@@ -429,6 +458,11 @@ PyObject *reorder_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
         need(k.dim() == 5 && v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type(), "a cache is [n_layers, num_blocks, Hkv, block_size, ...]");
         need(k.size(1) == ring_blocks(rest[3], rest[4], rest[6]), "free.blocks has an entry for every block of the cache");
         need(k.size(3) > 0, "blocks of no rows");
+        const int32_t K = fit32(table.size(1)), M = fit32(parent.size(1));
+        at::Tensor own;
+        const at::Tensor *ws = maybe(rest[8], "workspace");
+        if (!ws) ws = &(own = workspace_for(etv_reorder_beams_workspace_bytes(fit32(B), K, M, fit32(table.size(2))), table));
+        need(ws->is_contiguous() && ws->device() == table.device(), "the workspace is contiguous and on the tables' device");
         if (q4) {
             const Q4Shapes c = q4_shapes(args, 1, k.size(4) * 2);
             etv_q4_desc d{};
@@ -441,9 +475,10 @@ PyObject *reorder_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
             d.max_blocks = fit32(table.size(2));
             d.num_blocks = fit32(c.blocks);
             d.layer_rows = c.blocks * c.heads * c.size;
-            return bytes_of(d);
+            return launch(&etv_reorder_beams_q4, &d, args[0], args[1], args[2], args[3], rest[0], rest[1], K, rest[2], M, rest[3], rest[4], rest[5], rest[6],
+                          rest[7], ws->data_ptr(), bytes_in(*ws));
         }
-        if (type_code(k) < 0) Py_RETURN_NONE;
+        if (type_code(k) < 0) return unsupported();
         etv_cache_desc d{};
         d.B = fit32(B);
         d.Hkv = fit32(k.size(2));
@@ -454,7 +489,8 @@ PyObject *reorder_desc(PyObject *, PyObject *const *args, Py_ssize_t n) {
         d.max_blocks = fit32(table.size(2));
         d.num_blocks = fit32(k.size(1));
         d.cache_layer_stride = k.numel() / (k.size(0) > 0 ? k.size(0) : 1);
-        return bytes_of(d);
+        return launch(&etv_reorder_beams, &d, args[0], args[1], rest[0], rest[1], K, rest[2], M, rest[3], rest[4], rest[5], rest[6], rest[7], ws->data_ptr(),
+                      bytes_in(*ws));
     } catch (const Refused &) {
         return nullptr;
     }
@@ -469,13 +505,10 @@ PyMethodDef methods[] = {ETV_METHOD(build_tree_mask), ETV_METHOD(tensorize_tree)
                          ETV_METHOD(pack_lm_head), ETV_METHOD(replicate_branches), ETV_METHOD(commit_path_indices),
                          ETV_METHOD_HERE(quantize_kv_q4), ETV_METHOD_HERE(commit_accepted_kv_q4), ETV_METHOD_HERE(dequantize_kv_q4),
                          ETV_METHOD_HERE(tree_verify_attention_q4),
-                         ETV_METHOD_HERE(resize_block_tables), ETV_METHOD_HERE(reorder_beams), ETV_METHOD_HERE(reorder_beams_q4),
-                         {"rotary_write_kv", (PyCFunction)(void (*)(void))call<&etv_rotary_write_kv, true, 0x38e>, METH_FASTCALL, nullptr},
-                         {"beam_select", (PyCFunction)(void (*)(void))call<&etv_beam_select, true, 0x2>, METH_FASTCALL, nullptr},
-                         {"pages_desc", (PyCFunction)(void (*)(void))pages_desc, METH_FASTCALL, nullptr},
-                         {"rotary_desc", (PyCFunction)(void (*)(void))rotary_desc, METH_FASTCALL, nullptr},
-                         {"beam_desc", (PyCFunction)(void (*)(void))beam_desc, METH_FASTCALL, nullptr},
-                         {"reorder_desc", (PyCFunction)(void (*)(void))reorder_desc, METH_FASTCALL, nullptr},
+                         {"resize_block_tables", (PyCFunction)(void (*)(void))resize_block_tables, METH_FASTCALL, nullptr},
+                         {"rotary_write_kv", (PyCFunction)(void (*)(void))rotary_write_kv, METH_FASTCALL, nullptr},
+                         {"beam_select", (PyCFunction)(void (*)(void))beam_select, METH_FASTCALL, nullptr},
+                         {"reorder_beams", (PyCFunction)(void (*)(void))reorder_beams, METH_FASTCALL, nullptr},
                          {"commit_desc", (PyCFunction)(void (*)(void))commit_desc, METH_FASTCALL, nullptr},
                          {"q4_desc", (PyCFunction)(void (*)(void))q4_desc, METH_FASTCALL, nullptr},
                          {"q4_attn_check", (PyCFunction)(void (*)(void))q4_attn_check, METH_FASTCALL, nullptr},
