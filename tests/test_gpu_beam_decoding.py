@@ -1,0 +1,241 @@
+"""Beam search over the paged cache with the calls together, as a program runs them: a small model decoded step by step against the same search written
+down plainly, which computes every beam's whole sequence anew in 64 bits; and the step as a captured graph."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import beam_plain
+from paper_2603_08088_amd import api
+
+pytestmark = pytest.mark.gpu
+LAYERS, HQ, HKV, D, WIDE, V, SIZE = 2, 4, 2, 64, 48, 96, 16
+AXES = [0] * 8 + [1] * 8 + [2] * 16
+
+
+class Model:
+    def __init__(self, seed):
+        rng = np.random.default_rng(seed)
+        mat = lambda *s: (rng.standard_normal(s) / math.sqrt(s[-1])).astype(np.float32)
+        self.embed, self.head = 2 * mat(V, WIDE) * math.sqrt(WIDE), 4 * mat(V, WIDE)
+        self.qkv = [mat((HQ + 2 * HKV) * D, WIDE) for _ in range(LAYERS)]
+        self.out = [mat(WIDE, HQ * D) for _ in range(LAYERS)]
+        self.inv_freq = (1000.0 ** (-np.arange(32) / 32)).astype(np.float32)
+        self.on = {k: [torch.from_numpy(x).cuda() for x in v] if isinstance(v, list) else torch.from_numpy(v).cuda()
+                   for k, v in vars(self).items()}
+        self.rotary = api.Rotary(self.on["inv_freq"], axis_of=AXES)
+
+    def positions(self, n):
+        """Three axes: a text whose second axis stands still in the middle, and whose third counts in rows of five."""
+        i = np.arange(n)
+        return np.stack((i, np.where((i > 10) & (i < 20), 10, i), i % 5 + i // 5))
+
+    def logits64(self, tokens):
+        """The last position's logits after a whole sequence, in float64."""
+        x = self.embed[tokens].astype(np.float64)
+        n = len(tokens)
+        pos = self.positions(n)[:, None]
+        for qkv, out in zip(self.qkv, self.out):
+            y = (x @ qkv.T.astype(np.float64)).reshape(n, HQ + 2 * HKV, D)
+            q, k = (beam_plain.rotate(t[None], pos, self.inv_freq, AXES, False)[0] for t in (y[:, :HQ], y[:, HQ:HQ + HKV]))
+            o = np.zeros((n, HQ, D))
+            for h in range(HQ):
+                s = q[:, h] @ k[:, h // (HQ // HKV)].T / math.sqrt(D)
+                s[np.triu_indices(n, 1)] = -np.inf
+                p = np.exp(s - s.max(1, keepdims=True))
+                o[:, h] = p / p.sum(1, keepdims=True) @ y[:, HQ + HKV + h // (HQ // HKV)]
+            x = x + o.reshape(n, -1) @ out.T.astype(np.float64)
+        return x[-1] @ self.head.T.astype(np.float64)
+
+
+def plain_search(model, prompts, K, steps, end):
+    """-> per step the beams (tokens, score, finished) of every request, and the smallest gap that a choice hung on."""
+    beams = [[(list(p), 0.0, False)] for p in prompts]
+    seen, gap = [], math.inf
+    for _ in range(steps):
+        for b, live in enumerate(beams):
+            offers = []
+            for i, (toks, score, done) in enumerate(live):
+                if done:
+                    offers.append((score, i, end))
+                    continue
+                x = model.logits64(toks)
+                lp = score + x - (x.max() + math.log(np.exp(x - x.max()).sum()))
+                offers += [(lp[v], i, v) for v in range(V)]
+            offers.sort(key=lambda o: (-o[0], o[1], o[2]))
+            gap = min([gap] + [offers[i][0] - offers[i + 1][0] for i in range(min(K, len(offers) - 1))])
+            beams[b] = [(live[i][0] + [v], s, live[i][2] or v == end) for s, i, v in offers[:K]]
+        seen.append([list(x) for x in beams])
+    return seen, gap
+
+
+class Decoder:
+    """The state of a search on the GPU, and its steps."""
+
+    def __init__(self, model, B, K, capacity, blocks, end):
+        self.m, self.B, self.K, self.end, self.capacity = model, B, K, end, capacity
+        self.width = capacity // SIZE
+        self.k_cache, self.v_cache = (torch.full((LAYERS, blocks, HKV, SIZE, D), 9.0, device="cuda") for _ in range(2))
+        self.free = api.FreeBlocks.all(blocks)
+
+    def forward(self, tokens, positions, table, length, slots, bitmask):
+        """tokens [N, T] behind `length` rows of the cache -> logits [N, T, V]; the rows' k and v go into the cache first."""
+        N, T = tokens.shape
+        x, n = self.m.on["embed"][tokens], torch.full((N,), T, dtype=torch.int32, device="cuda")
+        for layer in range(LAYERS):
+            y = (x @ self.m.on["qkv"][layer].T).view(N, T, HQ + 2 * HKV, D)
+            q, k, v = y.split([HQ, HKV, HKV], 2)
+            q = api.rotary_write_kv(q, k, v, positions, self.m.rotary, slot_map=slots, k_cache=self.k_cache[layer], v_cache=self.v_cache[layer])["q"]
+            o, _ = api.tree_verify_attention(q, self.k_cache[layer], self.v_cache[layer], length, None, None, bitmask, n, P_max=self.capacity - T, block_table=table, want_lse=False)
+            x = x + o.view(N, T, HQ * D) @ self.m.on["out"][layer].T
+        return x @ self.m.on["head"].T
+
+    def prompt(self, prompts):
+        B, T = prompts.shape
+        table = torch.full((B, self.width), -1, dtype=torch.int32, device="cuda")
+        zero, full = (torch.full((B,), x, dtype=torch.int32, device="cuda") for x in (0, T))
+        r = api.resize_block_tables(table, zero, full, self.free, SIZE, T)
+        self.free, self.length = self.free.after(r), r["length"]
+        chain = torch.arange(-1, T - 1, device="cuda").clamp(min=0).int().expand(B, T).contiguous()
+        mask = api.build_tree_mask(chain, full, want_dense=False)["bitmask"]
+        pos = torch.from_numpy(self.m.positions(T).astype(np.int32)).cuda()[:, None].expand(3, B, T).contiguous()
+        logits = self.forward(prompts, pos, table, zero, r["slot_map"], mask)[:, -1:]
+        self.table, self.scores, self.finished = table.view(B, 1, self.width), torch.zeros((B, 1), device="cuda"), None
+        self.choose(logits)
+
+    def choose(self, logits):
+        r = api.beam_select(logits, self.scores, self.K, finished=self.finished, end_token=self.end)
+        self.scores, self.parent, self.tokens, self.finished = r["scores"], r["parent"], r["token"], r["finished"]
+        self.status = [r["status"]]
+        r = api.reorder_beams(self.k_cache, self.v_cache, self.table, self.length, self.parent, self.free)
+        self.free, self.table = self.free.after(r), r["block_table"]
+        self.status.append(r["status"])
+
+    def step(self, positions):
+        """positions int32 [3, all of them, 1] on the device: the table that the current length picks from."""
+        B, K = self.B, self.K
+        flat, lens = self.table.view(B * K, self.width), self.length.repeat_interleave(K)
+        r = api.resize_block_tables(flat, lens, lens + 1, self.free, SIZE, 1)
+        self.free, grown = self.free.after(r), r["status"]
+        pos = positions[:, lens.long()].view(3, B * K, 1).contiguous()
+        logits = self.forward(self.tokens.view(B * K, 1), pos, flat, lens, r["slot_map"], torch.ones((B * K, 1, 1), dtype=torch.int64, device="cuda"))
+        self.length = self.length + 1
+        self.choose(logits.view(B, K, V))
+        self.status.append(grown)
+
+
+def check_step(dec, lines, want, tol):
+    parent, token = dec.parent.cpu().numpy(), dec.tokens.cpu().numpy()
+    assert all(not s.any() for s in dec.status)
+    for b in range(dec.B):
+        lines[b] = [lines[b][p] + [int(t)] for p, t in zip(parent[b], token[b])]
+        assert lines[b] == [list(map(int, toks)) for toks, _, _ in want[b]]
+        assert dec.finished[b].tolist() == [int(f) for _, _, f in want[b]]
+        assert np.abs(dec.scores[b].cpu().numpy() - [s for _, s, _ in want[b]]).max() <= tol
+    return lines
+
+
+@pytest.mark.parametrize("seed,P,K", [(1, 13, 4), (2, 16, 6), (3, 30, 1)])
+def test_a_search_is_the_plain_one(seed, P, K):
+    B, steps, end = 3, 24, 7
+    model = Model(seed)
+    prompts = np.random.default_rng(seed).integers(0, V, (B, P))
+    want, gap = plain_search(model, prompts, K, steps, end)
+    # fp32 against 64 bits: two layers' products and an attention leave some 1e-5 in a logit, and a score adds up one a step
+    assert gap > 1e-4
+    dec = Decoder(model, B, K, 64, 100, end)
+    dec.prompt(torch.from_numpy(prompts).cuda())
+    lines = [[list(map(int, p))] for p in prompts]
+    pos = torch.from_numpy(model.positions(80).astype(np.int32)).cuda()
+    lines = check_step(dec, lines, want[0], 1e-3)
+    for i in range(1, steps):
+        dec.step(pos)
+        lines = check_step(dec, lines, want[i], 1e-3)
+    # the end: one beam is kept, then nothing, and every block is free again
+    best = torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    r = api.reorder_beams(dec.k_cache, dec.v_cache, dec.table, dec.length, best, dec.free)
+    free = dec.free.after(r)
+    assert free.state.tolist()[1] == 100 - B * beam_plain.cover(P + steps - 1, SIZE)
+    r = api.resize_block_tables(r["block_table"].view(B, -1), dec.length, torch.zeros_like(dec.length), free, SIZE, 1)
+    free = free.after(r)
+    assert free.state.tolist()[1] == 100 and sorted(free.blocks.tolist()) == list(range(100))
+
+
+def test_a_captured_step_replayed_is_the_eager_one():
+    """The whole step in a graph, its state in place: each replay against the eager step, with eager work between them."""
+    B, K, P, steps, end = 2, 4, 11, 20, 3
+    model = Model(5)
+    prompts = torch.from_numpy(np.random.default_rng(5).integers(0, V, (B, P))).cuda()
+    pos = torch.from_numpy(model.positions(80).astype(np.int32)).cuda()
+    eager, dec = (Decoder(model, B, K, 64, 80, end) for _ in range(2))
+    for d in (eager, dec):
+        d.prompt(prompts)
+    names = ("table", "length", "scores", "finished", "tokens")
+    hold = {n: getattr(dec, n).clone() for n in names}
+    state, ring = dec.free.state.clone(), dec.free.blocks
+
+    def captured():
+        for n in names:
+            setattr(dec, n, hold[n])
+        dec.free = api.FreeBlocks(ring, state)
+        dec.step(pos)
+        for n in names:
+            hold[n].copy_(getattr(dec, n))
+        state.copy_(dec.free.state)
+    # a run ahead of the capture, taken back
+    saved = {n: t.clone() for n, t in hold.items()}, state.clone(), ring.clone(), dec.k_cache.clone(), dec.v_cache.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured()
+    for n in names:
+        hold[n].copy_(saved[0][n])
+    for t, s in zip((state, ring, dec.k_cache, dec.v_cache), saved[1:]):
+        t.copy_(s)
+    for _ in range(steps):
+        eager.step(pos)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in names:
+            assert torch.equal(hold[n], getattr(eager, n)), n
+        assert torch.equal(state, eager.free.state) and torch.equal(ring, eager.free.blocks)
+        assert torch.equal(dec.k_cache, eager.k_cache) and torch.equal(dec.v_cache, eager.v_cache)
+
+
+def test_calls_on_two_streams_at_once():
+    """The same calls with their own tensors on two streams, many times over: each gives what it gives alone."""
+    rng = np.random.default_rng(8)
+    jobs = []
+    for s in range(2):
+        x = torch.from_numpy(rng.standard_normal((4, 5, 9000)).astype(np.float32)).cuda()
+        sc = torch.from_numpy(-rng.random((4, 5)).astype(np.float32)).cuda()
+        table = torch.from_numpy(rng.permutation(200)[:4 * 5 * 9].reshape(4, 5, 9).astype(np.int32)).cuda()
+        free = api.FreeBlocks(torch.arange(180, 380, dtype=torch.int32, device="cuda") % 200, torch.tensor([0, 20], dtype=torch.int32, device="cuda"))
+        k, v = (torch.from_numpy(rng.standard_normal((2, 200, 1, 16, 64)).astype(np.float32)).cuda() for _ in range(2))
+        length, parent = torch.tensor([140, 33, 16, 0], dtype=torch.int32, device="cuda"), torch.from_numpy(rng.integers(0, 5, (4, 5)).astype(np.int32)).cuda()
+        jobs.append((x, sc, table, free, k, v, length, parent))
+
+    def run(j):
+        x, sc, table, free, k, v, length, parent = j
+        r = api.beam_select(x, sc, 6)
+        o = api.reorder_beams(k, v, table, length, parent, free)
+        return r["scores"], r["parent"], r["token"], o["block_table"], o["free_state"], o["status"]
+    alone = [run(j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(30):
+        got = []
+        for j, s in zip(jobs, streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(run(j))
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        for a, g in zip(alone, got):
+            assert all(torch.equal(p, q) for p, q in zip(a, g))
