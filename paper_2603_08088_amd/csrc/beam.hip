@@ -362,6 +362,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     };
     __shared__ Total s_total[kMergeCap + 4], s_best[ETV_MAX_BEAMS];
     __shared__ unsigned int s_again[2];
+    __shared__ Candidate s_head[4][kMergeThreads];
     const int b = blockIdx.x, t = threadIdx.x;
     const int lists = dsc.K * splits, M = dsc.M;
     heads += (size_t)b * lists;
@@ -369,12 +370,13 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     if (t == 0) s_status = 0;
     if (t < 2) s_again[t] = 0;
     __syncthreads();
-    // a thread's first list, on its way while the sums are joined: how many, and the first two
+    // a thread's first list, on its way while the sums are joined: how many, and the first four
     int head_n = 0;
-    int4 head = {};
+    int4 head[2] = {};
     if (t < lists) {
         head_n = heads[t].n;
-        head = *reinterpret_cast<const int4 *>(cands + (size_t)t * list);
+        head[0] = *reinterpret_cast<const int4 *>(cands + (size_t)t * list);
+        head[1] = *reinterpret_cast<const int4 *>(cands + (size_t)t * list + 2);
     }
     // 2^width lanes a beam
     for (int k0 = 0; k0 < dsc.K; k0 += kMergeThreads >> width) {
@@ -413,6 +415,11 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             s_base[k] = base, s_max[k] = most, s_state[k] = state;
         }
     }
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        s_head[2 * i][t] = {__int_as_float(head[i].x), head[i].y};
+        s_head[2 * i + 1][t] = {__int_as_float(head[i].z), head[i].w};
+    }
     __syncthreads();
     // entry i of list l, of beam k; places order as (beam, token) do
     const auto value = [&](const Candidate &c, int k, double &x, long &place) {
@@ -421,9 +428,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     };
     const auto entry = [&](int l, int k, int i, double &x, long &place) {
         if (s_state[k] == kBeamLive) {
-            Candidate c = {__int_as_float(i ? +head.z : +head.x), i ? +head.w : +head.y};
-            if (l != t || i > 1) c = cands[(size_t)l * list + i];
-            value(c, k, x, place);
+            value(l == t && i < 4 ? s_head[i][t] : cands[(size_t)l * list + i], k, x, place);
         } else {
             x = s_base[k];
             place = (long)k << 32 | (uint32_t)dsc.end_token;
@@ -504,9 +509,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
                     if (at < kMergeCap) s_total[at] = {x, place};
                     return true;
                 };
-                if (have > 0 && collect(0) && have > 1 && collect(1))
-                    for (int i = 2; i < have && collect(i); i++) {
-                    }
+                for (int i = 0; i < have && collect(i); i++) {
+                }
             }
             __syncthreads();
             found = s_n;
@@ -643,7 +647,7 @@ static int beam_splits(const etv_beam_desc *h) {
     return (int)((h->V + segment - 1) / segment);
 }
 
-static int beam_list(const etv_beam_desc *h) { return (h->M + 1) & ~1; }
+static int beam_list(const etv_beam_desc *h) { return (h->M + 3) & ~3; }
 
 static int32_t check_beam(const etv_beam_desc *h) {
     if (!h || h->B < 0 || h->K < 1 || h->M < 1 || h->V < 1 || h->end_token < -1 || h->end_token >= h->V) return ETV_ERR_INVALID_ARG;
