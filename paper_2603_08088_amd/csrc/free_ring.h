@@ -1,4 +1,4 @@
-// The ring of free blocks (eagletv.h, "Beam decoding over a paged cache") and sums over a workgroup of 256 threads.
+// The ring of free blocks (eagletv.h, "Beam decoding over a paged cache") and sums over a workgroup of W wavefronts.
 #pragma once
 #include "etv_common.h"
 
@@ -28,29 +28,36 @@ struct Ring {
 };
 
 // Sum of v over the workgroup; every thread calls it.
+template <int W>
 __device__ __forceinline__ long block_sum(long v) {
-    __shared__ long s_part[4];
+    __shared__ long s_part[W];
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
     __syncthreads();  // the last call's readers are done
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
     __syncthreads();
-    return s_part[0] + s_part[1] + s_part[2] + s_part[3];
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < W; w++) v += s_part[w];
+    return v;
 }
 
 // `carry` plus the sum of v over the threads before and with each (whose total stays below 2^31); carry grows by that total.  Every thread
 // calls it.
+template <int W>
 __device__ __forceinline__ long block_scan_sum(int v, long &carry) {
-    __shared__ int s_wave[4];
-    const int w = threadIdx.x >> 6;
-    int x = wave_scan_sum(v);
+    __shared__ int s_wave[W];
+    int x = wave_scan_sum(v), all = 0;
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) s_wave[w] = x;
+    if ((threadIdx.x & 63) == 63) s_wave[threadIdx.x >> 6] = x;
     __syncthreads();
-    const int a = s_wave[0], b = s_wave[1], c = s_wave[2], d = s_wave[3];
-    x += (w > 0 ? a : 0) + (w > 1 ? b : 0) + (w > 2 ? c : 0);
+#pragma unroll
+    for (int w = 0; w < W; w++) {
+        if (w < (int)(threadIdx.x >> 6)) x += s_wave[w];
+        all += s_wave[w];
+    }
     const long before = carry;
-    carry += a + b + c + d;
+    carry += all;
     return before + x;
 }
 

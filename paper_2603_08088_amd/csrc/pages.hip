@@ -4,9 +4,10 @@
 
 namespace etv {
 
+constexpr int kPageWaves = 8, kPageThreads = 64 * kPageWaves;
 constexpr int kSlotsPerWg = 1024;  // elements of slot_map that a workgroup writes
 constexpr int kFewRows = 64;       // up to so many new rows a thread checks the blocks of a sequence by itself
-constexpr int kMaxRow = 1 << 22;   // longest table row: 256 of them are counted in 31 bits
+constexpr int kMaxRow = (1 << 22) - 1;   // longest table row: kPageThreads of them are counted in 31 bits
 
 // What the lengths alone say of a sequence.
 struct PagePlan {
@@ -28,7 +29,7 @@ __device__ __forceinline__ PagePlan page_plan(const etv_pages_desc &dsc, uint32_
     return p;
 }
 
-// Workgroup 0: what is given back, and the ring's new state.  256 sequences at a time; those that give are put in a list, whose sequences the
+// Workgroup 0: what is given back, and the ring's new state.  kPageThreads sequences at a time; those that give are put in a list, whose sequences the
 // wavefronts share out among themselves.
 __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int32_t *len, const int32_t *new_len, const int32_t *block_table,
                           int32_t *free_blocks, const Ring &ring, int32_t *free_state_out, int32_t *len_out, int32_t *status) {
@@ -36,12 +37,23 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
         int b, first, n, bad;
         long at;
     };
-    __shared__ Giver s_giver[256];
+    __shared__ Giver s_giver[kPageThreads];
     __shared__ unsigned long long s_most[2];
-    const int t = threadIdx.x, lane = t & 63;
+    const int t = threadIdx.x;
+    // a wavefront's way along a row, eight entries a lane on their way at a time
+    const auto walk = [&](const int32_t *row, int n, auto f) {
+        for (int j0 = t & 63; j0 < n; j0 += 8 * 64) {
+            int32_t block[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) block[i] = row[min(j0 + i * 64, n - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (j0 + i * 64 < n) f(j0 + i * 64, block[i]);
+        }
+    };
     if (t < 2) s_most[t] = 0;
     long taken = 0, given = 0;
-    for (int b0 = 0; b0 < dsc.B; b0 += 256) {
+    for (int b0 = 0; b0 < dsc.B; b0 += kPageThreads) {
         const int b = b0 + t;
         int L = 0, N = 0;
         PagePlan p{0, 0, 0};
@@ -50,24 +62,23 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
             p = page_plan(dsc, inv_bs, L, N);
         }
         const int take = p.take(), give = p.give();
-        const long t_end = block_scan_sum(take, taken);  // a barrier, too: s_most is set
+        const long t_end = block_scan_sum<kPageWaves>(take, taken);  // a barrier, too: s_most is set
         if (take > 0 && t_end <= ring.count) atomicMax(&s_most[0], (unsigned long long)t_end);
         if (!__syncthreads_or(give)) continue;
         long before = 0;
-        const int place = (int)block_scan_sum(give > 0, before) - 1, n = (int)before;
+        const int place = (int)block_scan_sum<kPageWaves>(give > 0, before) - 1, n = (int)before;
         if (give > 0) s_giver[place] = {b, p.want, give, 0, 0};
         __syncthreads();
-        for (int s = t >> 6; s < n; s += 4) {
+        for (int s = t >> 6; s < n; s += kPageWaves) {
             const int32_t *row = block_table + (size_t)s_giver[s].b * dsc.max_blocks + s_giver[s].first;
             int bad = 0;
-#pragma unroll 4
-            for (int j = lane; j < s_giver[s].n; j += 64) bad |= (uint32_t)row[j] >= (uint32_t)dsc.num_blocks;
+            walk(row, s_giver[s].n, [&](int, int32_t block) { bad |= (uint32_t)block >= (uint32_t)dsc.num_blocks; });
             if (bad) s_giver[s].bad = 1;
         }
         __syncthreads();
         // in the order of the sequences, which is that of the list
         const int good = give > 0 && !s_giver[place].bad ? give : 0;
-        const long g_end = block_scan_sum(good, given);
+        const long g_end = block_scan_sum<kPageWaves>(good, given);
         if (give > 0) {
             const int32_t st = !good ? ETV_COMMIT_BAD_BLOCK : g_end > ring.room() ? ETV_BRANCH_BAD_FREE : 0;
             if (!st) atomicMax(&s_most[1], (unsigned long long)g_end);
@@ -77,11 +88,10 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
             len_out[b] = st ? L : N;
         }
         __syncthreads();
-        for (int s = t >> 6; s < n; s += 4) {
+        for (int s = t >> 6; s < n; s += kPageWaves) {
             const Giver g = s_giver[s];
             const int32_t *row = block_table + (size_t)g.b * dsc.max_blocks + g.first;
-#pragma unroll 4
-            for (int j = lane; j < g.n; j += 64) free_blocks[ring.place(g.at + j)] = row[j];
+            walk(row, g.n, [&](int j, int32_t block) { free_blocks[ring.place(g.at + j)] = block; });
         }
         __syncthreads();
     }
@@ -101,10 +111,49 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
     uint32_t rem;
     const int b_lo = (int)fast_div(e0, dsc.S, inv_S, rem), b_hi = (int)fast_div(min(e0 + kSlotsPerWg - 1, last), dsc.S, inv_S, rem);
     const int nb = b_hi - b_lo + 1;
+    const int first_len = len[b_lo], first_new = new_len[b_lo];
     long mine = 0;
-    for (int b = t; b < b_lo; b += 256) mine += page_plan(dsc, inv_bs, len[b], new_len[b]).take();
-    long base = b_lo > 0 ? block_sum(mine) : 0;
-    for (int s0 = 0; s0 < nb; s0 += 256) {
+    for (int b = t; b < b_lo; b += kPageThreads) mine += page_plan(dsc, inv_bs, len[b], new_len[b]).take();
+    long base = b_lo > 0 ? block_sum<kPageWaves>(mine) : 0;
+    if (nb == 1) {
+        // all of one sequence, the usual place of a workgroup where rows are many: tail, share of the ring and slots' blocks are asked for at once
+        const PagePlan p = page_plan(dsc, inv_bs, first_len, first_new);
+        const int take = p.take(), rows = p.st ? 0 : first_new - first_len;
+        int32_t st = p.st;
+        if (!st && take > 0 && base + take > ring.count) st = ETV_BRANCH_NO_BLOCKS;
+        int32_t *row = block_table + (size_t)b_lo * dsc.max_blocks;
+        const bool inside = rows > 0 && (long)p.old * dsc.block_size != first_len;
+        const int32_t tail = inside ? row[p.old - 1] : 0;
+        int bad = 0, block[kSlotsPerWg / kPageThreads], slot_of[kSlotsPerWg / kPageThreads];
+#pragma unroll
+        for (int i = 0; i < kSlotsPerWg / kPageThreads; i++) {
+            const uint32_t e = e0 + t + i * kPageThreads, r = e - (uint32_t)b_lo * dsc.S;
+            uint32_t off = 0;
+            const int j = e <= last && (int)r < rows ? (int)fast_div((uint32_t)first_len + r, dsc.block_size, inv_bs, off) : -1;
+            slot_of[i] = (int)off;
+            block[i] = j < 0 ? -1 : j < p.old || st ? tail : free_blocks[ring.place(base + j - p.old)];
+        }
+        if (!st)
+#pragma unroll 4
+            for (int j = t; j < take; j += kPageThreads) bad |= (uint32_t)free_blocks[ring.place(base + j)] >= (uint32_t)dsc.num_blocks;
+        bad = __syncthreads_or(bad);
+        if (!st && inside && (uint32_t)tail >= (uint32_t)dsc.num_blocks) st = ETV_COMMIT_BAD_BLOCK;
+        if (!st && bad) st = ETV_BRANCH_BAD_FREE;
+        if (t == 0 && p.give() == 0 && (uint32_t)b_lo * dsc.S >= e0) {
+            status[b_lo] = st;
+            len_out[b_lo] = st ? first_len : first_new;
+        }
+#pragma unroll
+        for (int i = 0; i < kSlotsPerWg / kPageThreads; i++) {
+            const uint32_t e = e0 + t + i * kPageThreads, r = e - (uint32_t)b_lo * dsc.S;
+            if (e > last) continue;
+            const bool there = !st && (int)r < rows;
+            if (slot_map) slot_map[e] = there ? block[i] * dsc.block_size + slot_of[i] : -1;
+            if (there && slot_of[i] == 0) row[(first_len + r) / (uint32_t)dsc.block_size] = block[i];
+        }
+        return;
+    }
+    for (int s0 = 0; s0 < nb; s0 += kPageThreads) {
         const int s = s0 + t, b = b_lo + s;
         PagePlan p{0, 0, 0};
         int L = 0, N = 0;
@@ -113,7 +162,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
             p = page_plan(dsc, inv_bs, L, N);
         }
         const int take = p.take();
-        const long end = block_scan_sum(take, base);
+        const long end = block_scan_sum<kPageWaves>(take, base);
         if (s >= nb) continue;
         int32_t st = p.st, tail = 0;
         const int rows = st ? 0 : N - L;
@@ -145,7 +194,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
             const int take = (int)fast_div((uint32_t)s_len[s] + rows + dsc.block_size - 1, dsc.block_size, inv_bs, off) - s_old[s];
             int bad = 0;
 #pragma unroll 4
-            for (int j = t; j < take; j += 256) bad |= (uint32_t)free_blocks[ring.place(s_base[s] + j)] >= (uint32_t)dsc.num_blocks;
+            for (int j = t; j < take; j += kPageThreads) bad |= (uint32_t)free_blocks[ring.place(s_base[s] + j)] >= (uint32_t)dsc.num_blocks;
             bad = __syncthreads_or(bad);
             if (t == 0) {
                 if (bad) s_rows[s] = 0;
@@ -158,7 +207,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
         __syncthreads();
     }
 #pragma unroll 4
-    for (int r = t; r < kSlotsPerWg; r += 256) {
+    for (int r = t; r < kSlotsPerWg; r += kPageThreads) {
         const uint32_t e = e0 + r;
         if (e > last) continue;
         uint32_t i;
@@ -175,7 +224,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
     }
 }
 
-__global__ void __launch_bounds__(256) resize_tables_kernel(etv_pages_desc dsc, uint32_t inv_bs, uint32_t inv_S, const int32_t *len, const int32_t *new_len,
+__global__ void __launch_bounds__(kPageThreads) resize_tables_kernel(etv_pages_desc dsc, uint32_t inv_bs, uint32_t inv_S, const int32_t *len, const int32_t *new_len,
                                                             int32_t *block_table, int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out,
                                                             int32_t *len_out, int32_t *slot_map, int32_t *status) {
     const Ring ring(free_state, dsc.num_blocks);
@@ -194,7 +243,7 @@ extern "C" int32_t etv_resize_block_tables(const etv_pages_desc *h, const int32_
     if ((int64_t)h->B * h->S > INT32_MAX - etv::kSlotsPerWg || (int64_t)h->num_blocks * h->block_size > INT32_MAX || h->max_blocks > etv::kMaxRow)
         return ETV_ERR_UNSUPPORTED;
     const unsigned wgs = 1 + (unsigned)(((int64_t)h->B * h->S + etv::kSlotsPerWg - 1) / etv::kSlotsPerWg);
-    hipLaunchKernelGGL(etv::resize_tables_kernel, dim3(wgs), dim3(256), 0, etv::as_stream(stream), *h, etv::fast_div_inv(h->block_size),
+    hipLaunchKernelGGL(etv::resize_tables_kernel, dim3(wgs), dim3(etv::kPageThreads), 0, etv::as_stream(stream), *h, etv::fast_div_inv(h->block_size),
                        etv::fast_div_inv(h->S), len, new_len, block_table, free_blocks, free_state, free_state_out, len_out, slot_map, status);
     return etv::check_launch();
 }

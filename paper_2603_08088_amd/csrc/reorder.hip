@@ -223,11 +223,11 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         const int o = b0 + t;
         ChunkRecord r{0, 0, 0, 0};
         if (o <= b) r = request(sh, ws, o);
-        const long need_end = block_scan_sum(r.need, needs);
+        const long need_end = block_scan_sum<4>(r.need, needs);
         int32_t st = r.st;
         if (!st && r.need > 0 && need_end > ring.count) st = ETV_BRANCH_NO_BLOCKS, r.give = 0;
         else if (r.need > 0) atomicMax((unsigned long long *)&s_taken, (unsigned long long)need_end);
-        const long give_end = block_scan_sum(r.give, gives);
+        const long give_end = block_scan_sum<4>(r.give, gives);
         if (r.give > 0) {
             if (give_end > ring.room()) st |= ETV_BRANCH_BAD_FREE;
             else atomicMax((unsigned long long *)&s_given, (unsigned long long)give_end);
