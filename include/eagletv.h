@@ -602,10 +602,11 @@ ETV_API int32_t etv_resize_block_tables(const etv_pages_desc *h_desc, const int3
  *
  *  q [B, T, Hq, d], k, v [B, T, Hkv, d] in, q_out, k_out, v_out out: heads and channels are contiguous, the strides of sequences and
  *            tokens are h_desc's, in elements (multiples of 16 bytes; pointers 16-byte aligned).  q and q_out NULL with Hq == 0; k, v
- *            NULL with Hkv == 0, v also alone; k_out, v_out nullable.  An output may be its input (same pointer and strides).
+ *            NULL with Hkv == 0, v also alone; k_out, v_out nullable.  An output may be its input (same pointer and strides); its
+ *            rows must not overlap.
  *  positions int32 [n_axes, B, T];  inv_freq float [rot_dim / 2];  n_rows int32 [B]  nullable (=> T)
  *  slot_map  int32 [B, T], k_cache, v_cache one layer in the layouts of the attention; all three or none
- * Supported: dtype F32 or BF16 (fp32 arithmetic, rounded once), d and rot_dim multiples of 16, 16 <= rot_dim <= d <= 256. */
+ * Supported: dtype F32 or BF16 (fp32 arithmetic, rounded once), d and rot_dim multiples of 16, 16 <= rot_dim <= d <= 256, B * T < 2^24. */
 #define ETV_ROTARY_INTERLEAVED 1
 #define ETV_ROTARY_INVERSE 2
 
@@ -635,7 +636,7 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
  *   Status bits: ETV_BEAM_BAD_LOGITS (a live beam's logits hold NaN or +inf: that beam offers nothing), ETV_BEAM_BAD_SCORE (a beam's
  *   score is NaN or +inf: the same), ETV_BEAM_SHORT (fewer than M are offered).
  *
- *  logits in [B, K, V], rows contiguous, strides in elements from h_desc;  scores in float [B, K]
+ *  logits in [B, K, V], rows contiguous, strides in elements from h_desc (0: one row for several beams);  scores in float [B, K]
  *  n_beams in int32 [B] nullable (=> K);  finished in uint8 [B, K] nullable
  *  out_scores float [B, M]; parent, token int32 [B, M]; finished_out uint8 [B, M] nullable; status int32 [B]
  *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.
@@ -671,7 +672,7 @@ ETV_API int32_t etv_beam_select(const etv_beam_desc *h_desc, const void *logits,
  *   row of the beam that it was for is -1.
  *
  *  k_cache, v_cache in/out; block_table in int32 [B, K, max_blocks]; len in int32 [B]; parent in int32 [B, M]
- *  table_out out int32 [B, M, max_blocks] (must not alias block_table); status out int32 [B]
+ *  table_out out int32 [B, M, max_blocks] (must not overlap block_table); status out int32 [B]
  *  workspace: etv_reorder_beams_workspace_bytes(B, K, M, max_blocks) bytes, 16-byte aligned.
  * Requires 1 <= K, M <= ETV_MAX_BEAMS, a paged cache (ETV_ERR_UNIMPLEMENTED otherwise) and d * elem_bytes % 16 == 0. */
 ETV_API size_t etv_reorder_beams_workspace_bytes(int32_t B, int32_t K, int32_t M, int32_t max_blocks);

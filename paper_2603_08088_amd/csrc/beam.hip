@@ -651,11 +651,10 @@ static int beam_list(const etv_beam_desc *h) { return (h->M + 3) & ~3; }
 
 static int32_t check_beam(const etv_beam_desc *h) {
     if (!h || h->B < 0 || h->K < 1 || h->M < 1 || h->V < 1 || h->end_token < -1 || h->end_token >= h->V) return ETV_ERR_INVALID_ARG;
-    if (h->K > 1 && h->row_stride < h->V) return ETV_ERR_INVALID_ARG;
-    if (h->B > 1 && h->batch_stride < 0) return ETV_ERR_INVALID_ARG;
+    if (h->row_stride < 0 || h->batch_stride < 0) return ETV_ERR_INVALID_ARG;
     if (h->dtype != ETV_F32 && h->dtype != ETV_BF16) return ETV_ERR_UNSUPPORTED;
     if (h->K > ETV_MAX_BEAMS || h->M > ETV_MAX_BEAMS || h->V > INT32_MAX - 65536) return ETV_ERR_UNSUPPORTED;
-    if ((int64_t)h->B * h->K * beam_splits(h) > INT32_MAX) return ETV_ERR_UNSUPPORTED;
+    if ((int64_t)h->B * h->K * beam_splits(h) >= (1 << 26)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
     return ETV_OK;
 }
 

@@ -6,7 +6,7 @@
 
 namespace etv {
 
-constexpr int kCols = 128;  // columns of the tables of one request that a workgroup takes
+constexpr int kCols = 64;  // columns of the tables of one request that a workgroup -- one wavefront -- takes
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
@@ -31,18 +31,15 @@ __device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len
     return ((long)len + sh.block_size - 1) / sh.block_size > sh.max_blocks ? ETV_COMMIT_CAPACITY : 0;
 }
 
-// grid (chunks, B), 128 threads: a thread per column of the table.  The old beams' entries of its column are asked for eight at a time; FEW: they
-// are eight at most and stay in its registers.
+// grid (chunks, B), one wavefront: a lane per column of the table, and per new beam.  The old beams' entries of its column are asked for eight at a
+// time; FEW: they are eight at most and stay in its registers.
 template <bool FEW>
 __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
                                                                int32_t *table_out, ReorderWorkspace ws) {
     extern __shared__ int32_t s_table[];  // [K][kCols]
-    __shared__ int s_parent[ETV_MAX_BEAMS];
-    __shared__ unsigned int s_alive[2];
-    const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 63, col = c * kCols + t;
+    const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, col = c * kCols + t;
     const int32_t *src = block_table + (size_t)b * sh.K * sh.max_blocks + min(col, sh.max_blocks - 1);
-    if (t < 2) s_alive[t] = 0;
-    const int p = t < sh.M ? parent[(size_t)b * sh.M + t] : -1;
+    int p = t < sh.M ? parent[(size_t)b * sh.M + t] : -1;
     int32_t id[8];
     for (int k0 = 0; k0 < sh.K; k0 += 8) {
 #pragma unroll
@@ -53,13 +50,11 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
         if (FEW) break;
     }
     int32_t st = length_status(sh, len[b]);
-    const int L = st ? 0 : len[b], full = L / sh.block_size, cols = (int)(((long)L + sh.block_size - 1) / sh.block_size);
-    __syncthreads();
-    const bool ok = p >= 0 && p < sh.K;
-    if (t < sh.M) s_parent[t] = ok ? p : -1;
-    if (ok) atomicOr(&s_alive[p >> 5], 1u << (p & 31));
-    if (__syncthreads_or(!ok && p != -1)) st |= ETV_COMMIT_BAD_NODE;
-    const uint64_t alive = s_alive[0] | (uint64_t)s_alive[1] << 32;
+    const int L = st ? 0 : len[b], full = (int)((uint32_t)L / (uint32_t)sh.block_size), rows = L - full * sh.block_size, cols = full + (rows > 0);
+    if (__ballot(p < -1 || p >= sh.K)) st |= ETV_COMMIT_BAD_NODE;
+    if (p >= sh.K) p = -1;
+    const auto either = [](uint32_t x, uint32_t y) { return x | y; };
+    const uint64_t alive = wave_best(p >= 0 && p < 32 ? 1u << p : 0u, either) | (uint64_t)wave_best(p >= 32 ? 1u << (p - 32) : 0u, either) << 32;
     const auto outside = [&](int32_t x) { return (uint32_t)x >= (uint32_t)sh.num_blocks; };
     int bad = 0;
     if (col < cols) {
@@ -70,11 +65,10 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
             for (int k = 0; k < sh.K; k++) bad |= (alive >> k & 1) && outside(s_table[k * kCols + t]);
         }
     }
-    if (__syncthreads_or(bad)) st |= ETV_COMMIT_BAD_BLOCK;
+    if (__ballot(bad)) st |= ETV_COMMIT_BAD_BLOCK;
     if (col < sh.max_blocks)
-#pragma unroll 4
         for (int i = 0; i < sh.M; i++) {
-            const int from = s_parent[i];
+            const int from = __builtin_amdgcn_readlane(p, i);
             table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && from >= 0 && col < cols ? s_table[from * kCols + t] : -1;
         }
     // blocks of beams without a child that neither a parent nor an earlier such beam has
@@ -100,27 +94,22 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
             }
         }
     }
-    __shared__ int s_wave[2];
-    const int count = __popcll(gone);
-    const int upto = wave_scan_sum(count);
-    if (lane == 63) s_wave[t >> 6] = upto;
-    __syncthreads();
+    const int count = __popcll(gone), upto = wave_scan_sum(count), all = __builtin_amdgcn_readlane(upto, 63);
     int32_t *list = ws.give + ((size_t)b * sh.chunks + c) * kCols * sh.K;
-    int at = upto - count + (t >= 64 ? s_wave[0] : 0);
-    for (; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kCols + t];
+    for (int at = upto - count; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kCols + t];
     // the half-filled block: its first child keeps it
-    const bool here = !st && L % sh.block_size != 0 && full / kCols == c;
+    const bool here = !st && rows > 0 && full / kCols == c;
     int need = 0;
-    if (t < 64) {
-        const int from = lane < sh.M ? s_parent[lane] : -1;
-        const int32_t own = here && from >= 0 ? s_table[from * kCols + full % kCols] : -1;
+    if (here) {
+        __syncthreads();  // another lane's column
+        const int32_t own = p >= 0 ? s_table[p * kCols + full % kCols] : -1;
         bool later = false;
-        for (int j = 0; j < sh.M; j++) later |= j < lane && __builtin_amdgcn_readlane(own, j) == own;
+        for (int j = 0; j < sh.M; j++) later |= j < t && __builtin_amdgcn_readlane(own, j) == own;
         later = later && own >= 0;
         need = __popcll(__ballot(later));
-        if (here && lane < sh.M) ws.from[(size_t)b * sh.M + lane] = later ? own : -1;
+        if (t < sh.M) ws.from[(size_t)b * sh.M + t] = later ? own : -1;
     }
-    if (t == 0) ws.records[(size_t)b * sh.chunks + c] = {st, need, s_wave[0] + s_wave[1], 0};
+    if (t == 0) ws.records[(size_t)b * sh.chunks + c] = {st, need, all, 0};
 }
 
 // What all chunks of a request say.
@@ -214,38 +203,64 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         }
         return;
     }
-    __shared__ long s_need, s_give, s_taken, s_given;
-    __shared__ int s_st, s_any;
+    __shared__ long s_need, s_give;
+    __shared__ unsigned long long s_taken, s_given;
+    __shared__ int s_part[6][4], s_chunk[256];
+    __shared__ long s_at[256];
     const int b = blockIdx.x;
-    if (t == 0) s_taken = s_given = 0;
-    long needs = 0, gives = 0;
-    for (int b0 = 0; b0 <= b; b0 += 256) {
-        const int o = b0 + t;
-        ChunkRecord r{0, 0, 0, 0};
-        if (o <= b) r = request(sh, ws, o);
-        const long need_end = block_scan_sum<4>(r.need, needs);
-        int32_t st = r.st;
-        if (!st && r.need > 0 && need_end > ring.count) st = ETV_BRANCH_NO_BLOCKS, r.give = 0;
-        else if (r.need > 0) atomicMax((unsigned long long *)&s_taken, (unsigned long long)need_end);
-        const long give_end = block_scan_sum<4>(r.give, gives);
-        if (r.give > 0) {
-            if (give_end > ring.room()) st |= ETV_BRANCH_BAD_FREE;
-            else atomicMax((unsigned long long *)&s_given, (unsigned long long)give_end);
-        }
-        if (o == b) s_st = st, s_need = need_end - r.need, s_give = give_end - r.give, s_any = r.need;
+    // what the requests before need and give, this one, and whether one of them is refused: sums over their records
+    int v[6] = {0, 0, 0, 0, 0, 0};
+    for (int i = t; i < (b + 1) * sh.chunks; i += 256) {
+        const ChunkRecord r = ws.records[i];
+        const bool own = i >= b * sh.chunks;
+        v[0] += own ? 0 : r.need;
+        v[1] += own ? r.need : 0;
+        v[2] += own ? 0 : r.give & 0xffff;
+        v[3] += own ? 0 : r.give >> 16;
+        v[4] += own ? r.give : 0;
+        v[5] |= r.st;
+    }
+#pragma unroll
+    for (int i = 0; i < 6; i++) {
+        const int sum = __builtin_amdgcn_readlane(wave_scan_sum(i < 5 ? v[i] : v[5] != 0), 63);
+        if (lane == 0) s_part[i][t >> 6] = sum;
     }
     __syncthreads();
-    int32_t st = s_st;
-    if (b == sh.B - 1 && t == 0) ring.leave(free_state_out, s_taken, s_given);
+#pragma unroll
+    for (int i = 0; i < 6; i++) v[i] = s_part[i][0] + s_part[i][1] + s_part[i][2] + s_part[i][3];
+    long need_at = v[0], give_at = v[2] + ((long)v[3] << 16), taken = need_at + v[1], given = give_at + v[4];
+    int own_need = v[1];
+    int32_t st = 0;
+    if (v[5] || taken > ring.count || given > ring.room()) {  // some are refused: one after the other
+        if (t == 0) s_taken = s_given = 0;
+        long needs = 0, gives = 0;
+        for (int b0 = 0; b0 <= b; b0 += 256) {
+            const int o = b0 + t;
+            ChunkRecord r{0, 0, 0, 0};
+            if (o <= b) r = request(sh, ws, o);
+            const long need_end = block_scan_sum<4>(r.need, needs);
+            int32_t os = r.st;
+            if (!os && r.need > 0 && need_end > ring.count) os = ETV_BRANCH_NO_BLOCKS, r.give = 0;
+            else if (r.need > 0) atomicMax(&s_taken, (unsigned long long)need_end);
+            const long give_end = block_scan_sum<4>(r.give, gives);
+            if (r.give > 0) {
+                if (give_end > ring.room()) os |= ETV_BRANCH_BAD_FREE;
+                else atomicMax(&s_given, (unsigned long long)give_end);
+            }
+            if (o == b) s_part[0][0] = os, s_part[1][0] = r.need, s_need = need_end - r.need, s_give = give_end - r.give;
+        }
+        __syncthreads();
+        st = s_part[0][0], own_need = s_part[1][0], need_at = s_need, give_at = s_give, taken = (long)s_taken, given = (long)s_given;
+    }
+    if (b == sh.B - 1 && t == 0) ring.leave(free_state_out, taken, given);
     const int L = len[b];
-    const long give_at = s_give;
     if (st) {
         for (size_t i = t; i < (size_t)sh.M * sh.max_blocks; i += 256) table_out[(size_t)b * sh.M * sh.max_blocks + i] = -1;
     } else {
-        if (s_any) {
+        if (own_need) {
             const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
             uint64_t todo = __ballot(from >= 0);
-            for (long i = s_need; todo; i++, todo &= todo - 1) {
+            for (long i = need_at; todo; i++, todo &= todo - 1) {
                 const int32_t dst = free_blocks[ring.place(i)];
                 int32_t *row = table_out + ((size_t)b * sh.M + __builtin_ctzll(todo)) * sh.max_blocks;
                 if ((uint32_t)dst < (uint32_t)sh.num_blocks) {
@@ -257,11 +272,17 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
             }
         }
         long at = ring.count + give_at;
-        for (int c = 0; c < sh.chunks; c++) {
-            const int n = ws.records[(size_t)b * sh.chunks + c].give;
-            const int32_t *list = ws.give + ((size_t)b * sh.chunks + c) * kCols * sh.K;
-            for (int i = t; i < n; i += 256) free_blocks[ring.place(at + i)] = list[i];
-            at += n;
+        for (int c0 = 0; v[4] && c0 < sh.chunks; c0 += 256) {  // the records of 256 chunks at a time, for the chunks that give anything
+            const int n = c0 + t < sh.chunks ? ws.records[(size_t)b * sh.chunks + c0 + t].give : 0;
+            const long end = block_scan_sum<4>(n, at);
+            s_chunk[t] = n;
+            s_at[t] = end - n;
+            __syncthreads();
+            for (int c = t >> 6; c < min(256, sh.chunks - c0); c += 4) {
+                const int32_t *list = ws.give + ((size_t)b * sh.chunks + c0 + c) * kCols * sh.K;
+                for (int i = lane; i < s_chunk[c]; i += 64) free_blocks[ring.place(s_at[c] + i)] = list[i];
+            }
+            __syncthreads();
         }
     }
     if (t == 0) status[b] = st;
@@ -290,7 +311,8 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
         hipLaunchKernelGGL(ring_copy_kernel, dim3(1), dim3(2), 0, s, free_state, free_state_out);
         return check_launch();
     }
-    if (!block_table || !len || !parent || !table_out || !status || table_out == block_table) return ETV_ERR_INVALID_ARG;
+    if (!block_table || !len || !parent || !table_out || !status) return ETV_ERR_INVALID_ARG;
+    if (table_out < block_table + (size_t)sh.B * sh.K * sh.max_blocks && block_table < table_out + (size_t)sh.B * sh.M * sh.max_blocks) return ETV_ERR_INVALID_ARG;
     for (int i = 0; i < cache.parts; i++)
         if ((double)cache.Hkv * sh.block_size * cache.row_bytes[i] >= 0x1p32) return ETV_ERR_UNSUPPORTED;
     for (int i = 0; i < cache.parts; i++)
@@ -305,7 +327,7 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
     const int64_t one = (int64_t)sh.B * cache.n_layers * cache.parts;
     int64_t G = 2048 / one;
     G = G < 1 ? 1 : G > sh.M ? sh.M : G;
-    if (sh.B + one * G > INT32_MAX) return ETV_ERR_UNSUPPORTED;
+    if (sh.B + one * G >= (1 << 24) || (int64_t)sh.chunks * sh.B >= (1 << 26)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
     hipLaunchKernelGGL(sh.K <= 8 ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(kCols), sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
     const int32_t rc = check_launch();
     if (rc != ETV_OK) return rc;

@@ -152,7 +152,7 @@ extern "C" int32_t etv_rotary_write_kv(const etv_rotary_desc *h, const void *q, 
     if (h->flags & ~(ETV_ROTARY_INTERLEAVED | ETV_ROTARY_INVERSE) || !(h->scale - h->scale == 0)) return ETV_ERR_INVALID_ARG;
     if (h->dtype != ETV_F32 && h->dtype != ETV_BF16) return ETV_ERR_UNSUPPORTED;
     if (h->d < 16 || h->d > 256 || h->d % 16 || h->rot_dim < 16 || h->rot_dim > h->d || h->rot_dim % 16) return ETV_ERR_UNSUPPORTED;
-    if ((int64_t)h->B * h->T > INT32_MAX || h->Hq > (1 << 16) || h->Hkv > (1 << 16)) return ETV_ERR_UNSUPPORTED;
+    if ((int64_t)h->B * h->T >= (1 << 24) || h->Hq > (1 << 16) || h->Hkv > (1 << 16)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
     for (int i = 0; i < h->rot_dim / 2; i++)
         if (h->axis_of[i] >= h->n_axes) return ETV_ERR_INVALID_ARG;
     if (h->B == 0) return ETV_OK;
@@ -161,16 +161,23 @@ extern "C" int32_t etv_rotary_write_kv(const etv_rotary_desc *h, const void *q, 
     if ((slot_map != nullptr) != (k_cache != nullptr) || (slot_map != nullptr) != (v_cache != nullptr) || (slot_map && (!k || !v || h->cache_rows < 0)))
         return ETV_ERR_INVALID_ARG;
     if (k && !k_out && !k_cache) return ETV_ERR_INVALID_ARG;  // k would go nowhere
+    etv_rotary_desc d = *h;
+    if (d.scale == 0) d.scale = 1;
     const void *ends[8] = {q, k, v, q_out, k_out, v_out, k_cache, v_cache};
     for (int i = 0; i < 8; i++) {
         if ((uintptr_t)ends[i] & 15) return ETV_ERR_INVALID_ARG;
         if (i >= 6 || !ends[i]) continue;
-        const int64_t unit = h->dtype == ETV_BF16 ? 8 : 4;
-        if (h->strides[2 * i] % unit || h->strides[2 * i + 1] % unit) return ETV_ERR_INVALID_ARG;
+        int64_t &seq = d.strides[2 * i], &tok = d.strides[2 * i + 1];
+        if (d.B == 1) seq = 0;  // of one sequence, of one token: not used
+        if (d.T == 1) tok = 0;
+        const int64_t unit = d.dtype == ETV_BF16 ? 8 : 4, row = (int64_t)(i % 3 ? d.Hkv : d.Hq) * d.d;
+        if (seq % unit || tok % unit || seq < 0 || tok < 0) return ETV_ERR_INVALID_ARG;
+        if (i < 3) continue;
+        // no two rows of an output lie on one another
+        if ((d.B > 1 && seq < row) || (d.T > 1 && tok < row)) return ETV_ERR_INVALID_ARG;
+        if (d.B > 1 && d.T > 1 && seq < (d.T - 1) * tok + row && tok < (d.B - 1) * seq + row) return ETV_ERR_INVALID_ARG;
     }
     if (!positions || !inv_freq) return ETV_ERR_INVALID_ARG;
-    etv_rotary_desc d = *h;
-    if (d.scale == 0) d.scale = 1;
     const etv::RotaryPtrs p{q, k, v, q_out, k_out, v_out, k_cache, v_cache};
     const bool inter = d.flags & ETV_ROTARY_INTERLEAVED;
     const auto kernel = d.dtype == ETV_BF16 ? (inter ? etv::rotary_kernel<uint16_t, true> : etv::rotary_kernel<uint16_t, false>)

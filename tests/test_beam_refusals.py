@@ -45,7 +45,7 @@ def rotary(d, q=A, k=A, v=A, pos=A, freq=A, n=A, qo=A, ko=A, vo=A, slots=A, kc=A
 
 @pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(T=0), -1), (dict(Hq=-1), -1), (dict(Hq=0, Hkv=0), -1), (dict(n_axes=0), -1), (dict(flags=4), -1), (dict(block_size=-1), -1),
                                    (dict(scale=math.nan), -1), (dict(scale=math.inf), -1), (dict(dtype=2), -2), (dict(d=72), -2), (dict(d=272), -2), (dict(rot_dim=0), -2),
-                                   (dict(rot_dim=80), -2), (dict(rot_dim=24), -2), (dict(cache_rows=-1), -1), (dict(B=1 << 16, T=1 << 16), -2), (dict(B=0), 0)])
+                                   (dict(rot_dim=80), -2), (dict(rot_dim=24), -2), (dict(cache_rows=-1), -1), (dict(B=1 << 12, T=1 << 12), -2), (dict(B=0), 0)])
 def test_rotary_descriptors(kw, rc):
     assert rotary(rotary_desc(**kw)) == rc
 
@@ -59,9 +59,20 @@ def test_rotary_pointers_strides_and_axes():
     assert rotary(d, ko=None, slots=None, kc=None, vc=None) == -1                    # k would go nowhere
     assert rotary(rotary_desc(Hq=0)) == rotary(rotary_desc(Hkv=0)) == -1             # heads that are not there
     for i in range(12):
-        bad = rotary_desc()
-        bad.strides[i] += 4
-        assert rotary(bad) == -1, i
+        for wrong in (4, -1 << 20):
+            bad = rotary_desc()
+            bad.strides[i] += wrong
+            assert rotary(bad) == -1, i
+        if i >= 6:                                                                   # rows of an output on one another
+            bad = rotary_desc()
+            bad.strides[i] = 0
+            assert rotary(bad) == -1, i
+    bad = rotary_desc(T=2)
+    bad.strides[6:8] = [256, 264]
+    assert rotary(bad) == -1
+    one = rotary_desc(B=1, T=1, block_size=-1)                                       # one row: its strides are not looked at, the rest is
+    one.strides[:] = [3] * 12
+    assert rotary(one) == -1
     d.axis_of[31] = 3
     assert rotary(d) == -1
     d.axis_of[31], d.axis_of[32] = 2, 9                                              # behind the last pair: not looked at
@@ -77,7 +88,7 @@ def select(d, x=A, s=A, n=A, f=A, o=A, p=A, t=A, fo=A, st=A, ws=A, size=1 << 40)
     return api.lib().etv_beam_select(C.byref(d), x, s, n, f, o, p, t, fo, st, ws, size, None)
 
 
-@pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(K=0), -1), (dict(M=0), -1), (dict(V=0), -1), (dict(end_token=-2), -1), (dict(end_token=1000), -1), (dict(row_stride=999), -1),
+@pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(K=0), -1), (dict(M=0), -1), (dict(V=0), -1), (dict(end_token=-2), -1), (dict(end_token=1000), -1), (dict(row_stride=-1), -1), (dict(batch_stride=-1), -1), (dict(B=1 << 20, K=64, V=1 << 20), -2),
                                    (dict(K=65), -2), (dict(M=65), -2), (dict(dtype=3), -2), (dict(V=2 ** 31 - 1, row_stride=2 ** 31), -2), (dict(B=0), 0)])
 def test_beam_descriptors(kw, rc):
     assert select(beam_desc(**kw)) == rc
@@ -117,6 +128,8 @@ def test_reorder_pointers_beams_and_workspace():
     d = cache_desc()
     for name in ("k", "v", "bt", "len", "p", "fb", "fs", "to", "fo", "st"):
         assert reorder(d, **{name: None}) == -1, name
+    assert reorder(d, to=A + 4 * 2 * 4 * 8 - 4) == reorder(d, to=A - 4 * 2 * 4 * 8 + 4) == -1          # overlapping tables
+    assert reorder(cache_desc(Hkv=1 << 15, d=256, block_size=256, num_blocks=4)) == -2              # a block of a layer beyond 32 bits
     assert reorder(d, k=A + 8) == reorder(d, to=A) == reorder(d, fo=A) == reorder(d, ws=A + 4) == -1
     assert reorder(d, K=0) == reorder(d, M=0) == -1 and reorder(d, K=65) == reorder(d, M=65) == -2
     need = api.reorder_beams_workspace_bytes(2, 4, 4, 8)

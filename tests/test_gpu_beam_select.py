@@ -69,6 +69,13 @@ def test_rows_apart_and_odd_vocabularies(dtype, pad):
     check(x, -rng.random((B, K)), 7, on=whole.cuda()[1:, 1:, :V])
 
 
+def test_one_row_for_all_beams():
+    rng = np.random.default_rng(21)
+    x = normal(rng, (3, 1, 6001), "bf16")
+    check(x.expand(3, 4, 6001), -rng.random((3, 4)), 9, on=x.cuda().expand(3, 4, 6001))
+    check(x[:1].expand(3, 4, 6001), -rng.random((3, 4)), 9, on=x[:1].cuda().expand(3, 4, 6001))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M", [1, 4, 33, 64])
 def test_ties_go_to_the_lowest(dtype, M):
@@ -138,6 +145,69 @@ def test_close_calls_between_beams():
     assert (gap < 1e-6).all()
     if (gap > 2e-8).all():
         check(x, scores, 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [7, 3000, 30001])
+@pytest.mark.parametrize("M", [2, 5])
+def test_calls_decided_by_the_last_bit_of_a_score(M, V, dtype):
+    """Rows with the same logits in other orders, whose sums are equal but for their rounding, and scores 2^-24 apart: the later beams are better."""
+    rng = np.random.default_rng(V)
+    x = normal(rng, (40, 1, V), dtype, 3.0).expand(40, 3, V).clone()
+    for b in range(40):
+        for k in range(3):
+            x[b, k] = x[b, k, torch.from_numpy(rng.permutation(V))]
+    scores = np.full((40, 3), -0.75) + np.arange(3) * 2.0 ** -24
+    r = check(x, scores, M)
+    assert (r["parent"][:, 0] == 2).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["normal", "ramp", "three lanes", "odd end"])
+def test_segments_of_many_steps(dtype, kind):
+    """As many rows as give a wavefront eight steps of a row; the beams of a request share one row, so that the definition is quick: their totals
+    are sums of a score and a logarithm, and the best are among the best of each."""
+    rng = np.random.default_rng(31)
+    B, K, M, step = 64, 64, 8, 2048 if dtype == "bf16" else 1024
+    V = 16 * step + (77 if kind == "odd end" else 0)
+    f = 2.0 * rng.standard_normal((B, V))
+    if kind == "ramp":
+        f = f * 1e-3 + np.linspace(6, -6, V) * rng.choice([-1, 1], (B, 1))
+    if kind == "three lanes":                     # all that is large lies with three lanes, in every step
+        lane = np.arange(V) // (8 if dtype == "bf16" else 4) % 64
+        f = np.where((lane > 20) & (lane < 24), f + 30, f)
+    x = torch.from_numpy(f.astype(np.float32)).to(DT[dtype])
+    scores = (-6 * rng.random((B, K))).astype(np.float32)
+    r = api.beam_select(x.cuda()[:, None].expand(B, K, V), dev(scores, np.float32), M)
+    f = x.double().numpy()
+    for b in range(B):
+        top = np.argsort(-f[b], kind="stable")[:M]
+        lse = f[b].max() + math.log(math.fsum(np.exp(f[b] - f[b].max())))
+        totals = scores[b].astype(np.float64)[:, None] + (f[b, top] - lse)
+        order = sorted(((-totals[k, i], k, int(top[i])) for k in range(K) for i in range(M)))[:M]
+        assert r["parent"][b].tolist() == [k for _, k, _ in order] and r["token"][b].tolist() == [v for _, _, v in order], b
+        want = np.array([-t for t, _, _ in order])
+        off = np.abs(r["scores"][b].double().cpu().numpy() - want)
+        assert (off <= slack(f[b][None, None], np.zeros((1, M), dtype=int))[0] + 2.0 ** -24 * np.abs(want) * (1 + 1e-6)).all()
+
+
+@pytest.mark.parametrize("M", [3, 16, 64])
+def test_logits_that_differ_in_their_last_bits(M):
+    """fp32 logits that agree in their upper halves: no bound tells them apart."""
+    rng = np.random.default_rng(41)
+    x = torch.from_numpy((1 + rng.permuted(np.tile(np.arange(9000), (2, 3, 1)), axis=-1) * 2.0 ** -23).astype(np.float32))
+    check(x, -rng.random((2, 3)) * 1e-3, M)
+
+
+@pytest.mark.parametrize("M", [5, 16, 40, 64])
+def test_more_candidates_than_a_merge_holds(M):
+    """Many lists, a few beams far ahead of the others; all totals alike."""
+    rng = np.random.default_rng(51)
+    x = normal(rng, (1, 64, 40000), "bf16")
+    scores = np.full((1, 64), -50.0) - rng.random((1, 64))
+    scores[0, [7, 20, 21]] = -rng.random(3)
+    check(x, scores, M)
+    check(torch.zeros((1, 64, 4100)), np.zeros((1, 64)), M)
 
 
 def test_the_workspace_may_hold_anything():

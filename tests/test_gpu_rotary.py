@@ -163,6 +163,27 @@ def test_values_that_are_not_finite_stay_with_their_pairs():
     assert torch.equal(~torch.isfinite(r), bad)
 
 
+def test_layouts_of_inputs_and_outputs():
+    """Tokens before sequences, one row of a larger tensor, one sequence for all: any strides that keep rows apart."""
+    c = Case(8, 3, 5, 4, 2, 64, "bf16", axes=2)
+    p = dev(c.positions)
+    want = api.rotary_write_kv(c.q, c.k, None, p, c.rotary)
+    turned = torch.empty((5, 3, 4, 64), dtype=c.dtype, device="cuda").transpose(0, 1)
+    r = api.rotary_write_kv(c.q.transpose(0, 1).contiguous().transpose(0, 1), None, None, p, c.rotary, out=dict(q=turned))
+    assert torch.equal(r["q"], want["q"])
+    r = api.rotary_write_kv(c.q[:1].expand(3, 5, 4, 64), None, None, p, c.rotary)
+    for b in range(3):
+        alone = api.rotary_write_kv(c.q[:1], None, None, p[:, b:b + 1].contiguous(), c.rotary)
+        assert torch.equal(r["q"][b], alone["q"][0])
+    one = c.q[1:2, 2:3].as_strided((1, 1, 4, 64), (1, 3, 64, 1))
+    r = api.rotary_write_kv(one, None, None, p[:, 1:2, 2:3].contiguous(), c.rotary)
+    assert torch.equal(r["q"][0, 0], want["q"][1, 2])
+    with pytest.raises(api.EtvError):
+        api.rotary_write_kv(c.q, None, None, p, c.rotary, out=dict(q=want["q"][:1].expand(3, 5, 4, 64)))
+    with pytest.raises(ValueError):                       # channels of a head that are not side by side with the next head's
+        api.rotary_write_kv(c.q[..., 8:40], None, None, p, api.Rotary(dev(freqs(16), np.float32)))
+
+
 def test_an_empty_batch():
     q = torch.empty((0, 3, 2, 64), device="cuda")
     r = api.rotary_write_kv(q, None, None, torch.empty((0, 3), dtype=torch.int32, device="cuda"), api.Rotary(dev(freqs(32), np.float32)))
