@@ -239,3 +239,45 @@ def test_calls_on_two_streams_at_once():
         torch.cuda.synchronize()
         for a, g in zip(alone, got):
             assert all(torch.equal(p, q) for p, q in zip(a, g))
+
+
+def test_a_draft_tree_grown_level_by_level():
+    """The candidates of a draft tree: each level the best continuations of the last one's nodes, their parents as the calls on trees take them."""
+    rng = np.random.default_rng(9)
+    B, width, levels = 3, 5, 4
+    head = (3 * rng.standard_normal((V, V))).astype(np.float32)            # a draft model that looks at one token
+    on, tokens = torch.from_numpy(head).cuda(), torch.from_numpy(rng.integers(0, V, (B, 1)).astype(np.int32)).cuda()
+    scores, first = torch.zeros((B, 1), device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    parents, nodes, base = [first], [tokens], 0
+    plain = [[(int(tokens[b, 0]), 0.0)] for b in range(B)]
+    plain_parent = [[0] for _ in range(B)]
+    for level in range(levels):
+        r = api.beam_select(on[tokens.long()], scores, width)
+        scores, tokens = r["scores"], r["token"]
+        parents.append(r["parent"] + base)
+        nodes.append(tokens)
+        for b in range(B):
+            offers = []
+            for i, (tok, score) in enumerate(plain[b]):
+                x = head[tok].astype(np.float64)
+                lp = score + x - (x.max() + math.log(np.exp(x - x.max()).sum()))
+                offers += [(-lp[v], i, v) for v in range(V)]
+            offers.sort()
+            plain_parent[b] += [base + i for _, i, _ in offers[:width]]
+            plain[b] = [(v, -s) for s, _, v in offers[:width]]
+            assert tokens[b].tolist() == [t for t, _ in plain[b]]
+        base += 1 if level == 0 else width
+    parent = torch.cat(parents, 1).contiguous()
+    assert parent.tolist() == plain_parent
+    n = torch.full((B,), parent.shape[1], dtype=torch.int32, device="cuda")
+    m = api.tensorize_tree(parent, n, torch.tensor([10, 0, 3], dtype=torch.int32, device="cuda"), 32, levels + 1)
+    assert m["status"].tolist() == [0] * B
+    level_of = [0] + [1 + i // width for i in range(levels * width)]
+    assert m["depth"].tolist() == [level_of] * B
+    # and the draft's rows at the nodes' positions
+    q = torch.randn((B, parent.shape[1], 2, 64), device="cuda")
+    rot = api.Rotary(torch.from_numpy((100.0 ** (-np.arange(32) / 32)).astype(np.float32)).cuda())
+    got = api.rotary_write_kv(q, None, None, m["position_ids"], rot)["q"].double().cpu().numpy()
+    pos = np.array([[p + d for d in level_of] for p in (10, 0, 3)])[None]
+    want = beam_plain.rotate(q.double().cpu().numpy(), pos, rot.inv_freq.cpu().numpy(), [0] * 32, False)
+    assert np.abs(got - want).max() <= 5 * 2.0 ** -24 * 2 * q.abs().max().item()
