@@ -8,9 +8,9 @@ namespace etv {
 // --------------------------------------------------------------------------------------------------------------
 // beam_select
 // --------------------------------------------------------------------------------------------------------------
-// What a wavefront leaves of its segment of one row, relative to the segment's largest logit, and the list of its best logits in order.
+// What a wavefront leaves of its segment of one row: a sum, and the list of its best logits in order.
 struct ScanHead {
-    float m;    // largest logit, -inf: none
+    float m;    // the segment's reference, its largest logit or up to kSlack less; -inf: it has none
     int32_t n;  // candidates in the list
     double s;   // sum of exp(x - m); NaN where a logit is NaN or +inf
 };
@@ -61,11 +61,12 @@ struct Logits<uint16_t> {
     static __device__ float one(uint16_t x) { return bf16_bits_to_float(x); }
 };
 
-// The largest of three.  (fmaxf costs an instruction more for each operand that might be a signalling NaN; one here makes the sum NaN.)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
+// The largest of nine.  (fmaxf costs an instruction more for each operand that might be a signalling NaN; one here makes the sum NaN.)
+__device__ __forceinline__ float max9(float m, const float *x) {
+    asm("v_max3_f32 %0, %1, %2, %0\n\tv_max3_f32 %0, %3, %4, %0\n\tv_max3_f32 %0, %5, %6, %0\n\tv_max3_f32 %0, %7, %8, %0"
+        : "+v"(m)
+        : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]));
+    return m;
 }
 
 // Order of fp32 numbers as unsigned integers, and back.
@@ -157,10 +158,11 @@ __device__ __forceinline__ double exp2_fast(double z) {
     return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
 }
 
-// exp(t) for t <= 0 in fp32: within 2^-23 (1 + |t|) of itself, and without an error that many terms have in common: log2(e) is in two parts, and
+// exp(t) for t <= kSlack in fp32: within 2^-23 (1 + |t|) of itself, and without an error that many terms have in common: log2(e) is in two parts, and
 // what the hardware's 2^y is off by in the mean (-3.4e-9, measured) is taken out of the sums.
 __device__ __forceinline__ float term(float t) { return __builtin_amdgcn_exp2f(fmaf(t, 1.44269502f, t * 1.92596299e-8f)); }
 constexpr double kTermMean = 1 + 3.4e-9;
+constexpr float kSlack = 16;
 
 // A segment of one row of logits by one wavefront: `steps` times 64 lanes' four vectors, the next step's on their way while one is worked on.  Every
 // logit takes part in the running sum; of the order only the largest of every two vectors is kept, the best two of them for each lane.  Those bound the
@@ -210,16 +212,17 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 #pragma unroll
         for (int i = 0; i < E; i++) r[i] = Logits<T>::get(raw[i / N], i % N);
 #pragma unroll
-        for (int i = 0; i < E / 2; i += 2) {
-            half[0] = max3(r[i], r[i + 1], half[0]);
-            half[1] = max3(r[E / 2 + i], r[E / 2 + i + 1], half[1]);
+        for (int i = 0; i < E / 2; i += 8) {
+            half[0] = max9(half[0], r + i);
+            half[1] = max9(half[1], r + E / 2 + i);
         }
         const float most = fmaxf(half[0], half[1]);
         s_most[step * 64 + t] = most;
         second = fmaxf(fmaxf(second, fminf(half[0], half[1])), fminf(best, most));
         best = fmaxf(best, most);
-        const float top = wave_best(most, [](float p, float q) { return fmaxf(p, q); });
-        if (top > ref) {
+        // the reference is the largest logit, give or take 16: a wavefront's maximum is taken where it may have to move, at first above all
+        if (__ballot(most > ref + kSlack)) {
+            const float top = wave_best(most, [](float p, float q) { return fmaxf(p, q); });
             s *= exp2_fast(fmax(((double)ref - (double)top) * kLog2e, -1000.0));
             ref = top;
         }
@@ -344,7 +347,7 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 }
 
 // A request: the logarithms of its beams' sums, then the M best of all candidates.
-//   total = (x - largest logit) + (score - log of the sum relative to it): nothing is lost where logits are large
+//   total = (x - reference) + (score - log of the sum relative to it): nothing is lost where logits are large
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
 // other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them.
 template <class T>
