@@ -576,7 +576,7 @@ ETV_API int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h_desc, const 
  *
  *  len, new_len  in  int32 [B];  block_table in/out int32 [B, max_blocks];  free_blocks in/out, free_state in, free_state_out out
  *  len_out int32 [B] (must alias neither length);  slot_map int32 [B, S]  nullable;  status int32 [B]
- * Requires B * S and num_blocks * block_size below 2^31. */
+ * Requires B * S (rounded up to 1024) and num_blocks * block_size below 2^31, and max_blocks < 2^22. */
 typedef struct etv_pages_desc {
     int32_t B;
     int32_t S;          /* row length of slot_map, and the most rows a sequence may grow by; at least 1 */
@@ -640,7 +640,8 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
  *  n_beams in int32 [B] nullable (=> K);  finished in uint8 [B, K] nullable
  *  out_scores float [B, M]; parent, token int32 [B, M]; finished_out uint8 [B, M] nullable; status int32 [B]
  *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.
- * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V. */
+ * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V < 2^31 - 65536; B * K times the segments of a row (1024 to 16384 logits
+ * each) below 2^26. */
 #define ETV_BEAM_BAD_LOGITS 1
 #define ETV_BEAM_BAD_SCORE 2
 #define ETV_BEAM_SHORT 4
@@ -674,7 +675,8 @@ ETV_API int32_t etv_beam_select(const etv_beam_desc *h_desc, const void *logits,
  *  k_cache, v_cache in/out; block_table in int32 [B, K, max_blocks]; len in int32 [B]; parent in int32 [B, M]
  *  table_out out int32 [B, M, max_blocks] (must not overlap block_table); status out int32 [B]
  *  workspace: etv_reorder_beams_workspace_bytes(B, K, M, max_blocks) bytes, 16-byte aligned.
- * Requires 1 <= K, M <= ETV_MAX_BEAMS, a paged cache (ETV_ERR_UNIMPLEMENTED otherwise) and d * elem_bytes % 16 == 0. */
+ * Requires 1 <= K, M <= ETV_MAX_BEAMS, a paged cache (ETV_ERR_UNIMPLEMENTED otherwise), d * elem_bytes % 16 == 0, B <= 65535,
+ * max_blocks <= 2^22, B * K * max_blocks and num_blocks * block_size below 2^31, and a block of one layer below 2^32 bytes. */
 ETV_API size_t etv_reorder_beams_workspace_bytes(int32_t B, int32_t K, int32_t M, int32_t max_blocks);
 
 ETV_API int32_t etv_reorder_beams(const etv_cache_desc *h_desc, void *k_cache, void *v_cache, const int32_t *block_table, const int32_t *len,

@@ -11,19 +11,16 @@ constexpr int kCols = 64;  // columns of the tables of one request that a workgr
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 struct ReorderShape {
-    int B, K, M, max_blocks, num_blocks, block_size, chunks;
+    int B, K, M, max_blocks, num_blocks, block_size, chunks, stride;
 };
-// What the first launch finds in one chunk of a request's columns.
-struct ChunkRecord {
-    int32_t st;    // status bits
-    int32_t need;  // blocks to copy into (the chunk that holds the half-filled block)
-    int32_t give;  // blocks given back; their ids follow in the chunk's list
-    int32_t pad;
-};
+// What the first launch finds.  Every workgroup of the second adds up what the requests before its own need and give, so that this is kept small
+// and apart, for loads of 16 bytes: 256 requests of 4096 columns are 16 KB of status and took 69 us as records of 16 bytes a chunk.
 struct ReorderWorkspace {
-    ChunkRecord *records;  // [B][chunks]
-    int32_t *from;         // [B][M]: the block to copy from, -1: none
-    int32_t *give;         // [B][chunks][kCols * K]
+    uint8_t *st;    // [B][stride]: status bits of a chunk of columns; 0 behind the chunks
+    int32_t *give;  // [B][stride]: blocks that the chunk gives back
+    int32_t *need;  // [B]: blocks to copy into, if the request is not refused
+    int32_t *from;  // [B][M]: the block to copy from, -1: none
+    int32_t *list;  // [B][chunks][kCols * K]: the ids of the blocks given back
 };
 
 __device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len) {
@@ -95,7 +92,7 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
         }
     }
     const int count = __popcll(gone), upto = wave_scan_sum(count), all = __builtin_amdgcn_readlane(upto, 63);
-    int32_t *list = ws.give + ((size_t)b * sh.chunks + c) * kCols * sh.K;
+    int32_t *list = ws.list + ((size_t)b * sh.chunks + c) * kCols * sh.K;
     for (int at = upto - count; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kCols + t];
     // the half-filled block: its first child keeps it
     const bool here = !st && rows > 0 && full / kCols == c;
@@ -109,21 +106,46 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
         need = __popcll(__ballot(later));
         if (t < sh.M) ws.from[(size_t)b * sh.M + t] = later ? own : -1;
     }
-    if (t == 0) ws.records[(size_t)b * sh.chunks + c] = {st, need, all, 0};
+    // one chunk says what the request needs: the half-filled block's, or the first (what a length is refused for, every chunk finds)
+    if (t == 0 && c == (rows > 0 ? full / kCols : 0)) ws.need[b] = need;
+    if (t < (c == sh.chunks - 1 ? sh.stride - c : 1)) {
+        ws.st[(size_t)b * sh.stride + c + t] = t == 0 ? st : 0;
+        ws.give[(size_t)b * sh.stride + c + t] = t == 0 ? all : 0;
+    }
 }
 
 // What all chunks of a request say.
-__device__ __forceinline__ ChunkRecord request(const ReorderShape &sh, const ReorderWorkspace &ws, int b) {
-    ChunkRecord r{0, 0, 0, 0};
+struct Request {
+    int32_t st, need, give;
+};
+__device__ __forceinline__ Request request(const ReorderShape &sh, const ReorderWorkspace &ws, int b) {
+    Request r{0, ws.need[b], 0};
     for (int c = 0; c < sh.chunks; c++) {
-        const ChunkRecord x = ws.records[(size_t)b * sh.chunks + c];
-        r.st |= x.st;
-        r.need += x.need;
-        r.give += x.give;
+        r.st |= ws.st[(size_t)b * sh.stride + c];
+        r.give += ws.give[(size_t)b * sh.stride + c];
     }
     if (r.st) r.need = r.give = 0;
     return r;
 }
+
+// Element i of n, 0 behind them; and f of the elements from one on, `threads` of them at a time and eight a thread on their way.  Few requests have as
+// few elements as threads: those are asked for together, and the loop is for the rest.
+template <class V>
+__device__ __forceinline__ V element(const V *x, int i, int n) {
+    return i < n ? x[i] : V{};
+}
+template <class V, class F>
+__device__ __forceinline__ void elements(const V *x, int from, int n, int threads, F f) {
+    for (int i0 = from; i0 < n; i0 += 8 * threads) {
+        V v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = x[min(i0 + i * threads, n - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i0 + i * threads < n) f(i0 + i * threads, v[i]);
+    }
+}
+__device__ __forceinline__ uint32_t any_of(const u32x4 &v) { return v.x | v.y | v.z | v.w; }
 
 struct CacheParts {
     uint8_t *base[4];
@@ -132,21 +154,6 @@ struct CacheParts {
     int parts, Hkv, n_layers;
 };
 
-// Blocks to copy into for requests [from, to), by one wavefront; `st` collects their status.
-__device__ __forceinline__ int needs(const ReorderShape &sh, const ReorderWorkspace &ws, int from, int to, int &st) {
-    int sum = 0, any = 0;
-    for (int i = from * sh.chunks + (threadIdx.x & 63); i < to * sh.chunks; i += 64) {
-        const ChunkRecord r = ws.records[i];
-        sum += r.need;
-        any |= r.st;
-    }
-    st = __ballot(any) != 0;
-    if (st && to - from > 1) {  // a refused request needs none
-        sum = 0;
-        for (int o = from + (threadIdx.x & 63); o < to; o += 64) sum += request(sh, ws, o).need;
-    }
-    return __builtin_amdgcn_readlane(wave_scan_sum(sum), 63);
-}
 
 // The rows of a half-filled block: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is shorter; AHEAD a
 // thread on their way.  (A block of one layer has less than 2^32 bytes.)
@@ -185,13 +192,22 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         const int part = x % cache.parts;
         x /= cache.parts;
         const int l = x % cache.n_layers, b = x / cache.n_layers;
-        int st, others;
         const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
         const int rows = (int)((uint32_t)len[b] % (uint32_t)sh.block_size);
-        const int need = needs(sh, ws, b, b + 1, st);
-        if (st || g >= need) return;
-        const long before = needs(sh, ws, 0, b, others);
-        if (before + need > ring.count) return;
+        const u32x4 *status = reinterpret_cast<const u32x4 *>(ws.st);
+        const int vectors = (b + 1) * (sh.stride / 16), need = ws.need[b];
+        int before = element(ws.need, lane, b);
+        uint32_t any = any_of(element(status, lane, vectors));
+        if (g >= need) return;
+        elements(ws.need, lane + 64, b, 64, [&](int, int n) { before += n; });
+        elements(status, lane + 64, vectors, 64, [&](int, const u32x4 &v) { any |= any_of(v); });
+        if (__ballot(any)) {  // a refused request needs none
+            if (request(sh, ws, b).st) return;
+            before = 0;
+            for (int o = lane; o < b; o += 64) before += request(sh, ws, o).need;
+        }
+        before = __builtin_amdgcn_readlane(wave_scan_sum(before), 63);
+        if ((long)before + need > ring.count) return;
         uint8_t *layer = cache.base[part] + (size_t)l * cache.layer_bytes[part];
         uint64_t todo = __ballot(from >= 0);
         for (int i = 0; i < need; i++, todo &= todo - 1) {
@@ -205,38 +221,43 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
     }
     __shared__ long s_need, s_give;
     __shared__ unsigned long long s_taken, s_given;
-    __shared__ int s_part[6][4], s_chunk[256];
-    __shared__ long s_at[256];
+    __shared__ int s_part[4][4];
     const int b = blockIdx.x;
-    // what the requests before need and give, this one, and whether one of them is refused: sums over their records
-    int v[6] = {0, 0, 0, 0, 0, 0};
-    for (int i = t; i < (b + 1) * sh.chunks; i += 256) {
-        const ChunkRecord r = ws.records[i];
-        const bool own = i >= b * sh.chunks;
-        v[0] += own ? 0 : r.need;
-        v[1] += own ? r.need : 0;
-        v[2] += own ? 0 : r.give & 0xffff;
-        v[3] += own ? 0 : r.give >> 16;
-        v[4] += own ? r.give : 0;
-        v[5] |= r.st;
-    }
+    // what the requests before need and give, this one, and whether one of them is refused.  (What all give is below 2^31: so are all entries.)
+    const u32x4 *gives = reinterpret_cast<const u32x4 *>(ws.give), *refused = reinterpret_cast<const u32x4 *>(ws.st);
+    const int own_at = b * (sh.stride / 4), gives_n = own_at + sh.stride / 4, refused_n = (b + 1) * (sh.stride / 16);
+    int v[4] = {0, 0, 0, 0}, own_need = ws.need[b];
+    const auto add_need = [&](int, int n) { v[0] += n; };
+    const auto add_give = [&](int i, const u32x4 &x) {
+        const int sum = (int)(x.x + x.y + x.z + x.w);
+        v[1] += i < own_at ? sum : 0;
+        v[2] += i < own_at ? 0 : sum;
+    };
+    const auto add_refused = [&](int, const u32x4 &x) { v[3] |= any_of(x) != 0; };
+    const int need0 = element(ws.need, t, b);
+    const u32x4 give0 = element(gives, t, gives_n), refused0 = element(refused, t, refused_n);
+    add_need(t, need0);
+    add_give(t, give0);
+    add_refused(t, refused0);
+    elements(ws.need, t + 256, b, 256, add_need);
+    elements(gives, t + 256, gives_n, 256, add_give);
+    elements(refused, t + 256, refused_n, 256, add_refused);
 #pragma unroll
-    for (int i = 0; i < 6; i++) {
-        const int sum = __builtin_amdgcn_readlane(wave_scan_sum(i < 5 ? v[i] : v[5] != 0), 63);
+    for (int i = 0; i < 4; i++) {
+        const int sum = __builtin_amdgcn_readlane(wave_scan_sum(v[i]), 63);
         if (lane == 0) s_part[i][t >> 6] = sum;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 6; i++) v[i] = s_part[i][0] + s_part[i][1] + s_part[i][2] + s_part[i][3];
-    long need_at = v[0], give_at = v[2] + ((long)v[3] << 16), taken = need_at + v[1], given = give_at + v[4];
-    int own_need = v[1];
+    for (int i = 0; i < 4; i++) v[i] = s_part[i][0] + s_part[i][1] + s_part[i][2] + s_part[i][3];
+    long need_at = v[0], give_at = v[1], taken = need_at + own_need, given = give_at + v[2];
     int32_t st = 0;
-    if (v[5] || taken > ring.count || given > ring.room()) {  // some are refused: one after the other
+    if (v[3] || taken > ring.count || given > ring.room()) {  // some are refused: one after the other
         if (t == 0) s_taken = s_given = 0;
         long needs = 0, gives = 0;
         for (int b0 = 0; b0 <= b; b0 += 256) {
             const int o = b0 + t;
-            ChunkRecord r{0, 0, 0, 0};
+            Request r{0, 0, 0};
             if (o <= b) r = request(sh, ws, o);
             const long need_end = block_scan_sum<4>(r.need, needs);
             int32_t os = r.st;
@@ -272,17 +293,16 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
             }
         }
         long at = ring.count + give_at;
-        for (int c0 = 0; v[4] && c0 < sh.chunks; c0 += 256) {  // the records of 256 chunks at a time, for the chunks that give anything
-            const int n = c0 + t < sh.chunks ? ws.records[(size_t)b * sh.chunks + c0 + t].give : 0;
-            const long end = block_scan_sum<4>(n, at);
-            s_chunk[t] = n;
-            s_at[t] = end - n;
-            __syncthreads();
-            for (int c = t >> 6; c < min(256, sh.chunks - c0); c += 4) {
-                const int32_t *list = ws.give + ((size_t)b * sh.chunks + c0 + c) * kCols * sh.K;
-                for (int i = lane; i < s_chunk[c]; i += 64) free_blocks[ring.place(s_at[c] + i)] = list[i];
+        for (int c0 = 0; v[2] && c0 < sh.chunks; c0 += 256) {  // 256 chunks at a time
+            const int n = c0 + t < sh.chunks ? ws.give[(size_t)b * sh.stride + c0 + t] : 0;
+            const long first = block_scan_sum<4>(n, at) - n;
+            for (uint64_t todo = __ballot(n > 0); todo; todo &= todo - 1) {  // those of a wavefront's lanes, one after the other
+                const int c = __builtin_ctzll(todo);
+                const int32_t *list = ws.list + ((size_t)b * sh.chunks + c0 + (t & ~63) + c) * kCols * sh.K;
+                const int count = __shfl(n, c);
+                const long to = __shfl(first, c);
+                for (int i = lane; i < count; i += 64) free_blocks[ring.place(to + i)] = list[i];
             }
-            __syncthreads();
         }
     }
     if (t == 0) status[b] = st;
@@ -291,20 +311,33 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
 // An empty batch takes and gives nothing.
 __global__ void ring_copy_kernel(const int32_t *free_state, int32_t *free_state_out) { free_state_out[threadIdx.x] = free_state[threadIdx.x]; }
 
-static int reorder_chunks(int max_blocks) { return (max_blocks + kCols - 1) / kCols; }
+static int reorder_chunks(int max_blocks) { return (max_blocks - 1) / kCols + 1; }
+static int reorder_stride(int chunks) { return (chunks + 15) & ~15; }
+
+// The shapes whose sums and launches stay in their types: less than 2^31 entries in all tables, less than 2^32 threads.
+static int32_t check_reorder(int64_t B, int64_t K, int64_t M, int64_t max_blocks) {
+    if (B < 0 || K < 1 || M < 1 || max_blocks < 1) return ETV_ERR_INVALID_ARG;
+    if (K > ETV_MAX_BEAMS || M > ETV_MAX_BEAMS || B > 65535 || max_blocks > (1 << 22) || B * K * max_blocks > INT32_MAX) return ETV_ERR_UNSUPPORTED;
+    return B * reorder_chunks((int)max_blocks) >= (1 << 26) ? ETV_ERR_UNSUPPORTED : ETV_OK;
+}
+
+static ReorderShape reorder_shape(int B, int K, int M, int max_blocks, int num_blocks, int block_size) {
+    const int chunks = max_blocks > 0 ? reorder_chunks(max_blocks) : 0;
+    return {B, K, M, max_blocks, num_blocks, block_size, chunks, reorder_stride(chunks)};
+}
 
 static size_t reorder_bytes(int64_t B, int64_t K, int64_t M, int max_blocks) {
-    const size_t lists = (size_t)B * reorder_chunks(max_blocks);
-    return lists * sizeof(ChunkRecord) + (size_t)B * M * 4 + lists * kCols * K * 4;
+    const size_t chunks = reorder_chunks(max_blocks);
+    return (size_t)B * (reorder_stride((int)chunks) * 5 + 4 + M * 4 + chunks * kCols * K * 4);
 }
 
 static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const int32_t *block_table, const int32_t *len, const int32_t *parent,
                        int32_t *free_blocks, const int32_t *free_state, int32_t *table_out, int32_t *free_state_out, int32_t *status, void *workspace,
                        size_t workspace_bytes, void *stream) {
     const ReorderShape sh = shape;
-    if (sh.B < 0 || sh.K < 1 || sh.M < 1 || sh.max_blocks < 1 || sh.num_blocks < 1 || cache.n_layers < 1 || cache.Hkv < 1) return ETV_ERR_INVALID_ARG;
-    if (sh.K > ETV_MAX_BEAMS || sh.M > ETV_MAX_BEAMS || sh.B > 65535 || sh.max_blocks > (1 << 22) || (int64_t)sh.num_blocks * sh.block_size > INT32_MAX)
-        return ETV_ERR_UNSUPPORTED;
+    const int32_t shape_rc = check_reorder(sh.B, sh.K, sh.M, sh.max_blocks);
+    if (shape_rc == ETV_ERR_INVALID_ARG || sh.num_blocks < 1 || cache.n_layers < 1 || cache.Hkv < 1) return ETV_ERR_INVALID_ARG;
+    if (shape_rc != ETV_OK || (int64_t)sh.num_blocks * sh.block_size > INT32_MAX) return ETV_ERR_UNSUPPORTED;
     if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
     hipStream_t s = as_stream(stream);
     if (sh.B == 0) {
@@ -320,15 +353,18 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
     if ((uintptr_t)workspace & 15) return ETV_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < reorder_bytes(sh.B, sh.K, sh.M, sh.max_blocks)) return ETV_ERR_WORKSPACE_TOO_SMALL;
     ReorderWorkspace ws;
-    ws.records = static_cast<ChunkRecord *>(workspace);
-    ws.from = reinterpret_cast<int32_t *>(ws.records + (size_t)sh.B * sh.chunks);
-    ws.give = ws.from + (size_t)sh.B * sh.M;
+    ws.st = static_cast<uint8_t *>(workspace);
+    ws.give = reinterpret_cast<int32_t *>(ws.st + (size_t)sh.B * sh.stride);
+    ws.need = ws.give + (size_t)sh.B * sh.stride;
+    ws.from = ws.need + sh.B;
+    ws.list = ws.from + (size_t)sh.B * sh.M;
     // a workgroup per copy while they are few, a loop over a request's copies beyond
     const int64_t one = (int64_t)sh.B * cache.n_layers * cache.parts;
     int64_t G = 2048 / one;
     G = G < 1 ? 1 : G > sh.M ? sh.M : G;
-    if (sh.B + one * G >= (1 << 24) || (int64_t)sh.chunks * sh.B >= (1 << 26)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
-    hipLaunchKernelGGL(sh.K <= 8 ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(kCols), sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
+    if (sh.B + one * G >= (1 << 24)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
+    hipLaunchKernelGGL(sh.K <= 8 ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(kCols),
+                       sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
     const int32_t rc = check_launch();
     if (rc != ETV_OK) return rc;
     hipLaunchKernelGGL(reorder_copy_kernel, dim3((unsigned)(sh.B + one * G)), dim3(256), 0, s, sh, cache, (int)G, len, free_blocks, free_state, table_out,
@@ -339,7 +375,7 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
 }  // namespace etv
 
 extern "C" size_t etv_reorder_beams_workspace_bytes(int32_t B, int32_t K, int32_t M, int32_t max_blocks) {
-    if (B < 0 || K < 1 || M < 1 || K > ETV_MAX_BEAMS || M > ETV_MAX_BEAMS || B > 65535 || max_blocks < 1 || max_blocks > (1 << 22)) return 0;
+    if (etv::check_reorder(B, K, M, max_blocks) != ETV_OK) return 0;
     return etv::reorder_bytes(B, K, M, max_blocks);
 }
 
@@ -349,7 +385,7 @@ extern "C" int32_t etv_reorder_beams(const etv_cache_desc *h, void *k_cache, voi
     if (!h || h->block_size < 0 || h->d < 1 || h->cache_layer_stride < 0) return ETV_ERR_INVALID_ARG;
     if (h->block_size == 0) return ETV_ERR_UNIMPLEMENTED;
     if ((h->elem_bytes != 2 && h->elem_bytes != 4) || (int64_t)h->d * h->elem_bytes % 16 || h->d > (1 << 16)) return ETV_ERR_UNSUPPORTED;
-    const etv::ReorderShape sh{h->B, K, M, h->max_blocks, h->num_blocks, h->block_size, etv::reorder_chunks(h->max_blocks)};
+    const etv::ReorderShape sh = etv::reorder_shape(h->B, K, M, h->max_blocks, h->num_blocks, h->block_size);
     etv::CacheParts cache{};
     cache.parts = 2, cache.Hkv = h->Hkv, cache.n_layers = h->n_layers;
     for (int i = 0; i < 2; i++) {
@@ -368,7 +404,7 @@ extern "C" int32_t etv_reorder_beams_q4(const etv_q4_desc *h, uint8_t *k_codes, 
     if (!h || h->block_size < 0 || h->layer_rows < 0) return ETV_ERR_INVALID_ARG;
     if (h->block_size == 0) return ETV_ERR_UNIMPLEMENTED;
     if (h->block_size % 16 || (h->d != 64 && h->d != 128)) return ETV_ERR_UNSUPPORTED;
-    const etv::ReorderShape sh{h->B, K, M, h->max_blocks, h->num_blocks, h->block_size, etv::reorder_chunks(h->max_blocks)};
+    const etv::ReorderShape sh = etv::reorder_shape(h->B, K, M, h->max_blocks, h->num_blocks, h->block_size);
     etv::CacheParts cache{};
     cache.parts = 4, cache.Hkv = h->Hkv, cache.n_layers = h->n_layers;
     uint8_t *base[4] = {k_codes, v_codes, k_scales, v_scales};

@@ -132,6 +132,7 @@ def test_reorder_pointers_beams_and_workspace():
     assert reorder(cache_desc(Hkv=1 << 15, d=256, block_size=256, num_blocks=4)) == -2              # a block of a layer beyond 32 bits
     assert reorder(d, k=A + 8) == reorder(d, to=A) == reorder(d, fo=A) == reorder(d, ws=A + 4) == -1
     assert reorder(d, K=0) == reorder(d, M=0) == -1 and reorder(d, K=65) == reorder(d, M=65) == -2
+    assert reorder(cache_desc(B=1 << 13, max_blocks=1 << 16)) == -2 and api.reorder_beams_workspace_bytes(1 << 13, 4, 4, 1 << 16) == 0   # 2^31 entries
     need = api.reorder_beams_workspace_bytes(2, 4, 4, 8)
     assert need > 0 and reorder(d, size=need - 1) == reorder(d, ws=None) == -3
     assert api.reorder_beams_workspace_bytes(2, 65, 4, 8) == api.reorder_beams_workspace_bytes(-1, 4, 4, 8) == 0

@@ -89,6 +89,30 @@ def test_lengths_at_the_borders_of_blocks_and_chunks(L, parent):
         assert after[1] == state[1] + len(set(table[0][table[0] >= 0].tolist())) and (out == -1).all()
 
 
+@pytest.mark.parametrize("refused", [(), (3,), (65, 300, 699)])
+def test_many_requests_of_several_chunks(refused):
+    """What the requests before a request need and give is added up over more of them than a workgroup takes at a time."""
+    rng = np.random.default_rng(700)
+    B, size = 700, 1
+    lens = [int(rng.integers(70, 140)) if b % 50 == 0 else int(rng.integers(1, 10)) for b in range(B)]
+    table, ring, state = beams(rng, B, 2, lens, size, 140, B)
+    size = 16
+    lens = [(L - 1) * size + 1 + L % size for L in lens]      # the same columns, most of them with a half-filled block
+    parent = rng.integers(0, 2, (B, 2))
+    for b in refused:
+        if b % 2: parent[b, 1] = 2                            # no such beam
+        else: table[b, 0, 0], table[b, 1, 0] = -7, -7         # no such block, in another chunk than the one being filled
+    *_, status, copies = check(rng, table, lens, parent, ring, state, size, layers=1, Hkv=1)
+    assert [b for b, st in enumerate(status) if st] == list(refused) and len(copies) > 200
+
+
+def test_a_long_table():
+    rng = np.random.default_rng(8)
+    table, ring, state = beams(rng, 1, 3, [20000 * 2 + 1], 2, 20002, 9, apart=2500)
+    *_, status, copies = check(rng, table, [40001], [[2, 2, -1]], ring, state, 2, layers=1, Hkv=1)
+    assert status == [0] and len(copies) == 1
+
+
 def test_beams_that_share_the_block_being_filled_part():
     """A table that was copied row by row: every beam but the first gets a block of its own, and rows without a beam do not count."""
     rng = np.random.default_rng(3)
