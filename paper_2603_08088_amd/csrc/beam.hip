@@ -5,9 +5,6 @@
 
 namespace etv {
 
-// --------------------------------------------------------------------------------------------------------------
-// beam_select
-// --------------------------------------------------------------------------------------------------------------
 // What a wavefront leaves of its segment of one row: a sum, and the list of its best logits in order.
 struct ScanHead {
     float m;    // the segment's reference, its largest logit or up to kSlack less; -inf: it has none
@@ -352,8 +349,9 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them.
 template <class T>
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
-                                                         const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list, const ScanHead *heads, const Candidate *cands,
-                                                         float *out_scores, int32_t *parent, int32_t *token, uint8_t *finished_out, int32_t *status) {
+                                                                   const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list,
+                                                                   const ScanHead *heads, const Candidate *cands, float *out_scores, int32_t *parent,
+                                                                   int32_t *token, uint8_t *finished_out, int32_t *status) {
     constexpr double kClose = 0x1p-22;
     __shared__ double s_base[ETV_MAX_BEAMS], s_max[ETV_MAX_BEAMS];
     __shared__ int s_state[ETV_MAX_BEAMS], s_status, s_n;
@@ -616,6 +614,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             if (s_state[k] != kBeamLive) continue;
             const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
             double s = 0;
+#pragma unroll 4
             for (int v = t; v < dsc.V; v += kMergeThreads) s += exp2_fast(fmax(((double)Logits<T>::one(x[v]) - s_max[k]) * kLog2e, -1000.0));
             s = block_sum(s);
             // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
