@@ -3,6 +3,7 @@
 // logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 11.1 us at the rate of a
 // large copy (5.17 TB/s).  The call takes 23.5 us there: the scan 17.3, the merge 6.3.
 #include "etv_common.h"
+#include <algorithm>
 #include <cfloat>
 #include <type_traits>
 
@@ -18,7 +19,7 @@ struct Candidate {
     float x;
     int32_t v;
 };
-constexpr int kMaxSteps = 8;     // steps of a segment
+constexpr int kMaxSteps = 16;    // steps of a segment
 constexpr int kMergeThreads = 512;
 constexpr int kMergeCap = 2048;  // candidates that a request collects; where more are close to its M-th best it looks for one after the other
 
@@ -144,8 +145,7 @@ __device__ __forceinline__ void block_best(K &key, P &place) {
 constexpr double kLog2e = 1.4426950408889634;
 
 // 2^z for |z| <= 1000, to 1.9e-9 of itself: a whole number n, taken off by a sum whose last bit is a one, and a polynomial in what is left (the
-// smallest relative error on [-1/2, 1/2] at its degree, by Remez's exchange); n goes into the exponent.  For the few exponentials that join sums, and
-// for the sums taken again: over all logits it would take 35 us where the scan takes 17.
+// smallest relative error on [-1/2, 1/2] at its degree, by Remez's exchange); n goes into the exponent.  For the few exponentials that join sums.
 __device__ __forceinline__ double exp2_fast(double z) {
     const double shifted = z + 6755399441055744.0;  // 1.5 * 2^52
     const double f = z - (shifted - 6755399441055744.0);
@@ -159,17 +159,18 @@ __device__ __forceinline__ double exp2_fast(double z) {
     return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
 }
 
-// exp(t) for t <= kSlack in fp32: within 2^-23 (1 + |t|) of itself, and without an error that many terms have in common: log2(e) is in two parts, and
-// what the hardware's 2^y is off by in the mean (-3.4e-9, measured) is taken out of the sums.
-__device__ __forceinline__ float term(float t) { return __builtin_amdgcn_exp2f(fmaf(t, 1.44269502f, t * 1.92596299e-8f)); }
+// exp(x) / 2^r in fp32, for a t = x - r ln(2) up to kSlack and |x| where it is not 0 up to kFarthest: within 2^-23 (1 + |t|) of itself, and without an error
+// that many terms have in common: log2(e) is in two parts, the first product is rounded behind the subtraction, and what the
+// hardware's 2^y is off by in the mean (-3.4e-9, measured) is taken out of the sums.
+__device__ __forceinline__ float term(float x, float r) { return __builtin_amdgcn_exp2f(fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -r))); }
 constexpr double kTermMean = 1 + 3.4e-9;
-constexpr float kSlack = 16;
+constexpr float kSlack = 1, kFarthest = 1 << 20;
 
 // A segment of one row of logits by one wavefront: `steps` times 64 lanes' four vectors, the next step's on their way while one is worked on.  Every
 // logit takes part in the running sum; of the order only the largest of every two vectors is kept, the best two of them for each lane.  Those bound the
 // M-th best of the segment from below (a number that M of them reach), and the few vectors that reach the bound are read again, from the
 // caches, for the candidates, which are ranked by counting.  TINY: fewer logits than a vector holds.
-// One wavefront a workgroup, so that no barrier stops the stream; segments of one step up to eight, by kFullWaves.  Bounds: memory where
+// One wavefront a workgroup, so that no barrier stops the stream.  Bounds: memory where
 // rows are many -- of the 17.3 us above the loads alone take 11.5, exponentials and sums 2.5, bound, candidates and ranking 3.5 --, and the
 // chain load, work, bound, candidates where they are few: 4 rows of 32000 fp32 logits 4.5 us, of which an empty launch is some 2.  Measured and left: wavefronts that
 // go from segment to segment with the next one's first loads under way (24.3 to 26.0 us: 135 registers leave 12 of them a CU, 86 leave 20).
@@ -178,8 +179,8 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
                                                        const uint8_t *finished, int splits, uint32_t inv_splits, uint32_t inv_K, int steps, int list, int room,
                                                        ScanHead *heads, Candidate *cands) {
     constexpr int N = Logits<T>::N, G = 4, E = G * N;
-    __shared__ float s_most[kMaxSteps * 64];
     extern __shared__ __attribute__((aligned(16))) Candidate s_cand[];  // [room + 8]
+    float *s_most = reinterpret_cast<float *>(s_cand + room + 8);       // [steps][64]
     __shared__ int s_n;
     uint32_t split, k;
     const int t = threadIdx.x;
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
     vec raw[G];
     load(raw, 0);
     if (beam_state(dsc, scores, n_beams, finished, b, k) != kBeamLive) return;
-    float ref = -INFINITY, best = -INFINITY, second = -INFINITY;
+    float ref = -INFINITY, ref2 = 0, best = -INFINITY, second = -INFINITY;
     double s = 0;
     const auto work = [&](const vec *raw, int step) {
         float r[E], half[2] = {-INFINITY, -INFINITY};
@@ -225,17 +226,17 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         s_most[step * 64 + t] = most;
         second = fmaxf(fmaxf(second, fminf(half[0], half[1])), fminf(best, most));
         best = fmaxf(best, most);
-        // the reference is the largest logit, give or take 16: a wavefront's maximum is taken where it may have to move, at first above all
+        // the reference is the largest logit, or up to 1 less: a wavefront's maximum is taken where it may have to move, at first above all
         if (__ballot(most > ref + kSlack)) {
             const float top = wave_best(most, [](float p, float q) { return fmaxf(p, q); });
-            s *= exp2_fast(fmax(((double)ref - (double)top) * kLog2e, -1000.0));
-            ref = top;
+            const float top2 = (float)(top * kLog2e);
+            if (ref > -INFINITY) s *= exp2_fast(fmax((double)ref2 - (double)top2, -1000.0));
+            ref = top, ref2 = top2;
         }
-        // NaN and +inf make the sum NaN; before the first logit that is neither masked nor NaN there is nothing but zeros and NaN to add
-        const float from = ref > -INFINITY ? ref : 0;
+        // a NaN makes the sum NaN; before the first logit that is neither masked nor NaN there is nothing but zeros and NaN to add
         float part[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < E; i++) part[i % 4] += term(r[i] - from);
+        for (int i = 0; i < E; i++) part[i % 4] += term(r[i], ref2);
         s += (double)(part[0] + part[1]) + (double)(part[2] + part[3]);
     };
     const int count = (v_end - v_begin + 64 * E - 1) / (64 * E);
@@ -250,6 +251,14 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
     const bool reaches_behind = v_begin + count * (64 * E) > V;
     if (reaches_behind) mask(raw, count - 1);
     work(raw, count - 1);
+    const auto all = [&](auto f) {
+        for (int v = v_begin + t; v < v_end; v += 64) f(v, Logits<T>::one(x[v]));
+    };
+    if (fabsf(ref) < kFarthest) s *= exp2_fast((double)ref2 - ref * kLog2e);  // relative to ref instead of what 32 bits hold of its logarithm
+    else if (ref != -INFINITY) {  // the differences themselves; with +inf they make the sum NaN
+        s = 0;
+        all([&](int, float y) { s += term(y - ref, 0); });
+    }
     s = lanes_sum(s, 6) * kTermMean;
     const uint32_t key = order_of(best) >> 16, key2 = order_of(second) >> 16;
     const float cut = reached_by([&](uint32_t c) { return __popcll(__ballot(key >= c)) + __popcll(__ballot(key2 >= c)); }, dsc.M);
@@ -274,9 +283,6 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
     Candidate *out = cands + (size_t)blockIdx.x * list;
     int n = s_n;
     if (n > room) {  // large ones side by side in a few lanes: a bound from all logits
-        const auto all = [&](auto f) {
-            for (int v = v_begin + t; v < v_end; v += 64) f(v, Logits<T>::one(x[v]));
-        };
         const float closer = reached_by<1>(
             [&](uint32_t c) {
                 int mine = 0;
@@ -354,7 +360,8 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // A request: the logarithms of its beams' sums, then the M best of all candidates.
 //   total = (x - reference) + (score - log of the sum relative to it): nothing is lost where logits are large
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
-// other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them.
+// other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them: so the order is that of
+// 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
 // Bound by the chain of its loads and barriers: 5.0 us for one request of 4 beams, 6.3 for 32 of 8 beams with 32 lists a row.  A scan whose
 // last workgroup merges would save this launch's 4 us on the host, but needs a counter that somebody clears, and a release to the whole device by every wavefront.
 template <class T>
@@ -362,7 +369,6 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
                                                                    const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list,
                                                                    const ScanHead *heads, const Candidate *cands, float *out_scores, int32_t *parent,
                                                                    int32_t *token, uint8_t *finished_out, int32_t *status) {
-    constexpr double kClose = 0x1p-22;
     __shared__ double s_base[ETV_MAX_BEAMS], s_max[ETV_MAX_BEAMS];
     __shared__ int s_state[ETV_MAX_BEAMS], s_status, s_n;
     __shared__ float s_cut[kMergeThreads / 64];
@@ -376,6 +382,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     __shared__ Candidate s_head[4][kMergeThreads];
     const int b = blockIdx.x, t = threadIdx.x;
     const int lists = dsc.K * splits, M = dsc.M;
+    const double close = 0x1p-22 * (6 + kSlack + 0.6932f * (32 - __builtin_clz(dsc.V)));
     heads += (size_t)b * lists;
     cands += (size_t)b * lists * list;
     if (t == 0) s_status = 0;
@@ -507,7 +514,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         for (int w = 1; w < kMergeThreads / 64; w++) cut = fmaxf(cut, s_cut[w]);
         int found;
         for (bool counted = false;; counted = true) {
-            cut = fmaxf(cut - fmaxf(fabsf(cut) * 0x1p-21f, 0x1p-20f), -FLT_MAX);  // and those too close to it
+            cut = fmaxf(cut - (fabsf(cut) * 0x1p-21f + (float)close), -FLT_MAX);  // and those too close to it
             for (int l = t; l < lists; l += kMergeThreads) {
                 int k;
                 const int have = entries(l, k);
@@ -596,7 +603,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         // equal rows.)
         const auto call = [&](const Total &a, const Total &o) {
             const int k = (int)(a.place >> 32), k1 = (int)(o.place >> 32);
-            if (k != k1 && a.x > o.x && a.x - o.x < kClose) {
+            if (k != k1 && a.x > o.x && a.x - o.x < close) {
                 atomicOr(&s_again[k >> 5], 1u << (k & 31));
                 atomicOr(&s_again[k1 >> 5], 1u << (k1 & 31));
             }
@@ -625,7 +632,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
             double s = 0;
 #pragma unroll 4
-            for (int v = t; v < dsc.V; v += kMergeThreads) s += exp2_fast(fmax(((double)Logits<T>::one(x[v]) - s_max[k]) * kLog2e, -1000.0));
+            for (int v = t; v < dsc.V; v += kMergeThreads) s += exp((double)Logits<T>::one(x[v]) - s_max[k]);
             s = block_sum(s);
             // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
             if (t == 0) s_base[k] = rint(((double)scores[(size_t)b * dsc.K + k] - log(s)) * 0x1p40) * 0x1p-40;
@@ -645,14 +652,19 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     if (t == 0) status[b] = s_status | (n < M ? ETV_BEAM_SHORT : 0);
 }
 
-// Steps of a wavefront's segment: as many as leave 4096 wavefronts, 16 a CU, for more of them mean fewer lists to merge.
-constexpr int kFullWaves = 4096;
+// Steps of a wavefront's segment: more of them mean fewer bounds to find and fewer lists to merge, and fewer wavefronts to hide that behind.  As many as
+// leave 1536 wavefronts, 6 a CU, up to eight (32 requests of 8 beams and 128000 logits: 22.3 us with 8 steps, 23.6 with 4, 24.5 with 2), sixteen where 4096 are
+// left (four times the requests: 60 us, 65 with 8 steps); a single one instead of two (64 requests of 4 beams and 32000 logits: 14.5 us, 15.0).  Segments are
+// as even as steps allow.  Large M: no more than eight, for each segment leaves M candidates.
+constexpr int kFullWaves = 1536, kManyWaves = 4096;
 static int beam_step(const etv_beam_desc *h) { return 64 * (h->dtype == ETV_BF16 ? 32 : 16); }
 static int beam_steps(const etv_beam_desc *h) {
-    const int64_t rows = (int64_t)h->B * h->K, all = (h->V + beam_step(h) - 1) / beam_step(h);
-    int n = 1;
-    while (n < kMaxSteps && rows * ((all + 2 * n - 1) / (2 * n)) >= kFullWaves) n *= 2;
-    return n;
+    const int64_t all = (h->V + beam_step(h) - 1) / beam_step(h), steps = (int64_t)h->B * h->K * all;
+    int64_t n = std::min<int64_t>(steps / kFullWaves, 8);
+    if (n < 3) n = 1;
+    if (h->M <= 16) n = std::max(n, std::min<int64_t>(steps / kManyWaves, kMaxSteps));
+    const int64_t splits = (all + n - 1) / n;
+    return (int)((all + splits - 1) / splits);
 }
 static int beam_splits(const etv_beam_desc *h) {
     const int64_t segment = (int64_t)beam_step(h) * beam_steps(h);
@@ -699,7 +711,7 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
         const uint32_t inv_splits = etv::fast_div_inv(splits);
         // room for the candidates: some times M where lists are short against the lanes, more of it fewer wavefronts at a time
         const int room = h->M <= 16 ? 256 : h->M <= 32 ? 512 : 1024;
-        hipLaunchKernelGGL(scan, dim3(lists), dim3(64), (room + 8) * sizeof(etv::Candidate), s, *h, x, scores, n_beams, finished, splits, inv_splits,
+        hipLaunchKernelGGL(scan, dim3(lists), dim3(64), (room + 8) * sizeof(etv::Candidate) + steps * 256, s, *h, x, scores, n_beams, finished, splits, inv_splits,
                            etv::fast_div_inv(h->K), steps, list, room, heads, cands);
         const int32_t rc = etv::check_launch();
         if (rc != ETV_OK) return rc;

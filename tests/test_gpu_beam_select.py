@@ -18,8 +18,9 @@ def dev(a, dtype=np.int32):
 
 def slack(x, parent):
     """How far a total may be off before its rounding: the relative error of its beam's sum.  A term exp(t) is an fp32 exponential of y = t log2(e):
-    t is rounded (2^-24 |t|), y is (2^-24 |t| in exp(t)), and the function is good to a unit in the last place (2^-23); so 2^-23 (1 + |t|), weighted
-    with the terms.  At most 10 fp32 additions lie between a term and the 64-bit sum (2^-24 each)."""
+    y is rounded twice (2^-24 |t| in exp(t) each time), and the function is good to a unit in the last place (2^-23); so 2^-23 (1 + |t|), weighted
+    with the terms.  t is relative to a reference that may lie 1 below the row's maximum, which adds 1 to its size at most: 2^-23 (2 + |x - max|).  At
+    most 10 fp32 additions lie between a term and the 64-bit sum (2^-24 each)."""
     off = np.zeros(parent.shape)
     with np.errstate(invalid="ignore", over="ignore"):
         t = x - x.max(-1, keepdims=True)
@@ -27,7 +28,7 @@ def slack(x, parent):
         mean = np.where(p > 0, p * -t, 0).sum(-1) / p.sum(-1)
     for b in range(len(parent)):
         off[b] = np.nan_to_num(mean[b])[np.maximum(parent[b], 0)]
-    return 2.0 ** -23 * (1 + off) + 10 * 2.0 ** -24
+    return 2.0 ** -23 * (2 + off) + 10 * 2.0 ** -24
 
 
 def check(logits, scores, M, n_beams=None, finished=None, end=-1, **kw):
@@ -131,6 +132,18 @@ def test_totals_far_apart_and_close_together(spread):
     check(big, [[0.0, -1.0]], 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [300.0, -3e5, 7e5, 1048576.0, -2e6, 1e9, -1e30, 3e38])
+def test_logits_far_from_zero(offset, dtype):
+    """Terms are relative to a reference whose product with log2(e) 32 bits round; masks of the type's lowest value are far from every reference."""
+    rng = np.random.default_rng(17)
+    x = (normal(rng, (2, 3, 9001), "f32", 2.0) + offset).to(DT[dtype])
+    x[:, 1, ::3] = torch.finfo(DT[dtype]).min
+    x[1, 2, :5000] = -math.inf
+    x[0, 0, 8000] += x[0, 0].abs().max() * 0.01
+    check(x, -rng.random((2, 3)), 5)
+
+
 def test_close_calls_between_beams():
     """Totals of different beams that differ by a few 1e-8: decided as in 64 bits."""
     rng = np.random.default_rng(13)
@@ -208,6 +221,26 @@ def test_more_candidates_than_a_merge_holds(M):
     scores[0, [7, 20, 21]] = -rng.random(3)
     check(x, scores, M)
     check(torch.zeros((1, 64, 4100)), np.zeros((1, 64)), M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_few_values_whose_totals_nearly_meet(dtype):
+    """All terms of such a row are off by the same: scores bring the best totals of two beams to within an fp32 step of each other, either way."""
+    rng = np.random.default_rng(61)
+    B, V = 64, 20000
+    x = torch.zeros((B, 2, V))
+    for b in range(B):
+        for k in range(2):
+            low, n = -float(rng.uniform(1, 11)), int(rng.integers(1, 9))
+            x[b, k] = low
+            x[b, k, torch.from_numpy(rng.permutation(V)[:n])] = 0
+    x = x.to(DT[dtype])
+    f = x.double().numpy()
+    lse = np.log(np.exp(f).sum(-1))
+    scores = np.stack((np.full(B, -0.25), -0.25 + lse[:, 1] - lse[:, 0]), 1).astype(np.float32)
+    gap = (scores[:, 0].astype(np.float64) - lse[:, 0]) - (scores[:, 1].astype(np.float64) - lse[:, 1])
+    assert (np.abs(gap) < 1e-6).all() and (np.abs(gap) > 2.0 ** -39).all() and (gap > 0).any() and (gap < 0).any()
+    check(x, scores, 12)
 
 
 def test_the_workspace_may_hold_anything():
