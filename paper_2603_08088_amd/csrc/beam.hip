@@ -1,7 +1,7 @@
 // The best continuations over beams and vocabulary, total[k, v] = score[k] + x[k, v] - log sum_v' exp(x[k, v']): one pass over the logits, which
 // leaves of every segment of a row its sum relative to a reference and its M best logits in order, then a merge per request.  Floor: the
 // logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 11.1 us at the rate of a
-// large copy (5.17 TB/s).  The call takes 23.5 us there: the scan 17.3, the merge 6.3.
+// large copy (5.17 TB/s).  The call takes 22.4 us there: the scan 16.0, the merge 6.5.
 #include "etv_common.h"
 #include <algorithm>
 #include <cfloat>
@@ -171,9 +171,9 @@ constexpr float kSlack = 1, kFarthest = 1 << 20;
 // M-th best of the segment from below (a number that M of them reach), and the few vectors that reach the bound are read again, from the
 // caches, for the candidates, which are ranked by counting.  TINY: fewer logits than a vector holds.
 // One wavefront a workgroup, so that no barrier stops the stream.  Bounds: memory where
-// rows are many -- of the 17.3 us above the loads alone take 11.5, exponentials and sums 2.5, bound, candidates and ranking 3.5 --, and the
+// rows are many -- of the 16.0 us above the loads alone take 11.5, the rest are exponentials and sums, and bound, candidates and ranking --, and the
 // chain load, work, bound, candidates where they are few: 4 rows of 32000 fp32 logits 4.5 us, of which an empty launch is some 2.  Measured and left: wavefronts that
-// go from segment to segment with the next one's first loads under way (24.3 to 26.0 us: 135 registers leave 12 of them a CU, 86 leave 20).
+// go from segment to segment with the next one's first loads under way (half a us to two longer: 135 registers leave 12 of them a CU, 86 leave 20).
 template <class T, bool TINY>
 __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
                                                        const uint8_t *finished, int splits, uint32_t inv_splits, uint32_t inv_K, int steps, int list, int room,
@@ -362,9 +362,10 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
 // other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them: so the order is that of
 // 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
-// Bound by the chain of its loads and barriers: 5.0 us for one request of 4 beams, 6.3 for 32 of 8 beams with 32 lists a row.  A scan whose
+// Bound by the chain of its loads and barriers: 5.2 us for one request of 4 beams, some 6.5 for 32 of 8 beams with 8 lists each.  A scan whose
 // last workgroup merges would save this launch's 4 us on the host, but needs a counter that somebody clears, and a release to the whole device by every wavefront.
-template <class T>
+// SHARED: few lists against M, which are therefore gone into deeply, by several threads each.
+template <class T, bool SHARED>
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
                                                                    const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list,
                                                                    const ScanHead *heads, const Candidate *cands, float *out_scores, int32_t *parent,
@@ -388,13 +389,18 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     if (t == 0) s_status = 0;
     if (t < 2) s_again[t] = 0;
     __syncthreads();
-    // a thread's first list, on its way while the sums are joined: how many, and the first four
+    // A list is gone through by 2^share threads.  A thread's first one is on its way while the sums are joined: how many, and the first four of the
+    // thread's entries, 2^share apart.
+    int share = 0;
+    if (SHARED)
+        while (lists << (share + 1) <= kMergeThreads) share++;
+    const int own = t >> share, deep = t & ((1 << share) - 1), apart = 1 << share;
     int head_n = 0;
-    int4 head[2] = {};
-    if (t < lists) {
-        head_n = heads[t].n;
-        head[0] = *reinterpret_cast<const int4 *>(cands + (size_t)t * list);
-        head[1] = *reinterpret_cast<const int4 *>(cands + (size_t)t * list + 2);
+    Candidate head[4] = {};
+    if (own < lists) {
+        head_n = heads[own].n;
+#pragma unroll
+        for (int i = 0; i < 4; i++) head[i] = cands[(size_t)own * list + min(deep + i * apart, list - 1)];
     }
     // 2^width lanes a beam
     for (int k0 = 0; k0 < dsc.K; k0 += kMergeThreads >> width) {
@@ -434,34 +440,33 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         }
     }
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        s_head[2 * i][t] = {__int_as_float(head[i].x), head[i].y};
-        s_head[2 * i + 1][t] = {__int_as_float(head[i].z), head[i].w};
-    }
+    for (int i = 0; i < 4; i++) s_head[i][t] = head[i];
     __syncthreads();
-    // entry i of list l, of beam k; places order as (beam, token) do
+    // entry `deep` + i * `apart` of list l, of beam k; places order as (beam, token) do
     const auto value = [&](const Candidate &c, int k, double &x, long &place) {
         x = ((double)c.x - s_max[k]) + s_base[k];
         place = (long)k << 32 | (uint32_t)c.v;
     };
     const auto entry = [&](int l, int k, int i, double &x, long &place) {
         if (s_state[k] == kBeamLive) {
-            value(l == t && i < 4 ? s_head[i][t] : cands[(size_t)l * list + i], k, x, place);
+            value(l == own && i < 4 ? s_head[i][t] : cands[(size_t)l * list + deep + i * apart], k, x, place);
         } else {
             x = s_base[k];
             place = (long)k << 32 | (uint32_t)dsc.end_token;
         }
     };
-    const auto entries = [&](int l, int &k) {
+    // how many a list has, and how many of them are the thread's
+    const auto length = [&](int l, int &k) {
         uint32_t rest;
         k = (int)fast_div(l, splits, inv_splits, rest);
         const int state = s_state[k];
-        return state == kBeamLive ? l == t ? head_n : heads[l].n : state == kBeamDone && rest == 0 ? 1 : 0;
+        return state == kBeamLive ? l == own ? head_n : heads[l].n : state == kBeamDone && rest == 0 ? 1 : 0;
     };
+    const auto entries = [&](int l, int &k) { return (length(l, k) - deep + apart - 1) >> share; };
     int n;
     for (int round = 0;; round++) {
         float top = -INFINITY;
-        for (int l = t; l < lists; l += kMergeThreads) {
+        for (int l = own; l < lists; l += kMergeThreads) {
             int k;
             if (entries(l, k) > 0) {
                 double x;
@@ -473,27 +478,24 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         const uint32_t key = order_of(top) >> 16;
         if (t == 0) s_n = 0;
         if (M > 16) {
-            // samples of all lists: where lists are few several threads look into one, `apart` entries from each other
-            int share = 0;
-            while (lists << (share + 1) <= kMergeThreads) share++;
-            const int apart = (M + (1 << share) - 1) >> share, deep = t & ((1 << share) - 1);
+            // samples of all lists: where several threads look into one, `gap` entries from each other
+            const int gap = (M + apart - 1) >> share;
             uint32_t sample = key;
-            if (share) {
+            if (deep) {
                 int k;
-                const int l = t >> share;
                 sample = 0;
-                if (l < lists && deep * apart < entries(l, k)) {
+                if (own < lists && deep * gap < length(own, k)) {
                     double x;
                     long place;
-                    entry(l, k, deep * apart, x, place);
+                    value(cands[(size_t)own * list + deep * gap], k, x, place);
                     sample = order_of((float)x) >> 16;
                 }
             }
-            // a first sample stands for one entry, each further one for `apart`; the parts of a count alternate between two places, for one barrier each
+            // a first sample stands for one entry, each further one for `gap`; the parts of a count alternate between two places, for one barrier each
             int turn = 0;
             const float all = reached_by<1>(
                 [&](uint32_t c) {
-                    const int part = __popcll(__ballot(!deep && sample >= c)) + apart * __popcll(__ballot(deep && sample >= c));
+                    const int part = __popcll(__ballot(!deep && sample >= c)) + gap * __popcll(__ballot(deep && sample >= c));
                     turn ^= 1;
                     if ((t & 63) == 0) s_part[turn][t >> 6] = part;
                     __syncthreads();
@@ -515,7 +517,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         int found;
         for (bool counted = false;; counted = true) {
             cut = fmaxf(cut - (fabsf(cut) * 0x1p-21f + (float)close), -FLT_MAX);  // and those too close to it
-            for (int l = t; l < lists; l += kMergeThreads) {
+            for (int l = own; l < lists; l += kMergeThreads) {
                 int k;
                 const int have = entries(l, k);
                 const auto collect = [&](int i) {
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             cut = reached_by<1>(
                 [&](uint32_t c) {
                     int n = 0;
-                    for (int l = t; l < lists; l += kMergeThreads) {
+                    for (int l = own; l < lists; l += kMergeThreads) {
                         int k, lo = 0, hi = entries(l, k);
                         while (lo < hi) {
                             const int i = (lo + hi) >> 1;
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             for (n = 0; n < M; n++) {
                 double best = -INFINITY;
                 long at = INT64_MAX;
-                for (int l = t; l < lists; l += kMergeThreads) {
+                for (int l = own; l < lists; l += kMergeThreads) {
                     int k;
                     const int have = entries(l, k);
                     for (int i = 0; i < have; i++) {
@@ -612,7 +614,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         if (n == M && found <= kMergeCap) {
             for (int i = t; i < found; i += kMergeThreads) call(s_best[M - 1], s_total[i]);
         } else if (n == M) {
-            for (int l = t; l < lists; l += kMergeThreads) {
+            for (int l = own; l < lists; l += kMergeThreads) {
                 int k;
                 const int have = entries(l, k);
                 for (int i = 0; i < have; i++) {
@@ -717,7 +719,9 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
         if (rc != ETV_OK) return rc;
         int width = 0;  // as many lanes a beam as it has segments, up to a wavefront
         while (width < 6 && (1 << width) < splits) width++;
-        hipLaunchKernelGGL(etv::beam_merge_kernel<T>, dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits,
+        // 64 requests of 10 beams in 4 lists each 24.5 us, 27.3 with a thread a list; 8 requests of 4 beams in 63 lists 11.5 us, 12.2 if they were shared
+        const bool shared = splits * h->K <= 16 * h->M && splits * h->K <= etv::kMergeThreads / 2;
+        hipLaunchKernelGGL((shared ? etv::beam_merge_kernel<T, true> : etv::beam_merge_kernel<T, false>), dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits,
                            width, list, heads, cands, out_scores, parent, token, finished_out, status);
         return etv::check_launch();
     };
