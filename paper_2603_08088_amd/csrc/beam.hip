@@ -1,7 +1,7 @@
 // The best continuations over beams and vocabulary, total[k, v] = score[k] + x[k, v] - log sum_v' exp(x[k, v']): one pass over the logits, which
 // leaves of every segment of a row its sum relative to a reference and its M best logits in order, then a merge per request.  Floor: the
 // logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 11.1 us at the rate of a
-// large copy (5.17 TB/s).  The call takes 22.4 us there: the scan 16.0, the merge 6.5.
+// large copy (5.17 TB/s).  The call takes 21.5 us there: the scan 15.6, the merge 6.
 #include "etv_common.h"
 #include <algorithm>
 #include <cfloat>
@@ -179,8 +179,8 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
                                                        const uint8_t *finished, int splits, uint32_t inv_splits, uint32_t inv_K, int steps, int list, int room,
                                                        ScanHead *heads, Candidate *cands) {
     constexpr int N = Logits<T>::N, G = 4, E = G * N;
-    extern __shared__ __attribute__((aligned(16))) Candidate s_cand[];  // [room + 8]
-    float *s_most = reinterpret_cast<float *>(s_cand + room + 8);       // [steps][64]
+    extern __shared__ __attribute__((aligned(16))) Candidate s_cand[];  // [room + 16]
+    float *s_most = reinterpret_cast<float *>(s_cand + room + 16);       // [steps][64]
     __shared__ int s_n;
     uint32_t split, k;
     const int t = threadIdx.x;
@@ -322,19 +322,20 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         __syncthreads();
     }
     if (n <= room) {
-        if (t < 8) s_cand[n + t] = {-INFINITY, INT32_MAX};  // to a multiple of eight
+        if (t < 16) s_cand[n + t] = {-INFINITY, INT32_MAX};  // to a multiple of sixteen
         __syncthreads();
-        for (int i = t; i < n; i += 64) {
+        for (int i = t >> 2; i < n; i += 16) {  // four lanes a candidate, with a quarter of the others each
             const Candidate own = s_cand[i];
-            int rank = 0;
+            float rank = 0;
 #pragma unroll 1
-            for (int j0 = 0; j0 < n; j0 += 8)
+            for (int j0 = t & 3; j0 < n; j0 += 16)
 #pragma unroll
-                for (int j = j0; j < j0 + 8; j++) {
+                for (int j = j0; j < j0 + 16; j += 4) {
                     const Candidate o = s_cand[j];
                     rank += (o.x > own.x) | ((o.x == own.x) & (o.v < own.v));
                 }
-            if (rank < dsc.M) out[rank] = own;
+            rank = lanes_sum(rank, 2);
+            if (rank < dsc.M && (t & 3) == 0) out[(int)rank] = own;
         }
     } else {  // many equal ones: the next best after the last, a round each
         Candidate last = {INFINITY, -1};
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         double x;
         long place;
     };
-    __shared__ Total s_total[kMergeCap + 4], s_best[ETV_MAX_BEAMS];
+    __shared__ Total s_total[kMergeCap + 16], s_best[ETV_MAX_BEAMS];
     __shared__ unsigned int s_again[2];
     __shared__ Candidate s_head[4][kMergeThreads];
     const int b = blockIdx.x, t = threadIdx.x;
@@ -559,19 +560,20 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             __syncthreads();
         }
         if (found <= kMergeCap) {
-            if (t < 4) s_total[found + t] = {-INFINITY, INT64_MAX};  // to a multiple of four
+            if (t < 16) s_total[found + t] = {-INFINITY, INT64_MAX};  // to a multiple of sixteen
             __syncthreads();
-            for (int i = t; i < found; i += kMergeThreads) {
+            for (int i = t >> 2; i < found; i += kMergeThreads / 4) {  // four lanes a candidate, with a quarter of the others each
                 const Total own = s_total[i];
-                int rank = 0;
+                float rank = 0;
 #pragma unroll 1
-                for (int j0 = 0; j0 < found; j0 += 4)
+                for (int j0 = t & 3; j0 < found; j0 += 16)
 #pragma unroll
-                    for (int j = j0; j < j0 + 4; j++) {
+                    for (int j = j0; j < j0 + 16; j += 4) {
                         const Total o = s_total[j];
                         rank += (o.x > own.x) | ((o.x == own.x) & (o.place < own.place));
                     }
-                if (rank < M) s_best[rank] = own;
+                rank = lanes_sum(rank, 2);
+                if (rank < M && (t & 3) == 0) s_best[(int)rank] = own;
             }
             n = min(found, M);
         } else {
@@ -713,7 +715,7 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
         const uint32_t inv_splits = etv::fast_div_inv(splits);
         // room for the candidates: some times M where lists are short against the lanes, more of it fewer wavefronts at a time
         const int room = h->M <= 16 ? 256 : h->M <= 32 ? 512 : 1024;
-        hipLaunchKernelGGL(scan, dim3(lists), dim3(64), (room + 8) * sizeof(etv::Candidate) + steps * 256, s, *h, x, scores, n_beams, finished, splits, inv_splits,
+        hipLaunchKernelGGL(scan, dim3(lists), dim3(64), (room + 16) * sizeof(etv::Candidate) + steps * 256, s, *h, x, scores, n_beams, finished, splits, inv_splits,
                            etv::fast_div_inv(h->K), steps, list, room, heads, cands);
         const int32_t rc = etv::check_launch();
         if (rc != ETV_OK) return rc;
