@@ -1,7 +1,7 @@
 // The best continuations over beams and vocabulary, total[k, v] = score[k] + x[k, v] - log sum_v' exp(x[k, v']): one pass over the logits, which
 // leaves of every segment of a row its sum relative to a reference and its M best logits in order, then a merge per request.  Floor: the
 // logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 11.1 us at the rate of a
-// large copy (5.17 TB/s).  The call takes 21.5 us there: the scan 15.6, the merge 6.
+// large copy (5.17 TB/s).  The call takes 20.6 us there: the scan 15.8, the merge 5.9.
 #include "etv_common.h"
 #include <algorithm>
 #include <cfloat>
@@ -171,7 +171,7 @@ constexpr float kSlack = 1, kFarthest = 1 << 20;
 // M-th best of the segment from below (a number that M of them reach), and the few vectors that reach the bound are read again, from the
 // caches, for the candidates, which are ranked by counting.  TINY: fewer logits than a vector holds.
 // One wavefront a workgroup, so that no barrier stops the stream.  Bounds: memory where
-// rows are many -- of the 16.0 us above the loads alone take 11.5, the rest are exponentials and sums, and bound, candidates and ranking --, and the
+// rows are many -- of the 15.8 us above the loads alone take 11.5, the rest are exponentials and sums, and bound, candidates and ranking --, and the
 // chain load, work, bound, candidates where they are few: 4 rows of 32000 fp32 logits 4.5 us, of which an empty launch is some 2.  Measured and left: wavefronts that
 // go from segment to segment with the next one's first loads under way (half a us to two longer: 135 registers leave 12 of them a CU, 86 leave 20).
 template <class T, bool TINY>
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
 // other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them: so the order is that of
 // 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
-// Bound by the chain of its loads and barriers: 5.2 us for one request of 4 beams, some 6.5 for 32 of 8 beams with 8 lists each.  A scan whose
+// Bound by the chain of its loads and barriers: 5.1 us for one request of 4 beams, 5.9 for 32 of 8 beams with 8 lists each.  A scan whose
 // last workgroup merges would save this launch's 4 us on the host, but needs a counter that somebody clears, and a release to the whole device by every wavefront.
 // SHARED: few lists against M, which are therefore gone into deeply, by several threads each.
 template <class T, bool SHARED>
@@ -657,9 +657,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
 }
 
 // Steps of a wavefront's segment: more of them mean fewer bounds to find and fewer lists to merge, and fewer wavefronts to hide that behind.  As many as
-// leave 1536 wavefronts, 6 a CU, up to eight (32 requests of 8 beams and 128000 logits: 22.3 us with 8 steps, 23.6 with 4, 24.5 with 2), sixteen where 4096 are
-// left (four times the requests: 60 us, 65 with 8 steps); a single one instead of two (64 requests of 4 beams and 32000 logits: 14.5 us, 15.0).  Segments are
-// as even as steps allow.  Large M: no more than eight, for each segment leaves M candidates.
+// leave 1536 wavefronts, 6 a CU, up to eight (32 requests of 8 beams and 128000 logits: 8 steps take 1.3 us less than 4, and 2.2 less than 2), sixteen where 4096
+// are left (four times the requests: 5 us less than with 8); a single one instead of two (64 requests of 4 beams and 32000 logits: half a us less).  Segments
+// are as even as steps allow.  Large M: no more than eight, for each segment leaves M candidates.
 constexpr int kFullWaves = 1536, kManyWaves = 4096;
 static int beam_step(const etv_beam_desc *h) { return 64 * (h->dtype == ETV_BF16 ? 32 : 16); }
 static int beam_steps(const etv_beam_desc *h) {
@@ -721,7 +721,7 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
         if (rc != ETV_OK) return rc;
         int width = 0;  // as many lanes a beam as it has segments, up to a wavefront
         while (width < 6 && (1 << width) < splits) width++;
-        // 64 requests of 10 beams in 4 lists each 24.5 us, 27.3 with a thread a list; 8 requests of 4 beams in 63 lists 11.5 us, 12.2 if they were shared
+        // 64 requests of 10 beams in 4 lists each: 2.8 us less than with a thread a list; 8 requests of 4 beams in 63 lists each would take 0.7 more
         const bool shared = splits * h->K <= 16 * h->M && splits * h->K <= etv::kMergeThreads / 2;
         hipLaunchKernelGGL((shared ? etv::beam_merge_kernel<T, true> : etv::beam_merge_kernel<T, false>), dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits,
                            width, list, heads, cands, out_scores, parent, token, finished_out, status);
