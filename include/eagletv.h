@@ -575,7 +575,7 @@ ETV_API int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h_desc, const 
  *   share of the ring, unused.
  *
  *  len, new_len  in  int32 [B];  block_table in/out int32 [B, max_blocks];  free_blocks in/out, free_state in, free_state_out out
- *  len_out int32 [B] (must alias neither length);  slot_map int32 [B, S]  nullable;  status int32 [B]
+ *  len_out int32 [B], slot_map int32 [B, S] nullable, status int32 [B]: none of them may overlap len or new_len
  * Requires B * S (rounded up to 1024) and num_blocks * block_size below 2^31, and max_blocks < 2^22. */
 typedef struct etv_pages_desc {
     int32_t B;
@@ -595,7 +595,7 @@ ETV_API int32_t etv_resize_block_tables(const etv_pages_desc *h_desc, const int3
  *   angle = positions[a, b, t] * inv_freq[i] (the product, its sine and cosine good to fp32 at any 32-bit position)
  *   (x, y) -> scale * (x cos - y sin, y cos + x sin)
  * where (x, y) are channels (i, i + rot_dim/2), or (2i, 2i+1) with ETV_ROTARY_INTERLEAVED; channels from rot_dim on are copied.
- * ETV_ROTARY_INVERSE turns by -angle: the gradient of the call, and the way back to unencoded rows.
+ * ETV_ROTARY_INVERSE turns by -angle: the gradient of the call and, with a scale of 1, the way back to unencoded rows.
  * Rows t >= n_rows[b] are padding: nothing is written for them.
  * A row of k and v goes to slot slot_map[b, t] of the cache (as etv_resize_block_tables writes them; contiguous: b * P_cap + p), unless
  * that is outside [0, cache_rows).  Two rows of a call must not have one slot.
@@ -628,7 +628,7 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
 /* beam_select -- the M best continuations of a request over its K beams (or frontier nodes) and the vocabulary:
  *   total[k, v] = scores[b, k] + logits[b, k, v] - log sum_v' exp(logits[b, k, v'])
  * the M largest in descending order, ties to the lower k, then the lower v.  A beam with finished[b, k] != 0 offers (k, end_token) at
- * scores[b, k] and nothing else.  Beams k >= n_beams[b], scores of -inf and logits of -inf offer nothing.  Where fewer than M are
+ * scores[b, k] and nothing else.  Beams k >= n_beams[b], scores of -inf and logits of -inf offer nothing, nor do totals that are -inf in fp32.  Where fewer than M are
  * offered the rest is parent = token = -1 with a score of -inf.  Totals are formed and compared in 64 bits and rounded once; the
  * exponentials are fp32 (the logarithm of a sum is off by 1e-8 as a rule), but where totals of two beams that decide a choice or its place lie
  * within 2^-22 (7 + ln V), what the sums may be off by, both are taken again in 64 bits first.
@@ -640,8 +640,9 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
  *  n_beams in int32 [B] nullable (=> K);  finished in uint8 [B, K] nullable
  *  out_scores float [B, M]; parent, token int32 [B, M]; finished_out uint8 [B, M] nullable; status int32 [B]
  *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.
- * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V < 2^31 - 65536; B * K times the segments of a row (1024 to 16384 logits
- * each) below 2^26. */
+ *  With M == K out_scores may be scores and finished_out finished; otherwise they must not overlap.
+ * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V < 2^31 - 65536; B * K times the segments of a row (1024 to 32768 logits
+ * each) below 2^26, B below 2^23. */
 #define ETV_BEAM_BAD_LOGITS 1
 #define ETV_BEAM_BAD_SCORE 2
 #define ETV_BEAM_SHORT 4
@@ -673,7 +674,7 @@ ETV_API int32_t etv_beam_select(const etv_beam_desc *h_desc, const void *logits,
  *   row of the beam that it was for is -1.
  *
  *  k_cache, v_cache in/out; block_table in int32 [B, K, max_blocks]; len in int32 [B]; parent in int32 [B, M]
- *  table_out out int32 [B, M, max_blocks] (must not overlap block_table); status out int32 [B]
+ *  table_out out int32 [B, M, max_blocks] (must not overlap block_table); status out int32 [B] (not len)
  *  workspace: etv_reorder_beams_workspace_bytes(B, K, M, max_blocks) bytes, 16-byte aligned.
  * Requires 1 <= K, M <= ETV_MAX_BEAMS, a paged cache (ETV_ERR_UNIMPLEMENTED otherwise), d * elem_bytes % 16 == 0, B <= 65535,
  * max_blocks <= 2^22, B * K * max_blocks and num_blocks * block_size below 2^31, and a block of one layer below 2^32 bytes. */

@@ -683,7 +683,7 @@ static int32_t check_beam(const etv_beam_desc *h) {
     if (h->row_stride < 0 || h->batch_stride < 0) return ETV_ERR_INVALID_ARG;
     if (h->dtype != ETV_F32 && h->dtype != ETV_BF16) return ETV_ERR_UNSUPPORTED;
     if (h->K > ETV_MAX_BEAMS || h->M > ETV_MAX_BEAMS || h->V > INT32_MAX - 65536) return ETV_ERR_UNSUPPORTED;
-    if ((int64_t)h->B * h->K * beam_splits(h) >= (1 << 26)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
+    if ((int64_t)h->B * h->K * beam_splits(h) >= (1 << 26) || h->B >= (1 << 23)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
     return ETV_OK;
 }
 
@@ -704,6 +704,10 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
     if (!logits || !scores || !out_scores || !parent || !token || !status || (finished && h->end_token < 0)) return ETV_ERR_INVALID_ARG;
     if ((uintptr_t)logits % (h->dtype == ETV_BF16 ? 2 : 4) || (uintptr_t)workspace & 15) return ETV_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < etv_beam_select_workspace_bytes(h)) return ETV_ERR_WORKSPACE_TOO_SMALL;
+    // a request's scores and flags may take the place of its own old ones
+    const size_t in = (size_t)h->B * h->K, out = (size_t)h->B * h->M;
+    if (etv::overlap(scores, in * 4, out_scores, out * 4) && (scores != out_scores || in != out)) return ETV_ERR_INVALID_ARG;
+    if (etv::overlap(finished, in, finished_out, out) && (finished != finished_out || in != out)) return ETV_ERR_INVALID_ARG;
     const int splits = etv::beam_splits(h), list = etv::beam_list(h), steps = etv::beam_steps(h);
     const unsigned lists = (unsigned)h->B * h->K * splits;
     auto *heads = static_cast<etv::ScanHead *>(workspace);

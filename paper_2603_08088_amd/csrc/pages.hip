@@ -5,13 +5,14 @@
 // call, 5.4 us there and 2.7 us for 64 sequences that grow by a token.
 #include "etv_common.h"
 #include "free_ring.h"
+#include <initializer_list>
 
 namespace etv {
 
 constexpr int kPageWaves = 8, kPageThreads = 64 * kPageWaves;
 constexpr int kSlotsPerWg = 1024;  // elements of slot_map that a workgroup writes
 constexpr int kFewRows = 64;       // up to so many new rows a thread checks the blocks of a sequence by itself
-constexpr int kMaxRow = (1 << 22) - 1;   // longest table row: kPageThreads of them are counted in 31 bits
+constexpr int kMaxRow = (1 << 22) - 1;  // longest table row: kPageThreads of them are counted in 31 bits
 
 // What the lengths alone say of a sequence.
 struct PagePlan {
@@ -243,9 +244,12 @@ extern "C" int32_t etv_resize_block_tables(const etv_pages_desc *h, const int32_
                                            int32_t *slot_map, int32_t *status, void *stream) {
     if (!h || h->B < 0 || h->S < 1 || h->block_size < 1 || h->max_blocks < 1 || h->num_blocks < 1) return ETV_ERR_INVALID_ARG;
     if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
-    if (h->B > 0 && (!len || !new_len || !block_table || !len_out || !status || len_out == len || len_out == new_len)) return ETV_ERR_INVALID_ARG;
+    if (h->B > 0 && (!len || !new_len || !block_table || !len_out || !status)) return ETV_ERR_INVALID_ARG;
     if ((int64_t)h->B * h->S > INT32_MAX - etv::kSlotsPerWg || (int64_t)h->num_blocks * h->block_size > INT32_MAX || h->max_blocks > etv::kMaxRow)
         return ETV_ERR_UNSUPPORTED;
+    const size_t lens = 4 * (size_t)h->B;  // all workgroups read them
+    for (const int32_t *in : {len, new_len})
+        if (etv::overlap(in, lens, len_out, lens) || etv::overlap(in, lens, status, lens) || etv::overlap(in, lens, slot_map, lens * h->S)) return ETV_ERR_INVALID_ARG;
     const unsigned wgs = 1 + (unsigned)(((int64_t)h->B * h->S + etv::kSlotsPerWg - 1) / etv::kSlotsPerWg);
     hipLaunchKernelGGL(etv::resize_tables_kernel, dim3(wgs), dim3(etv::kPageThreads), 0, etv::as_stream(stream), *h, etv::fast_div_inv(h->block_size),
                        etv::fast_div_inv(h->S), len, new_len, block_table, free_blocks, free_state, free_state_out, len_out, slot_map, status);

@@ -350,7 +350,8 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
         return check_launch();
     }
     if (!block_table || !len || !parent || !table_out || !status) return ETV_ERR_INVALID_ARG;
-    if (table_out < block_table + (size_t)sh.B * sh.K * sh.max_blocks && block_table < table_out + (size_t)sh.B * sh.M * sh.max_blocks) return ETV_ERR_INVALID_ARG;
+    const size_t columns = (size_t)sh.B * sh.max_blocks * 4, lens = (size_t)sh.B * 4;
+    if (overlap(table_out, columns * sh.M, block_table, columns * sh.K) || overlap(status, lens, len, lens)) return ETV_ERR_INVALID_ARG;
     for (int i = 0; i < cache.parts; i++)
         if ((double)cache.Hkv * sh.block_size * cache.row_bytes[i] >= 0x1p32) return ETV_ERR_UNSUPPORTED;
     for (int i = 0; i < cache.parts; i++)

@@ -176,7 +176,8 @@ extern "C" int32_t etv_rotary_write_kv(const etv_rotary_desc *h, const void *q, 
         const int64_t unit = d.dtype == ETV_BF16 ? 8 : 4, row = (int64_t)(i % 3 ? d.Hkv : d.Hq) * d.d;
         if (seq % unit || tok % unit || seq < 0 || tok < 0) return ETV_ERR_INVALID_ARG;
         if (i < 3) continue;
-        // no two rows of an output lie on one another
+        // an output that is its input moves nothing; no two rows of an output lie on one another
+        if (ends[i] == ends[i - 3] && (seq != d.strides[2 * i - 6] || tok != d.strides[2 * i - 5])) return ETV_ERR_INVALID_ARG;
         if ((d.B > 1 && seq < row) || (d.T > 1 && tok < row)) return ETV_ERR_INVALID_ARG;
         if (d.B > 1 && d.T > 1 && seq < (d.T - 1) * tok + row && tok < (d.B - 1) * seq + row) return ETV_ERR_INVALID_ARG;
     }

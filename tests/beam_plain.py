@@ -152,6 +152,9 @@ def rotate(x, positions, inv_freq, axis_of, interleaved, scale=1.0, inverse=Fals
     return y
 
 
+LEAST = float.fromhex("0x1.ffffffp127")      # half an fp32 step beyond the largest
+
+
 def select(logits, scores, M, n_beams=None, finished=None, end=-1):
     """logits float64 [B, K, V] -> scores float64, parent, token, finished, status"""
     B, K, V = logits.shape
@@ -174,7 +177,7 @@ def select(logits, scores, M, n_beams=None, finished=None, end=-1):
                 totals[k] = s + ((x - m) - math.log(math.fsum(np.exp(x - m))))     # m apart: it may be as large as fp32 goes
         order = np.argsort(-totals.ravel(), kind="stable")[:M]
         for i, at in enumerate(order):
-            if totals.ravel()[at] > -math.inf:
+            if totals.ravel()[at] > -LEAST:          # what rounds to less has no fp32 number
                 best[b, i], parent[b, i], token[b, i] = totals.ravel()[at], at // V, at % V
                 ended[b, i] = bool(finished is not None and finished[b, parent[b, i]]) or token[b, i] == end
         if (parent[b] < 0).any():

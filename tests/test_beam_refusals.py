@@ -12,7 +12,7 @@ from paper_2603_08088_amd import api
 A = 1 << 20      # an aligned address that nobody follows
 
 
-def pages(d, len=A, new=2 * A, bt=A, fb=A, fs=A, fo=2 * A, lo=3 * A, slots=A, st=A):
+def pages(d, len=A, new=2 * A, bt=A, fb=A, fs=A, fo=2 * A, lo=3 * A, slots=5 * A, st=4 * A):
     return api.lib().etv_resize_block_tables(C.byref(d), len, new, bt, fb, fs, fo, lo, slots, st, None)
 
 
@@ -31,6 +31,7 @@ def test_pages_pointers_and_aliases():
     for name in ("len", "new", "bt", "fb", "fs", "fo", "lo", "st"):
         assert pages(d, **{name: None}) == -1, name
     assert pages(d, fo=A) == pages(d, lo=A) == pages(d, lo=2 * A) == -1
+    assert pages(d, st=A + 4) == pages(d, st=2 * A - 4) == pages(d, slots=A) == pages(d, slots=2 * A - 28) == pages(d, lo=A - 4) == -1
 
 
 def rotary_desc(**kw):
@@ -70,6 +71,9 @@ def test_rotary_pointers_strides_and_axes():
     bad = rotary_desc(T=2)
     bad.strides[6:8] = [256, 264]
     assert rotary(bad) == -1
+    moved = rotary_desc()                                                            # in place, but the rows somewhere else
+    moved.strides[6] += 64
+    assert rotary(moved) == -1
     one = rotary_desc(B=1, T=1, block_size=-1)                                       # one row: its strides are not looked at, the rest is
     one.strides[:] = [3] * 12
     assert rotary(one) == -1
@@ -84,11 +88,11 @@ def beam_desc(**kw):
     return api.BeamDesc(**{**dict(B=2, K=4, V=1000, M=4, dtype=api.BF16, end_token=7, batch_stride=4000, row_stride=1000), **kw})
 
 
-def select(d, x=A, s=A, n=A, f=A, o=A, p=A, t=A, fo=A, st=A, ws=A, size=1 << 40):
+def select(d, x=A, s=A, n=A, f=2 * A, o=A, p=A, t=A, fo=2 * A, st=A, ws=A, size=1 << 40):
     return api.lib().etv_beam_select(C.byref(d), x, s, n, f, o, p, t, fo, st, ws, size, None)
 
 
-@pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(K=0), -1), (dict(M=0), -1), (dict(V=0), -1), (dict(end_token=-2), -1), (dict(end_token=1000), -1), (dict(row_stride=-1), -1), (dict(batch_stride=-1), -1), (dict(B=1 << 20, K=64, V=1 << 20), -2),
+@pytest.mark.parametrize("kw,rc", [(dict(B=-1), -1), (dict(K=0), -1), (dict(M=0), -1), (dict(V=0), -1), (dict(end_token=-2), -1), (dict(end_token=1000), -1), (dict(row_stride=-1), -1), (dict(batch_stride=-1), -1), (dict(B=1 << 20, K=64, V=1 << 20), -2), (dict(B=1 << 23, K=1, V=10), -2),
                                    (dict(K=65), -2), (dict(M=65), -2), (dict(dtype=3), -2), (dict(V=2 ** 31 - 1, row_stride=2 ** 31), -2), (dict(B=0), 0)])
 def test_beam_descriptors(kw, rc):
     assert select(beam_desc(**kw)) == rc
@@ -101,6 +105,7 @@ def test_beam_pointers_and_workspace():
     for name in ("x", "s", "o", "p", "t", "st"):
         assert select(d, **{name: None}) == -1, name
     assert select(d, x=A + 1) == select(d, ws=A + 8) == select(beam_desc(end_token=-1)) == -1
+    assert select(d, o=A + 4) == select(d, o=A - 28) == select(d, fo=2 * A + 7) == select(beam_desc(M=5)) == select(beam_desc(M=3), o=3 * A) == -1    # on old ones
     need = api.lib().etv_beam_select_workspace_bytes(C.byref(d))
     assert need > 0 and select(d, size=need - 1) == select(d, ws=None) == -3
 
@@ -109,7 +114,7 @@ def cache_desc(**kw):
     return api.CacheDesc(**{**dict(B=2, Hkv=2, d=64, elem_bytes=2, n_layers=2, block_size=16, max_blocks=8, num_blocks=20, P_cap=0, reserved=0, cache_layer_stride=20 * 2 * 16 * 64), **kw})
 
 
-def reorder(d, k=A, v=A, bt=A, len=A, K=4, p=A, M=4, fb=A, fs=A, to=2 * A, fo=2 * A, st=A, ws=A, size=1 << 40):
+def reorder(d, k=A, v=A, bt=A, len=A, K=4, p=A, M=4, fb=A, fs=A, to=2 * A, fo=2 * A, st=3 * A, ws=A, size=1 << 40):
     return api.lib().etv_reorder_beams(C.byref(d), k, v, bt, len, K, p, M, fb, fs, to, fo, st, ws, size, None)
 
 
@@ -130,6 +135,7 @@ def test_reorder_pointers_beams_and_workspace():
         assert reorder(d, **{name: None}) == -1, name
     assert reorder(d, to=A + 4 * 2 * 4 * 8 - 4) == reorder(d, to=A - 4 * 2 * 4 * 8 + 4) == -1          # overlapping tables
     assert reorder(cache_desc(Hkv=1 << 15, d=256, block_size=256, num_blocks=4)) == -2              # a block of a layer beyond 32 bits
+    assert reorder(d, st=A) == reorder(d, st=A + 4) == reorder(d, st=A - 4) == -1
     assert reorder(d, k=A + 8) == reorder(d, to=A) == reorder(d, fo=A) == reorder(d, ws=A + 4) == -1
     assert reorder(d, K=0) == reorder(d, M=0) == -1 and reorder(d, K=65) == reorder(d, M=65) == -2
     assert reorder(cache_desc(B=1 << 13, max_blocks=1 << 16)) == -2 and api.reorder_beams_workspace_bytes(1 << 13, 4, 4, 1 << 16) == 0   # 2^31 entries

@@ -243,6 +243,28 @@ def test_rows_of_few_values_whose_totals_nearly_meet(dtype):
     check(x, scores, 12)
 
 
+def test_totals_that_fp32_does_not_hold():
+    x = torch.tensor([[[0.0, -1e37, -3e38, 1.0], [5.0, -math.inf, 4.0, -2e37]]])
+    check(x, [[-3.4e38, -3.3e38]], 8)
+    check(x, [[-3.4028235e38, -3.4028235e38]], 8)
+
+
+def test_scores_and_flags_in_place():
+    """A request's new scores take the place of its own old ones, also where sums are taken again."""
+    rng = np.random.default_rng(71)
+    x = normal(rng, (300, 1, 3000), "bf16", 3.0).expand(300, 4, 3000).clone()
+    x[:, 1] = x[:, 1].flip(-1)
+    scores = np.stack((np.full(300, -0.75), np.full(300, -0.75 + 2.0 ** -24), -9 * rng.random(300), -2 - rng.random(300)), 1)
+    done = np.zeros((300, 4), dtype=np.uint8)
+    done[:, 3] = 1
+    s, f = dev(scores, np.float32), dev(done, np.uint8)
+    want = api.beam_select(x.cuda(), s.clone(), 4, finished=f.clone(), end_token=7)
+    r = api.beam_select(x.cuda(), s, 4, finished=f, end_token=7, out=dict(scores=s, finished=f))
+    assert all(torch.equal(r[n], want[n]) for n in want) and r["scores"] is s
+    with pytest.raises(api.EtvError):
+        api.beam_select(x.cuda(), s, 3, out=dict(scores=s.view(-1)[:900].view(300, 3)))
+
+
 def test_the_workspace_may_hold_anything():
     rng = np.random.default_rng(14)
     x = normal(rng, (3, 4, 7000), "bf16")
