@@ -274,3 +274,11 @@ def test_the_workspace_may_hold_anything():
         check(x, -rng.random((3, 4)), 5, [4, 0, 2], workspace=ws)
     r = api.beam_select(x.cuda()[:0], dev(np.zeros((0, 4)), np.float32), 5)
     assert r["parent"].shape == (0, 5)
+
+
+def test_rows_further_apart_than_32_bits_reach():
+    rng = np.random.default_rng(81)
+    x = normal(rng, (2, 4, 5001), "bf16")
+    far = torch.empty((1 << 32) + 8 + 3 * ((1 << 30) + 1) + 5001, dtype=torch.bfloat16, device="cuda").as_strided((2, 4, 5001), ((1 << 32) + 8, (1 << 30) + 1, 1))
+    far.copy_(x)
+    check(x, -rng.random((2, 4)), 6, on=far)

@@ -214,3 +214,23 @@ def test_a_run_of_steps_keeps_every_block_once():
             if lens.max() > 150:
                 r = api.resize_block_tables(table.view(B, width), dev(lens), dev([0] * B), free, size, 1)
                 free, lens, lines = free.after(r), lens * 0, [[[]] for _ in range(B)]
+
+
+def test_layers_of_more_than_2_32_bytes():
+    n, size = (1 << 20) + 64, 16
+    k, v = (torch.zeros((2, n, 2, size, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = np.array([[[n - 1, n - 2], [n - 1, n - 3]]])
+    ring = np.full(n, -1, dtype=np.int32)
+    ring[n - 1], ring[0] = 7, n - 4
+    for i, t in enumerate((k, v)):
+        t[:, n - 2] = 1 + i
+        t[:, n - 3] = 3 + i
+    free = api.FreeBlocks(dev(ring), dev([n - 1, 2]))
+    r = api.reorder_beams(k, v, dev(table), dev([16 + 9]), dev([[1, 1, 1]]), free)
+    assert r["status"].tolist() == [0] and r["block_table"].tolist() == [[[n - 1, n - 3], [n - 1, 7], [n - 1, n - 4]]]
+    assert r["free_state"].tolist() == [1, 1] and free.blocks[1].item() == n - 2
+    for i, t in enumerate((k, v)):
+        for block in (7, n - 4):
+            assert (t[:, block, :, :9] == 3 + i).all() and not t[:, block, :, 9:].any()
+        t[:, [7, n - 2, n - 3, n - 4]] = 0
+        assert not any(part.any() for part in t.view(-1).split(1 << 30))

@@ -188,3 +188,21 @@ def test_an_empty_batch():
     q = torch.empty((0, 3, 2, 64), device="cuda")
     r = api.rotary_write_kv(q, None, None, torch.empty((0, 3), dtype=torch.int32, device="cuda"), api.Rotary(dev(freqs(32), np.float32)))
     assert r["q"].shape == q.shape
+
+
+@pytest.mark.parametrize("paged", [True, False])
+def test_a_cache_of_more_than_2_32_elements(paged):
+    c = Case(23, 2, 5, 8, 8, 128, "bf16")
+    rows = (1 << 22) + 4096
+    shape = (rows // 16, 8, 16, 128) if paged else (2, rows // 2, 8, 128)
+    k, v = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    slots = np.array([[rows - 1, rows - 17, 0, 1 << 22, (1 << 22) - 1], [rows - 2, 5, rows, 1 << 21, rows // 2]])
+    plain = api.rotary_write_kv(c.q, c.k, c.v, dev(c.positions), c.rotary)
+    api.rotary_write_kv(c.q, c.k, c.v, dev(c.positions), c.rotary, slot_map=dev(slots), k_cache=k, v_cache=v, paged=paged)
+    for cache, want in ((k, plain["k"]), (v, c.v)):
+        for (b, t), s in np.ndenumerate(slots):
+            if s < rows:
+                got = cache[s // 16, :, s % 16] if paged else cache.view(rows, 8, 128)[s]
+                assert torch.equal(got, want[b, t]), s
+                got.zero_()
+        assert not any(part.any() for part in cache.view(-1).split(1 << 30))
