@@ -11,7 +11,7 @@ namespace etv {
 
 constexpr int kPageWaves = 8, kPageThreads = 64 * kPageWaves;
 constexpr int kSlotsPerWg = 1024;  // elements of slot_map that a workgroup writes
-constexpr int kFewRows = 64;       // up to so many new rows a thread checks the blocks of a sequence by itself
+constexpr int kFewBlocks = 8;      // so many blocks of a sequence are taken or given back by a thread, all asked for at once, more by a wavefront
 constexpr int kMaxRow = (1 << 22) - 1;  // longest table row: kPageThreads of them are counted in 31 bits
 
 // What the lengths alone say of a sequence.
@@ -34,8 +34,8 @@ __device__ __forceinline__ PagePlan page_plan(const etv_pages_desc &dsc, uint32_
     return p;
 }
 
-// Workgroup 0: what is given back, and the ring's new state.  kPageThreads sequences at a time; those that give are put in a list, whose sequences the
-// wavefronts share out among themselves.
+// Workgroup 0: what is given back, and the ring's new state.  kPageThreads sequences at a time, a thread each; those that give more than a thread holds
+// are put in a list, whose sequences the wavefronts share out among themselves.
 __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int32_t *len, const int32_t *new_len, const int32_t *block_table,
                           int32_t *free_blocks, const Ring &ring, int32_t *free_state_out, int32_t *len_out, int32_t *status) {
     struct Giver {
@@ -70,9 +70,19 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
         const long t_end = block_scan_sum<kPageWaves>(take, taken);  // a barrier, too: s_most is set
         if (take > 0 && t_end <= ring.count) atomicMax(&s_most[0], (unsigned long long)t_end);
         if (!__syncthreads_or(give)) continue;
+        const bool few = give <= kFewBlocks;
+        int32_t own[kFewBlocks] = {};
+        int bad = 0;
+        if (give > 0 && few) {
+            const int32_t *row = block_table + (size_t)b * dsc.max_blocks + p.want;
+#pragma unroll
+            for (int i = 0; i < kFewBlocks; i++) own[i] = row[min(i, give - 1)];
+#pragma unroll
+            for (int i = 0; i < kFewBlocks; i++) bad |= (uint32_t)own[i] >= (uint32_t)dsc.num_blocks;
+        }
         long before = 0;
-        const int place = (int)block_scan_sum<kPageWaves>(give > 0, before) - 1, n = (int)before;
-        if (give > 0) s_giver[place] = {b, p.want, give, 0, 0};
+        const int place = (int)block_scan_sum<kPageWaves>(!few, before) - 1, n = (int)before;
+        if (!few) s_giver[place] = {b, p.want, give, 0, 0};
         __syncthreads();
         for (int s = t >> 6; s < n; s += kPageWaves) {
             const int32_t *row = block_table + (size_t)s_giver[s].b * dsc.max_blocks + s_giver[s].first;
@@ -81,14 +91,22 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
             if (bad) s_giver[s].bad = 1;
         }
         __syncthreads();
-        // in the order of the sequences, which is that of the list
-        const int good = give > 0 && !s_giver[place].bad ? give : 0;
+        // in the order of the sequences
+        if (!few) bad = s_giver[place].bad;
+        const int good = bad ? 0 : give;
         const long g_end = block_scan_sum<kPageWaves>(good, given);
         if (give > 0) {
             const int32_t st = !good ? ETV_COMMIT_BAD_BLOCK : g_end > ring.room() ? ETV_BRANCH_BAD_FREE : 0;
             if (!st) atomicMax(&s_most[1], (unsigned long long)g_end);
-            s_giver[place].at = ring.count + g_end - good;
-            if (st) s_giver[place].n = 0;
+            const long at = ring.count + g_end - good;
+            if (few) {
+#pragma unroll
+                for (int i = 0; i < kFewBlocks; i++)
+                    if (!st && i < give) free_blocks[ring.place(at + i)] = own[i];
+            } else {
+                s_giver[place].at = at;
+                if (st) s_giver[place].n = 0;
+            }
             status[b] = st;
             len_out[b] = st ? L : N;
         }
@@ -109,7 +127,7 @@ __device__ void give_back(const etv_pages_desc &dsc, uint32_t inv_bs, const int3
 // are read here are written by nobody.
 __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S, const int32_t *len, const int32_t *new_len, int32_t *block_table,
                      const int32_t *free_blocks, const Ring &ring, int32_t *len_out, int32_t *slot_map, int32_t *status) {
-    __shared__ int s_len[kSlotsPerWg], s_rows[kSlotsPerWg], s_old[kSlotsPerWg], s_tail[kSlotsPerWg];
+    __shared__ int s_len[kSlotsPerWg], s_rows[kSlotsPerWg], s_old[kSlotsPerWg], s_tail[kSlotsPerWg], s_many;
     __shared__ long s_base[kSlotsPerWg];
     const int t = threadIdx.x;
     const uint32_t e0 = (blockIdx.x - 1) * kSlotsPerWg, last = (uint32_t)(dsc.B * dsc.S - 1);
@@ -158,6 +176,7 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
         }
         return;
     }
+    if (t == 0) s_many = 0;
     for (int s0 = 0; s0 < nb; s0 += kPageThreads) {
         const int s = s0 + t, b = b_lo + s;
         PagePlan p{0, 0, 0};
@@ -176,34 +195,45 @@ __device__ void grow(const etv_pages_desc &dsc, uint32_t inv_bs, uint32_t inv_S,
             tail = block_table[(size_t)b * dsc.max_blocks + p.old - 1];
             if (!st && (uint32_t)tail >= (uint32_t)dsc.num_blocks) st = ETV_COMMIT_BAD_BLOCK;
         }
-        if (!st && dsc.S <= kFewRows)
-            for (int j = 0; j < take; j++)
-                if ((uint32_t)free_blocks[ring.place(end - take + j)] >= (uint32_t)dsc.num_blocks) st = ETV_BRANCH_BAD_FREE;
+        const bool many = !st && take > kFewBlocks;
+        if (many) s_many = 1;  // behind the scan's barriers
+        if (!st && take > 0 && !many) {
+            int32_t block[kFewBlocks] = {free_blocks[ring.place(end - take)]};
+            if (take > 1) {
+#pragma unroll
+                for (int i = 1; i < kFewBlocks; i++) block[i] = free_blocks[ring.place(end - take + min(i, take - 1))];
+#pragma unroll
+                for (int i = 1; i < kFewBlocks; i++)
+                    if ((uint32_t)block[i] >= (uint32_t)dsc.num_blocks) st = ETV_BRANCH_BAD_FREE;
+            }
+            if ((uint32_t)block[0] >= (uint32_t)dsc.num_blocks) st = ETV_BRANCH_BAD_FREE;
+        }
         s_len[s] = L;
         s_rows[s] = st ? 0 : max(rows, 0);
         s_old[s] = p.old;
         s_tail[s] = tail;
         s_base[s] = end - take;
         const bool starts = (uint32_t)b * dsc.S >= e0;
-        if (starts && p.give() == 0 && (st || take == 0 || dsc.S <= kFewRows)) {
+        if (starts && p.give() == 0 && !many) {
             status[b] = st;
             len_out[b] = st ? L : N;
         }
     }
     __syncthreads();
-    if (dsc.S > kFewRows) {  // few sequences with many blocks each: every workgroup of a sequence checks all of its share of the ring
-        for (int s = 0; s < nb; s++) {
+    if (s_many) {  // every workgroup of a sequence checks all of its share of the ring
+        for (int s = t >> 6; s < nb; s += kPageWaves) {
             const int rows = s_rows[s], b = b_lo + s;
             if (rows <= 0) continue;
             uint32_t off;
             const int take = (int)fast_div((uint32_t)s_len[s] + rows + dsc.block_size - 1, dsc.block_size, inv_bs, off) - s_old[s];
+            if (take <= kFewBlocks) continue;
             int bad = 0;
 #pragma unroll 4
-            for (int j = t; j < take; j += kPageThreads) bad |= (uint32_t)free_blocks[ring.place(s_base[s] + j)] >= (uint32_t)dsc.num_blocks;
-            bad = __syncthreads_or(bad);
-            if (t == 0) {
+            for (int j = t & 63; j < take; j += 64) bad |= (uint32_t)free_blocks[ring.place(s_base[s] + j)] >= (uint32_t)dsc.num_blocks;
+            bad = __ballot(bad) != 0;
+            if ((t & 63) == 0) {
                 if (bad) s_rows[s] = 0;
-                if (take > 0 && (uint32_t)b * dsc.S >= e0) {
+                if ((uint32_t)b * dsc.S >= e0) {
                     status[b] = bad ? ETV_BRANCH_BAD_FREE : 0;
                     len_out[b] = s_len[s] + (bad ? 0 : rows);
                 }

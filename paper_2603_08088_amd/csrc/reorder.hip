@@ -31,23 +31,27 @@ __device__ __forceinline__ int32_t length_status(const ReorderShape &sh, int len
     return ((long)len + sh.block_size - 1) / sh.block_size > sh.max_blocks ? ETV_COMMIT_CAPACITY : 0;
 }
 
-// grid (chunks, B), one wavefront: a lane per column of the table, and per new beam, whose parents are then a ballot or a lane read away.  The old beams'
-// entries of its column are asked for eight at a time; FEW: they are eight at most and stay in its registers.  Bound by the chain of its loads
-// (3.5 us for one request) until the tables are large: 256 requests of 4 beams and 4096 columns, 33.6 MB, 16 us.
+// grid (chunks, B): a lane per column of the table, and per new beam, whose parents are then a ballot or a lane read away.  The old beams' entries of its
+// column are asked for eight at a time.  FEW: they are eight at most, stay in its registers, and one wavefront does it all; otherwise four share the
+// beams, and the columns in which beams differ -- the last ones, as a rule --, where a lane is a beam and one round finds all that have a
+// block.  Bound by the chain of its loads (3.5 us for one request) until the tables are large: 256 requests of 4 beams and 4096
+// columns, 33.6 MB, 16 us.
+constexpr int kPitch = kCols + 1;  // of a beam's columns in LDS: a column over the beams has no two in one bank
 template <bool FEW>
-__global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
-                                                               int32_t *table_out, ReorderWorkspace ws) {
-    extern __shared__ int32_t s_table[];  // [K][kCols]
-    const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, col = c * kCols + t;
+__global__ void __launch_bounds__(FEW ? kCols : 4 * kCols) reorder_tables_kernel(ReorderShape sh, const int32_t *block_table, const int32_t *len, const int32_t *parent,
+                                                                                int32_t *table_out, ReorderWorkspace ws) {
+    extern __shared__ int32_t s_table[];  // [K][kPitch]
+    constexpr int W = FEW ? 1 : 4;
+    const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x & 63, w = FEW ? 0 : threadIdx.x >> 6, col = c * kCols + t;
     const int32_t *src = block_table + (size_t)b * sh.K * sh.max_blocks + min(col, sh.max_blocks - 1);
     int p = t < sh.M ? parent[(size_t)b * sh.M + t] : -1;
     int32_t id[8];
-    for (int k0 = 0; k0 < sh.K; k0 += 8) {
+    for (int k0 = 8 * w; k0 < sh.K; k0 += 8 * W) {
 #pragma unroll
         for (int i = 0; i < 8; i++) id[i] = src[(size_t)min(k0 + i, sh.K - 1) * sh.max_blocks];
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (k0 + i < sh.K) s_table[(k0 + i) * kCols + t] = id[i];
+            if (k0 + i < sh.K) s_table[(k0 + i) * kPitch + t] = id[i];
         if (FEW) break;
     }
     int32_t st = length_status(sh, len[b]);
@@ -58,24 +62,38 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
     const uint64_t alive = wave_best(p >= 0 && p < 32 ? 1u << p : 0u, either) | (uint64_t)wave_best(p >= 32 ? 1u << (p - 32) : 0u, either) << 32;
     const auto outside = [&](int32_t x) { return (uint32_t)x >= (uint32_t)sh.num_blocks; };
     int bad = 0;
-    if (col < cols) {
-        if (FEW) {
+    __shared__ uint64_t s_differ[4], s_gone[kCols];
+    const int32_t first = FEW ? 0 : (__syncthreads(), s_table[(alive ? __builtin_ctzll(alive) : 0) * kPitch + t]);  // the entry of a beam that goes on, if any does
+    if (FEW) {
+        if (col < cols) {
 #pragma unroll
             for (int k = 0; k < 8; k++) bad |= (alive >> k & 1) && outside(id[k]);
-        } else {
-            for (int k = 0; k < sh.K; k++) bad |= (alive >> k & 1) && outside(s_table[k * kCols + t]);
         }
+        bad = __ballot(bad) != 0;
+    } else {
+        int differ = 0;
+        if (col < cols) {
+#pragma unroll 4
+            for (int k = w; k < sh.K; k += W) {
+                const int32_t x = s_table[k * kPitch + t];
+                bad |= (alive >> k & 1) && outside(x);
+                differ |= x != first;
+            }
+        }
+        const uint64_t columns = __ballot(differ);
+        if (t == 0) s_differ[w] = columns;
+        bad = __syncthreads_or(bad);
     }
-    if (__ballot(bad)) st |= ETV_COMMIT_BAD_BLOCK;
+    if (bad) st |= ETV_COMMIT_BAD_BLOCK;
     if (col < sh.max_blocks)
-        for (int i = 0; i < sh.M; i++) {
+        for (int i = w; i < sh.M; i += W) {
             const int from = __builtin_amdgcn_readlane(p, i);
-            table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && from >= 0 && col < cols ? s_table[from * kCols + t] : -1;
+            table_out[((size_t)b * sh.M + i) * sh.max_blocks + col] = !st && from >= 0 && col < cols ? s_table[from * kPitch + t] : -1;
         }
     // blocks of beams without a child that neither a parent nor an earlier such beam has
     uint64_t gone = 0;
-    if (col < cols && !st) {
-        if (FEW) {
+    if (FEW) {
+        if (col < cols && !st) {
 #pragma unroll
             for (int k = 0; k < 8; k++) {
                 bool mine = k < sh.K && !(alive >> k & 1) && !outside(id[k]);
@@ -84,26 +102,37 @@ __global__ void __launch_bounds__(kCols) reorder_tables_kernel(ReorderShape sh, 
                     if (j != k) mine &= !((j < k || (alive >> j & 1)) && id[j] == id[k]);
                 gone |= (uint64_t)mine << k;
             }
-        } else {
-            for (uint64_t dead = ~alive & (~0ull >> (64 - sh.K)); dead; dead &= dead - 1) {
-                const int k = __builtin_ctzll(dead);
-                const int32_t x = s_table[k * kCols + t];
-                bool mine = !outside(x);
-#pragma unroll 8
-                for (int j = 0; j < sh.K; j++) mine &= !((j < k || (alive >> j & 1)) && j != k && s_table[j * kCols + t] == x);
-                gone |= (uint64_t)mine << k;
-            }
         }
+    } else {
+        const uint64_t differ = s_differ[0] | s_differ[1] | s_differ[2] | s_differ[3];
+        int turn = 0;
+        for (uint64_t todo = st ? 0 : differ; todo; todo &= todo - 1) {
+            if ((turn++ & (W - 1)) != w) continue;
+            const int at = __builtin_ctzll(todo);
+            const int32_t x = t < sh.K ? s_table[t * kPitch + at] : -1;
+            uint64_t mine = 0;
+            for (uint64_t left = __ballot(!outside(x)) & ~alive; left;) {
+                const int k = __builtin_ctzll(left);
+                const uint64_t same = __ballot(x == __builtin_amdgcn_readlane(x, k)) & (~0ull >> (64 - sh.K));
+                if (!(same & alive)) mine |= 1ull << k;
+                left &= ~same;
+            }
+            if (t == 0) s_gone[at] = mine;
+        }
+        __syncthreads();
+        if (w) return;
+        // one block for all, if no beam goes on
+        if (col < cols && !st) gone = differ >> t & 1 ? s_gone[t] : alive || outside(first) ? 0 : 1;
     }
     const int count = __popcll(gone), upto = wave_scan_sum(count), all = __builtin_amdgcn_readlane(upto, 63);
     int32_t *list = ws.list + ((size_t)b * sh.chunks + c) * kCols * sh.K;
-    for (int at = upto - count; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kCols + t];
+    for (int at = upto - count; gone; gone &= gone - 1) list[at++] = s_table[__builtin_ctzll(gone) * kPitch + t];
     // the half-filled block: its first child keeps it
     const bool here = !st && rows > 0 && full / kCols == c;
     int need = 0;
     if (here) {
-        __syncthreads();  // another lane's column
-        const int32_t own = p >= 0 ? s_table[p * kCols + full % kCols] : -1;
+        if (FEW) __syncthreads();  // another lane's column
+        const int32_t own = p >= 0 ? s_table[p * kPitch + full % kCols] : -1;
         bool later = false;
         for (int j = 0; j < sh.M; j++) later |= j < t && __builtin_amdgcn_readlane(own, j) == own;
         later = later && own >= 0;
@@ -159,27 +188,56 @@ struct CacheParts {
 };
 
 
-// The rows of a half-filled block: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is shorter; AHEAD a
-// thread on their way.  (A block of one layer has less than 2^32 bytes.)
+// The rows of half-filled blocks, copies first, first + step, .. below n: one head's are consecutive.  Units of 16 bytes, or of 2 where a row is
+// shorter, those of all copies in a row (not where 64 of them might pass 32 bits), AHEAD a thread on their way.  (A block of one layer has
+// less than 2^32 bytes.)
 template <class U, int AHEAD>
-__device__ __forceinline__ void copy_rows(uint8_t *layer, int src, int dst, int Hkv, int block_size, int row_bytes, int rows) {
-    const uint32_t per_head = (uint32_t)(rows * row_bytes) / sizeof(U), all = per_head * Hkv, inv = per_head == 1 ? 0xffffffffu : 0xffffffffu / per_head;
+__device__ __forceinline__ void copy_rows(uint8_t *layer, const int2 *copies, int first, int step, int n, int num_blocks, int Hkv, int block_size,
+                                          int row_bytes, int rows) {
+    const uint32_t per_head = (uint32_t)(rows * row_bytes) / sizeof(U), all = per_head * Hkv;
+    const uint32_t inv = per_head == 1 ? 0xffffffffu : 0xffffffffu / per_head, inv_all = all == 1 ? 0xffffffffu : 0xffffffffu / all;
     const uint32_t head = (uint32_t)block_size * row_bytes;
-    const uint8_t *from = layer + (size_t)src * Hkv * head;
-    uint8_t *to = layer + (size_t)dst * Hkv * head;
-    for (uint32_t u0 = threadIdx.x; u0 < all; u0 += AHEAD * 256) {
+    const size_t block = (size_t)Hkv * head;
+    if (first + step >= n || all >= (1u << 24)) {  // a copy at a time
+        for (int copy = first; copy < n; copy += step) {
+            if ((uint32_t)copies[copy].y >= (uint32_t)num_blocks) continue;
+            const uint8_t *from = layer + copies[copy].x * block;
+            uint8_t *to = layer + copies[copy].y * block;
+            for (uint32_t u0 = threadIdx.x; u0 < all; u0 += AHEAD * 256) {
+                U x[AHEAD];
+                uint32_t at[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; i++) {
+                    uint32_t unit;
+                    const uint32_t h = fast_div(min(u0 + i * 256, all - 1), per_head, inv, unit);
+                    at[i] = h * head + unit * (uint32_t)sizeof(U);
+                    x[i] = *reinterpret_cast<const U *>(from + at[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < AHEAD; i++)
+                    if (u0 + i * 256 < all) *reinterpret_cast<U *>(to + at[i]) = x[i];
+            }
+        }
+        return;
+    }
+    const uint32_t units = ((n - 1 - first) / step + 1) * all;
+    for (uint32_t u0 = threadIdx.x; u0 < units; u0 += AHEAD * 256) {
         U x[AHEAD];
-        uint32_t at[AHEAD];
+        size_t to[AHEAD];
+        uint32_t there = 0;
 #pragma unroll
         for (int i = 0; i < AHEAD; i++) {
-            uint32_t unit;
-            const uint32_t h = fast_div(min(u0 + i * 256, all - 1), per_head, inv, unit);
-            at[i] = h * head + unit * (uint32_t)sizeof(U);
-            x[i] = *reinterpret_cast<const U *>(from + at[i]);
+            uint32_t unit, in_head;
+            const uint32_t copy = fast_div(min(u0 + i * 256, units - 1), all, inv_all, unit);
+            const int2 c = copies[first + copy * step];
+            const uint32_t at = fast_div(unit, per_head, inv, in_head) * head + in_head * (uint32_t)sizeof(U);
+            x[i] = *reinterpret_cast<const U *>(layer + c.x * block + at);
+            to[i] = c.y * block + at;
+            there |= (u0 + i * 256 < units && (uint32_t)c.y < (uint32_t)num_blocks) << i;
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; i++)
-            if (u0 + i * 256 < all) *reinterpret_cast<U *>(to + at[i]) = x[i];
+            if (there >> i & 1) *reinterpret_cast<U *>(layer + to[i]) = x[i];
     }
 }
 
@@ -214,14 +272,15 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
         before = __builtin_amdgcn_readlane(wave_scan_sum(before), 63);
         if ((long)before + need > ring.count) return;
         uint8_t *layer = cache.base[part] + (size_t)l * cache.layer_bytes[part];
-        uint64_t todo = __ballot(from >= 0);
-        for (int i = 0; i < need; i++, todo &= todo - 1) {
-            if (i % G != g) continue;
-            const int src = __shfl(from, __builtin_ctzll(todo)), dst = free_blocks[ring.place(before + i)];
-            if ((uint32_t)dst >= (uint32_t)sh.num_blocks) continue;
-            if (cache.row_bytes[part] % 16 == 0) copy_rows<u32x4, 8>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
-            else copy_rows<uint16_t, 2>(layer, src, dst, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+        __shared__ int2 s_copy[ETV_MAX_BEAMS];
+        const uint64_t copies = __ballot(from >= 0);
+        if (t < 64 && from >= 0) {
+            const int i = __popcll(copies & ((1ull << lane) - 1));
+            s_copy[i] = make_int2(from, free_blocks[ring.place(before + i)]);
         }
+        __syncthreads();
+        if (cache.row_bytes[part] % 16 == 0) copy_rows<u32x4, 8>(layer, s_copy, g, G, need, sh.num_blocks, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
+        else copy_rows<uint16_t, 2>(layer, s_copy, g, G, need, sh.num_blocks, cache.Hkv, sh.block_size, cache.row_bytes[part], rows);
         return;
     }
     __shared__ long s_need, s_give;
@@ -285,16 +344,14 @@ __global__ void __launch_bounds__(256) reorder_copy_kernel(ReorderShape sh, Cach
     } else {
         if (own_need) {
             const int32_t from = lane < sh.M ? ws.from[(size_t)b * sh.M + lane] : -1;
-            uint64_t todo = __ballot(from >= 0);
-            for (long i = need_at; todo; i++, todo &= todo - 1) {
-                const int32_t dst = free_blocks[ring.place(i)];
-                int32_t *row = table_out + ((size_t)b * sh.M + __builtin_ctzll(todo)) * sh.max_blocks;
-                if ((uint32_t)dst < (uint32_t)sh.num_blocks) {
-                    if (t == 0) row[L / sh.block_size] = dst;
-                } else {
-                    st |= ETV_BRANCH_BAD_FREE;
-                    for (int j = t; j < sh.max_blocks; j += 256) row[j] = -1;
-                }
+            const uint64_t copies = __ballot(from >= 0);
+            const int32_t dst = from >= 0 ? free_blocks[ring.place(need_at + __popcll(copies & ((1ull << lane) - 1)))] : 0;
+            const bool good = (uint32_t)dst < (uint32_t)sh.num_blocks;
+            if (t < 64 && from >= 0 && good) table_out[((size_t)b * sh.M + lane) * sh.max_blocks + L / sh.block_size] = dst;
+            for (uint64_t bad = __ballot(!good); bad; bad &= bad - 1) {
+                st |= ETV_BRANCH_BAD_FREE;
+                int32_t *row = table_out + ((size_t)b * sh.M + __builtin_ctzll(bad)) * sh.max_blocks;
+                for (int j = t; j < sh.max_blocks; j += 256) row[j] = -1;
             }
         }
         long at = ring.count + give_at;
@@ -369,8 +426,9 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
     int64_t G = 2048 / one;
     G = G < 1 ? 1 : G > sh.M ? sh.M : G;
     if (sh.B + one * G >= (1 << 24)) return ETV_ERR_UNSUPPORTED;  // a launch has less than 2^32 threads
-    hipLaunchKernelGGL(sh.K <= 8 ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(kCols),
-                       sizeof(int32_t) * sh.K * kCols, s, sh, block_table, len, parent, table_out, ws);
+    const bool few = sh.K <= 8;
+    hipLaunchKernelGGL(few ? reorder_tables_kernel<true> : reorder_tables_kernel<false>, dim3(sh.chunks, sh.B), dim3(few ? kCols : 4 * kCols),
+                       sizeof(int32_t) * sh.K * kPitch, s, sh, block_table, len, parent, table_out, ws);
     const int32_t rc = check_launch();
     if (rc != ETV_OK) return rc;
     hipLaunchKernelGGL(reorder_copy_kernel, dim3((unsigned)(sh.B + one * G)), dim3(256), 0, s, sh, cache, (int)G, len, free_blocks, free_state, table_out,

@@ -58,24 +58,31 @@ struct Vec<uint16_t> {
     }
 };
 
-// One token a workgroup.  A thread has the same place in every head it comes to -- two 16-byte vectors, both members of a channel pair among them -- so
+// One token a workgroup, or as many as its 256 threads take at once: a token of 24 heads of 64 channels occupies 96 of them.  A thread has the same
+// place in every head it comes to -- two 16-byte vectors, both members of a channel pair among them -- so
 // that its sines and cosines, worked out once for the token and passed around by LDS, stay in its registers.  What bounds it is memory,
 // and for few tokens the chain of loads: what the arguments alone say the place of is asked for before the angles are worked out, the first
 // head's vectors among it, and every further head's before the one before it is finished.  8 tokens take 4.2 us; 32 trees of 60
 // nodes, 41.3 MB, 9.0 us where the bytes take 8.0.
-template <class T, bool INTER>
+template <class T, bool INTER, bool MANY>
 __global__ void __launch_bounds__(256) rotary_kernel(etv_rotary_desc dsc, RotaryPtrs p, const int32_t *positions, const float *inv_freq,
-                                                     const int32_t *n_rows, const int32_t *slot_map, uint32_t inv_T, uint32_t inv_upr, uint32_t inv_bs) {
+                                                     const int32_t *n_rows, const int32_t *slot_map, int tokens_a_wg, int lanes, uint32_t inv_T, uint32_t inv_upr,
+                                                     uint32_t inv_lanes, uint32_t inv_half, uint32_t inv_bs) {
     constexpr int N = Vec<T>::N;
-    __shared__ float2 s_turn[128];
-    const int t = threadIdx.x, half = dsc.rot_dim / 2, upr = dsc.d / (2 * N), turning = half / N;
-    uint32_t row, u32;
-    const uint32_t b = fast_div(blockIdx.x, dsc.T, inv_T, row);
-    const int first = (int)fast_div(t, upr, inv_upr, u32), u = (int)u32, step = (int)fast_div(256, upr, inv_upr, u32);
+    extern __shared__ float2 s_turn[];  // [tokens][half]
+    const int half = dsc.rot_dim / 2, upr = dsc.d / (2 * N), turning = half / N;
+    uint32_t row, u32, lane;
+    // `lanes` threads a token
+    const int tokens = MANY ? tokens_a_wg : 1;
+    const uint32_t mine = MANY ? fast_div(threadIdx.x, lanes, inv_lanes, lane) : 0;
+    const int t = MANY ? lane : threadIdx.x;
+    const uint32_t first_token = blockIdx.x * tokens, all = (uint32_t)dsc.B * dsc.T, token = MANY ? min(first_token + mine, all - 1) : first_token;
+    const uint32_t b = fast_div(token, dsc.T, inv_T, row);
+    const int first = (int)fast_div(t, upr, inv_upr, u32), u = (int)u32, step = (int)fast_div(MANY ? lanes : 256, upr, inv_upr, u32);
     const bool turns = u < turning;
     const int at = !turns ? dsc.rot_dim + (u - turning) * 2 * N : (INTER ? 2 : 1) * u * N, gap = turns && !INTER ? half : N;
     // heads of q, then of k, then of v; the remainder of the 256 threads has none
-    const int heads = first < step ? dsc.Hq + dsc.Hkv + (p.v ? dsc.Hkv : 0) : 0;
+    const int heads = first < step && (!MANY || ((int)mine < tokens && first_token + mine < all)) ? dsc.Hq + dsc.Hkv + (p.v ? dsc.Hkv : 0) : 0;
     const auto rows_of = [&](const void *base, int i) { return static_cast<const T *>(base) + b * dsc.strides[2 * i] + row * dsc.strides[2 * i + 1]; };
     const T *src[3] = {rows_of(p.q, 0), rows_of(p.k, 1), rows_of(p.v, 2)};
     const auto pick = [&](int head, const auto &q, const auto &k, const auto &v, int &h) {
@@ -92,10 +99,18 @@ __global__ void __launch_bounds__(256) rotary_kernel(etv_rotary_desc dsc, Rotary
     u32x4 ra = {}, rb = {};
     if (first < heads) load(first, ra, rb);
     const int rows = n_rows ? n_rows[b] : dsc.T;
-    long slot = slot_map ? slot_map[blockIdx.x] : -1;
-    if (t < half) {
-        const float f = inv_freq[t];
-        s_turn[t] = turn_of(positions[((size_t)dsc.axis_of[t] * dsc.B + b) * dsc.T + row], f, dsc.scale, dsc.flags & ETV_ROTARY_INVERSE);
+    long slot = slot_map ? slot_map[token] : -1;
+    const auto turn_at = [&](int i, uint32_t pair, uint32_t of) {
+        s_turn[i] = turn_of(positions[(size_t)dsc.axis_of[pair] * all + of], inv_freq[pair], dsc.scale, dsc.flags & ETV_ROTARY_INVERSE);
+    };
+    if (MANY) {
+        for (int i = threadIdx.x; i < tokens * half; i += 256) {
+            uint32_t pair;
+            const uint32_t of = fast_div(i, half, inv_half, pair);
+            turn_at(i, pair, min(first_token + of, all - 1));
+        }
+    } else if (t < half) {
+        turn_at(t, t, token);
     }
     __syncthreads();
     if ((int)row >= rows) return;
@@ -108,7 +123,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(etv_rotary_desc dsc, Rotary
     T *out[3] = {const_cast<T *>(rows_of(p.q_out, 3)), const_cast<T *>(rows_of(p.k_out, 4)), const_cast<T *>(rows_of(p.v_out, 5))};
     float2 turn[N];
 #pragma unroll
-    for (int j = 0; j < N; j++) turn[j] = turns ? s_turn[u * N + j] : make_float2(1, 0);
+    for (int j = 0; j < N; j++) turn[j] = turns ? s_turn[(heads ? mine * half : 0) + u * N + j] : make_float2(1, 0);
     for (int head = first; head < heads; head += step) {
         u32x4 na = {}, nb = {};
         if (head + step < heads) load(head + step, na, nb);
@@ -184,9 +199,17 @@ extern "C" int32_t etv_rotary_write_kv(const etv_rotary_desc *h, const void *q, 
     if (!positions || !inv_freq) return ETV_ERR_INVALID_ARG;
     const etv::RotaryPtrs p{q, k, v, q_out, k_out, v_out, k_cache, v_cache};
     const bool inter = d.flags & ETV_ROTARY_INTERLEAVED;
-    const auto kernel = d.dtype == ETV_BF16 ? (inter ? etv::rotary_kernel<uint16_t, true> : etv::rotary_kernel<uint16_t, false>)
-                                            : (inter ? etv::rotary_kernel<float, true> : etv::rotary_kernel<float, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(d.B * d.T)), dim3(256), 0, etv::as_stream(stream), d, p, positions, inv_freq, n_rows, slot_map,
-                       etv::fast_div_inv(d.T), etv::fast_div_inv(d.d * (d.dtype == ETV_BF16 ? 2 : 4) / 32), d.block_size ? etv::fast_div_inv(d.block_size) : 0);
+    // threads of one token that have a head at once, and tokens a workgroup takes with that
+    const int upr = d.d * (d.dtype == ETV_BF16 ? 2 : 4) / 32, units = upr * (d.Hq + d.Hkv + (v ? d.Hkv : 0)), half = d.rot_dim / 2;
+    const int tokens = units < 256 ? 256 / units : 1, lanes = tokens > 1 ? units : 256 / upr * upr;
+    const auto choose = [&](auto type) {
+        using T = decltype(type);
+        return tokens > 1 ? (inter ? etv::rotary_kernel<T, true, true> : etv::rotary_kernel<T, false, true>)
+                          : (inter ? etv::rotary_kernel<T, true, false> : etv::rotary_kernel<T, false, false>);
+    };
+    const auto kernel = d.dtype == ETV_BF16 ? choose(uint16_t{}) : choose(float{});
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((d.B * d.T + tokens - 1) / tokens)), dim3(256), (size_t)tokens * half * sizeof(float2), etv::as_stream(stream),
+                       d, p, positions, inv_freq, n_rows, slot_map, tokens, lanes, etv::fast_div_inv(d.T), etv::fast_div_inv(upr), etv::fast_div_inv(lanes),
+                       etv::fast_div_inv(half), d.block_size ? etv::fast_div_inv(d.block_size) : 0);
     return etv::check_launch();
 }
