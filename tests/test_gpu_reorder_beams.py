@@ -89,6 +89,20 @@ def test_lengths_at_the_borders_of_blocks_and_chunks(L, parent):
         assert after[1] == state[1] + len(set(table[0][table[0] >= 0].tolist())) and (out == -1).all()
 
 
+@pytest.mark.parametrize("K", [9, 20, 33, 64])
+@pytest.mark.parametrize("apart,M", [(0, 5), (3, 64), (200, 3)])
+@pytest.mark.parametrize("kept", [0, 2, 40])
+def test_many_beams_that_part_early_or_late(K, apart, M, kept):
+    """Columns that all beams share, that groups share and that each has to itself, over several chunks; few beams go on, or none."""
+    rng = np.random.default_rng(K + apart)
+    lens = [16 * 150 + 3, 16 * 70, 5, 0]
+    table, ring, state = beams(rng, 4, K, lens, 16, 152, 4 * M, apart=apart)
+    parent = rng.integers(0, min(K, kept), (4, M)) if kept else np.full((4, M), -1)
+    table[1, K - 1, :3] = [-9, len(ring), 2 ** 30]               # of a beam that does not go on, unless all may
+    *_, status, _ = check(rng, table, lens, parent, ring, state, 16, layers=1, Hkv=1)
+    assert kept == 40 or status == [0] * 4
+
+
 @pytest.mark.parametrize("refused", [(), (3,), (65, 300, 699)])
 def test_many_requests_of_several_chunks(refused):
     """What the requests before a request need and give is added up over more of them than a workgroup takes at a time."""
