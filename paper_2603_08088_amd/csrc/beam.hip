@@ -76,6 +76,13 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+// The least number whose order has these upper 16 bits, -FLT_MAX for that of -inf.
+__device__ __forceinline__ float least_of(uint32_t key) {
+    if (key <= 0x007fu) return -FLT_MAX;
+    const uint32_t full = key << 16;
+    return __uint_as_float(full & 0x80000000u ? full ^ 0x80000000u : ~full);
+}
+
 // A number that at least R values reach, none below -FLT_MAX: the R-th largest with the low 16 of its 32 bits cut off, found bit by bit.  `count` tells how
 // many have a key of at least its argument.
 template <int UNROLL = 16, class F>
@@ -86,9 +93,7 @@ __device__ __forceinline__ float reached_by(F count, int R) {
         const uint32_t trial = cut | 1u << bit;
         if (count(trial) >= R) cut = trial;
     }
-    if (cut <= 0x007fu) return -FLT_MAX;  // the order of -inf
-    const uint32_t full = cut << 16;
-    return __uint_as_float(full & 0x80000000u ? full ^ 0x80000000u : ~full);
+    return least_of(cut);
 }
 
 // The largest, and the sum, over 2^width neighbouring lanes, in each of them: within a row of sixteen by lane moves of the vector unit.
@@ -145,7 +150,8 @@ __device__ __forceinline__ void block_best(K &key, P &place) {
 constexpr double kLog2e = 1.4426950408889634;
 
 // 2^z for |z| <= 1000, to 1.9e-9 of itself: a whole number n, taken off by a sum whose last bit is a one, and a polynomial in what is left (the
-// smallest relative error on [-1/2, 1/2] at its degree, by Remez's exchange); n goes into the exponent.  For the few exponentials that join sums.
+// smallest relative error on [-1/2, 1/2] at its degree, by Remez's exchange); n goes into the exponent.  For the few exponentials that join sums, and
+// for sums that are taken again.
 __device__ __forceinline__ double exp2_fast(double z) {
     const double shifted = z + 6755399441055744.0;  // 1.5 * 2^52
     const double f = z - (shifted - 6755399441055744.0);
@@ -276,13 +282,16 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
             const int j = __builtin_ctz(hits);
             hits &= hits - 1;
             const int v = min(place(i, j / N), V - N) + j % N, at = atomicAdd(&s_n, 1);
-            if (at < room) s_cand[at] = {Logits<T>::one(x[v]), v};
+            if (at < room) s_cand[at].v = v;
         }
     }
     __syncthreads();
     Candidate *out = cands + (size_t)blockIdx.x * list;
     int n = s_n;
-    if (n > room) {  // large ones side by side in a few lanes: a bound from all logits
+    if (n <= room) {  // their logits, all at once
+        for (int i = t; i < n; i += 64) s_cand[i].x = Logits<T>::one(x[s_cand[i].v]);
+        __syncthreads();
+    } else {  // large ones side by side in a few lanes: a bound from all logits
         const float closer = reached_by<1>(
             [&](uint32_t c) {
                 int mine = 0;
@@ -302,10 +311,16 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         n = s_n;
     }
     if (n <= room && n > 2 * dsc.M + 64) {  // ranking takes n^2 steps: first those below a closer bound go
+        constexpr int A = 16;  // `room` at its largest
+        uint32_t keys[A];
+#pragma unroll
+        for (int i = 0; i < A; i++) keys[i] = i * 64 + t < n ? order_of(s_cand[i * 64 + t].x) >> 16 : 0;
         const float closer = reached_by<1>(
             [&](uint32_t c) {
                 int all = 0;
-                for (int i0 = 0; i0 < n; i0 += 64) all += __popcll(__ballot(i0 + t < n && order_of(s_cand[min(i0 + t, n - 1)].x) >> 16 >= c));
+#pragma unroll
+                for (int i = 0; i < A; i++)
+                    if (i * 64 < n) all += __popcll(__ballot(keys[i] >= c));
                 return all;
             },
             dsc.M);
@@ -361,12 +376,13 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // A request: the logarithms of its beams' sums, then the M best of all candidates.
 //   total = (x - reference) + (score - log of the sum relative to it): nothing is lost where logits are large
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
-// other are closer than their sums are good for, these are taken again in 64 bits from the logits, and the order with them: so the order is that of
-// 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
+// other are closer than their sums are good for, these are taken again from the logits, with exp2_fast and, if that does not tell either, with exponentials
+// of full precision: so the order is that of 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
 // Bound by the chain of its loads and barriers: 5.1 us for one request of 4 beams, 5.9 for 32 of 8 beams with 8 lists each.  A scan whose
 // last workgroup merges would save this launch's 4 us on the host, but needs a counter that somebody clears, and a release to the whole device by every wavefront.
-// SHARED: few lists against M, which are therefore gone into deeply, by several threads each.
-template <class T, bool SHARED>
+// SHARED: few lists against M, which are therefore gone into deeply, by several threads each.  MANY: M above 16, where the heads of a wavefront's lists
+// say too little; a kernel of its own, for code that is not run costs the other 0.2 us.
+template <class T, bool SHARED, bool MANY>
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
                                                                    const uint8_t *finished, int splits, uint32_t inv_splits, int width, int list,
                                                                    const ScanHead *heads, const Candidate *cands, float *out_scores, int32_t *parent,
@@ -374,7 +390,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     __shared__ double s_base[ETV_MAX_BEAMS], s_max[ETV_MAX_BEAMS];
     __shared__ int s_state[ETV_MAX_BEAMS], s_status, s_n;
     __shared__ float s_cut[kMergeThreads / 64];
-    __shared__ int s_part[2][kMergeThreads / 64];
+    __shared__ uint32_t s_sample[kMergeThreads];
+    __shared__ int s_count[2][kMergeThreads / 64];
     struct Total {
         double x;
         long place;
@@ -384,7 +401,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     __shared__ Candidate s_head[4][kMergeThreads];
     const int b = blockIdx.x, t = threadIdx.x;
     const int lists = dsc.K * splits, M = dsc.M;
-    const double close = 0x1p-22 * (6 + kSlack + 0.6932f * (32 - __builtin_clz(dsc.V)));
+    // totals of two beams closer than this are not told apart: by the scan's sums, and then by sums of exp2_fast
+    double close = 0x1p-22 * (6 + kSlack + 0.6932f * (32 - __builtin_clz(dsc.V)));
     heads += (size_t)b * lists;
     cands += (size_t)b * lists * list;
     if (t == 0) s_status = 0;
@@ -396,10 +414,12 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
     if (SHARED)
         while (lists << (share + 1) <= kMergeThreads) share++;
     const int own = t >> share, deep = t & ((1 << share) - 1), apart = 1 << share;
+    const int gap = (M + apart - 1) >> share;
     int head_n = 0;
-    Candidate head[4] = {};
+    Candidate head[4] = {}, deeper = {};
     if (own < lists) {
         head_n = heads[own].n;
+        if (MANY && SHARED) deeper = cands[(size_t)own * list + min(deep * gap, list - 1)];
 #pragma unroll
         for (int i = 0; i < 4; i++) head[i] = cands[(size_t)own * list + min(deep + i * apart, list - 1)];
     }
@@ -478,35 +498,43 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         }
         const uint32_t key = order_of(top) >> 16;
         if (t == 0) s_n = 0;
-        if (M > 16) {
+        if (MANY) {
             // samples of all lists: where several threads look into one, `gap` entries from each other
-            const int gap = (M + apart - 1) >> share;
             uint32_t sample = key;
-            if (deep) {
+            if (SHARED && deep) {
                 int k;
                 sample = 0;
                 if (own < lists && deep * gap < length(own, k)) {
                     double x;
                     long place;
-                    value(cands[(size_t)own * list + deep * gap], k, x, place);
+                    value(deeper, k, x, place);
                     sample = order_of((float)x) >> 16;
                 }
             }
-            // a first sample stands for one entry, each further one for `gap`; the parts of a count alternate between two places, for one barrier each
-            int turn = 0;
-            const float all = reached_by<1>(
-                [&](uint32_t c) {
-                    const int part = __popcll(__ballot(!deep && sample >= c)) + gap * __popcll(__ballot(deep && sample >= c));
-                    turn ^= 1;
-                    if ((t & 63) == 0) s_part[turn][t >> 6] = part;
-                    __syncthreads();
-                    int sum = 0;
+            // A first sample stands for one entry, each further one for `gap`.  Three bits of the bound at a time: every wavefront has all samples and counts
+            // what reaches its digit, for a barrier each; the counts alternate between two places.
+            s_sample[t] = sample;
+            __syncthreads();
+            constexpr int A = kMergeThreads / 64;
+            static_assert(A == 8, "a wavefront a digit");
+            const int lane = t & 63;
+            const int weight = SHARED && (lane & (apart - 1)) ? gap : 1;  // (2^share beyond a wavefront: a gap of 1)
+            uint32_t all[A], bound = 0;
 #pragma unroll
-                    for (int w = 0; w < kMergeThreads / 64; w++) sum += s_part[turn][w];
-                    return sum;
-                },
-                M);
-            if ((t & 63) == 0) s_cut[t >> 6] = all;
+            for (int i = 0; i < A; i++) all[i] = s_sample[i * 64 + lane];
+#pragma unroll
+            for (int shift = 15; shift >= 0; shift -= 3) {
+                const uint32_t c = bound | (uint32_t)(t >> 6) << shift;
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < A; i++) n += all[i] >= c;
+                n = __builtin_amdgcn_readlane(wave_scan_sum(n * weight), 63);
+                int *counts = s_count[shift & 1];
+                if (lane == 0) counts[t >> 6] = n;
+                __syncthreads();
+                bound |= (uint32_t)__popcll(__ballot(lane > 0 && lane < A && counts[lane & (A - 1)] >= M)) << shift;
+            }
+            if (lane == 0) s_cut[t >> 6] = least_of(bound);
         } else {  // those of one wavefront are enough, and take no barrier for each bit
             const float mine = reached_by([&](uint32_t c) { return __popcll(__ballot(key >= c)); }, M);
             if ((t & 63) == 0) s_cut[t >> 6] = mine;
@@ -602,7 +630,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             }
         }
         __syncthreads();
-        if (round) break;
+        if (round == 2) break;
         // Two totals of different beams too close to call: neighbours of the M best, or the last of them and one left out.  (Equal ones are those of
         // equal rows.)
         const auto call = [&](const Total &a, const Total &o) {
@@ -634,14 +662,35 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             const int k = __builtin_ctzll(again);
             if (s_state[k] != kBeamLive) continue;
             const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
+            const double m = s_max[k];
             double s = 0;
+            if (round == 0) {
+                constexpr int N = Logits<T>::N, AHEAD = 4;
+                const auto add = [&](float y) { s += exp2_fast(fmax(((double)y - m) * kLog2e, -1000.0)); };
+                const int vecs = dsc.V / N;
+                for (int i0 = t; i0 < vecs; i0 += AHEAD * kMergeThreads) {
+                    typename Logits<T>::vec raw[AHEAD];
+#pragma unroll
+                    for (int i = 0; i < AHEAD; i++) raw[i] = *reinterpret_cast<const typename Logits<T>::vec_at *>(x + (size_t)min(i0 + i * kMergeThreads, vecs - 1) * N);
+#pragma unroll
+                    for (int i = 0; i < AHEAD; i++)
+                        if (i0 + i * kMergeThreads < vecs) {
+#pragma unroll
+                            for (int j = 0; j < N; j++) add(Logits<T>::get(raw[i], j));
+                        }
+                }
+                for (int v = vecs * N + t; v < dsc.V; v += kMergeThreads) add(Logits<T>::one(x[v]));
+            } else {
 #pragma unroll 4
-            for (int v = t; v < dsc.V; v += kMergeThreads) s += exp((double)Logits<T>::one(x[v]) - s_max[k]);
+                for (int v = t; v < dsc.V; v += kMergeThreads) s += exp((double)Logits<T>::one(x[v]) - m);
+            }
             s = block_sum(s);
             // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
             if (t == 0) s_base[k] = rint(((double)scores[(size_t)b * dsc.K + k] - log(s)) * 0x1p40) * 0x1p-40;
         }
+        close = 0x1p-27;
         __syncthreads();
+        if (t < 2) s_again[t] = 0;  // read behind further barriers, and read by all before this one
     }
     if (t < M) {
         const bool found = t < n;
@@ -727,7 +776,9 @@ extern "C" int32_t etv_beam_select(const etv_beam_desc *h, const void *logits, c
         while (width < 6 && (1 << width) < splits) width++;
         // 64 requests of 10 beams in 4 lists each: 2.8 us less than with a thread a list; 8 requests of 4 beams in 63 lists each would take 0.7 more
         const bool shared = splits * h->K <= 16 * h->M && splits * h->K <= etv::kMergeThreads / 2;
-        hipLaunchKernelGGL((shared ? etv::beam_merge_kernel<T, true> : etv::beam_merge_kernel<T, false>), dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits,
+        const auto merge = h->M > 16 ? (shared ? etv::beam_merge_kernel<T, true, true> : etv::beam_merge_kernel<T, false, true>)
+                                     : (shared ? etv::beam_merge_kernel<T, true, false> : etv::beam_merge_kernel<T, false, false>);
+        hipLaunchKernelGGL(merge, dim3(h->B), dim3(etv::kMergeThreads), 0, s, *h, x, scores, n_beams, finished, splits, inv_splits,
                            width, list, heads, cands, out_scores, parent, token, finished_out, status);
         return etv::check_launch();
     };
