@@ -206,3 +206,28 @@ def test_a_cache_of_more_than_2_32_elements(paged):
                 assert torch.equal(got, want[b, t]), s
                 got.zero_()
         assert not any(part.any() for part in cache.view(-1).split(1 << 30))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d,rot", [(900, 32, 8, 128, None), (10000, 3, 1, 64, 32), (2100, 1, 1, 16, None)])
+@pytest.mark.parametrize("dtype,inter", [("bf16", False), ("f32", True)])
+def test_padding_of_many_rows_is_left_alone(T, Hq, Hkv, d, rot, dtype, inter):
+    """Batches large enough that padding is not even read; tokens that share a workgroup are of two sequences, of padding and of none."""
+    B = 3
+    c = Case(T, B, T, Hq, Hkv, d, dtype, rot=rot, inter=inter, axes=2)
+    n = [T - 1, 0, T // 2 + 3]
+    every = api.rotary_write_kv(c.q, c.k, None, dev(c.positions), c.rotary)
+    c.close(every["q"], c.host[0])
+    slots = c.rng.permutation(B * T).reshape(B, T)
+    kc, vc = (torch.full((B, T, Hkv, d), 3, dtype=c.dtype, device="cuda") for _ in range(2))
+    out = dict(q=torch.full_like(c.q, 7), k=torch.full_like(c.k, 7), v=torch.full_like(c.v, 7))
+    api.rotary_write_kv(c.q, c.k, c.v, dev(c.positions), c.rotary, n_rows=dev(n), slot_map=dev(slots), k_cache=kc, v_cache=vc, paged=False, out=out)
+    there = torch.zeros((B, T), dtype=torch.bool, device="cuda")
+    for b in range(B):
+        there[b, :n[b]] = True
+    for name, want in (("q", every["q"]), ("k", every["k"]), ("v", c.v)):
+        assert torch.equal(out[name], torch.where(there[..., None, None], want, torch.full_like(want, 7))), name
+    at = torch.from_numpy(slots).cuda()[there]
+    for cache, want in ((kc, every["k"]), (vc, c.v)):
+        expect = torch.full_like(cache, 3)
+        expect.view(B * T, Hkv, d)[at] = want[there]
+        assert torch.equal(cache, expect)
