@@ -63,8 +63,8 @@ struct Vec<uint16_t> {
 // place in every head it comes to -- two 16-byte vectors, both members of a channel pair among them -- so
 // that its sines and cosines, worked out once for the token and passed around by LDS, stay in its registers.  What bounds it is memory,
 // and for few tokens the chain of loads: what the arguments alone say the place of is asked for before the angles are worked out, the first
-// head's vectors among it, and every further head's before the one before it is finished.  8 tokens take 4.2 us; 32 trees of 60
-// nodes, 41.3 MB, 9.0 us where the bytes take 8.0.
+// head's vectors among it, and every further head's before the one before it is finished.  8 tokens take 4.4 us; 32 trees of 60
+// nodes, 41.3 MB, 9.2 us where the bytes take 8.0.
 template <class T, bool INTER, bool MANY, bool ROWS_FIRST>
 __global__ void __launch_bounds__(256) rotary_kernel(etv_rotary_desc dsc, RotaryPtrs p, const int32_t *positions, const float *inv_freq,
                                                      const int32_t *n_rows, const int32_t *slot_map, int tokens_a_wg, int lanes, uint32_t inv_T, uint32_t inv_upr,
