@@ -310,20 +310,22 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         __syncthreads();
         n = s_n;
     }
-    if (n <= room && n > 2 * dsc.M + 64) {  // ranking takes n^2 steps: first those below a closer bound go
-        constexpr int A = 16;  // `room` at its largest
-        uint32_t keys[A];
+    if (n <= room && n > dsc.M + 32) {  // ranking takes n^2 steps: first those below a closer bound go
+        const auto closer_by = [&](auto at_most) {
+            constexpr int A = decltype(at_most)::value;
+            uint32_t keys[A];
 #pragma unroll
-        for (int i = 0; i < A; i++) keys[i] = i * 64 + t < n ? order_of(s_cand[i * 64 + t].x) >> 16 : 0;
-        const float closer = reached_by<1>(
-            [&](uint32_t c) {
-                int all = 0;
+            for (int i = 0; i < A; i++) keys[i] = i * 64 + t < n ? order_of(s_cand[i * 64 + t].x) >> 16 : 0;
+            return reached_by<1>(
+                [&](uint32_t c) {
+                    int all = 0;
 #pragma unroll
-                for (int i = 0; i < A; i++)
-                    if (i * 64 < n) all += __popcll(__ballot(keys[i] >= c));
-                return all;
-            },
-            dsc.M);
+                    for (int i = 0; i < A; i++) all += __popcll(__ballot(keys[i] >= c));
+                    return all;
+                },
+                dsc.M);
+        };
+        const float closer = n <= 256 ? closer_by(std::integral_constant<int, 4>{}) : closer_by(std::integral_constant<int, 16>{});  // of `room` at its largest
         int kept = 0;
         for (int i0 = 0; i0 < n; i0 += 64) {  // closing up behind the reads
             const Candidate own = s_cand[min(i0 + t, n - 1)];
