@@ -21,6 +21,7 @@ struct Candidate {
 };
 constexpr int kMaxSteps = 16;    // steps of a segment
 constexpr int kMergeThreads = 512;
+constexpr int kThin = 320;       // candidates that are ranked as they are
 constexpr int kMergeCap = 2048;  // candidates that a request collects; where more are close to its M-th best it looks for one after the other
 
 // What a beam offers: nothing, its end token, or its row of logits.
@@ -589,6 +590,41 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
             if (t == 0) s_n = 0;
             __syncthreads();
         }
+        if (MANY && found > kThin && found <= kMergeCap) {
+            // ranking takes found^2 steps: first those below a closer bound go, which is found among the candidates themselves
+            constexpr int A = kMergeCap / kMergeThreads;
+            Total mine[A];
+            uint32_t keys[A];
+#pragma unroll
+            for (int i = 0; i < A; i++) {
+                mine[i] = s_total[min(t + i * kMergeThreads, found - 1)];
+                keys[i] = t + i * kMergeThreads < found ? order_of((float)mine[i].x) >> 16 : 0;
+            }
+            int turn = 0;
+            float closer = reached_by<1>(
+                [&](uint32_t c) {
+                    int n = 0;
+#pragma unroll
+                    for (int i = 0; i < A; i++) n += __popcll(__ballot(keys[i] >= c));
+                    turn ^= 1;
+                    if ((t & 63) == 0) s_count[turn][t >> 6] = n;
+                    __syncthreads();
+                    n = 0;
+#pragma unroll
+                    for (int w = 0; w < kMergeThreads / 64; w++) n += s_count[turn][w];
+                    return n;
+                },
+                M);
+            closer = fmaxf(closer - (fabsf(closer) * 0x1p-21f + (float)close), -FLT_MAX);
+            if (t == 0) s_n = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < A; i++)
+                if (keys[i] && (float)mine[i].x >= closer) s_total[atomicAdd(&s_n, 1)] = mine[i];
+            __syncthreads();
+            found = s_n;
+            __syncthreads();
+        }
         if (found <= kMergeCap) {
             if (t < 16) s_total[found + t] = {-INFINITY, INT64_MAX};  // to a multiple of sixteen
             __syncthreads();
@@ -710,13 +746,15 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
 // Steps of a wavefront's segment: more of them mean fewer bounds to find and fewer lists to merge, and fewer wavefronts to hide that behind.  As many as
 // leave 1536 wavefronts, 6 a CU, up to eight (32 requests of 8 beams and 128000 logits: 8 steps take 1.3 us less than 4, and 2.2 less than 2), sixteen where 4096
 // are left (four times the requests: 5 us less than with 8); a single one instead of two (64 requests of 4 beams and 32000 logits: half a us less).  Segments
-// are as even as steps allow.  Large M: no more than eight, for each segment leaves M candidates.
-constexpr int kFullWaves = 1536, kManyWaves = 4096;
+// are as even as steps allow.  M above 16, where each segment leaves many candidates to bound, rank and merge: from 768 wavefronts on (3 requests of 13 beams
+// and 156000 logits, M = 37: 4.5 us less than from 1536), but no more than eight steps.
+constexpr int kFullWaves = 1536, kManyWaves = 4096, kFewWaves = 768;
 static int beam_step(const etv_beam_desc *h) { return 64 * (h->dtype == ETV_BF16 ? 32 : 16); }
 static int beam_steps(const etv_beam_desc *h) {
     const int64_t all = (h->V + beam_step(h) - 1) / beam_step(h), steps = (int64_t)h->B * h->K * all;
     int64_t n = std::min<int64_t>(steps / kFullWaves, 8);
     if (n < 3) n = 1;
+    if (h->M > 16) n = std::max(n, std::min<int64_t>(steps / kFewWaves, 8));
     if (h->M <= 16) n = std::max(n, std::min<int64_t>(steps / kManyWaves, kMaxSteps));
     const int64_t splits = (all + n - 1) / n;
     return (int)((all + splits - 1) / splits);

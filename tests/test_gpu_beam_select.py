@@ -212,6 +212,14 @@ def test_logits_that_differ_in_their_last_bits(M):
     check(x, -rng.random((2, 3)) * 1e-3, M)
 
 
+@pytest.mark.parametrize("B,K,V", [(4, 32, 28000), (2, 50, 17000), (1, 64, 9000)])
+@pytest.mark.parametrize("alike", [0.0, 1e-3, 6.0])
+def test_hundreds_of_candidates_above_the_first_bound(B, K, V, alike):
+    """Many lists that are gone into at two places: beams alike, nearly alike and apart."""
+    rng = np.random.default_rng(K)
+    check(normal(rng, (B, K, V), "bf16", 2.0), -alike * rng.random((B, K)), 64)
+
+
 @pytest.mark.parametrize("M", [5, 16, 40, 64])
 def test_more_candidates_than_a_merge_holds(M):
     """Many lists, a few beams far ahead of the others; all totals alike."""
