@@ -71,17 +71,17 @@ __device__ __forceinline__ float max9(float m, const float *x) {
     return m;
 }
 
-// Order of fp32 numbers as unsigned integers.
+// Order of fp32 numbers as unsigned integers, and back.
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float number_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 
 // The least number whose order has these upper 16 bits, -FLT_MAX for that of -inf.
 __device__ __forceinline__ float least_of(uint32_t key) {
     if (key <= 0x007fu) return -FLT_MAX;
-    const uint32_t full = key << 16;
-    return __uint_as_float(full & 0x80000000u ? full ^ 0x80000000u : ~full);
+    return number_of(key << 16);
 }
 
 // A number that at least R values reach, none below -FLT_MAX: the R-th largest with the low 16 of its 32 bits cut off, found bit by bit.  `count` tells how
@@ -340,20 +340,24 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         __syncthreads();
     }
     if (n <= room) {
-        if (t < 16) s_cand[n + t] = {-INFINITY, INT32_MAX};  // to a multiple of sixteen
-        __syncthreads();
-        for (int i = t >> 2; i < n; i += 16) {  // four lanes a candidate, with a quarter of the others each
+        // as one number each, larger for a larger logit (of which -0 is 0) and a lower place
+        static_assert(sizeof(Candidate) == sizeof(uint64_t), "one number each");
+        for (int i = t; i < n; i += 64) {
             const Candidate own = s_cand[i];
-            float rank = 0;
+            s_cand[i] = __builtin_bit_cast(Candidate, (uint64_t)order_of(own.x + 0.0f) << 32 | ~(uint32_t)own.v);
+        }
+        if (t < 16) s_cand[n + t] = {0, 0};  // to a multiple of sixteen
+        __syncthreads();
+        const auto order = [&](int i) { return __builtin_bit_cast(uint64_t, s_cand[i]); };
+        for (int i = t >> 2; i < n; i += 16) {  // four lanes a candidate, with a quarter of the others each
+            const uint64_t own = order(i);
+            int above = 0;
 #pragma unroll 1
             for (int j0 = t & 3; j0 < n; j0 += 16)
 #pragma unroll
-                for (int j = j0; j < j0 + 16; j += 4) {
-                    const Candidate o = s_cand[j];
-                    rank += (o.x > own.x) | ((o.x == own.x) & (o.v < own.v));
-                }
-            rank = lanes_sum(rank, 2);
-            if (rank < dsc.M && (t & 3) == 0) out[(int)rank] = own;
+                for (int j = j0; j < j0 + 16; j += 4) above += order(j) > own;
+            const float rank = lanes_sum((float)above, 2);
+            if (rank < dsc.M && (t & 3) == 0) out[(int)rank] = {number_of((uint32_t)(own >> 32)), (int32_t)~(uint32_t)own};
         }
     } else {  // many equal ones: the next best after the last, a round each
         Candidate last = {INFINITY, -1};
