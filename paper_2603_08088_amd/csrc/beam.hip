@@ -236,8 +236,15 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
         // the reference is the largest logit, or up to 1 less: a wavefront's maximum is taken where it may have to move, at first above all
         if (__ballot(most > ref + kSlack)) {
             const float top = wave_best(most, [](float p, float q) { return fmaxf(p, q); });
-            const float top2 = (float)(top * kLog2e);
-            if (ref > -INFINITY) s *= exp2_fast(fmax((double)ref2 - (double)top2, -1000.0));
+            // Finite where -inf may still be added: exp2(-inf - -inf) would be NaN.
+            const float top2 = fmaxf((float)(top * kLog2e), -FLT_MAX);
+            // The sum up to here weighs nothing against 2^-1000 of what comes, and behind a reference of a mask's value it may be infinite, since ref2 is
+            // then off by more than exponents of fp32: only whether it is a number goes on.  (A reference that moves less is exact enough: within a
+            // segment such moves come from -kFarthest - 16 * 694 at most.)
+            if (ref > -INFINITY) {
+                if (((double)ref - (double)top) * kLog2e < -1000) s = s == s ? 0 : s;
+                else s *= exp2_fast(fmax((double)ref2 - (double)top2, -1000.0));
+            }
             ref = top, ref2 = top2;
         }
         // a NaN makes the sum NaN; before the first logit that is neither masked nor NaN there is nothing but zeros and NaN to add

@@ -290,3 +290,60 @@ def test_rows_further_apart_than_32_bits_reach():
     far = torch.empty((1 << 32) + 8 + 3 * ((1 << 30) + 1) + 5001, dtype=torch.bfloat16, device="cuda").as_strided((2, 4, 5001), ((1 << 32) + 8, (1 << 30) + 1, 1))
     far.copy_(x)
     check(x, -rng.random((2, 4)), 6, on=far)
+
+
+def masked_steps(rng, B, K, V, dtype):
+    """Rows in which whole steps of a wavefront hold nothing but a mask's finite value, before others that hold logits of ordinary size; a value and a
+    layout for each request."""
+    step = 2048 if dtype == "bf16" else 1024
+    x, at = normal(rng, (B, K, V), dtype), np.arange(V) // step
+    lows = [torch.finfo(DT[dtype]).min, -1e30, -1e12, -1e10, -3e9, -4e6, -1e4]
+    climb = [-3e38, -1e30, -1e20, -1e10, -3e9, -2e9, -1e7, -2e6, -1.1e6, -1048579, -1048573, -1e6, -5e5, -900, -30, 0]
+    for b in range(B):
+        low, layout = lows[b % 7], b // 7 % 7
+        for k in range(K):
+            if layout == 0:                                           # some steps
+                mask = (rng.random(at[-1] + 1) < 0.5)[at]
+            elif layout == 1:                                         # all but the last logits
+                mask = np.arange(V) < V - 100
+            elif layout == 2:                                         # all but a few tokens that a grammar allows
+                mask = np.ones(V, dtype=bool)
+                mask[rng.integers(0, V, 12)] = False
+            elif layout == 3:                                         # the first half
+                mask = np.arange(V) < V // 2 + k
+            elif layout == 4:                                         # all of a row, and steps that are masked in two ways
+                mask = np.ones(V, dtype=bool) if k == 0 else at % 4 < 3
+                x[b, k, torch.from_numpy(at % 4 == 1)] = -math.inf
+            elif layout == 5:                                         # both masks side by side
+                mask = (rng.random(at[-1] + 1) < 0.7)[at]
+                x[b, k, torch.from_numpy(mask & (rng.random(V) < 0.5))] = -math.inf
+            else:                                                     # every step's logits above those of the step before
+                base = np.array(climb)[np.sort(rng.integers(0, len(climb), at[-1] + 1))]
+                x[b, k] = (x[b, k].double() + torch.from_numpy(base)[at]).to(DT[dtype])
+                continue
+            x[b, k, torch.from_numpy(mask) & (x[b, k] > -math.inf)] = low
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [5, 20])
+def test_steps_of_masked_logits_before_others(M, dtype):
+    """72 requests of 4 beams: a wavefront's segment is three to eight steps of a row."""
+    rng = np.random.default_rng(91)
+    x = masked_steps(rng, 72, 4, 32000, dtype)
+    check(x, -rng.random((72, 4)), M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_masked_step_with_what_is_not_a_number(dtype):
+    """The sum so far is of no weight behind a masked step, but for the news of a logit that is not finite."""
+    rng = np.random.default_rng(92)
+    B, K, V = 72, 4, 32000
+    x = normal(rng, (B, K, V), dtype)
+    x[:8, :, :16384] = torch.finfo(DT[dtype]).min
+    x[4:8, :, 5:9000:2] = -math.inf
+    for b, what in enumerate((math.nan, math.inf, -math.nan, math.nan) * 2):
+        x[b, b % 3, int(rng.integers(0, 16384))] = what
+    n = [K] * 8 + [0] * (B - 8)
+    r = check(x, -rng.random((B, K)), 5, n)
+    assert r["status"].tolist() == [1] * 8 + [4] * (B - 8)
