@@ -498,6 +498,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         return state == kBeamLive ? l == own ? head_n : heads[l].n : state == kBeamDone && rest == 0 ? 1 : 0;
     };
     const auto entries = [&](int l, int &k) { return (length(l, k) - deep + apart - 1) >> share; };
+    // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
+    const auto base_of = [&](int k, double s) { return rint(((double)scores[(size_t)b * dsc.K + k] - log(s)) * 0x1p40) * 0x1p-40; };
     int n;
     for (int round = 0;; round++) {
         float top = -INFINITY;
@@ -680,11 +682,12 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         }
         __syncthreads();
         if (round == 2) break;
-        // Two totals of different beams too close to call: neighbours of the M best, or the last of them and one left out.  (Equal ones are those of
-        // equal rows.)
+        // Two totals of different beams too close to call: neighbours of the M best, or the last of them and one left out.  Equal ones are among
+        // them: sums of different rows may be equal in what was formed in 32 bits, and of beams alike, beside a third, all are taken again or none, so that
+        // they stay alike.  Finished beams have no sum.
         const auto call = [&](const Total &a, const Total &o) {
             const int k = (int)(a.place >> 32), k1 = (int)(o.place >> 32);
-            if (k != k1 && a.x > o.x && a.x - o.x < close) {
+            if (k != k1 && a.x - o.x < close && (s_state[k] == kBeamLive || s_state[k1] == kBeamLive)) {
                 atomicOr(&s_again[k >> 5], 1u << (k & 31));
                 atomicOr(&s_again[k1 >> 5], 1u << (k1 & 31));
             }
@@ -707,12 +710,18 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         __syncthreads();
         uint64_t again = s_again[0] | (uint64_t)s_again[1] << 32;
         if (!again) break;
-        for (; again; again &= again - 1) {
+        double s = 0;
+        for (bool had = false; again; again &= again - 1) {
             const int k = __builtin_ctzll(again);
             if (s_state[k] != kBeamLive) continue;
             const T *x = logits + b * dsc.batch_stride + k * dsc.row_stride;
             const double m = s_max[k];
-            double s = 0;
+            if (had && dsc.row_stride == 0) {  // one row for all beams: the same sum
+                if (t == 0) s_base[k] = base_of(k, s);
+                continue;
+            }
+            had = true;
+            s = 0;
             if (round == 0) {
                 constexpr int N = Logits<T>::N, AHEAD = 4;
                 const auto add = [&](float y) { s += exp2_fast(fmax(((double)y - m) * kLog2e, -1000.0)); };
@@ -734,8 +743,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
                 for (int v = t; v < dsc.V; v += kMergeThreads) s += exp((double)Logits<T>::one(x[v]) - m);
             }
             s = block_sum(s);
-            // to multiples of 2^-40: rows with the same logits in another order tie, whatever order they were added in
-            if (t == 0) s_base[k] = rint(((double)scores[(size_t)b * dsc.K + k] - log(s)) * 0x1p40) * 0x1p-40;
+            if (t == 0) s_base[k] = base_of(k, s);
         }
         close = 0x1p-27;
         __syncthreads();

@@ -347,3 +347,89 @@ def test_a_masked_step_with_what_is_not_a_number(dtype):
     n = [K] * 8 + [0] * (B - 8)
     r = check(x, -rng.random((B, K)), 5, n)
     assert r["status"].tolist() == [1] * 8 + [4] * (B - 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("copies", [False, True])
+@pytest.mark.parametrize("K", [3, 6])
+@pytest.mark.parametrize("M", [4, 6, 12, 40])
+def test_equal_beams_whose_best_tokens_lie_close(M, K, copies, dtype):
+    """One row for all beams, or the same row at several places, and two best logits a step of their type apart: (0, A) (1, A) .. (0, B) (1, B) .."""
+    rng = np.random.default_rng(101)
+    for V in (600, 9001):
+        x = torch.from_numpy(rng.uniform(-8, -1, (4, 1, V)).astype(np.float32)).to(DT[dtype])
+        a, b = (2.0 ** -13 + 2.0 ** -20, 2.0 ** -13) if dtype == "bf16" else (5.0 + 2.0 ** -21, 5.0)
+        for i in range(4):
+            at = rng.permutation(V)[:2]
+            x[i, 0, int(at[0])], x[i, 0, int(at[1])] = a, b
+        x = x.expand(4, K, V)
+        check(x, np.full((4, K), -1.25), M, on=(x.contiguous().cuda() if copies else x[:, :1].cuda().expand(4, K, V)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("third", [0, 1, 2])
+@pytest.mark.parametrize("M", [1, 2, 3, 8, 30])
+def test_equal_beams_and_one_close_by(M, third, dtype):
+    """Two beams alike, and another row whose best total is an fp32 step above or below theirs."""
+    rng = np.random.default_rng(102)
+    B, V = 32, 5001
+    x = normal(rng, (B, 2, V), dtype, 3.0)
+    f = x.double().numpy()
+    best = f.max(-1) - np.array([[f[b, k].max() + math.log(math.fsum(np.exp(f[b, k] - f[b, k].max()))) for k in range(2)] for b in range(B)])
+    alike, other = np.full(B, -6.0, dtype=np.float32), (-6.0 + best[:, 0] - best[:, 1]).astype(np.float32)
+    gap = other + best[:, 1] - (alike + best[:, 0])
+    assert (np.abs(gap) < 1e-6).all() and (np.abs(gap) > 2.0 ** -39).all() and (gap > 0).any() and (gap < 0).any()
+    order = [0, 0]
+    order.insert(third, 1)
+    check(x[:, order].contiguous(), np.stack((alike, other), 1)[:, order], M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("third", [0, 1, 2])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("M", [1, 2, 3, 20])
+def test_equal_beams_and_one_closer_than_the_second_sum_tells(M, sign, third, dtype):
+    """Two beams alike, and one with the same logits in another order whose score is 2^-28 off."""
+    rng = np.random.default_rng(103)
+    B, V = 32, 5001
+    x = normal(rng, (B, 1, V), dtype, 3.0).expand(B, 3, V).clone()
+    for b in range(B):
+        x[b, third] = x[b, third, torch.from_numpy(rng.permutation(V))]
+    scores = np.full((B, 3), np.float32(-0.05))
+    scores[:, third] += sign * 2.0 ** -28
+    assert (scores == scores.astype(np.float32)).all()
+    check(x, scores, M)
+
+
+@pytest.mark.parametrize("V", [2, 5000])
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("M", [1, 2, 4, 20])
+def test_sums_that_fp32_does_not_tell_apart(M, far, V):
+    """Rows of two tokens a thread adds up, [0, -a] and [0, -a'] with a' an fp32 step behind a, or both so far that 1 + exp(-a) is 1: the totals differ in
+    64 bits alone, the better beam first or second."""
+    rng = np.random.default_rng(104)
+    B = 64
+    x = torch.full((B, 2, V), -math.inf)
+    a = (rng.uniform(17.5, 22, B) if far else rng.uniform(1, 10, B)).astype(np.float32)
+    behind = a + np.float32(0.5) if far else np.nextafter(a, np.float32(99))
+    for b in range(B):
+        at = 2 * int(rng.integers(0, V // 2))
+        x[b, :, at] = 0
+        x[b, b % 2, at + 1], x[b, 1 - b % 2, at + 1] = float(-a[b]), float(-behind[b])
+    gap = np.log1p(np.exp(-a.astype(np.float64))) - np.log1p(np.exp(-behind.astype(np.float64)))
+    assert (gap > 2.0 ** -39).all()
+    r = check(x, np.full((B, 2), -0.5), M)
+    assert (r["parent"][:, 0].cpu() == 1 - torch.arange(B) % 2).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_equal_totals_of_finished_and_running_beams(dtype):
+    """A finished beam's score against a running beam's best total: a row of one token has a probability of 1 whatever its logit is."""
+    rng = np.random.default_rng(105)
+    x = torch.full((40, 4, 3001), -math.inf, dtype=DT[dtype])
+    for b in range(40):
+        for k in range(4):
+            x[b, k, int(rng.integers(3001))] = float(rng.normal())
+    done = (rng.random((40, 4)) < 0.5).astype(np.uint8)
+    for M in (2, 4):
+        check(x, np.full((40, 4), -0.75), M, None, done, 17)
