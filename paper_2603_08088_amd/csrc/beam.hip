@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(etv_beam_desc
         // they stay alike.  Finished beams have no sum.
         const auto call = [&](const Total &a, const Total &o) {
             const int k = (int)(a.place >> 32), k1 = (int)(o.place >> 32);
-            if (k != k1 && a.x - o.x < close && (s_state[k] == kBeamLive || s_state[k1] == kBeamLive)) {
+            if (k != k1 && a.x >= o.x && a.x - o.x < close && (s_state[k] == kBeamLive || s_state[k1] == kBeamLive)) {
                 atomicOr(&s_again[k >> 5], 1u << (k & 31));
                 atomicOr(&s_again[k1 >> 5], 1u << (k1 & 31));
             }
