@@ -639,7 +639,8 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
  *  logits in [B, K, V], rows contiguous, strides in elements from h_desc (0: one row for several beams);  scores in float [B, K]
  *  n_beams in int32 [B] nullable (=> K);  finished in uint8 [B, K] nullable
  *  out_scores float [B, M]; parent, token int32 [B, M]; finished_out uint8 [B, M] nullable; status int32 [B]
- *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.
+ *  workspace: etv_beam_select_workspace_bytes(h_desc) bytes, 16-byte aligned.  What B, K, V and M need is enough for every call of the type
+ *            with as many or fewer of each.
  *  With M == K out_scores may be scores and finished_out finished; otherwise they must not overlap.
  * Supported: F32 or BF16 logits, 1 <= K, M <= ETV_MAX_BEAMS, 1 <= V < 2^31 - 65536; B * K times the segments of a row (1024 to 32768 logits
  * each) below 2^26, B below 2^23. */

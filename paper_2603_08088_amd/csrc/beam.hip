@@ -783,6 +783,14 @@ static int beam_splits(const etv_beam_desc *h) {
     return (int)((h->V + segment - 1) / segment);
 }
 
+// Lists that a workspace holds: as many as any call with this many requests, beams and logits or fewer has, so that one sized for the largest of a
+// program's calls does for the others, whose segments are shorter.  With `all` steps of all rows and n of them a segment there are at most all / n + rows lists;
+// n is 1 below 3 * kFullWaves alone, from there on all / n stays below that until n is at its largest.
+static int64_t beam_lists(const etv_beam_desc *h) {
+    const int64_t rows = (int64_t)h->B * h->K, all = rows * ((h->V + beam_step(h) - 1) / beam_step(h));
+    return std::min(all, std::max<int64_t>(3 * kFullWaves, all / (h->M > 16 ? 8 : kMaxSteps)) + rows);
+}
+
 // room for a list: a multiple of four, since the merge asks for its first four at once
 static int beam_list(const etv_beam_desc *h) { return (h->M + 3) & ~3; }
 
@@ -799,7 +807,7 @@ static int32_t check_beam(const etv_beam_desc *h) {
 
 extern "C" size_t etv_beam_select_workspace_bytes(const etv_beam_desc *h) {
     if (etv::check_beam(h) != ETV_OK) return 0;
-    const size_t lists = (size_t)h->B * h->K * etv::beam_splits(h);
+    const size_t lists = (size_t)etv::beam_lists(h);
     return lists * (sizeof(etv::ScanHead) + etv::beam_list(h) * sizeof(etv::Candidate));
 }
 

@@ -232,3 +232,18 @@ def test_the_oracle_by_hand():
     assert ended[0].tolist() == [0, 1, 1, 0, 0] and status == [4]
     best, parent, token, ended, _ = beam_plain.select(p, np.array([[-1.0, -0.1]]), 2, None, np.array([[0, 1]]), 1)
     assert parent[0].tolist() == [1, 0] and token[0].tolist() == [1, 0] and ended[0].tolist() == [1, 0] and best[0, 0] == -0.1
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_workspace_for_the_largest_selection_fits_smaller_ones(dtype):
+    """A program sizes it once: fewer requests, beams, logits or continuations need no more, although their rows are in more segments."""
+    size = lambda B, K, V, M: api.beam_select_workspace_bytes(B, K, V, M, dtype)
+    assert all(size(B, 4, 32000, 4) <= size(B + 1, 4, 32000, 4) for B in range(1, 300))
+    assert all(size(B, 8, 128000, 20) <= size(B + 1, 8, 128000, 20) for B in range(1, 150))
+    assert all(size(40, K, 50021, 17) <= size(40, K + 1, 50021, 17) for K in range(1, 64))
+    assert all(size(30, 10, V, 10) <= size(30, 10, V + 700, 10) for V in range(1, 400000, 700))
+    assert all(size(32, 8, 128000, M) <= size(32, 8, 128000, M + 1) for M in range(1, 64))
+    rng = np.random.default_rng(5)
+    for _ in range(2000):
+        most = [int(np.exp(rng.uniform(0, np.log(n)))) for n in (2000, 64, 300000, 64)]
+        assert size(*(int(rng.integers(1, n + 1)) for n in most)) <= size(*most), most

@@ -433,3 +433,14 @@ def test_equal_totals_of_finished_and_running_beams(dtype):
     done = (rng.random((40, 4)) < 0.5).astype(np.uint8)
     for M in (2, 4):
         check(x, np.full((40, 4), -0.75), M, None, done, 17)
+
+
+def test_one_workspace_for_every_batch():
+    """Sized for the largest batch; the smaller ones leave what is behind it alone, and so does the largest."""
+    rng = np.random.default_rng(107)
+    x = normal(rng, (80, 4, 32000), "bf16")
+    n = api.beam_select_workspace_bytes(80, 4, 32000, 4, torch.bfloat16)
+    whole = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+    for B in (80, 72, 71, 64, 1):
+        check(x[:B], -rng.random((B, 4)), 4, workspace=whole[:n])
+        assert bool((whole[n:] == 77).all())
