@@ -444,3 +444,18 @@ def test_one_workspace_for_every_batch():
     for B in (80, 72, 71, 64, 1):
         check(x[:B], -rng.random((B, 4)), 4, workspace=whole[:n])
         assert bool((whole[n:] == 77).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,M", [(2, 2), (2, 8), (5, 5), (5, 20)])
+def test_close_calls_between_rows_of_any_kind(K, M, dtype):
+    """Scores that bring the best totals of all beams to within an fp32 step of each other: whatever lies between them, the order is that of 64 bits."""
+    rng = np.random.default_rng(106)
+    B, V = 24, 20000
+    x = normal(rng, (B, K, V), dtype, 3.0)
+    f = x.double().numpy()
+    top = np.array([[-math.log(math.fsum(np.exp(f[b, k] - f[b, k].max()))) for k in range(K)] for b in range(B)])
+    scores = (-6 - top).astype(np.float32)
+    totals = np.sort(top + scores, 1)
+    assert (totals[:, -1] - totals[:, 0] < 1e-6).all() and (np.diff(totals) > 2.0 ** -39).all()
+    check(x, scores, M)
