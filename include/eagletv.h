@@ -592,7 +592,7 @@ ETV_API int32_t etv_resize_block_tables(const etv_pages_desc *h_desc, const int3
 
 /* rotary_write_kv -- rotary position encoding of q and k by positions on one or several axes (time, height, width), and the write
  * of k and v into the cache, in one pass.  Channel pair i (i < rot_dim / 2) of every head turns with axis a = axis_of[i]:
- *   angle = positions[a, b, t] * inv_freq[i] (the product, its sine and cosine good to fp32 at any 32-bit position)
+ *   angle = positions[a, b, t] * inv_freq[i] (its sine and cosine good to fp32 at any 32-bit position, for angles below 2^50)
  *   (x, y) -> scale * (x cos - y sin, y cos + x sin)
  * where (x, y) are channels (i, i + rot_dim/2), or (2i, 2i+1) with ETV_ROTARY_INTERLEAVED; channels from rot_dim on are copied.
  * ETV_ROTARY_INVERSE turns by -angle: the gradient of the call and, with a scale of 1, the way back to unencoded rows.

@@ -13,13 +13,16 @@ struct RotaryPtrs {
     void *q_out, *k_out, *v_out, *k_cache, *v_cache;
 };
 
-// Sine and cosine of pos * f.  The product has 55 bits of which 53 are kept, the quarter turns are split off in 64 bits, and what is left, at most
-// half a quarter, goes to the fp32 functions: its rounding is 2^-26 of a quarter turn.
+// Sine and cosine of pos * f.  The product has up to 55 bits, in two parts; so is 2 / pi.  The quarter turns are split off within a fused multiply-add, the
+// low parts added, and what is left, at most half a quarter, goes to the fp32 functions: its rounding is 2^-26 of a quarter turn.  (Without the low parts an
+// angle near 2^31 is off by up to 7 * 2^-24.)
 __device__ __forceinline__ float2 turn_of(int pos, float f, float scale, bool inverse) {
-    const double quarters = (double)pos * (double)f * 0.63661977236758134308;  // 2 / pi
-    const double whole = rint(quarters);
+    constexpr double kQuarter = 0.6366197723675814, kQuarterLow = -3.935735335036497e-17;  // 2 / pi
+    const double angle = (double)pos * (double)f, rest = fma((double)pos, (double)f, -angle);
+    const double whole = rint(angle * kQuarter);
+    const double part = fma(angle, kQuarter, -whole) + fma(angle, kQuarterLow, rest * kQuarter);
     float s, c;
-    sincospif(0.5f * (float)(quarters - whole), &s, &c);
+    sincospif(0.5f * (float)part, &s, &c);
     const int n = (int)(long)(whole - 4.0 * floor(0.25 * whole));
     float cs = (n & 1) ? -s : c, sn = (n & 1) ? c : s;
     if (n & 2) cs = -cs, sn = -sn;

@@ -231,3 +231,21 @@ def test_padding_of_many_rows_is_left_alone(T, Hq, Hkv, d, rot, dtype, inter):
         expect = torch.full_like(cache, 3)
         expect.view(B * T, Hkv, d)[at] = want[there]
         assert torch.equal(cache, expect)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("far", [2 ** 24, 2 ** 28, 2 ** 31])
+def test_far_positions_are_good_to_fp32(far, dtype, inter):
+    """The bound of near positions holds for all of them, of either sign, with frequencies of 24 bits: what 64 bits lose of the product and of 2 / pi is
+    added again."""
+    c = Case(9, 2, 601, 3, 2, 64, dtype, axes=2, inter=inter)
+    c.positions = c.rng.integers(-far, far, (2, 2, 601))
+    c.positions[:, 0, :4] = [-far, far - 1, far // 2 + 1, 1 - far]
+    c.inv_freq = c.rng.uniform(0.5, 1.5, 32).astype(np.float32)
+    c.rotary = api.Rotary(dev(c.inv_freq, np.float32), axis_of=c.axis_of, interleaved=inter)
+    p = dev(c.positions)
+    for inverse in (False, True):
+        r = api.rotary_write_kv(c.q, c.k, None, p, c.rotary, inverse=inverse)
+        c.close(r["q"], c.host[0], inverse)
+        c.close(r["k"], c.host[1], inverse)
