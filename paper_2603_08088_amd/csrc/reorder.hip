@@ -194,9 +194,9 @@ struct CacheParts {
 template <class U, int AHEAD>
 __device__ __forceinline__ void copy_rows(uint8_t *layer, const int2 *copies, int first, int step, int n, int num_blocks, int Hkv, int block_size,
                                           int row_bytes, int rows) {
-    const uint32_t per_head = (uint32_t)(rows * row_bytes) / sizeof(U), all = per_head * Hkv;
+    const uint32_t per_head = (uint32_t)((uint32_t)rows * (uint32_t)row_bytes / sizeof(U)), all = per_head * Hkv;
     const uint32_t inv = per_head == 1 ? 0xffffffffu : 0xffffffffu / per_head, inv_all = all == 1 ? 0xffffffffu : 0xffffffffu / all;
-    const uint32_t head = (uint32_t)block_size * row_bytes;
+    const uint32_t head = (uint32_t)block_size * (uint32_t)row_bytes;
     const size_t block = (size_t)Hkv * head;
     if (first + step >= n || all >= (1u << 24)) {  // a copy at a time
         for (int copy = first; copy < n; copy += step) {

@@ -248,3 +248,18 @@ def test_layers_of_more_than_2_32_bytes():
             assert (t[:, block, :, :9] == 3 + i).all() and not t[:, block, :, 9:].any()
         t[:, [7, n - 2, n - 3, n - 4]] = 0
         assert not any(part.any() for part in t.view(-1).split(1 << 30))
+
+
+@pytest.mark.parametrize("size,d", [((1 << 23) + 16, 128), ((1 << 15) + 100, 1 << 15)])
+def test_a_head_s_rows_in_a_block_of_more_than_2_31_bytes(size, d):
+    """Blocks may have up to 2^32 bytes, those of one head too: their offsets are unsigned."""
+    k, v = (torch.zeros((1, 3, 1, size, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for t in (k, v):
+        t.view(torch.int16)[0, 1].random_(generator=gen)
+    free, rows = api.FreeBlocks(dev([2, 0, -1]), dev([0, 2])), size - 5
+    r = api.reorder_beams(k, v, dev([[[1]]]), dev([rows]), dev([[0, 0]]), free)
+    assert r["status"].tolist() == [0] and r["block_table"].tolist() == [[[1], [2]]] and r["free_state"].tolist() == [1, 1]
+    for t in (k, v):
+        t = t.view(torch.int16)[0, :, 0]
+        assert torch.equal(t[2, :rows], t[1, :rows]) and not t[2, rows:].any() and not t[0].any()
