@@ -555,7 +555,7 @@ ETV_API int32_t etv_tree_verify_attention_q4(const etv_attn_desc *h_desc, const 
  * The free blocks of a pool are a ring: free_blocks int32 [num_blocks] and free_state int32 [2] = (first, count), all on the
  * device; the free ones are free_blocks[(first + i) % num_blocks], 0 <= i < count.  A call takes blocks from the front and puts
  * blocks behind the end; what it puts there it does not take itself.  The state is read from free_state and written to
- * free_state_out (which must not alias it).  A state outside 0 <= first < num_blocks, 0 <= count <= num_blocks counts as an empty
+ * free_state_out (which must not overlap it).  A state outside 0 <= first < num_blocks, 0 <= count <= num_blocks counts as an empty
  * ring that takes nothing back, and stays as it is.
  * ------------------------------------------------------------------------- */
 #define ETV_MAX_BEAMS 64 /* largest number of beams of one request, before and after a step */

@@ -273,7 +273,7 @@ extern "C" int32_t etv_resize_block_tables(const etv_pages_desc *h, const int32_
                                            int32_t *free_blocks, const int32_t *free_state, int32_t *free_state_out, int32_t *len_out,
                                            int32_t *slot_map, int32_t *status, void *stream) {
     if (!h || h->B < 0 || h->S < 1 || h->block_size < 1 || h->max_blocks < 1 || h->num_blocks < 1) return ETV_ERR_INVALID_ARG;
-    if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
+    if (!free_blocks || !free_state || !free_state_out || etv::overlap(free_state, 8, free_state_out, 8)) return ETV_ERR_INVALID_ARG;
     if (h->B > 0 && (!len || !new_len || !block_table || !len_out || !status)) return ETV_ERR_INVALID_ARG;
     if ((int64_t)h->B * h->S > INT32_MAX - etv::kSlotsPerWg || (int64_t)h->num_blocks * h->block_size > INT32_MAX || h->max_blocks > etv::kMaxRow)
         return ETV_ERR_UNSUPPORTED;

@@ -400,7 +400,7 @@ static int32_t reorder(const ReorderShape &shape, const CacheParts &cache, const
     const int32_t shape_rc = check_reorder(sh.B, sh.K, sh.M, sh.max_blocks);
     if (shape_rc == ETV_ERR_INVALID_ARG || sh.num_blocks < 1 || cache.n_layers < 1 || cache.Hkv < 1) return ETV_ERR_INVALID_ARG;
     if (shape_rc != ETV_OK || (int64_t)sh.num_blocks * sh.block_size > INT32_MAX) return ETV_ERR_UNSUPPORTED;
-    if (!free_blocks || !free_state || !free_state_out || free_state == free_state_out) return ETV_ERR_INVALID_ARG;
+    if (!free_blocks || !free_state || !free_state_out || overlap(free_state, 8, free_state_out, 8)) return ETV_ERR_INVALID_ARG;
     hipStream_t s = as_stream(stream);
     if (sh.B == 0) {
         hipLaunchKernelGGL(ring_copy_kernel, dim3(1), dim3(2), 0, s, free_state, free_state_out);

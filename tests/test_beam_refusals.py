@@ -247,3 +247,12 @@ def test_a_workspace_for_the_largest_selection_fits_smaller_ones(dtype):
     for _ in range(2000):
         most = [int(np.exp(rng.uniform(0, np.log(n)))) for n in (2000, 64, 300000, 64)]
         assert size(*(int(rng.integers(1, n + 1)) for n in most)) <= size(*most), most
+
+
+@pytest.mark.parametrize("by", [-4, 4])
+def test_the_ring_s_new_state_beside_its_old_one(by):
+    """Every workgroup reads the old state while one writes the new: half of one on the other is refused like all of it."""
+    assert pages(pages_desc(), fs=2 * A, fo=2 * A + by) == pages(pages_desc(B=0), fs=2 * A, fo=2 * A + by) == -1
+    assert reorder(cache_desc(), fs=2 * A, fo=2 * A + by) == reorder(cache_desc(B=0), fs=2 * A, fo=2 * A + by) == -1
+    q = api.Q4Desc(B=2, rows=1, Hkv=2, d=64, n_layers=2, block_size=16, max_blocks=8, num_blocks=20, layer_rows=640)
+    assert api.lib().etv_reorder_beams_q4(C.byref(q), A, A, A, A, A, A, 4, A, 4, A, 2 * A, 2 * A, 2 * A + by, A, A, 1 << 40, None) == -1
