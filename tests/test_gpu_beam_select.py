@@ -459,3 +459,18 @@ def test_close_calls_between_rows_of_any_kind(K, M, dtype):
     totals = np.sort(top + scores, 1)
     assert (totals[:, -1] - totals[:, 0] < 1e-6).all() and (np.diff(totals) > 2.0 ** -39).all()
     check(x, scores, M)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3, 5, 8, 9, 601, 4099, 8193, 16384, 16385, 16391, 33000])
+def test_rows_that_differ_in_one_logit(V, dtype):
+    """Copies of a row, and rows like it but for one place, where a logit is -18.5 instead of -18: better by 6e-9, wherever that place is."""
+    rng = np.random.default_rng(V)
+    for at in {0, 1, V - 1, V // 3}:
+        x = torch.full((4, 4, V), -math.inf, dtype=DT[dtype])
+        for b in range(4):
+            top = int(rng.choice([v for v in (0, 1, 2, V - 2) if v != at]))
+            x[b, :, top], x[b, :, at] = 0, -18
+            x[b, torch.from_numpy(rng.random(4) < 0.5), at] = -18.5
+        for M in (1, 4, 8):
+            check(x, np.full((4, 4), -0.5), M)
