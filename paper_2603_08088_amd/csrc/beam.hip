@@ -1,7 +1,7 @@
 // The best continuations over beams and vocabulary, total[k, v] = score[k] + x[k, v] - log sum_v' exp(x[k, v']): one pass over the logits, which
 // leaves of every segment of a row its sum relative to a reference and its M best logits in order, then a merge per request.  Floor: the
-// logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 11.1 us at the rate of a
-// large copy (5.17 TB/s).  The call takes 20.4 us there: the scan 16.1, the merge 6.0.
+// logits of the live beams once; 32 requests of 8 beams, 7 of them live, with 128000 bf16 logits are 57.3 MB, 8.0 us at the rate of a
+// large read (7.15 TB/s).  The call takes 20.8 us there: the scan 16.6, the merge 6.6.
 #include "etv_common.h"
 #include <algorithm>
 #include <cfloat>
@@ -169,7 +169,7 @@ __device__ __forceinline__ double exp2_fast(double z) {
 // exp(x) / 2^r in fp32, for a t = x - r ln(2) up to kSlack and |x| where it is not 0 up to kFarthest: within 2^-23 (1 + |t|) of itself.  log2(e) is in two
 // parts, and the first product is rounded behind the subtraction.  The second one is less than half a unit of an exponent of 1 or more and mostly rounds
 // away there, so that terms have an error in common: with it sums over logits of normal distribution are off by 1e-8 to 1e-7, within that bound.  What the
-// hardware's 2^y is off by in the mean (-3.4e-9, measured) is taken out of the sums.
+// hardware's 2^y is off by in the mean (-3.4e-9, measured) is taken out of the sums.  (In 64 bits all exponentials take the scan 35 us where these take 17.)
 __device__ __forceinline__ float term(float x, float r) { return __builtin_amdgcn_exp2f(fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -r))); }
 constexpr double kTermMean = 1 + 3.4e-9;
 constexpr float kSlack = 1, kFarthest = 1 << 20;
@@ -178,10 +178,10 @@ constexpr float kSlack = 1, kFarthest = 1 << 20;
 // logit takes part in the running sum; of the order only the largest of every two vectors is kept, the best two of them for each lane.  Those bound the
 // M-th best of the segment from below (a number that M of them reach), and the few vectors that reach the bound are read again, from the
 // caches, for the candidates, which are ranked by counting.  TINY: fewer logits than a vector holds.
-// One wavefront a workgroup, so that no barrier stops the stream.  Bounds: memory where
-// rows are many -- of the 16.1 us above the loads alone take 11.5, the rest are exponentials and sums, and bound, candidates and ranking --, and the
-// chain load, work, bound, candidates where they are few: 4 rows of 32000 fp32 logits 4.6 us, of which an empty launch is some 2.  Measured and left: wavefronts that
-// go from segment to segment with the next one's first loads under way (half a us to two longer: 135 registers leave 12 of them a CU, 86 leave 20).
+// One wavefront a workgroup, so that no barrier stops the stream.  Bounds: memory and the vector unit where rows are many -- of the 16.6 us above the
+// loads alone take 11.5 and the vector instructions, 9.4 a logit, some 7.6; the rest are bound, candidates and ranking --, and the chain load, work, bound,
+// candidates where they are few: 4 rows of 32000 fp32 logits 4.6 us, of which an empty launch is some 2.  Measured and left: wavefronts that go from
+// segment to segment with the next one's first loads under way (half a us to two longer: 135 registers leave 12 of them a CU, 86 leave 20).
 template <class T, bool TINY>
 __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const T *logits, const float *scores, const int32_t *n_beams,
                                                        const uint8_t *finished, int splits, uint32_t inv_splits, uint32_t inv_K, int steps, int list, int room,
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(64) beam_scan_kernel(etv_beam_desc dsc, const 
 // As in the scan: a bound on the M-th best from below, here from the heads of the lists, then only those above it.  Where two beams' totals next to each
 // other are closer than their sums are good for, these are taken again from the logits, with exp2_fast and, if that does not tell either, with exponentials
 // of full precision: so the order is that of 64-bit sums.  A sum is good to 2^-23 times 1 + kSlack + 5 (ten additions in 32 bits) + the mean of max - x over its weights, which is at most ln V.
-// Bound by the chain of its loads and barriers: 5.4 us for one request of 4 beams, 6.0 for 32 of 8 beams with 8 lists each.  A scan whose
+// Bound by the chain of its loads and barriers: 5.2 us for one request of 4 beams, 6.6 for 32 of 8 beams with 8 lists each.  A scan whose
 // last workgroup merges would save this launch's 4 us on the host, but needs a counter that somebody clears, and a release to the whole device by every wavefront.
 // SHARED: few lists against M, which are therefore gone into deeply, by several threads each.  MANY: M above 16, where the heads of a wavefront's lists
 // say too little; a kernel of its own, for code that is not run costs the other 0.2 us.
