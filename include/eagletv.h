@@ -631,7 +631,8 @@ ETV_API int32_t etv_rotary_write_kv(const etv_rotary_desc *h_desc, const void *q
  * scores[b, k] and nothing else.  Beams k >= n_beams[b], scores of -inf and logits of -inf offer nothing, nor do totals that are -inf in fp32.  Where fewer than M are
  * offered the rest is parent = token = -1 with a score of -inf.  Totals are formed and compared in 64 bits and rounded once; the
  * exponentials are fp32 (the logarithm of a sum is off by 1e-8 to 1e-7 as a rule), but where totals of two beams that decide a choice or its place
- * lie within 2^-22 (7 + ln V), what the sums may be off by, equal ones among them, both are taken again in 64 bits first.
+ * lie within 2^-22 (7 + ln V), what the sums may be off by, equal ones among them, both are taken again in 64 bits first (to
+ * multiples of 2^-40, so that rows with the same logits in another order tie).
  *   finished_out[b, m] = 1 if the parent was finished or the token is end_token, else 0
  *   Status bits: ETV_BEAM_BAD_LOGITS (a live beam's logits hold NaN or +inf: that beam offers nothing), ETV_BEAM_BAD_SCORE (a beam's
  *   score is NaN or +inf: the same), ETV_BEAM_SHORT (fewer than M are offered).
